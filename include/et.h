@@ -45,6 +45,17 @@
  *   out_features a multiple of 64), the gathered matrix a_{l+1} is never formed: the dense layer's three
  *   GEMMs fetch the patches themselves, and the gather's forward and backward launch nothing.
  *
+ *   A layer of kind ET_LAYER_EMBEDDING looks rows of a table up; it can only be layer 0.  The stack input x is then
+ *   int32 device [M], one token id per row, and
+ *       a_1[i] = s * T[x_i]                    T = tensor 0, [in_features = vocabulary x out_features], storage dtype
+ *   with the scale s of et_stack_set_embedding_scale (1 when never set).  An id outside [0, in_features) gives a row
+ *   of zeros and takes no part in the gradient.  Tensor 0 is selected, costed (t_dw: the whole gradient; t_dy = 0),
+ *   weighed by Eq. 2 and updated like every tensor; there is no tensor 1 (its b pointer may be NULL, its mask bit must
+ *   be 0, its slots are ignored).  The gradient  dT[v] = s * sum of G_1's rows i with x_i = v  is formed by sorting
+ *   the ids and adding the rows of each id in order: the sums do not depend on scheduling.  An exported gradient is
+ *   written whole, rows without a token as 0; plain SGD updates the rows that tokens name and reads no others.  Any
+ *   vocabulary; act = ET_ACT_NONE, fold = 1, residual_src = -1, and no layer's residual_src may be 0.
+ *
  *   A layer of kind ET_LAYER_NORM is a layer normalisation over the features of each row
  *   (Section 5.2 treats normalisation layers as two trainable tensors, Gamma and Beta;
  *   Section 5.4 says LayerNorm behaves like batch normalisation in this respect):
@@ -98,7 +109,8 @@ typedef enum {
 typedef enum { ET_F32 = 0, ET_BF16 = 1 } et_dtype;
 typedef enum { ET_ACT_NONE = 0, ET_ACT_GELU_TANH = 1, ET_ACT_RELU = 2 } et_act;
 typedef enum {
-  ET_LAYER_DENSE = 0, ET_LAYER_NORM = 1, ET_LAYER_ATTENTION = 2, ET_LAYER_IM2COL = 3, ET_LAYER_BATCHNORM = 4
+  ET_LAYER_DENSE = 0, ET_LAYER_NORM = 1, ET_LAYER_ATTENTION = 2, ET_LAYER_IM2COL = 3, ET_LAYER_BATCHNORM = 4,
+  ET_LAYER_EMBEDDING = 5
 } et_layer_kind;
 
 /* Cost-model reading for the selector (Section 2.2 / Eq. 7 versus the example after Eq. 3). */
@@ -230,6 +242,10 @@ et_status et_stack_set_optimizer(et_stack* s, const et_optimizer_config* cfg, fl
 /* Step number t >= 1 (Adam's bias correction) and weight decay of the next updating call. */
 et_status et_stack_set_optimizer_step(et_stack* s, int32_t step, float weight_decay);
 
+/* Scale s of the lookup of a stack whose layer 0 is ET_LAYER_EMBEDDING (finite; host state, used by the forward and
+ * backward calls that follow; a backward call has to find the scale of its forward pass). */
+et_status et_stack_set_embedding_scale(et_stack* s, float scale);
+
 /* ---- forward and loss (precede the hot path; Eq. 3's T_forward) -------------------- */
 
 /* x: device [M x in_features(0)], y: device [M x width(a_L)], storage dtype.  Saves every
@@ -242,6 +258,71 @@ et_status et_forward_stack(et_stack* s, const void* x, void* y, void* stream);
  * y, target, dY: device, storage dtype; loss_dev: device float (may be NULL). */
 et_status et_loss_mse_grad(et_stack* s, const void* y, const void* target, void* dY,
                            float* loss_dev, void* stream);
+
+/* Losses on tokens.  y holds logits, one token per row:  z_ij = logit_scale * y_ij  for the columns j < vocab
+ * (0: all columns; columns from vocab on are padding, whatever they hold, and get gradient 0), and
+ *     lp_i = z_i,t - log sum_j exp z_ij,    t = targets[i]
+ * is the log probability of the token that was taken.
+ *   y        device [M x width(a_L)], storage dtype, 16-byte aligned
+ *   targets  device int32[M].  A row whose target lies outside [0, vocab) is left out, as is one of weight 0: its y is
+ *            not read (it may hold anything), its gradient is 0, its log probability is reported as 0
+ *   weights  device float[M], or NULL (see the call)
+ *   dY       device, shape and type of y: d loss / d y.  May be y itself (the logits are overwritten), otherwise it must not
+ *            overlap it; NULL: no gradient is formed
+ * Logits of -inf (or the type's lowest value) are tokens of probability 0; a row without a finite logit, with one of
+ * +inf or with a NaN gives NaN.  Reported numbers are added up in 64 bits and a fixed order.  They use rows of the workspace:
+ * two of these calls on one stack must not overlap.  Asynchronous on `stream`. */
+
+/* lp_i of every row into logp (device float[M]): the old and the reference log probabilities of the losses below. */
+et_status et_token_logp(et_stack* s, const void* y, const int32_t* targets, int32_t vocab, float logit_scale, float* logp,
+                        void* stream);
+
+typedef struct {
+  int32_t vocab;          /* 0, or the number of columns that are logits */
+  float logit_scale;      /* > 0: one over the sampling temperature */
+  float clip_low;         /* in [0, 1] */
+  float clip_high;        /* >= 0 */
+  float kl_coef;          /* >= 0; needs logp_ref when > 0 */
+} et_policy_config;
+
+/* Clipped policy loss with a KL term, and its gradient:
+ *     r_i  = exp(lp_i - logp_old_i)                                 logp_old NULL: r_i = 1, slope that of lp
+ *     kl_i = exp(d_i) - 1 - d_i,   d_i = logp_ref_i - lp_i          logp_ref NULL: 0
+ *     loss = sum_i w_i ( -min(r_i A_i, clip(r_i, 1 - clip_low, 1 + clip_high) A_i) + kl_coef kl_i )
+ *   weights NULL: w_i = 1 / M.  advantages, logp_old, logp_ref: device float[M].
+ *   logp      device float[M] or NULL: lp_i
+ *   loss_dev  device float[4] or NULL: the loss, its first part, sum w_i kl_i, sum of the w_i whose ratio is clipped
+ * Where both arguments of the min are equal the first one's slope counts. */
+et_status et_loss_policy_grad(et_stack* s, const void* y, const int32_t* targets, const float* weights, const float* advantages,
+                              const float* logp_old, const float* logp_ref, const et_policy_config* cfg, void* dY,
+                              float* logp, float* loss_dev, void* stream);
+
+typedef enum { ET_PREF_SIGMOID = 0, ET_PREF_IPO = 1, ET_PREF_HINGE = 2 } et_preference_kind;
+typedef struct {
+  int32_t kind;             /* et_preference_kind */
+  int32_t vocab;            /* 0, or the number of columns that are logits */
+  float logit_scale;        /* > 0 */
+  float beta;               /* > 0 */
+  float label_smoothing;    /* e in [0, 0.5); ET_PREF_SIGMOID only */
+} et_preference_config;
+
+/* Preference loss over pairs of sequences, and its gradient.  Sequence q is the rows seq_begin[q] .. seq_begin[q+1]-1;
+ * sequences 2p and 2p + 1 are the chosen and the rejected answer of pair p.
+ *     S_q = sum of w_i lp_i over the sequence's rows                weights NULL: w_i = 1
+ *     x_p = beta ((S_2p - ref_2p) - (S_2p+1 - ref_2p+1))            ref_logp NULL: 0
+ *     loss = mean over p of   -(1-e) log sigmoid(x) - e log sigmoid(-x)     ET_PREF_SIGMOID
+ *                             (x / beta - 1 / (2 beta))^2                   ET_PREF_IPO
+ *                             max(0, 1 - x)                                 ET_PREF_HINGE
+ *   seq_begin  device int32[2 pairs + 1], non-decreasing, in [0, M].  Rows of no sequence are left out.  (Bounds outside
+ *              that range are clamped, an end before its begin is an empty sequence; for bounds that are not
+ *              non-decreasing no more is said than that nothing out of range is read or written.)
+ *   pairs      1 .. M (ET_ERR_TOO_LARGE above)
+ *   ref_logp   device float[2 pairs] or NULL;  seq_logp  device float[2 pairs] or NULL: S_q
+ *   loss_dev   device float[4] or NULL: the loss, the means of beta (S - ref) of the chosen and of the rejected answers,
+ *              the share of pairs with x > 0 */
+et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* targets, const float* weights,
+                                  const int32_t* seq_begin, int32_t pairs, const float* ref_logp,
+                                  const et_preference_config* cfg, void* dY, float* seq_logp, float* loss_dev, void* stream);
 
 /* ---- the hot path ----------------------------------------------------------------- */
 
@@ -308,6 +389,22 @@ et_status et_sgd_masked(et_stack* s, const uint8_t* mask, int32_t n_tensors, flo
 et_status et_update_masked(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads,
                            float lr, void* stream);
 
+/* Global norm of the selected gradients and clipping by it:
+ *     norm = sqrt( sum over selected k of sum_i grads[k]_i^2 ),   factor = max_norm / norm where norm > max_norm, else 1
+ * (squares and sums in 64 bits, in an order that does not depend on scheduling).  With a norm that is not finite the factor is 0.
+ *   norm_dev  device float[2]: norm, factor (the clipping calls take NULL).  Nothing selected: 0, 1.
+ * et_grad_norm reports the norm alone (its factor is 1, or 0 for a norm that is not finite).
+ * et_clip_grads writes clipped[k] = factor * grads[k] for selected k; clipped[k] may be grads[k] itself (then nothing is
+ * written where the factor is 1), else it must not overlap any gradient.  A factor of 0 writes zeros.
+ * et_update_clipped is et_update_masked on factor * grads[k] without writing the clipped gradients; a factor of 0 leaves
+ * weights and optimiser state as they are.  max_norm > 0 (infinity: no clipping, only the test for finiteness).
+ * Uses workspace partials: calls on one stack must not overlap.  Asynchronous on `stream`. */
+et_status et_grad_norm(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float* norm_dev, void* stream);
+et_status et_clip_grads(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float* const* clipped,
+                        float max_norm, float* norm_dev, void* stream);
+et_status et_update_clipped(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float lr, float max_norm,
+                            float* norm_dev, void* stream);
+
 /* Bias gradient without any allocation.  (The paper has no counterpart for this call; it
  * exists for how this library gets embedded.)
  *
@@ -345,7 +442,7 @@ et_status et_bias_grad_noalloc(const void* dZ, int64_t M, int32_t width, et_dtyp
  * and fills per-TENSOR cost vectors of length 2L following Section 5.1: kernel tensor:
  * t_dw = weight-gradient time, t_dy = error-gradient time (with the fused backward of the
  * non-trainable work below it, Section 5.3); bias tensor: t_dw = bias-gradient time,
- * t_dy = 0.  A normalisation layer is one black box (Section 5.2): the time of its whole
+ * t_dy = 0.  An embedding layer's gradient goes to t_dw of its table.  A normalisation layer is one black box (Section 5.2): the time of its whole
  * backward kernel (error gradient and d gamma together) plus its two finishing kernels goes
  * to t_dy of beta; t_dw of gamma and beta and t_dy of gamma are 0.  An attention layer is a
  * non-trainable layer (Section 5.3): its backward time is added to t_dy of the bias of the layer below.

@@ -23,6 +23,10 @@ or, for a batch normalisation layer (Section 5.2's subject; training mode, no ru
     xhat    = (a_l - mean) / sqrt(var + eps)         mean, biased var of each feature over all rows
     a_{l+1} = act_l( xhat * gamma_l + beta_l )
 
+or, for an embedding layer (layer 0 only; tensor 0 is the table, there is no tensor 1; a_0 holds ids),
+
+    a_1[i]  = scale * W_0[a_0[i]]                     rows of zeros for ids outside [0, vocabulary)
+
 or, for a patch-gather layer (no trainable tensors; with the dense layer after it, it is a k x k
 convolution with stride 1 and zero padding k // 2 on NHWC rows, the convolutional layer of Section 5.1),
 
@@ -52,6 +56,7 @@ import numpy as np
 
 ACT_NONE, ACT_GELU_TANH, ACT_RELU = 0, 1, 2
 KIND_DENSE, KIND_NORM, KIND_ATTENTION, KIND_IM2COL, KIND_BATCHNORM = 0, 1, 2, 3, 4
+KIND_EMBEDDING = 5
 STRICT, INCLUSIVE = 0, 1
 
 
@@ -100,6 +105,13 @@ def forward(layers, W: Sequence[np.ndarray], b: Sequence[np.ndarray], x: np.ndar
     a = [np.asarray(x, dtype=np.float64)]
     Z = []
     for l, ly in enumerate(layers):
+        if _kind(ly) == KIND_EMBEDDING:
+            ids = np.asarray(x).astype(np.int64).reshape(-1)
+            ok = (ids >= 0) & (ids < ly.in_features)
+            scale = getattr(ly, "scale", 1.0)
+            Z.append((ids, ok))
+            a.append(scale * np.asarray(W[l], dtype=np.float64)[np.where(ok, ids, 0)] * ok[:, None])
+            continue
         if _kind(ly) == KIND_BATCHNORM:
             # batch normalisation, training mode: mean and biased variance of each feature over all rows;
             # Z keeps (xhat, 1/sqrt(var + eps), pre-activation)
@@ -219,6 +231,13 @@ def _backward_sweep(layers, W, saved: Saved, dY: np.ndarray, stop: int,
     for l in range(L - 1, stop - 1, -1):
         ly = layers[l]
         g_out = G[l + 1]
+        if _kind(ly) == KIND_EMBEDDING:
+            if want_w[l]:
+                ids, ok = saved.Z[l]
+                g = np.zeros((ly.in_features, ly.out_features))
+                np.add.at(g, ids[ok], getattr(ly, "scale", 1.0) * g_out[ok])
+                grads[2 * l] = g
+            continue
         if _kind(ly) == KIND_BATCHNORM:
             xhat, rstd, z = saved.Z[l]
             dz = g_out * act_derivative(z, ly.act)

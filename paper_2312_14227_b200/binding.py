@@ -37,6 +37,20 @@ class et_layer_desc(C.Structure):
 
 
 ET_LAYER_DENSE, ET_LAYER_NORM, ET_LAYER_ATTENTION, ET_LAYER_IM2COL, ET_LAYER_BATCHNORM = 0, 1, 2, 3, 4
+ET_LAYER_EMBEDDING = 5
+
+
+class et_policy_config(C.Structure):
+    _fields_ = [("vocab", C.c_int32), ("logit_scale", C.c_float), ("clip_low", C.c_float), ("clip_high", C.c_float),
+                ("kl_coef", C.c_float)]
+
+
+ET_PREF_SIGMOID, ET_PREF_IPO, ET_PREF_HINGE = 0, 1, 2
+
+
+class et_preference_config(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("vocab", C.c_int32), ("logit_scale", C.c_float), ("beta", C.c_float),
+                ("label_smoothing", C.c_float)]
 
 
 class et_optimizer_config(C.Structure):
@@ -72,6 +86,13 @@ _SIGS = {
     "et_loss_mse_grad": [_vp, _vp, _vp, _vp, _vp, _vp],
     "et_backward_elastic": [_vp, _vp, _vp, _i32, _vp, _vp, _vp, _u32, _f32, _vp, _vp],
     "et_backward_elastic_host": [_vp, _vp, _vp, _i32, _vp, _vp, _vp, _u32, _f32, _vp, _vp],
+    "et_token_logp": [_vp, _vp, _vp, _i32, _f32, _vp, _vp],
+    "et_loss_policy_grad": [_vp] * 12,
+    "et_loss_preference_grad": [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp],
+    "et_grad_norm": [_vp, _vp, _i32, _vp, _vp, _vp],
+    "et_clip_grads": [_vp, _vp, _i32, _vp, _vp, _f32, _vp, _vp],
+    "et_update_clipped": [_vp, _vp, _i32, _vp, _f32, _f32, _vp, _vp],
+    "et_stack_set_embedding_scale": [_vp, _f32],
     "et_importance": [_vp, _vp, _i32, _vp, _vp, _vp, _vp],
     "et_tensor_metric": [_vp, _vp, _i32, _i32, _vp, _vp, _vp],
     "et_sgd_masked": [_vp, _vp, _i32, _vp, _f32, _vp],
@@ -308,6 +329,54 @@ def et_forward_stack(s: Stack, x, y, stream=None):
 def et_loss_mse_grad(s: Stack, y, target, dY, loss_dev=None, stream=None):
     _check(_lib.et_loss_mse_grad(s.handle, _ptr(y), _ptr(target), _ptr(dY), _ptr(loss_dev),
                                  _stream_ptr(stream)), "et_loss_mse_grad")
+
+
+def et_stack_set_embedding_scale(s: Stack, scale: float):
+    _check(_lib.et_stack_set_embedding_scale(s.handle, float(scale)), "et_stack_set_embedding_scale")
+
+
+def et_token_logp(s: Stack, y, targets, logp, vocab: int = 0, logit_scale: float = 1.0, stream=None):
+    _check(_lib.et_token_logp(s.handle, _ptr(y), _ptr(targets), vocab, logit_scale, _ptr(logp), _stream_ptr(stream)),
+           "et_token_logp")
+
+
+def et_loss_policy_grad(s: Stack, y, targets, advantages, dY=None, weights=None, logp_old=None, logp_ref=None, logp=None,
+                        loss_dev=None, vocab: int = 0, logit_scale: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2,
+                        kl_coef: float = 0.0, stream=None):
+    cfg = et_policy_config(vocab, logit_scale, clip_low, clip_high, kl_coef)
+    _check(_lib.et_loss_policy_grad(s.handle, _ptr(y), _ptr(targets), _ptr(weights), _ptr(advantages), _ptr(logp_old),
+                                    _ptr(logp_ref), C.addressof(cfg), _ptr(dY), _ptr(logp), _ptr(loss_dev),
+                                    _stream_ptr(stream)), "et_loss_policy_grad")
+
+
+def et_loss_preference_grad(s: Stack, y, targets, seq_begin, dY=None, weights=None, ref_logp=None, seq_logp=None, loss_dev=None,
+                            kind: int = ET_PREF_SIGMOID, vocab: int = 0, logit_scale: float = 1.0, beta: float = 0.1,
+                            label_smoothing: float = 0.0, pairs: Optional[int] = None, stream=None):
+    """`pairs`: taken from the length of seq_begin (2 pairs + 1) unless given."""
+    cfg = et_preference_config(kind, vocab, logit_scale, beta, label_smoothing)
+    if pairs is None:
+        pairs = (len(seq_begin) - 1) // 2
+    _check(_lib.et_loss_preference_grad(s.handle, _ptr(y), _ptr(targets), _ptr(weights), _ptr(seq_begin), pairs, _ptr(ref_logp),
+                                        C.addressof(cfg), _ptr(dY), _ptr(seq_logp), _ptr(loss_dev), _stream_ptr(stream)),
+           "et_loss_preference_grad")
+
+
+def et_grad_norm(s: Stack, mask, grads, norm_dev, stream=None):
+    m = _mask_arr(mask)
+    _check(_lib.et_grad_norm(s.handle, _ptr(m), len(m), _ptr_array(grads, len(m)), _ptr(norm_dev), _stream_ptr(stream)),
+           "et_grad_norm")
+
+
+def et_clip_grads(s: Stack, mask, grads, clipped, max_norm: float, norm_dev=None, stream=None):
+    m = _mask_arr(mask)
+    _check(_lib.et_clip_grads(s.handle, _ptr(m), len(m), _ptr_array(grads, len(m)), _ptr_array(clipped, len(m)), max_norm,
+                              _ptr(norm_dev), _stream_ptr(stream)), "et_clip_grads")
+
+
+def et_update_clipped(s: Stack, mask, grads, lr: float, max_norm: float, norm_dev=None, stream=None):
+    m = _mask_arr(mask)
+    _check(_lib.et_update_clipped(s.handle, _ptr(m), len(m), _ptr_array(grads, len(m)), lr, max_norm, _ptr(norm_dev),
+                                  _stream_ptr(stream)), "et_update_clipped")
 
 
 def _backward(fn, name, s, dY, mask, grads, delta, importance, flags, lr, report, stream):

@@ -23,6 +23,9 @@
 #include "attn.cuh"
 #include "im2col.cuh"
 #include "batchnorm.cuh"
+#include "embedding.cuh"
+#include "grad_clip.cuh"
+#include "token_loss.cuh"
 
 namespace {
 
@@ -199,7 +202,9 @@ struct LayerRT {
   bool big_gemm = false;    // its GEMMs run for tens of microseconds (10 GFLOP and more)
   int imp_count_w = 0, imp_count_b = 0;
   int img_h = 0, img_w = 0, ksize = 0;   // patch gather: K = channels, N = ksize^2 * K
-  bool trainable() const { return kind == ET_LAYER_DENSE || kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM; }
+  bool trainable() const { return kind == ET_LAYER_DENSE || kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM || kind == ET_LAYER_EMBEDDING; }
+  bool has_tensor(int k) const { return trainable() && (k == 0 || kind != ET_LAYER_EMBEDDING); }   // an embedding has no tensor 2l + 1
+  size_t off_keys[2] = {0, 0}, off_rows[2] = {0, 0}, off_hist = 0, off_epart = 0;   // embedding: sorting buffers, partial gradient rows
   bool vector_params() const { return kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM; }   // gamma, beta: [N]
   size_t off_means = 0;     // batch norm: the two column means of the backward formula
   size_t w_count() const { return !trainable() ? 0 : vector_params() ? (size_t)N : (size_t)K * N; }   // elements of tensor 2l
@@ -235,6 +240,9 @@ struct et_stack {
   std::vector<size_t> guards;          // offsets of the guard words that follow each workspace region (debug aid)
   size_t off_status = 0, off_partial = 0, off_imp_parts = 0, off_imp_offs = 0,
          off_imp_counts = 0, off_loss_parts = 0, off_dy_stage = 0, off_imp_stage = 0;
+  size_t off_tok_stats = 0, off_tok_logp = 0, off_tok_coef = 0, off_tok_parts = 0;   // token losses: per row
+  size_t off_norm_parts = 0;           // global gradient norm: one 64-bit partial per block
+  float emb_scale = 1.0f;              // ET_LAYER_EMBEDDING
   int imp_total = 0;
   char* ws = nullptr;
   bool bound = false, forwarded = false;
@@ -325,6 +333,23 @@ TilePlan choose_tiles(int rows, int cols, int kb_total, int sms, bool allow_spli
   }
   return best;
 }
+
+// How the gradient of an embedding with `vocab` rows of `d` is cut up for `rows` tokens.
+struct EmbPlan { int tiles, bits, passes, chunks, threads, col_tiles; };
+EmbPlan emb_plan(long long rows, int vocab, int d) {
+  EmbPlan p;
+  int bits = 1;
+  while (bits < 32 && ((unsigned long long)vocab >> bits) != 0) ++bits;    // keys 0 .. vocab (= left out)
+  p.passes = ceil_div(bits, et::kSortMaxBits);
+  p.bits = ceil_div(bits, p.passes);
+  p.tiles = ceil_div(rows, et::kSortTile);
+  p.chunks = ceil_div(rows, et::kEmbChunk);
+  p.threads = std::min(256, ceil_div(ceil_div(d, et::kVec), 32) * 32);
+  p.col_tiles = ceil_div(d, p.threads * et::kVec);
+  return p;
+}
+constexpr int kClipTensors = 256;          // tensors named by one launch's table
+inline int clip_launches(int n_tensors) { return ceil_div(n_tensors, kClipTensors); }
 
 // ---- per-kernel timing: an event pair around one launch ---------------------------------------
 cudaEvent_t take_event(et_stack* s) {
@@ -887,6 +912,69 @@ et_status run_im2col_backward(et_stack* s, int l, const void* dY, cudaStream_t s
   return after_launch();
 }
 
+// ---- embedding ------------------------------------------------------------------------------------
+template <typename T>
+et_status run_embed_forward(et_stack* s, void* y, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_FORWARD, st);
+  const LayerRT& L = s->ly[0];
+  T* out = s->L == 1 ? (T*)y : (T*)s->at(L.off_a_out);
+  const int grid = std::min(ceil_div(s->M, 8), s->sms * 16);
+  et::embed_forward_kernel<T><<<grid, 256, 0, st>>>((const T*)L.W, (const int32_t*)s->x, out, s->M, L.K, L.N, s->emb_scale);
+  return after_launch();
+}
+// The gradient of the table from G_1 (the caller's dY where the embedding is the only layer).
+template <typename T>
+et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* delta, bool sgd, float lr, int* launches,
+                             cudaStream_t st) {
+  const LayerRT& L = s->ly[0];
+  const EmbPlan p = emb_plan(s->M, L.K, L.N);
+  const int n = (int)s->M;
+  const uint32_t *keys = nullptr, *rows = nullptr;
+  const int32_t* ids = (const int32_t*)s->x;
+  uint32_t* hist = (uint32_t*)s->at(L.off_hist);
+  {
+    TimedLaunch tl(s, ET_K_WGRAD, st);
+    for (int pass = 0; pass < p.passes; ++pass) {
+      uint32_t* ko = (uint32_t*)s->at(L.off_keys[pass & 1]);
+      uint32_t* ro = (uint32_t*)s->at(L.off_rows[pass & 1]);
+      const int shift = pass * p.bits;
+      et::sort_hist_kernel<<<p.tiles, et::kSortThreads, 0, st>>>(ids, keys, n, L.K, shift, p.bits, hist);
+      ET_TRY(after_launch());
+      et::sort_scan_kernel<<<1, 1024, 0, st>>>(hist, p.tiles << p.bits);
+      ET_TRY(after_launch());
+      et::sort_scatter_kernel<<<p.tiles, et::kSortThreads, 0, st>>>(ids, keys, rows, n, L.K, shift, p.bits, hist, ko, ro);
+      ET_TRY(after_launch());
+      keys = ko; rows = ro;
+      *launches += 3;
+    }
+  }
+  et::EmbSink<T> sink;
+  sink.grad = grad; sink.delta = delta; sink.W = (T*)L.W; sink.master = L.W32; sink.m_state = L.st1[0]; sink.v_state = L.st2[0];
+  sink.opt = opt_params(s, lr); sink.do_sgd = sgd ? 1 : 0; sink.delta_is_snapshot = s->delta_is_snapshot ? 1 : 0;
+  float* imp = delta != nullptr ? (float*)s->at(s->off_imp_parts) + s->imp_offs[0] : nullptr;
+  const int used = 2 * p.chunks * p.col_tiles;
+  if (imp != nullptr && used < L.imp_count_w) CU_TRY(cudaMemsetAsync(imp + used, 0, sizeof(float) * (L.imp_count_w - used), st));
+  float* part = (float*)s->at(L.off_epart);
+  const dim3 grid(p.chunks, p.col_tiles);
+  {
+    TimedLaunch tl(s, ET_K_WGRAD, st);
+    et::embed_grad_kernel<T><<<grid, p.threads, 0, st>>>(grad_act<T>(s, 1, dY), keys, rows, n, L.K, L.N, s->emb_scale, part, imp, sink);
+    ET_TRY(after_launch());
+  }
+  TimedLaunch tl(s, ET_K_WGRAD_REDUCE, st);
+  et::embed_join_kernel<T><<<grid, p.threads, 0, st>>>(keys, n, L.K, L.N, s->emb_scale, part,
+                                                       imp != nullptr ? imp + p.chunks * p.col_tiles : nullptr, sink);
+  ET_TRY(after_launch());
+  *launches += 2;
+  if (grad != nullptr || (sgd && sink.opt.kind != et::kOptSgd)) {
+    sink.delta = nullptr;                                   // the importance sum has no term there
+    et::embed_untouched_kernel<T><<<ceil_div(L.K, 8), 256, 0, st>>>(keys, n, L.K, L.N, sink);
+    ET_TRY(after_launch());
+    ++*launches;
+  }
+  return ET_OK;
+}
+
 // dW_l = a_l^T dZ_l as split partials, then the reducer with grad / importance / SGD.
 template <typename T>
 et_status run_wgrad_layer(et_stack* s, int l, const void* dY, float* grad, const T* delta, bool sgd, float lr,
@@ -974,7 +1062,7 @@ et_status check_ready(const et_stack* s, const uint8_t* mask, int n_tensors) {
   if (s == nullptr || mask == nullptr) return ET_ERR_INVALID_ARG;
   if (n_tensors != 2 * s->L) return ET_ERR_INVALID_ARG;
   for (int t = 0; t < n_tensors; ++t)
-    if (mask[t] && !s->ly[t / 2].trainable()) return ET_ERR_INVALID_ARG;   // nothing there to select
+    if (mask[t] && !s->ly[t / 2].has_tensor(t & 1)) return ET_ERR_INVALID_ARG;   // nothing there to select
   if (!s->bound) return ET_ERR_STATE;
   return ET_OK;
 }
@@ -1360,6 +1448,13 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
     if (two) CU_TRY(cudaEventRecord(s->chain_ev[L], cs));  // dZ_{L-1} is ready
     for (int l = L - 1; l >= d; --l) {
       const LayerRT& Y = s->ly[l];
+      if (Y.kind == ET_LAYER_EMBEDDING) {
+        if (!mask[2 * l]) continue;
+        if (two) CU_TRY(cudaStreamWaitEvent(st, s->chain_ev[l + 1], 0));   // G_1 is complete
+        ET_TRY(run_embed_backward<T>(s, dY, grads ? grads[0] : nullptr, delta ? (const T*)delta[0] : nullptr, sgd, lr,
+                                     &launches, st));
+        continue;
+      }
       const bool norm = Y.vector_params();
       const double gemm = Y.kind != ET_LAYER_DENSE ? 0.0 : 2.0 * (double)s->M * Y.K * Y.N;
       if (mask[2 * l + 1]) {
@@ -1549,7 +1644,7 @@ et_status forward_list(et_stack* s, const void* x, void* y, cudaStream_t st, boo
 template <typename T>
 et_status forward_impl(et_stack* s, const void* x, void* y, cudaStream_t st) {
   if constexpr (is_bf16<T>::value) {
-    if (s->x != x || !s->forwarded) ET_TRY(make_tmaps(&s->map_x, x, s->ly[0].K, s->M));
+    if ((s->x != x || !s->forwarded) && s->ly[0].kind != ET_LAYER_EMBEDDING) ET_TRY(make_tmaps(&s->map_x, x, s->ly[0].K, s->M));
     if (s->map_y_ptr != y) {
       ET_TRY(make_tmaps(&s->map_y, y, s->out_width(), s->M));
       s->map_y_ptr = y;
@@ -1566,6 +1661,7 @@ et_status forward_impl(et_stack* s, const void* x, void* y, cudaStream_t st) {
   for (int l = 0; l < s->L; ++l) {
     if (s->ly[l].kind == ET_LAYER_NORM) ET_TRY(run_norm_forward<T>(s, l, y, st));
     else if (s->ly[l].kind == ET_LAYER_BATCHNORM) ET_TRY(run_bn_forward<T>(s, l, y, st));
+    else if (s->ly[l].kind == ET_LAYER_EMBEDDING) ET_TRY(run_embed_forward<T>(s, y, st));
     else if (s->ly[l].kind == ET_LAYER_ATTENTION) ET_TRY(run_attn_forward(s, l, st));
     else if (s->ly[l].kind == ET_LAYER_IM2COL) { if (!s->ly[l].implicit) ET_TRY(run_im2col_forward<T>(s, l, st)); }
     else ET_TRY(run_forward_layer<T>(s, l, y, st));
@@ -1612,8 +1708,12 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     if (d.fold > 1 && d.act != ET_ACT_NONE) { err = ET_ERR_UNSUPPORTED; break; }
     y.K = d.in_features; y.N = d.out_features; y.fold = d.fold; y.Nw = d.out_features / d.fold;
     y.act = d.act; y.residual_src = d.residual_src;
-    if (d.kind < ET_LAYER_DENSE || d.kind > ET_LAYER_BATCHNORM) { err = ET_ERR_INVALID_ARG; break; }
+    if (d.kind < ET_LAYER_DENSE || d.kind > ET_LAYER_EMBEDDING) { err = ET_ERR_INVALID_ARG; break; }
     y.kind = d.kind; y.eps = d.eps;
+    if (y.kind == ET_LAYER_EMBEDDING) {
+      if (y.fold != 1 || y.act != ET_ACT_NONE || y.residual_src != -1) { err = ET_ERR_INVALID_ARG; break; }
+      if (l != 0) { err = ET_ERR_UNSUPPORTED; break; }
+    }
     if (y.kind == ET_LAYER_BATCHNORM) {
       if (y.K != y.N || y.fold != 1 || y.residual_src != -1 || !(y.eps >= 0.f)) { err = ET_ERR_INVALID_ARG; break; }
       if (y.N % 8) { err = ET_ERR_UNSUPPORTED; break; }
@@ -1649,6 +1749,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     if (d.residual_src < -1 || d.residual_src > l) { err = ET_ERR_INVALID_ARG; break; }
     if (d.residual_src >= 0) {
       if (width[d.residual_src] != y.Nw) { err = ET_ERR_SHAPE; break; }
+      if (d.residual_src == 0 && s->ly[0].kind == ET_LAYER_EMBEDDING) { err = ET_ERR_INVALID_ARG; break; }   // a_0 holds ids
       if (d.residual_src >= 1) {          // a_0's gradient is never formed, no bookkeeping needed
         LayerRT& src = s->ly[d.residual_src];
         if (src.consumer >= 0) { err = ET_ERR_UNSUPPORTED; break; }   // one skip consumer per activation
@@ -1656,7 +1757,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       }
     }
     if (dtype == ET_BF16) {
-      if (y.K % 8 || y.N % 8 || y.Nw % 8) { err = ET_ERR_UNSUPPORTED; break; }
+      if ((y.K % 8 && y.kind != ET_LAYER_EMBEDDING) || y.N % 8 || y.Nw % 8) { err = ET_ERR_UNSUPPORTED; break; }
       if (y.fold > 1 && y.Nw % 256) { err = ET_ERR_UNSUPPORTED; break; }
     }
   }
@@ -1703,6 +1804,14 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       y.off_stats = take((size_t)M * sizeof(float2));
       y.norm_blocks = std::min(ceil_div(M, et::kNormWarps), s->sms * 8);
       y.off_gpart = take((size_t)y.norm_blocks * y.N * sizeof(float));
+    } else if (y.kind == ET_LAYER_EMBEDDING) {
+      const EmbPlan p = emb_plan(M, y.K, y.N);
+      for (int k = 0; k < 2; ++k) {
+        y.off_keys[k] = take((size_t)M * sizeof(uint32_t));
+        y.off_rows[k] = take((size_t)M * sizeof(uint32_t));
+      }
+      y.off_hist = take(((size_t)p.tiles << p.bits) * sizeof(uint32_t));
+      y.off_epart = take((size_t)p.chunks * 2 * y.N * sizeof(float));
     } else if (dtype == ET_BF16) {
       const int kb_n = ceil_div(y.Nw, et::tc::BK) * y.fold;
       const TilePlan f = choose_tiles((int)M, y.Nw, ceil_div(y.K, et::tc::BK) * y.fold, s->sms, false, false, 0);
@@ -1748,6 +1857,16 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       s->imp_counts[2 * l] = s->imp_counts[2 * l + 1] = 0;
       continue;
     }
+    if (y.kind == ET_LAYER_EMBEDDING) {                    // partial importances: those of et_importance or of the two gradient kernels
+      const EmbPlan p = emb_plan(M, y.K, y.N);
+      const long long n = std::max<long long>(((long long)y.K * y.N + et::kEltThreads * et::kVec - 1) / (et::kEltThreads * et::kVec),
+                                              2ll * p.chunks * p.col_tiles);
+      if (n + imp_total > (1ll << 30)) { delete s; return ET_ERR_UNSUPPORTED; }
+      y.imp_count_w = (int)n; y.imp_count_b = 0;
+      s->imp_offs[2 * l] = imp_total; s->imp_counts[2 * l] = y.imp_count_w; imp_total += y.imp_count_w;
+      s->imp_offs[2 * l + 1] = imp_total; s->imp_counts[2 * l + 1] = 0;
+      continue;
+    }
     // Weight gradients that run persistently beside the error-gradient chain (dense masks) need not fill the
     // GPU by themselves: at most two splits keep the partial-sum traffic and the reducers small, the chain
     // takes the SMs they leave free (ViT-B full backprop 4.33 -> 4.02 ms; "as many splits as give every SM
@@ -1790,6 +1909,11 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     s->off_rtab = take((size_t)L * sizeof(et::ReduceEntry));
     s->off_btab = take((size_t)L * sizeof(et::BiasEntry));
   }
+  s->off_tok_stats = take((size_t)M * sizeof(float2));
+  s->off_tok_logp = take((size_t)M * sizeof(float));
+  s->off_tok_coef = take((size_t)M * sizeof(float));
+  s->off_tok_parts = take((size_t)M * 4 * sizeof(double));
+  s->off_norm_parts = take((size_t)clip_launches(2 * L) * s->sms * et::kClipBlocksPerSm * sizeof(double));
   s->ws_bytes = off;
   *out = s;
   return ET_OK;
@@ -1843,7 +1967,8 @@ et_status et_stack_bind(et_stack* s, void* const* W, void* const* b, void* works
   if (workspace_bytes < s->ws_bytes || ((uintptr_t)workspace & 255) != 0) return ET_ERR_WORKSPACE;
   for (int l = 0; l < s->L; ++l) {
     if (!s->ly[l].trainable()) continue;                  // no tensors: its pointers are ignored
-    if (W[l] == nullptr || b[l] == nullptr || ((uintptr_t)W[l] & 15) || ((uintptr_t)b[l] & 15)) return ET_ERR_INVALID_ARG;
+    if (W[l] == nullptr || ((uintptr_t)W[l] & 15)) return ET_ERR_INVALID_ARG;
+    if (s->ly[l].has_tensor(1) && (b[l] == nullptr || ((uintptr_t)b[l] & 15))) return ET_ERR_INVALID_ARG;
   }
   cudaStream_t st = (cudaStream_t)stream;
   s->bound = false;
@@ -1897,9 +2022,10 @@ et_status et_stack_bind_master(et_stack* s, float* const* W32, float* const* b32
   if ((W32 == nullptr) != (b32 == nullptr)) return ET_ERR_INVALID_ARG;
   if (W32 != nullptr)
     for (int l = 0; l < s->L; ++l)
-      if (s->ly[l].trainable() &&
-          (W32[l] == nullptr || b32[l] == nullptr || ((uintptr_t)W32[l] & 15) || ((uintptr_t)b32[l] & 15)))
-        return ET_ERR_INVALID_ARG;
+      for (int k = 0; k < 2; ++k) {
+        const float* p = s->ly[l].has_tensor(k) ? (k == 0 ? W32[l] : b32[l]) : nullptr;
+        if (s->ly[l].has_tensor(k) && (p == nullptr || ((uintptr_t)p & 15))) return ET_ERR_INVALID_ARG;
+      }
   for (int l = 0; l < s->L; ++l) {
     s->ly[l].W32 = W32 ? W32[l] : nullptr;
     s->ly[l].b32 = b32 ? b32[l] : nullptr;
@@ -1980,8 +2106,12 @@ et_status et_importance(et_stack* s, const uint8_t* mask, int32_t n_tensors, flo
     const LayerRT& y = s->ly[t / 2];
     const bool is_w = (t & 1) == 0;
     const size_t count = is_w ? y.w_count() : (size_t)y.N;
-    const int blocks = s->imp_counts[t];
+    int blocks = s->imp_counts[t];
     float* out = parts + s->imp_offs[t];
+    if (y.kind == ET_LAYER_EMBEDDING) {                    // it has more slots where the gradient kernels need more
+      blocks = ceil_div((long long)count, et::kEltThreads * et::kVec);
+      if (blocks < s->imp_counts[t]) CU_TRY(cudaMemsetAsync(out + blocks, 0, sizeof(float) * (s->imp_counts[t] - blocks), st));
+    }
     const bool wide = is_w && !y.vector_params();           // 8 elements per thread; gamma goes like a bias
     if (s->dtype == ET_BF16) {
       if (wide) et::importance_kernel<bf16, 8><<<blocks, et::kEltThreads, 0, st>>>(grads[t], (const bf16*)delta[t], count, out);
@@ -2015,8 +2145,12 @@ et_status et_tensor_metric(et_stack* s, const uint8_t* mask, int32_t n_tensors, 
     const LayerRT& y = s->ly[t / 2];
     const bool is_w = (t & 1) == 0;
     const size_t count = is_w ? y.w_count() : (size_t)y.N;
-    const int blocks = s->imp_counts[t];
+    int blocks = s->imp_counts[t];
     float* out = parts + s->imp_offs[t];
+    if (y.kind == ET_LAYER_EMBEDDING) {                    // it has more slots where the gradient kernels need more
+      blocks = ceil_div((long long)count, et::kEltThreads * et::kVec);
+      if (blocks < s->imp_counts[t]) CU_TRY(cudaMemsetAsync(out + blocks, 0, sizeof(float) * (s->imp_counts[t] - blocks), st));
+    }
     const bool wide = is_w && !y.vector_params();
     const float* f32 = kind == ET_METRIC_GRADIENT_MAGNITUDE ? grads[t] : (is_w ? y.W32 : y.b32);   // masters if attached
     const void* stored = is_w ? y.W : y.b;
@@ -2073,6 +2207,225 @@ et_status et_update_masked(et_stack* s, const uint8_t* mask, int32_t n_tensors, 
   return update_masked_impl(s, mask, n_tensors, grads, lr, stream, false);
 }
 
+et_status et_stack_set_embedding_scale(et_stack* s, float scale) {
+  if (s == nullptr || !std::isfinite(scale)) return ET_ERR_INVALID_ARG;
+  if (s->ly[0].kind != ET_LAYER_EMBEDDING) return ET_ERR_INVALID_ARG;
+  s->emb_scale = scale;
+  return ET_OK;
+}
+
+}  // extern "C"
+namespace {
+// The selected tensors in tables of at most kClipTensors; `go(table)` launches on one of them.
+template <typename F>
+et_status for_each_clip_table(et_stack* s, const uint8_t* mask, int n_tensors, float* const* grads, float* const* outs,
+                              bool update, F&& go) {
+  auto fill = [&](auto& tab, int cap, int& t) {
+    tab.n = 0;
+    tab.blocks = 0;
+    for (; t < n_tensors && tab.n < cap; ++t) {
+      if (!mask[t]) continue;
+      const LayerRT& y = s->ly[t / 2];
+      const bool is_w = (t & 1) == 0;
+      et::ClipEntry& e = tab.e[tab.n++];
+      e.g = grads[t];
+      e.out = outs != nullptr ? outs[t] : nullptr;
+      e.W = update ? (is_w ? y.W : y.b) : nullptr;
+      e.master = update ? (is_w ? y.W32 : y.b32) : nullptr;
+      e.m_state = update ? y.st1[t & 1] : nullptr;
+      e.v_state = update ? y.st2[t & 1] : nullptr;
+      e.count = is_w ? y.w_count() : (size_t)y.N;
+      e.block_begin = tab.blocks;
+      tab.blocks += (long long)((e.count + et::kClipBlock - 1) / et::kClipBlock);
+    }
+  };
+  int selected = 0;
+  for (int t = 0; t < n_tensors; ++t) selected += mask[t] ? 1 : 0;
+  int t = 0;
+  while (selected > 0) {
+    // a small table costs less to pass than a large one
+    if (selected <= 8) {
+      et::ClipTable<8> tab; fill(tab, 8, t);
+      ET_TRY(go(tab)); selected -= tab.n;
+    } else if (selected <= 64) {
+      et::ClipTable<64> tab; fill(tab, 64, t);
+      ET_TRY(go(tab)); selected -= tab.n;
+    } else {
+      et::ClipTable<kClipTensors> tab; fill(tab, kClipTensors, t);
+      ET_TRY(go(tab)); selected -= tab.n;
+    }
+  }
+  return ET_OK;
+}
+int clip_grid(const et_stack* s, long long blocks) {
+  return (int)std::max<long long>(1, std::min<long long>(blocks, (long long)s->sms * et::kClipBlocksPerSm));
+}
+et_status check_clip(const et_stack* s, const uint8_t* mask, int n_tensors, float* const* grads, float* const* outs) {
+  if (s == nullptr || mask == nullptr || grads == nullptr || outs == nullptr || n_tensors != 2 * s->L) return ET_ERR_INVALID_ARG;
+  for (int t = 0; t < n_tensors; ++t)
+    if (mask[t] && (grads[t] == nullptr || outs[t] == nullptr)) return ET_ERR_INVALID_ARG;
+  return check_ready(s, mask, n_tensors);
+}
+// Squares of every selected gradient into the workspace's partials; *n_parts of them.
+et_status run_sumsq(et_stack* s, const uint8_t* mask, int n_tensors, float* const* grads, int* n_parts, cudaStream_t st) {
+  double* parts = (double*)s->at(s->off_norm_parts);
+  *n_parts = 0;
+  return for_each_clip_table(s, mask, n_tensors, grads, nullptr, false, [&](const auto& tab) -> et_status {
+    constexpr int N = sizeof(tab.e) / sizeof(tab.e[0]);
+    const int grid = clip_grid(s, tab.blocks);
+    et::sumsq_kernel<N><<<grid, et::kClipThreads, 0, st>>>(tab, parts + *n_parts);
+    *n_parts += grid;
+    return after_launch();
+  });
+}
+}  // namespace
+extern "C" {
+
+et_status et_grad_norm(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float* norm_dev, void* stream) {
+  if (norm_dev == nullptr) return ET_ERR_INVALID_ARG;
+  ET_TRY(check_clip(s, mask, n_tensors, grads, grads));
+  cudaStream_t st = (cudaStream_t)stream;
+  TimedLaunch tl(s, ET_K_OTHER, st);
+  int n_parts = 0;
+  ET_TRY(run_sumsq(s, mask, n_tensors, grads, &n_parts, st));
+  et::norm_finalize_kernel<<<1, et::kClipThreads, 0, st>>>((const double*)s->at(s->off_norm_parts), n_parts, INFINITY, norm_dev);
+  return after_launch();
+}
+
+et_status et_clip_grads(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float* const* clipped,
+                        float max_norm, float* norm_dev, void* stream) {
+  if (!(max_norm > 0.f)) return ET_ERR_INVALID_ARG;
+  ET_TRY(check_clip(s, mask, n_tensors, grads, clipped));
+  cudaStream_t st = (cudaStream_t)stream;
+  TimedLaunch tl(s, ET_K_OTHER, st);
+  int n_parts = 0;
+  ET_TRY(run_sumsq(s, mask, n_tensors, grads, &n_parts, st));
+  const double* parts = (const double*)s->at(s->off_norm_parts);
+  if (n_parts == 0) {                                       // nothing selected: the norm is 0, the factor 1
+    if (norm_dev == nullptr) return ET_OK;
+    et::norm_finalize_kernel<<<1, et::kClipThreads, 0, st>>>(parts, 0, max_norm, norm_dev);
+    return after_launch();
+  }
+  return for_each_clip_table(s, mask, n_tensors, grads, clipped, false, [&](const auto& tab) -> et_status {
+    constexpr int N = sizeof(tab.e) / sizeof(tab.e[0]);
+    et::clip_kernel<N><<<clip_grid(s, tab.blocks), et::kClipThreads, 0, st>>>(tab, parts, n_parts, max_norm, norm_dev);
+    return after_launch();
+  });
+}
+
+et_status et_update_clipped(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float lr, float max_norm,
+                            float* norm_dev, void* stream) {
+  if (!(max_norm > 0.f)) return ET_ERR_INVALID_ARG;
+  ET_TRY(check_clip(s, mask, n_tensors, grads, grads));
+  cudaStream_t st = (cudaStream_t)stream;
+  TimedLaunch tl(s, ET_K_OTHER, st);
+  int n_parts = 0;
+  ET_TRY(run_sumsq(s, mask, n_tensors, grads, &n_parts, st));
+  const double* parts = (const double*)s->at(s->off_norm_parts);
+  if (n_parts == 0) {
+    if (norm_dev == nullptr) return ET_OK;
+    et::norm_finalize_kernel<<<1, et::kClipThreads, 0, st>>>(parts, 0, max_norm, norm_dev);
+    return after_launch();
+  }
+  const et::OptParams o = opt_params(s, lr);
+  return for_each_clip_table(s, mask, n_tensors, grads, nullptr, true, [&](const auto& tab) -> et_status {
+    constexpr int N = sizeof(tab.e) / sizeof(tab.e[0]);
+    const int grid = clip_grid(s, tab.blocks);
+    if (s->dtype == ET_BF16)
+      et::update_clipped_kernel<bf16, N><<<grid, et::kClipThreads, 0, st>>>(tab, parts, n_parts, max_norm, norm_dev, o);
+    else
+      et::update_clipped_kernel<float, N><<<grid, et::kClipThreads, 0, st>>>(tab, parts, n_parts, max_norm, norm_dev, o);
+    return after_launch();
+  });
+}
+
+// ---- losses on token logits --------------------------------------------------------------------
+}  // extern "C"
+namespace {
+et_status check_tokens(const et_stack* s, const void* y, const int32_t* targets, int32_t vocab, float scale, const void* dY,
+                       int32_t* vocab_out) {
+  if (s == nullptr || y == nullptr || targets == nullptr) return ET_ERR_INVALID_ARG;
+  if (((uintptr_t)y & 15) || ((uintptr_t)dY & 15)) return ET_ERR_INVALID_ARG;
+  if (vocab < 0 || vocab > s->out_width() || !(scale > 0.f) || !std::isfinite(scale)) return ET_ERR_INVALID_ARG;
+  *vocab_out = vocab == 0 ? s->out_width() : vocab;
+  return s->bound ? ET_OK : ET_ERR_STATE;
+}
+template <int MODE>
+et_status launch_tokens(et_stack* s, const et::tok::Args& a, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_OTHER, st);
+  if (s->dtype == ET_BF16) et::tok::token_row_kernel<bf16, MODE><<<(unsigned)s->M, 256, 0, st>>>(a);
+  else                     et::tok::token_row_kernel<float, MODE><<<(unsigned)s->M, 256, 0, st>>>(a);
+  return after_launch();
+}
+}  // namespace
+extern "C" {
+
+et_status et_token_logp(et_stack* s, const void* y, const int32_t* targets, int32_t vocab, float logit_scale, float* logp,
+                        void* stream) {
+  if (logp == nullptr) return ET_ERR_INVALID_ARG;
+  et::tok::Args a{};
+  ET_TRY(check_tokens(s, y, targets, vocab, logit_scale, nullptr, &a.vocab));
+  a.y = y; a.targets = targets; a.logp = logp; a.width = s->out_width(); a.scale = logit_scale; a.default_weight = 1.f;
+  return launch_tokens<et::tok::kScore>(s, a, (cudaStream_t)stream);
+}
+
+et_status et_loss_policy_grad(et_stack* s, const void* y, const int32_t* targets, const float* weights, const float* advantages,
+                              const float* logp_old, const float* logp_ref, const et_policy_config* cfg, void* dY,
+                              float* logp, float* loss_dev, void* stream) {
+  if (advantages == nullptr || cfg == nullptr) return ET_ERR_INVALID_ARG;
+  if (!(cfg->clip_low >= 0.f && cfg->clip_low <= 1.f) || !(cfg->clip_high >= 0.f) || !(cfg->kl_coef >= 0.f) ||
+      !std::isfinite(cfg->kl_coef))
+    return ET_ERR_INVALID_ARG;
+  if (cfg->kl_coef > 0.f && logp_ref == nullptr) return ET_ERR_INVALID_ARG;
+  if (dY == nullptr && logp == nullptr && loss_dev == nullptr) return ET_ERR_INVALID_ARG;
+  et::tok::Args a{};
+  ET_TRY(check_tokens(s, y, targets, cfg->vocab, cfg->logit_scale, dY, &a.vocab));
+  cudaStream_t st = (cudaStream_t)stream;
+  a.y = y; a.dY = dY; a.targets = targets; a.weights = weights; a.advantages = advantages; a.logp_old = logp_old;
+  a.logp_ref = logp_ref; a.logp = logp; a.parts = loss_dev != nullptr ? (double*)s->at(s->off_tok_parts) : nullptr;
+  a.width = s->out_width(); a.scale = cfg->logit_scale; a.default_weight = (float)(1.0 / (double)s->M);
+  a.clip_low = cfg->clip_low; a.clip_high = cfg->clip_high; a.kl_coef = cfg->kl_coef;
+  ET_TRY(launch_tokens<et::tok::kPolicy>(s, a, st));
+  if (loss_dev == nullptr) return ET_OK;
+  et::tok::policy_finalize_kernel<<<1, 1024, 0, st>>>(a.parts, (int)s->M, cfg->kl_coef, loss_dev);
+  return after_launch();
+}
+
+et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* targets, const float* weights,
+                                  const int32_t* seq_begin, int32_t pairs, const float* ref_logp,
+                                  const et_preference_config* cfg, void* dY, float* seq_logp, float* loss_dev, void* stream) {
+  if (seq_begin == nullptr || cfg == nullptr || pairs < 1) return ET_ERR_INVALID_ARG;
+  if (cfg->kind < ET_PREF_SIGMOID || cfg->kind > ET_PREF_HINGE) return ET_ERR_INVALID_ARG;
+  if (!(cfg->beta > 0.f) || !std::isfinite(cfg->beta)) return ET_ERR_INVALID_ARG;
+  if (!(cfg->label_smoothing >= 0.f && cfg->label_smoothing < 0.5f)) return ET_ERR_INVALID_ARG;
+  if (cfg->label_smoothing > 0.f && cfg->kind != ET_PREF_SIGMOID) return ET_ERR_UNSUPPORTED;
+  if (dY == nullptr && seq_logp == nullptr && loss_dev == nullptr) return ET_ERR_INVALID_ARG;
+  if (s != nullptr && pairs > s->M) return ET_ERR_TOO_LARGE;
+  et::tok::Args a{};
+  ET_TRY(check_tokens(s, y, targets, cfg->vocab, cfg->logit_scale, dY, &a.vocab));
+  cudaStream_t st = (cudaStream_t)stream;
+  a.y = y; a.targets = targets; a.weights = weights; a.width = s->out_width(); a.scale = cfg->logit_scale;
+  a.default_weight = 1.f;
+  a.logp = (float*)s->at(s->off_tok_logp);
+  a.stats = (float2*)s->at(s->off_tok_stats);
+  ET_TRY(launch_tokens<et::tok::kScore>(s, a, st));
+  float* coef = (float*)s->at(s->off_tok_coef);
+  CU_TRY(cudaMemsetAsync(coef, 0, sizeof(float) * (size_t)s->M, st));   // rows outside every sequence
+  et::tok::PairArgs p{};
+  p.logp = a.logp; p.weights = weights; p.targets = targets; p.begin = seq_begin; p.ref = ref_logp; p.seq_logp = seq_logp;
+  p.parts = (double*)s->at(s->off_tok_parts); p.coef = coef; p.rows = (int)s->M; p.pairs = pairs; p.vocab = a.vocab;
+  p.kind = cfg->kind; p.beta = cfg->beta; p.smoothing = cfg->label_smoothing;
+  et::tok::pair_kernel<<<pairs, 256, 0, st>>>(p);
+  ET_TRY(after_launch());
+  if (loss_dev != nullptr) {
+    et::tok::pair_finalize_kernel<<<1, 32, 0, st>>>(p.parts, pairs, loss_dev);
+    ET_TRY(after_launch());
+  }
+  if (dY == nullptr) return ET_OK;
+  a.dY = dY; a.coef = coef; a.logp = nullptr;
+  return launch_tokens<et::tok::kGrad>(s, a, st);
+}
+
 et_status et_stack_set_optimizer(et_stack* s, const et_optimizer_config* cfg, float* const* state1,
                                  float* const* state2) {
   if (s == nullptr) return ET_ERR_INVALID_ARG;
@@ -2086,7 +2439,7 @@ et_status et_stack_set_optimizer(et_stack* s, const et_optimizer_config* cfg, fl
     return ET_ERR_INVALID_ARG;
   const int n = 2 * s->L;
   for (int t = 0; t < n; ++t) {
-    if (!s->ly[t / 2].trainable()) continue;
+    if (!s->ly[t / 2].has_tensor(t & 1)) continue;
     if (c.kind != ET_OPT_SGD && (state1[t] == nullptr || ((uintptr_t)state1[t] & 15))) return ET_ERR_INVALID_ARG;
     if (c.kind == ET_OPT_ADAM && (state2[t] == nullptr || ((uintptr_t)state2[t] & 15))) return ET_ERR_INVALID_ARG;
   }
@@ -2141,7 +2494,8 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
     if (t_fwd != nullptr) *t_fwd = fwd;
     std::vector<uint8_t> ones(2 * L, 1);
     for (int l = 0; l < L; ++l)
-      if (!s->ly[l].trainable()) ones[2 * l] = ones[2 * l + 1] = 0;
+      for (int k = 0; k < 2; ++k)
+        if (!s->ly[l].has_tensor(k)) ones[2 * l + k] = 0;
     ET_TRY(et_backward_elastic(s, dY, ones.data(), 2 * L, nullptr, nullptr, nullptr, 0, 0.f, nullptr, stream));
     s->chain_shares_gpu = false;                              // the launches below run one at a time
     s->shared_plan = false;
@@ -2170,7 +2524,16 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
       struct AddCarried {
         double* slot; double v;
         ~AddCarried() { *slot += v; }
-      } add_carried{&t_dy[2 * l + 1], carried};
+      } add_carried{&t_dy[2 * l + (s->ly[l].has_tensor(1) ? 1 : 0)], carried};
+      if (s->ly[l].kind == ET_LAYER_EMBEDDING) {
+        // nothing lies below it: all of its backward time is the gradient of the table
+        t_dw[2 * l + 1] = 0.0;
+        if (s->dtype == ET_BF16)
+          ET_TRY(timed([&]() { return run_embed_backward<bf16>(s, dY, nullptr, nullptr, false, 0.f, &dummy, st); }, &t_dw[2 * l]));
+        else
+          ET_TRY(timed([&]() { return run_embed_backward<float>(s, dY, nullptr, nullptr, false, 0.f, &dummy, st); }, &t_dw[2 * l]));
+        continue;
+      }
       if (s->ly[l].kind == ET_LAYER_BATCHNORM) {
         // Section 5.2, its own subject: one black box, all of its backward time in t_dy of beta
         t_dw[2 * l] = 0.0; t_dw[2 * l + 1] = 0.0;

@@ -1,0 +1,163 @@
+// Global gradient norm over many tensors, clipping, and the masked update on clipped gradients.
+//   n = sqrt( sum over all selected tensors of g^2 ),   k = max_norm / n where n > max_norm, else 1
+// The squares are formed and added in 64 bits (fp32 squares leave fp32's range both ways: 1e20, 1e-25), in an order
+// that depends on the tensors' sizes and the grid alone.  The tensors of a launch are named by a table in the
+// kernel's parameters, so nothing is copied to the device and a captured graph replays it as it is.
+#pragma once
+
+#include "kernels.cuh"
+
+namespace et {
+
+constexpr int kClipThreads = 256;
+constexpr int kClipVec = 16;                                // elements per thread and block of work
+constexpr int kClipBlock = kClipThreads * kClipVec;         // elements of one block of work
+constexpr int kClipBlocksPerSm = 8;
+
+struct ClipEntry {
+  const float* g;
+  float* out;                // clipped copy (clip) -- or the optimiser's operands (update):
+  void* W;
+  float* master;
+  float* m_state;
+  float* v_state;
+  unsigned long long count;
+  long long block_begin;     // first block of work of this tensor in the launch
+};
+template <int N>
+struct ClipTable {
+  long long blocks;          // blocks of work of the launch
+  int n;
+  ClipEntry e[N];
+};
+
+template <int N>
+__device__ __forceinline__ int clip_find(const ClipTable<N>& t, long long vb) {
+  int lo = 0, hi = t.n - 1;
+  while (lo < hi) {                                         // last entry with block_begin <= vb
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.e[mid].block_begin <= vb) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// 64-bit block sum, fixed order; result valid in thread 0.
+__device__ __forceinline__ double block_sum64(double v) {
+  __shared__ double part[32];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double r = 0.0;
+  if (threadIdx.x == 0)
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) r += part[w];
+  return r;
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads)
+sumsq_kernel(const __grid_constant__ ClipTable<N> tab, double* __restrict__ parts) {
+  double acc = 0.0;
+  for (long long vb = blockIdx.x; vb < tab.blocks; vb += gridDim.x) {
+    const ClipEntry& e = tab.e[clip_find(tab, vb)];
+    const size_t i0 = (size_t)(vb - e.block_begin) * kClipBlock;
+    const float* g = e.g;
+    float v[kClipVec / 4][4];
+#pragma unroll
+    for (int q = 0; q < kClipVec / 4; ++q) {
+      const size_t i = i0 + ((size_t)q * kClipThreads + threadIdx.x) * 4;
+      const long long left = (long long)e.count - (long long)i;
+      load_seg<4>(g + i, left < 0 ? 0 : (int)min(left, 4ll), v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < kClipVec / 4; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc = fma((double)v[q][i], (double)v[q][i], acc);
+  }
+  acc = block_sum64(acc);
+  if (threadIdx.x == 0) parts[blockIdx.x] = acc;
+}
+
+// Every block sums the partials itself, in the same order: (norm, factor).  A norm that is not finite gives factor 0.
+__device__ __forceinline__ float2 norm_and_factor(const double* __restrict__ parts, int n, float max_norm) {
+  __shared__ float2 sh;
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) s += parts[i];
+  s = block_sum64(s);
+  if (threadIdx.x == 0) {
+    const double norm = sqrt(s);
+    const bool finite = norm <= 1.7976931348623157e308;     // false for NaN too
+    const double f = !finite ? 0.0 : norm > (double)max_norm ? (double)max_norm / norm : 1.0;
+    sh = make_float2((float)norm, (float)f);
+  }
+  __syncthreads();
+  return sh;
+}
+static __global__ void __launch_bounds__(kClipThreads)
+norm_finalize_kernel(const double* __restrict__ parts, int n, float max_norm, float* __restrict__ out) {
+  const float2 nf = norm_and_factor(parts, n, max_norm);
+  if (threadIdx.x == 0) { out[0] = nf.x; out[1] = nf.y; }
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads)
+clip_kernel(const __grid_constant__ ClipTable<N> tab, const double* __restrict__ parts, int n_parts, float max_norm,
+            float* __restrict__ norm_out) {
+  const float2 nf = norm_and_factor(parts, n_parts, max_norm);
+  const float f = nf.y;
+  if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = nf.x; norm_out[1] = f; }
+  for (long long vb = blockIdx.x; vb < tab.blocks; vb += gridDim.x) {
+    const ClipEntry& e = tab.e[clip_find(tab, vb)];
+    if (f == 1.0f && e.out == e.g) continue;                // in place and nothing to clip: nothing changes
+    const size_t i0 = (size_t)(vb - e.block_begin) * kClipBlock;
+    float v[kClipVec / 4][4];
+    int left[kClipVec / 4];
+#pragma unroll
+    for (int q = 0; q < kClipVec / 4; ++q) {
+      const size_t i = i0 + ((size_t)q * kClipThreads + threadIdx.x) * 4;
+      const long long l = (long long)e.count - (long long)i;
+      left[q] = l < 0 ? 0 : (int)min(l, 4ll);
+      if (f != 0.0f) load_seg<4>(e.g + i, left[q], v[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < kClipVec / 4; ++q) {
+      const size_t i = i0 + ((size_t)q * kClipThreads + threadIdx.x) * 4;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[q][j] = f != 0.0f ? v[q][j] * f : 0.0f;
+      store_seg<4>(e.out + i, left[q], v[q]);
+    }
+  }
+}
+
+// The optimiser step of et_update_masked on g * factor, every tensor in one launch.  A norm that is not finite leaves
+// weights and optimiser state as they are.
+template <typename T, int N>
+__global__ void __launch_bounds__(kClipThreads)
+update_clipped_kernel(const __grid_constant__ ClipTable<N> tab, const double* __restrict__ parts, int n_parts, float max_norm,
+                      float* __restrict__ norm_out, const OptParams opt) {
+  const float2 nf = norm_and_factor(parts, n_parts, max_norm);
+  const float f = nf.y;
+  if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = nf.x; norm_out[1] = f; }
+  if (!(nf.x <= 3.402823466e38f)) return;
+  for (long long vb = blockIdx.x; vb < tab.blocks; vb += gridDim.x) {
+    const ClipEntry& e = tab.e[clip_find(tab, vb)];
+#pragma unroll
+    for (int q = 0; q < kClipVec / 8; ++q) {
+      const size_t i0 = (size_t)(vb - e.block_begin) * kClipBlock + ((size_t)q * kClipThreads + threadIdx.x) * 8;
+      if (i0 >= e.count) continue;
+      const int n = (int)min((size_t)8, (size_t)e.count - i0);
+      float g[8], w[8];
+      load_seg<8>(e.g + i0, n, g);
+      if (e.master != nullptr) load_seg<8>(e.master + i0, n, w);
+      else load_seg<8>((const T*)e.W + i0, n, w);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[i] *= f;
+      opt_update_seg(w, g, opt, e.m_state, e.v_state, i0, n);
+      if (e.master != nullptr) store_seg<8>(e.master + i0, n, w);
+      store_seg<8>((T*)e.W + i0, n, w);
+    }
+  }
+}
+
+}  // namespace et

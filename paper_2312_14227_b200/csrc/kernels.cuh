@@ -84,6 +84,38 @@ __device__ __forceinline__ void wgrad_reduce_block(int block, const float* parti
     if (threadIdx.x == 0) imp_part[block] = dot;
   }
 }
+// What becomes of kVec consecutive elements of a finished gradient (n of them exist); returns their share of sum(g * dw).
+template <typename T>
+__device__ __forceinline__ float consume_grad(size_t i0, int n, const float (&g)[kVec], float* grad,
+                                              const T* __restrict__ delta, T* __restrict__ W, const OptParams& opt, int do_sgd,
+                                              int delta_is_snapshot, float* __restrict__ master, float* __restrict__ m_state,
+                                              float* __restrict__ v_state) {
+  float dot = 0.0f;
+  float t[kVec], w[kVec];
+  if (grad != nullptr) store_seg<kVec>(grad + i0, n, g);
+  if (do_sgd || (delta != nullptr && delta_is_snapshot)) {      // the current weight is needed
+    if (master != nullptr) load_seg<kVec>(master + i0, n, w);
+    else load_seg<kVec>(W + i0, n, w);
+  }
+  if (delta != nullptr) {
+    if (delta_is_snapshot) {                        // dw = current weight - weight at the window start
+      if (master != nullptr) load_seg<kVec>(reinterpret_cast<const float*>(delta) + i0, n, t);
+      else load_seg<kVec>(delta + i0, n, t);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) t[i] = w[i] - t[i];
+    } else {
+      load_seg<kVec>(delta + i0, n, t);
+    }
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) dot = fmaf(g[i], t[i], dot);
+  }
+  if (do_sgd) {
+    opt_update_seg(w, g, opt, m_state, v_state, i0, n);
+    if (master != nullptr) store_seg<kVec>(master + i0, n, w);
+    store_seg<kVec>(W + i0, n, w);
+  }
+  return dot;
+}
 // The work on kVec consecutive elements starting at i0 < count; returns their share of sum(g * dw).
 template <typename T>
 __device__ __forceinline__ float wgrad_reduce_elems(size_t i0, const float* partial, int splits, size_t split_stride,
@@ -94,35 +126,14 @@ __device__ __forceinline__ float wgrad_reduce_elems(size_t i0, const float* part
   float dot = 0.0f;
   {
     const int n = (int)min((size_t)kVec, count - i0);
-    float g[kVec], t[kVec], w[kVec];
+    float g[kVec], t[kVec];
     load_seg<kVec>(partial + i0, n, g);
     for (int s = 1; s < splits; ++s) {
       load_seg<kVec>(partial + (size_t)s * split_stride + i0, n, t);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) g[i] += t[i];
     }
-    if (grad != nullptr) store_seg<kVec>(grad + i0, n, g);
-    if (do_sgd || (delta != nullptr && delta_is_snapshot)) {      // the current weight is needed
-      if (master != nullptr) load_seg<kVec>(master + i0, n, w);
-      else load_seg<kVec>(W + i0, n, w);
-    }
-    if (delta != nullptr) {
-      if (delta_is_snapshot) {                        // dw = current weight - weight at the window start
-        if (master != nullptr) load_seg<kVec>(reinterpret_cast<const float*>(delta) + i0, n, t);
-        else load_seg<kVec>(delta + i0, n, t);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) t[i] = w[i] - t[i];
-      } else {
-        load_seg<kVec>(delta + i0, n, t);
-      }
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) dot = fmaf(g[i], t[i], dot);
-    }
-    if (do_sgd) {
-      opt_update_seg(w, g, opt, m_state, v_state, i0, n);
-      if (master != nullptr) store_seg<kVec>(master + i0, n, w);
-      store_seg<kVec>(W + i0, n, w);
-    }
+    dot = consume_grad<T>(i0, n, g, grad, delta, W, opt, do_sgd, delta_is_snapshot, master, m_state, v_state);
   }
   return dot;
 }

@@ -28,6 +28,9 @@ DT_F32, DT_BF16 = 0, 1
 # layer kinds: a dense layer (kernel, bias) or a layer normalisation over the feature axis, whose two
 # trainable tensors gamma and beta take the kernel and bias slots (Section 5.2: Gamma and Beta)
 KIND_DENSE, KIND_NORM, KIND_ATTENTION, KIND_IM2COL, KIND_BATCHNORM = 0, 1, 2, 3, 4
+KIND_EMBEDDING = 5
+# KIND_EMBEDDING: lookup of token ids in a table [in_features x out_features] (the kernel slot; the bias slot is
+# empty), layer 0 only
 # KIND_BATCHNORM: batch normalisation in training mode (statistics of each feature over all rows), optional
 # activation after it; Gamma and Beta in the kernel and bias slots like KIND_NORM (Section 5.2)
 # KIND_IM2COL: the patch-gathering half of a k x k convolution (stride 1, zero padding k // 2) on NHWC
@@ -51,6 +54,7 @@ class Layer:
     height: int = 0            # KIND_IM2COL: rows are images of height x width pixels (row = (n, h, w)),
     width: int = 0             #   in_features = channels, out_features = ksize * ksize * channels,
     ksize: int = 0             #   column (kh * ksize + kw) * channels + c holds pixel (h + kh - k//2, w + kw - k//2)
+    scale: float = 1.0         # KIND_EMBEDDING: factor of the looked-up rows
 
     @property
     def out_width(self) -> int:
@@ -132,6 +136,10 @@ def vit_blocks(n_blocks: int, d: int, ffn: int) -> List[Layer]:
 
 def norm_layer(d: int, eps: float = 1e-5) -> Layer:
     return Layer(d, d, kind=KIND_NORM, eps=eps)
+
+
+def embedding_layer(vocab: int, d: int, scale: float = 1.0) -> Layer:
+    return Layer(vocab, d, kind=KIND_EMBEDDING, scale=scale)
 
 
 def batchnorm_layer(d: int, act: int = ACT_NONE, eps: float = 1e-5) -> Layer:

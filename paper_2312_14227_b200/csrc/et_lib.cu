@@ -34,6 +34,7 @@ std::atomic<long long> g_launches{0};
 std::atomic<int> g_guard_regions{0};      // et_debug_guard_regions: stacks created from now on get guard words
 constexpr size_t kGuardBytes = 256;
 constexpr unsigned char kGuardByte = 0xA5;
+constexpr int kDoneWord = 32;             // word of the status region (zeroed by et_stack_bind) that counts finished blocks
 
 #define CU_TRY(expr)                                   \
   do {                                                 \
@@ -2347,15 +2348,59 @@ et_status check_tokens(const et_stack* s, const void* y, const int32_t* targets,
   if (s == nullptr || y == nullptr || targets == nullptr) return ET_ERR_INVALID_ARG;
   if (((uintptr_t)y & 15) || ((uintptr_t)dY & 15)) return ET_ERR_INVALID_ARG;
   if (vocab < 0 || vocab > s->out_width() || !(scale > 0.f) || !std::isfinite(scale)) return ET_ERR_INVALID_ARG;
+  if (s->out_width() > (1 << 30)) return ET_ERR_UNSUPPORTED;               // 32-bit columns, a block's stride beyond the row
   *vocab_out = vocab == 0 ? s->out_width() : vocab;
   return s->bound ? ET_OK : ET_ERR_STATE;
+}
+// The arguments every token kernel shares.
+void token_args(const et_stack* s, et::tok::Args* a, const void* y, const int32_t* targets, float scale) {
+  a->y = y; a->targets = targets; a->rows = (int)s->M; a->width = s->out_width(); a->scale = scale;
+  const double k = (double)scale * 1.4426950408889634074;                 // log2(e)
+  float hi = (float)k;
+  if ((double)hi > k) hi = std::nextafterf(hi, 0.0f);
+  a->k_hi = hi;
+  a->k_lo = std::max((float)(k - (double)hi), 1e-30f);                      // > 0: keeps -inf at -inf
+  a->done = (uint32_t*)s->at(s->off_status) + kDoneWord;
+}
+template <typename T, int MODE, int THREADS, int NV>
+et_status launch_held(const et::tok::Args& a, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)a.rows * (unsigned)a.slices);
+  cfg.blockDim = dim3(THREADS);
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)a.slices;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = a.slices > 1 ? 1 : 0;
+  CU_TRY(cudaLaunchKernelEx(&cfg, et::tok::token_held_kernel<T, MODE, THREADS, NV>, a));
+  return after_launch();
+}
+template <typename T, int MODE>
+et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
+  constexpr int N = et::tok::VecOf<T>::N;
+  // 16-byte vectors of a row: the logits alone where nothing is written; one more where rows begin inside a vector
+  const int cols = a.dY != nullptr ? a.width : a.vocab;
+  const int vecs = ceil_div(cols, N) + (a.width % N != 0 ? 1 : 0);
+  const int cap = 512 * 8;                                                  // vectors a block can hold
+  int slices = 1;
+  while (slices < 8 && slices * cap < vecs) slices *= 2;
+  if (slices * cap < vecs) {
+    et::tok::token_row_kernel<T, MODE><<<(unsigned)a.rows, 512, 0, st>>>(a);
+    return after_launch();
+  }
+  a.slices = slices;
+  a.per = ceil_div(vecs, slices);
+  if (a.per <= 128 * 2) return launch_held<T, MODE, 128, 2>(a, st);
+  if (a.per <= 256 * 4) return launch_held<T, MODE, 256, 4>(a, st);
+  if (a.per <= 256 * 8) return launch_held<T, MODE, 256, 8>(a, st);
+  return launch_held<T, MODE, 512, 8>(a, st);
 }
 template <int MODE>
 et_status launch_tokens(et_stack* s, const et::tok::Args& a, cudaStream_t st) {
   TimedLaunch tl(s, ET_K_OTHER, st);
-  if (s->dtype == ET_BF16) et::tok::token_row_kernel<bf16, MODE><<<(unsigned)s->M, 256, 0, st>>>(a);
-  else                     et::tok::token_row_kernel<float, MODE><<<(unsigned)s->M, 256, 0, st>>>(a);
-  return after_launch();
+  return s->dtype == ET_BF16 ? launch_tokens_t<bf16, MODE>(s, a, st) : launch_tokens_t<float, MODE>(s, a, st);
 }
 }  // namespace
 extern "C" {
@@ -2365,7 +2410,8 @@ et_status et_token_logp(et_stack* s, const void* y, const int32_t* targets, int3
   if (logp == nullptr) return ET_ERR_INVALID_ARG;
   et::tok::Args a{};
   ET_TRY(check_tokens(s, y, targets, vocab, logit_scale, nullptr, &a.vocab));
-  a.y = y; a.targets = targets; a.logp = logp; a.width = s->out_width(); a.scale = logit_scale; a.default_weight = 1.f;
+  token_args(s, &a, y, targets, logit_scale);
+  a.logp = logp; a.default_weight = 1.f;
   return launch_tokens<et::tok::kScore>(s, a, (cudaStream_t)stream);
 }
 
@@ -2381,14 +2427,12 @@ et_status et_loss_policy_grad(et_stack* s, const void* y, const int32_t* targets
   et::tok::Args a{};
   ET_TRY(check_tokens(s, y, targets, cfg->vocab, cfg->logit_scale, dY, &a.vocab));
   cudaStream_t st = (cudaStream_t)stream;
-  a.y = y; a.dY = dY; a.targets = targets; a.weights = weights; a.advantages = advantages; a.logp_old = logp_old;
-  a.logp_ref = logp_ref; a.logp = logp; a.parts = loss_dev != nullptr ? (double*)s->at(s->off_tok_parts) : nullptr;
-  a.width = s->out_width(); a.scale = cfg->logit_scale; a.default_weight = (float)(1.0 / (double)s->M);
+  token_args(s, &a, y, targets, cfg->logit_scale);
+  a.dY = dY; a.weights = weights; a.advantages = advantages; a.logp_old = logp_old; a.logp_ref = logp_ref; a.logp = logp;
+  a.parts = loss_dev != nullptr ? (double*)s->at(s->off_tok_parts) : nullptr; a.out = loss_dev;
+  a.default_weight = (float)(1.0 / (double)s->M);
   a.clip_low = cfg->clip_low; a.clip_high = cfg->clip_high; a.kl_coef = cfg->kl_coef;
-  ET_TRY(launch_tokens<et::tok::kPolicy>(s, a, st));
-  if (loss_dev == nullptr) return ET_OK;
-  et::tok::policy_finalize_kernel<<<1, 1024, 0, st>>>(a.parts, (int)s->M, cfg->kl_coef, loss_dev);
-  return after_launch();
+  return launch_tokens<et::tok::kPolicy>(s, a, st);
 }
 
 et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* targets, const float* weights,
@@ -2404,26 +2448,33 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   et::tok::Args a{};
   ET_TRY(check_tokens(s, y, targets, cfg->vocab, cfg->logit_scale, dY, &a.vocab));
   cudaStream_t st = (cudaStream_t)stream;
-  a.y = y; a.targets = targets; a.weights = weights; a.width = s->out_width(); a.scale = cfg->logit_scale;
+  token_args(s, &a, y, targets, cfg->logit_scale);
+  a.weights = weights;
   a.default_weight = 1.f;
   a.logp = (float*)s->at(s->off_tok_logp);
   a.stats = (float2*)s->at(s->off_tok_stats);
+  a.coef = (float*)s->at(s->off_tok_coef);                   // set to 0: rows of no sequence keep it
   ET_TRY(launch_tokens<et::tok::kScore>(s, a, st));
-  float* coef = (float*)s->at(s->off_tok_coef);
-  CU_TRY(cudaMemsetAsync(coef, 0, sizeof(float) * (size_t)s->M, st));   // rows outside every sequence
   et::tok::PairArgs p{};
   p.logp = a.logp; p.weights = weights; p.targets = targets; p.begin = seq_begin; p.ref = ref_logp; p.seq_logp = seq_logp;
-  p.parts = (double*)s->at(s->off_tok_parts); p.coef = coef; p.rows = (int)s->M; p.pairs = pairs; p.vocab = a.vocab;
-  p.kind = cfg->kind; p.beta = cfg->beta; p.smoothing = cfg->label_smoothing;
-  et::tok::pair_kernel<<<pairs, 256, 0, st>>>(p);
-  ET_TRY(after_launch());
-  if (loss_dev != nullptr) {
-    et::tok::pair_finalize_kernel<<<1, 32, 0, st>>>(p.parts, pairs, loss_dev);
+  p.parts = (double*)s->at(s->off_tok_parts); p.done = a.done; p.out = loss_dev; p.coef = a.coef; p.rows = (int)s->M;
+  p.pairs = pairs; p.vocab = a.vocab; p.kind = cfg->kind; p.beta = cfg->beta; p.smoothing = cfg->label_smoothing;
+  {
+    TimedLaunch tl(s, ET_K_OTHER, st);
+    et::tok::pair_kernel<<<pairs, 256, 0, st>>>(p);
     ET_TRY(after_launch());
   }
   if (dY == nullptr) return ET_OK;
-  a.dY = dY; a.coef = coef; a.logp = nullptr;
-  return launch_tokens<et::tok::kGrad>(s, a, st);
+  a.dY = dY;
+  const int vec_elems = s->dtype == ET_BF16 ? 8 : 4;
+  const int vecs = ceil_div(a.width, vec_elems) + (a.width % vec_elems != 0 ? 1 : 0);
+  a.slices = ceil_div(vecs, et::tok::kGradThreads * et::tok::kGradVecs);
+  const long long blocks = (long long)a.rows * a.slices;
+  if (blocks > 0x7fffffffll) return ET_ERR_TOO_LARGE;
+  TimedLaunch tl(s, ET_K_OTHER, st);
+  if (s->dtype == ET_BF16) et::tok::token_grad_kernel<bf16><<<(unsigned)blocks, et::tok::kGradThreads, 0, st>>>(a);
+  else                     et::tok::token_grad_kernel<float><<<(unsigned)blocks, et::tok::kGradThreads, 0, st>>>(a);
+  return after_launch();
 }
 
 et_status et_stack_set_optimizer(et_stack* s, const et_optimizer_config* cfg, float* const* state1,

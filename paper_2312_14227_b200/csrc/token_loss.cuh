@@ -13,12 +13,31 @@
 namespace et {
 namespace tok {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-
 __device__ __forceinline__ float exp2_fast(float x) {      // ex2.approx: 2 ulp, 0 for -inf and underflow
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Two fp32 values in one 64-bit register: one instruction for both (add / mul / fma .f32x2).
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
 
@@ -33,24 +52,33 @@ struct Args {
   const float* logp_old;      // kPolicy; null: the current log probability (ratio 1)
   const float* logp_ref;      // kPolicy; null: no KL term
   float* logp;                // lp of each row, 0 where the row is left out; may be null
-  float2* stats;              // kScore writes, kGrad reads: (max of the row's y, 1 / sum exp2((y - max) k))
-  const float* coef;          // kGrad: c_i
+  float2* stats;              // kScore writes, kGrad reads: (max of the row's y, 1 / sum exp(scale (y - max))); may be null
+  float* coef;                // kGrad: c_i.  kScore sets it to 0 where it is not null
   double* parts;              // kPolicy: rows x 3: w * (-surrogate), w * kl, w * [clipped]; may be null
-  int32_t width, vocab;
+  uint32_t* done;             // kPolicy with parts: blocks that have finished; 0 between calls
+  float* out;                 // kPolicy with parts: {loss, policy part, kl part, clipped share}
+  int32_t rows, width, vocab;
+  int32_t slices, per;        // blocks (of one cluster) that share a row, 16-byte vectors of each
   float scale;
+  float k_hi, k_lo;           // scale * log2(e) as a sum: k_hi rounded towards 0, k_lo > 0 the rest
   float default_weight;
   float clip_low, clip_high, kl_coef;
 };
+// exp(scale d) for two differences d <= 0.  One fp32 constant for scale * log2(e) would be off by up to 2^-24 of it, the same
+// way in every term of every row: a bias of the log of the sum that sums over rows do not average out.  k_lo > 0 keeps
+// d = -inf at -inf (a negative or zero k_lo would make it NaN).
+__device__ __forceinline__ uint64_t scale2(uint64_t d, uint64_t k_hi, uint64_t k_lo) { return fma2(d, k_lo, mul2(d, k_hi)); }
+__device__ __forceinline__ float exp_diff(float d, const Args& a) { return exp2_fast(fmaf(d, a.k_lo, d * a.k_hi)); }
 
-// (max, sum) of a block's rows: all threads get the pair.  A thread without elements holds (-inf, 0).
-__device__ __forceinline__ void block_max_sum(float& m, float& s, float k) {
+// (max, sum) over a block: all threads get the pair.  A thread without elements holds (-inf, 0).
+__device__ __forceinline__ void block_max_sum(float& m, float& s, const Args& a) {
   __shared__ float sm[32], ss[32];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
   float wm = m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
   // fmaxf drops NaN; the sum carries it
-  float ws = m == -INFINITY ? s : s * exp2_fast((m - wm) * k);
+  float ws = m == -INFINITY ? s : s * exp_diff(m - wm, a);
   ws = warp_sum(ws);
   __syncthreads();
   if (lane == 0) { sm[wid] = wm; ss[wid] = ws; }
@@ -60,7 +88,7 @@ __device__ __forceinline__ void block_max_sum(float& m, float& s, float k) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
   float bs = lane < nw ? ss[lane] : 0.0f;
-  if (own != -INFINITY) bs *= exp2_fast((own - bm) * k);
+  if (own != -INFINITY) bs *= exp_diff(own - bm, a);
   s = warp_sum(bs);
   m = bm;
 }
@@ -68,104 +96,48 @@ __device__ __forceinline__ void block_max_sum(float& m, float& s, float k) {
 // d loss / d lp of a row of the policy loss, and its contributions to the reported sums.
 //   r = exp(lp - old),  surrogate = min(r A, clip(r, 1 - lo, 1 + hi) A),  kl = exp(d) - 1 - d with d = ref - lp
 // The clipped branch is constant in lp; at a tie the unclipped one counts.
-__device__ __forceinline__ float policy_coef(const Args& a, int row, float lp, float w, double* part) {
-  const float adv = a.advantages[row];
-  const float r = a.logp_old != nullptr ? expf(lp - a.logp_old[row]) : 1.0f;
+struct RowTerms { float adv, old, ref; };
+__device__ __forceinline__ RowTerms row_terms(const Args& a, int row) {
+  RowTerms r;
+  r.adv = a.advantages[row];
+  r.old = a.logp_old != nullptr ? a.logp_old[row] : 0.0f;
+  r.ref = a.logp_ref != nullptr ? a.logp_ref[row] : 0.0f;
+  return r;
+}
+__device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, float lp, float w, double* part) {
+  const float r = a.logp_old != nullptr ? expf(lp - t.old) : 1.0f;
   const float rc = fminf(fmaxf(r, 1.0f - a.clip_low), 1.0f + a.clip_high);
-  const bool clipped = r * adv > rc * adv;
-  float slope = clipped ? 0.0f : -adv * r;
+  const bool clipped = r * t.adv > rc * t.adv;
+  float slope = clipped ? 0.0f : -t.adv * r;
   float kl = 0.0f;
   if (a.logp_ref != nullptr) {
-    const float d = a.logp_ref[row] - lp, e = expm1f(d);
+    const float d = t.ref - lp, e = expm1f(d);
     kl = e - d;
     slope -= a.kl_coef * e;
   }
-  part[0] = -(double)w * (double)((clipped ? rc : r) * adv);
-  part[1] = (double)w * (double)kl;
-  part[2] = clipped ? (double)w : 0.0;
+  if (part != nullptr) {
+    part[0] = -(double)w * (double)((clipped ? rc : r) * t.adv);
+    part[1] = (double)w * (double)kl;
+    part[2] = clipped ? (double)w : 0.0;
+  }
   return w * slope;
 }
 
-// One block per row, two passes over the row: (max, sum) first, the gradient from a second read.
-template <typename T, int MODE>
-__global__ void __launch_bounds__(256)
-token_row_kernel(const Args a) {
-  constexpr int V = 8;
-  const int row = blockIdx.x;
-  const size_t base = (size_t)row * a.width;
-  const T* y = (const T*)a.y + base;
-  T* dY = a.dY != nullptr ? (T*)a.dY + base : nullptr;
-  const int t = a.targets[row];
-  const float w = a.weights != nullptr ? a.weights[row] : a.default_weight;
-  const bool live = w != 0.0f && t >= 0 && t < a.vocab && (MODE != kGrad || a.coef[row] != 0.0f);
-  const float k = a.scale * kLog2e;
-  float c = 0.0f, m = 0.0f, inv = 0.0f;
-  if (live) {
-    if constexpr (MODE == kGrad) {
-      const float2 st = a.stats[row];
-      m = st.x; inv = st.y;
-      c = a.coef[row];
-    } else {
-      m = -INFINITY;
-      float s = 0.0f;
-      for (int j = threadIdx.x * V; j < a.vocab; j += blockDim.x * V) {
-        float v[V];
-        const int n = min(V, a.vocab - j);
-        load_seg<V>(y + j, n, v);
-        float cm = m;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (i < n) cm = fmaxf(cm, v[i]);
-        if (cm != m) { s *= m == -INFINITY ? 0.0f : exp2_fast((m - cm) * k); m = cm; }
-        const float ref = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (i < n) s += exp2_fast((v[i] - ref) * k);
-      }
-      block_max_sum(m, s, k);
-      inv = 1.0f / s;
-      const float lp = kLn2 * ((to_f32(y[t]) - m) * k - log2f(s));
-      if (MODE == kPolicy) {
-        double part[3];
-        c = policy_coef(a, row, lp, w, part);
-        if (threadIdx.x == 0 && a.parts != nullptr)
-          for (int q = 0; q < 3; ++q) a.parts[(size_t)row * 3 + q] = part[q];
-      }
-      if (threadIdx.x == 0) {
-        if (a.logp != nullptr) a.logp[row] = lp;
-        if (a.stats != nullptr) a.stats[row] = make_float2(m, inv);
-      }
-      if (MODE == kPolicy && dY == (T*)y) __syncthreads();     // y[t] is read before it is overwritten
-    }
-  } else if (threadIdx.x == 0) {
-    if (MODE != kGrad && a.logp != nullptr) a.logp[row] = 0.0f;
-    if (MODE == kPolicy && a.parts != nullptr)
-      for (int q = 0; q < 3; ++q) a.parts[(size_t)row * 3 + q] = 0.0;
-  }
-  if (MODE == kScore || dY == nullptr) return;
-  const float cs = c * a.scale;
-  const float g = -cs * inv;
-  for (int j = threadIdx.x * V; j < a.width; j += blockDim.x * V) {
-    float v[V];
-    const int n = min(V, a.width - j);
-    if (live) load_seg<V>(y + j, n, v);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float p = exp2_fast((v[i] - m) * k);
-      v[i] = live && j + i < a.vocab ? fmaf(g, p, j + i == t ? cs : 0.0f) : 0.0f;
-    }
-    store_seg<V>(dY + j, n, v);
-  }
-}
-
-// Sums of the policy loss's row contributions, in a fixed order: out = {loss, policy part, kl part, clipped share}.
-static __global__ void __launch_bounds__(1024)
-policy_finalize_kernel(const double* __restrict__ parts, int rows, float kl_coef, float* __restrict__ out) {
+// Sums of the policy loss's row contributions by the block that finishes last, in a fixed order.
+__device__ __forceinline__ void policy_finish(const Args& a) {
+  __shared__ bool last;
   __shared__ double sh[3][32];
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = atomicAdd(a.done, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
   double s[3] = {0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < rows; i += blockDim.x)
+  for (int i = threadIdx.x; i < a.rows; i += blockDim.x)
 #pragma unroll
-    for (int q = 0; q < 3; ++q) s[q] += parts[(size_t)i * 3 + q];
+    for (int q = 0; q < 3; ++q) s[q] += __ldcg(a.parts + (size_t)i * 3 + q);
 #pragma unroll
   for (int q = 0; q < 3; ++q) {
 #pragma unroll
@@ -179,8 +151,334 @@ policy_finalize_kernel(const double* __restrict__ parts, int rows, float kl_coef
       r[q] = 0.0;
       for (int wq = 0; wq < (int)(blockDim.x >> 5); ++wq) r[q] += sh[q][wq];
     }
-    out[0] = (float)(r[0] + (double)kl_coef * r[1]);
-    out[1] = (float)r[0]; out[2] = (float)r[1]; out[3] = (float)r[2];
+    a.out[0] = (float)(r[0] + (double)a.kl_coef * r[1]);
+    a.out[1] = (float)r[0]; a.out[2] = (float)r[1]; a.out[3] = (float)r[2];
+    *a.done = 0u;
+  }
+}
+
+// ---- 16-byte vectors of a row ------------------------------------------------------------------
+// y's base is 16-byte aligned; a row of fp32 may begin inside a vector.  Vector v of a row covers its elements
+// v * N - mis .. + N - 1, mis = elements of the row's first vector that belong to the row before.  Vectors that lie in the row
+// whole are moved whole, the others element by element, so that no element of another row is read or written.
+template <typename T> struct VecOf;
+template <> struct VecOf<float> {
+  static constexpr int N = 4;
+  static constexpr uint32_t kNegInf = 0xff800000u;
+  static __device__ __forceinline__ float max_of(const uint4& q) {
+    return fmaxf(fmaxf(__uint_as_float(q.x), __uint_as_float(q.y)), fmaxf(__uint_as_float(q.z), __uint_as_float(q.w)));
+  }
+  static __device__ __forceinline__ void pairs(const uint4& q, uint64_t (&p)[2]) {
+    p[0] = pack2(__uint_as_float(q.x), __uint_as_float(q.y));
+    p[1] = pack2(__uint_as_float(q.z), __uint_as_float(q.w));
+  }
+  static __device__ __forceinline__ uint4 from_pairs(const uint64_t (&p)[2]) {
+    float a, b, c, d;
+    unpack2(p[0], a, b);
+    unpack2(p[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+  }
+};
+template <> struct VecOf<bf16> {
+  static constexpr int N = 8;
+  static constexpr uint32_t kNegInf = 0xff80ff80u;
+  static __device__ __forceinline__ float max_of(const uint4& q) {
+    auto h = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+    const __nv_bfloat162 m = __hmax2(__hmax2(h(q.x), h(q.y)), __hmax2(h(q.z), h(q.w)));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  static __device__ __forceinline__ void pairs(const uint4& q, uint64_t (&p)[4]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  static __device__ __forceinline__ uint4 from_pairs(const uint64_t (&p)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b;
+      unpack2(p[i], a, b);
+      w[i] = pack_bf16x2(a, b);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+// Loads are read once and stores written once: both with the streaming hint.
+template <typename T>
+__device__ __forceinline__ uint4 load_vec(const T* row, int e0, int vocab) {
+  constexpr int N = VecOf<T>::N;
+  if (e0 >= 0 && e0 + N <= vocab) return __ldcs(reinterpret_cast<const uint4*>(row + e0));
+  uint4 q = make_uint4(VecOf<T>::kNegInf, VecOf<T>::kNegInf, VecOf<T>::kNegInf, VecOf<T>::kNegInf);
+  T* h = reinterpret_cast<T*>(&q);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (e0 + i >= 0 && e0 + i < vocab) h[i] = row[e0 + i];
+  return q;
+}
+template <typename T>
+__device__ __forceinline__ void store_vec(T* row, int e0, int width, int vocab, uint4 q) {
+  constexpr int N = VecOf<T>::N;
+  if (e0 >= 0 && e0 + N <= vocab) {
+    __stcs(reinterpret_cast<uint4*>(row + e0), q);
+    return;
+  }
+  const T* h = reinterpret_cast<const T*>(&q);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (e0 + i >= 0 && e0 + i < width) row[e0 + i] = e0 + i < vocab ? h[i] : from_f32<T>(0.0f);
+}
+// g p + [j = t] c, p = exp(scale (y - m)) / sum, g = -c / sum, for one vector.
+template <typename T>
+__device__ __forceinline__ uint4 grad_vec(const uint4& q, float m, float g, float c, int hit /* t - e0 */, const Args& a) {
+  constexpr int P = VecOf<T>::N / 2;
+  uint64_t p[P];
+  VecOf<T>::pairs(q, p);
+  const uint64_t nm = pack2(-m, -m), kh = pack2(a.k_hi, a.k_hi), kl = pack2(a.k_lo, a.k_lo), gg = pack2(g, g);
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    float x, y;
+    unpack2(scale2(add2(p[i], nm), kh, kl), x, y);
+    p[i] = mul2(gg, pack2(exp2_fast(x), exp2_fast(y)));
+  }
+  if (hit >= 0 && hit < VecOf<T>::N) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      if (hit == 2 * i) p[i] = add2(p[i], pack2(c, 0.0f));
+      if (hit == 2 * i + 1) p[i] = add2(p[i], pack2(0.0f, c));
+    }
+  }
+  return VecOf<T>::from_pairs(p);
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ld_cluster(const float* p, int rank) {
+  uint32_t local = (uint32_t)__cvta_generic_to_shared(p), remote;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote) : "memory");
+  return v;
+}
+
+// One read of the logits, one write of the gradient: a.slices blocks of one cluster share a row, every thread holds up to
+// NV vectors of it in registers from the load to the store.  (max, sum) go through shuffles, shared memory and the cluster's
+// distributed shared memory.  kScore stops after the log probability.
+template <typename T, int MODE, int THREADS, int NV>
+__global__ void __launch_bounds__(THREADS)
+token_held_kernel(const Args a) {
+  constexpr int N = VecOf<T>::N, P = N / 2;
+  __shared__ float pair_ms[2];
+  const int row = blockIdx.x / a.slices, rank = blockIdx.x % a.slices;
+  const size_t base = (size_t)row * a.width;
+  const T* y = (const T*)a.y + base;
+  T* dY = (T*)a.dY + base;
+  const int t = a.targets[row];
+  const float w = a.weights != nullptr ? a.weights[row] : a.default_weight;
+  const bool live = w != 0.0f && t >= 0 && t < a.vocab;
+  const int mis = (int)(base % N);
+  const int v0 = rank * a.per;
+  if (live) {
+    uint4 q[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = i * THREADS + threadIdx.x;
+      const int e0 = (v0 + v) * N - mis;
+      // out of the slice or the row: nothing but -inf
+      q[i] = load_vec<T>(y, e0, v < a.per ? a.vocab : 0);
+    }
+    const float yt = to_f32(y[t]);
+    RowTerms terms{};
+    if (MODE == kPolicy) terms = row_terms(a, row);
+    float m = VecOf<T>::max_of(q[0]);
+#pragma unroll
+    for (int i = 1; i < NV; ++i) m = fmaxf(m, VecOf<T>::max_of(q[i]));
+    float s;
+    {
+      const float ref = m == -INFINITY ? 0.0f : m;
+      const uint64_t nm = pack2(-ref, -ref), kh = pack2(a.k_hi, a.k_hi), kl = pack2(a.k_lo, a.k_lo);
+      uint64_t acc[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        uint64_t p[P];
+        VecOf<T>::pairs(q[i], p);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+          float x0, x1;
+          unpack2(scale2(add2(p[j], nm), kh, kl), x0, x1);
+          acc[j & 1] = add2(acc[j & 1], pack2(exp2_fast(x0), exp2_fast(x1)));
+        }
+      }
+      float s0, s1;
+      unpack2(add2(acc[0], acc[1]), s0, s1);
+      s = s0 + s1;
+    }
+    block_max_sum(m, s, a);
+    if (a.slices > 1) {
+      if (threadIdx.x == 0) { pair_ms[0] = m; pair_ms[1] = s; }
+      cluster_arrive();
+      cluster_wait();
+      const int lane = threadIdx.x & 31;
+      const float om = lane < a.slices ? ld_cluster(&pair_ms[0], lane) : -INFINITY;
+      float os = lane < a.slices ? ld_cluster(&pair_ms[1], lane) : 0.0f;
+      cluster_arrive();                                     // all pairs have been read; waited for at the end
+      m = om;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      if (om != -INFINITY) os *= exp_diff(om - m, a);
+      s = warp_sum(os);
+    }
+    const float lp = fmaf(yt - m, a.scale, -logf(s));
+    const float inv = 1.0f / s;
+    const bool first = rank == 0 && threadIdx.x == 0;
+    float c = 0.0f;
+    if (MODE == kPolicy) {
+      double part[3];
+      c = policy_coef(a, terms, lp, w, part);
+      if (first && a.parts != nullptr)
+        for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = part[j];
+    }
+    if (first) {
+      if (a.logp != nullptr) a.logp[row] = lp;
+      if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
+      if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
+    }
+    if (MODE == kPolicy && a.dY != nullptr) {
+      const float cs = c * a.scale, g = -cs * inv;
+      // the packed words are what is kept: without this the compiler keeps the unpacked fp32 values too (98 registers
+      // a thread where 60 do, half the resident blocks)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) asm volatile("" : "+r"(q[i].x), "+r"(q[i].y), "+r"(q[i].z), "+r"(q[i].w));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int v = i * THREADS + threadIdx.x;
+        const int e0 = (v0 + v) * N - mis;
+        if (v < a.per && e0 < a.width) store_vec<T>(dY, e0, a.width, a.vocab, grad_vec<T>(q[i], m, g, cs, t - e0, a));
+      }
+    }
+    if (a.slices > 1) cluster_wait();
+  } else {
+    if (rank == 0 && threadIdx.x == 0) {
+      if (a.logp != nullptr) a.logp[row] = 0.0f;
+      if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
+      if (MODE == kPolicy && a.parts != nullptr)
+        for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
+    }
+    if (MODE == kPolicy && a.dY != nullptr)
+      for (int v = threadIdx.x; v < a.per; v += THREADS) {
+        const int e0 = (v0 + v) * N - mis;
+        if (e0 < a.width) store_vec<T>(dY, e0, a.width, a.width, make_uint4(0u, 0u, 0u, 0u));
+      }
+  }
+  if (MODE == kPolicy && a.parts != nullptr) policy_finish(a);
+}
+
+// Rows too long to be held: one block per row, two reads of the row ((max, sum) first, the gradient from the second).
+template <typename T, int MODE>
+__global__ void __launch_bounds__(512)
+token_row_kernel(const Args a) {
+  constexpr int N = VecOf<T>::N, P = N / 2;
+  const int row = blockIdx.x;
+  const size_t base = (size_t)row * a.width;
+  const T* y = (const T*)a.y + base;
+  T* dY = (T*)a.dY + base;
+  const int t = a.targets[row];
+  const float w = a.weights != nullptr ? a.weights[row] : a.default_weight;
+  const bool live = w != 0.0f && t >= 0 && t < a.vocab;
+  const int mis = (int)(base % N);
+  float c = 0.0f, m = -INFINITY, inv = 0.0f;
+  if (live) {
+    float s = 0.0f;
+    const uint64_t kh = pack2(a.k_hi, a.k_hi), kl = pack2(a.k_lo, a.k_lo);
+    for (int v = threadIdx.x; v * N - mis < a.vocab; v += 4 * blockDim.x) {
+      uint4 q[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = load_vec<T>(y, (v + i * (int)blockDim.x) * N - mis, a.vocab);
+      const float cm = fmaxf(fmaxf(fmaxf(VecOf<T>::max_of(q[0]), VecOf<T>::max_of(q[1])),
+                                   fmaxf(VecOf<T>::max_of(q[2]), VecOf<T>::max_of(q[3]))), m);
+      if (cm != m) { s *= m == -INFINITY ? (s != s ? s : 0.0f) : exp_diff(m - cm, a); m = cm; }
+      const float ref = m == -INFINITY ? 0.0f : m;
+      const uint64_t nm = pack2(-ref, -ref);
+      uint64_t acc = pack2(0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint64_t p[P];
+        VecOf<T>::pairs(q[i], p);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+          float x0, x1;
+          unpack2(scale2(add2(p[j], nm), kh, kl), x0, x1);
+          acc = add2(acc, pack2(exp2_fast(x0), exp2_fast(x1)));
+        }
+      }
+      float s0, s1;
+      unpack2(acc, s0, s1);
+      s += s0 + s1;
+    }
+    block_max_sum(m, s, a);
+    const float lp = fmaf(to_f32(y[t]) - m, a.scale, -logf(s));
+    inv = 1.0f / s;
+    if (MODE == kPolicy) {
+      double part[3];
+      c = policy_coef(a, row_terms(a, row), lp, w, part);
+      if (threadIdx.x == 0 && a.parts != nullptr)
+        for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = part[j];
+    }
+    if (threadIdx.x == 0) {
+      if (a.logp != nullptr) a.logp[row] = lp;
+      if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
+      if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
+    }
+    if (MODE == kPolicy && a.dY == a.y) __syncthreads();    // y[t] is read before it is overwritten
+  } else if (threadIdx.x == 0) {
+    if (a.logp != nullptr) a.logp[row] = 0.0f;
+    if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
+    if (MODE == kPolicy && a.parts != nullptr)
+      for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
+  }
+  if (MODE == kPolicy && a.dY != nullptr) {
+    const float cs = c * a.scale, g = -cs * inv;
+    for (int v = threadIdx.x; v * N - mis < a.width; v += blockDim.x) {
+      const int e0 = v * N - mis;
+      if (!live) store_vec<T>(dY, e0, a.width, a.width, make_uint4(0u, 0u, 0u, 0u));
+      else store_vec<T>(dY, e0, a.width, a.vocab, grad_vec<T>(load_vec<T>(y, e0, a.vocab), m, g, cs, t - e0, a));
+    }
+  }
+  if (MODE == kPolicy && a.parts != nullptr) policy_finish(a);
+}
+
+// The gradient from a row's (max, 1 / sum) and c, block (slice, row): nothing but a stream over the logits.
+constexpr int kGradThreads = 256, kGradVecs = 4;
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads)
+token_grad_kernel(const Args a) {
+  constexpr int N = VecOf<T>::N;
+  const int row = blockIdx.x / a.slices, v0 = (blockIdx.x % a.slices) * (kGradThreads * kGradVecs) + threadIdx.x;
+  const size_t base = (size_t)row * a.width;
+  const T* y = (const T*)a.y + base;
+  T* dY = (T*)a.dY + base;
+  const int mis = (int)(base % N);
+  const float c = a.coef[row];
+  if (c == 0.0f) {                                          // left out, or of no weight: the logits are not read
+#pragma unroll
+    for (int i = 0; i < kGradVecs; ++i) {
+      const int e0 = (v0 + i * kGradThreads) * N - mis;
+      if (e0 < a.width) store_vec<T>(dY, e0, a.width, a.width, make_uint4(0u, 0u, 0u, 0u));
+    }
+    return;
+  }
+  uint4 q[kGradVecs];
+#pragma unroll
+  for (int i = 0; i < kGradVecs; ++i) {
+    const int e0 = (v0 + i * kGradThreads) * N - mis;
+    q[i] = load_vec<T>(y, e0, a.vocab);
+  }
+  const float2 st = a.stats[row];
+  const int t = a.targets[row];
+  const float cs = c * a.scale, g = -cs * st.y;
+#pragma unroll
+  for (int i = 0; i < kGradVecs; ++i) {
+    const int e0 = (v0 + i * kGradThreads) * N - mis;
+    if (e0 < a.width) store_vec<T>(dY, e0, a.width, a.vocab, grad_vec<T>(q[i], st.x, g, cs, t - e0, a));
   }
 }
 
@@ -197,7 +495,9 @@ struct PairArgs {
   const float* ref;           // [2 pairs] or null (0)
   float* seq_logp;            // [2 pairs] or null
   double* parts;              // pairs x 4: loss, chosen reward, rejected reward, [chosen > rejected]
-  float* coef;                // [rows] c_i
+  uint32_t* done;             // blocks that have finished; 0 between calls
+  float* out;                 // their means, or null
+  float* coef;                // [rows] c_i, 0 for the rows of no sequence
   int32_t rows, pairs, vocab, kind;
   float beta, smoothing;
 };
@@ -260,19 +560,28 @@ pair_kernel(const PairArgs a) {
   for (int q = 0; q < 2; ++q)
     for (int i = b[q] + (int)threadIdx.x; i < e[q]; i += blockDim.x)
       a.coef[i] = (float)((double)pair_weight(a, i) * (q == 0 ? slope : -slope));
-}
-// Means over the pairs, in a fixed order: out = {loss, chosen reward, rejected reward, share chosen > rejected}.
-static __global__ void __launch_bounds__(32)
-pair_finalize_kernel(const double* __restrict__ parts, int pairs, float* __restrict__ out) {
+  if (a.out == nullptr) return;
+  // the block that finishes last adds the pairs up, in a fixed order
+  __shared__ bool last;
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = atomicAdd(a.done, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last || threadIdx.x >= 32) return;
+  __threadfence();
   double s[4] = {0.0, 0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < pairs; i += 32)
-    for (int q = 0; q < 4; ++q) s[q] += parts[(size_t)i * 4 + q];
+  for (int i = threadIdx.x; i < a.pairs; i += 32)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s[q] += __ldcg(a.parts + (size_t)i * 4 + q);
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) s[q] += __shfl_xor_sync(0xffffffffu, s[q], o);
-  if (threadIdx.x == 0)
-    for (int q = 0; q < 4; ++q) out[q] = (float)(s[q] / (double)pairs);
+  if (threadIdx.x == 0) {
+    for (int q = 0; q < 4; ++q) a.out[q] = (float)(s[q] / (double)a.pairs);
+    *a.done = 0u;
+  }
 }
 
 }  // namespace tok

@@ -2386,8 +2386,10 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
   const int cap = 512 * 8;                                                  // vectors a block can hold
   int slices = 1;
   while (slices < 8 && slices * cap < vecs) slices *= 2;
-  if (slices * cap < vecs) {
-    et::tok::token_row_kernel<T, MODE><<<(unsigned)a.rows, 512, 0, st>>>(a);
+  if (slices * cap < vecs || (MODE == et::tok::kScore && a.rows >= 2 * s->sms && vecs >= 1024)) {
+    a.slices = 1;
+    a.per = vecs;
+    et::tok::token_row_kernel<T, MODE><<<(unsigned)a.rows, et::tok::kRowThreads, 0, st>>>(a);
     return after_launch();
   }
   a.slices = slices;

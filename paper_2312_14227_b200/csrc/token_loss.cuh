@@ -70,27 +70,50 @@ struct Args {
 __device__ __forceinline__ uint64_t scale2(uint64_t d, uint64_t k_hi, uint64_t k_lo) { return fma2(d, k_lo, mul2(d, k_hi)); }
 __device__ __forceinline__ float exp_diff(float d, const Args& a) { return exp2_fast(fmaf(d, a.k_lo, d * a.k_hi)); }
 
+// Two ways to form a term exp(scale (y - m)) = exp2(u):
+//   exact   u = (y - m) (k_hi + k_lo): three packed operations.  fp32 rows, and log probabilities that are to be summed.
+//   lean    u = y k_hi + b, b = fl(-m k_hi): one.  For bf16 rows of a loss: the FMA pipe, at 4 scalar operations an element and pass,
+//           was what bounded the kernel.  b's rounding is common to all terms of the row and to the target's; without k_lo the
+//           log of the sum is off by k_lo ln 2 E_p[m - y], some 1e-8 absolute.
+// Lean needs m k_hi inside fp32's range: rows whose largest value is beyond +-1e37 (rows of nothing but the type's lowest
+// value among them) take the exact way.
+constexpr float kLeanMax = 1e37f;
+template <bool LEAN>
+__device__ __forceinline__ float rebase(float from, float to, const Args& a) {      // factor of a sum that moves from max `from` to `to`
+  if (LEAN && fabsf(from) <= kLeanMax && fabsf(to) <= kLeanMax) return exp2_fast(__fmul_rn(from, a.k_hi) - __fmul_rn(to, a.k_hi));
+  return exp_diff(from - to, a);
+}
+// lp of the target's logit from the row's (max, sum).
+template <bool LEAN>
+__device__ __forceinline__ float log_prob(float yt, float m, float s, const Args& a) {
+  if (LEAN && fabsf(m) <= kLeanMax) {
+    constexpr float kLn2 = 0.6931471805599453f;
+    return fmaf(fmaf(yt, a.k_hi, -(m * a.k_hi)) + (yt - m) * a.k_lo, kLn2, -logf(s));
+  }
+  return fmaf(yt - m, a.scale, -logf(s));
+}
+
+// (max, sum) over the lanes of a warp.  fmaxf drops NaN; the sum carries it.
+template <bool LEAN>
+__device__ __forceinline__ void join_lanes(float& m, float& s, const Args& a) {
+  const float own = m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (own != -INFINITY) s *= rebase<LEAN>(own, m, a);
+  s = warp_sum(s);
+}
 // (max, sum) over a block: all threads get the pair.  A thread without elements holds (-inf, 0).
+template <bool LEAN>
 __device__ __forceinline__ void block_max_sum(float& m, float& s, const Args& a) {
   __shared__ float sm[32], ss[32];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
-  float wm = m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
-  // fmaxf drops NaN; the sum carries it
-  float ws = m == -INFINITY ? s : s * exp_diff(m - wm, a);
-  ws = warp_sum(ws);
+  join_lanes<LEAN>(m, s, a);
   __syncthreads();
-  if (lane == 0) { sm[wid] = wm; ss[wid] = ws; }
+  if (lane == 0) { sm[wid] = m; ss[wid] = s; }
   __syncthreads();
-  float bm = lane < nw ? sm[lane] : -INFINITY;
-  const float own = bm;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
-  float bs = lane < nw ? ss[lane] : 0.0f;
-  if (own != -INFINITY) bs *= exp_diff(own - bm, a);
-  s = warp_sum(bs);
-  m = bm;
+  m = lane < nw ? sm[lane] : -INFINITY;
+  s = lane < nw ? ss[lane] : 0.0f;
+  join_lanes<LEAN>(m, s, a);
 }
 
 // d loss / d lp of a row of the policy loss, and its contributions to the reported sums.
@@ -104,7 +127,8 @@ __device__ __forceinline__ RowTerms row_terms(const Args& a, int row) {
   r.ref = a.logp_ref != nullptr ? a.logp_ref[row] : 0.0f;
   return r;
 }
-__device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, float lp, float w, double* part) {
+// `report`: this thread writes the contributions (64-bit arithmetic, so one thread's work, not a block's).
+__device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, int row, float lp, float w, bool report) {
   const float r = a.logp_old != nullptr ? expf(lp - t.old) : 1.0f;
   const float rc = fminf(fmaxf(r, 1.0f - a.clip_low), 1.0f + a.clip_high);
   const bool clipped = r * t.adv > rc * t.adv;
@@ -115,7 +139,8 @@ __device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, f
     kl = e - d;
     slope -= a.kl_coef * e;
   }
-  if (part != nullptr) {
+  if (report) {
+    double* part = a.parts + (size_t)row * 3;
     part[0] = -(double)w * (double)((clipped ? rc : r) * t.adv);
     part[1] = (double)w * (double)kl;
     part[2] = clipped ? (double)w : 0.0;
@@ -203,6 +228,21 @@ template <> struct VecOf<bf16> {
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
 };
+template <typename T, int B>
+__device__ __forceinline__ float max_of_all(const uint4 (&q)[B]) {
+  if constexpr (VecOf<T>::N == 4) {
+    float m = VecOf<T>::max_of(q[0]);
+#pragma unroll
+    for (int i = 1; i < B; ++i) m = fmaxf(m, VecOf<T>::max_of(q[i]));
+    return m;
+  } else {                                                  // packed pairs first
+    auto h = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+    __nv_bfloat162 m = h(q[0].x);
+#pragma unroll
+    for (int i = 0; i < B; ++i) m = __hmax2(m, __hmax2(__hmax2(h(q[i].x), h(q[i].y)), __hmax2(h(q[i].z), h(q[i].w))));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+}
 // Loads are read once and stores written once: both with the streaming hint.
 template <typename T>
 __device__ __forceinline__ uint4 load_vec(const T* row, int e0, int vocab) {
@@ -250,6 +290,52 @@ __device__ __forceinline__ uint4 grad_vec(const uint4& q, float m, float g, floa
   return VecOf<T>::from_pairs(p);
 }
 
+// Sum of the terms of B vectors over the reference `ref` (finite), added to s.
+template <typename T, bool LEAN, int B>
+__device__ __forceinline__ float add_terms(const uint4 (&x)[B], float ref, float s, const Args& a) {
+  constexpr int P = VecOf<T>::N / 2;
+  const uint64_t kh = pack2(a.k_hi, a.k_hi);
+  uint64_t acc[2] = {pack2(s, 0.0f), pack2(0.0f, 0.0f)};
+  auto all = [&](auto&& arg) {
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      uint64_t p[P];
+      VecOf<T>::pairs(x[i], p);
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        float x0, x1;
+        unpack2(arg(p[j]), x0, x1);
+        acc[j & 1] = add2(acc[j & 1], pack2(exp2_fast(x0), exp2_fast(x1)));
+      }
+    }
+  };
+  if (LEAN && fabsf(ref) <= kLeanMax) {
+    const float b = -(ref * a.k_hi);
+    const uint64_t bb = pack2(b, b);
+    all([&](uint64_t v) { return fma2(v, kh, bb); });
+  } else {
+    const uint64_t nm = pack2(-ref, -ref), kl = pack2(a.k_lo, a.k_lo);
+    all([&](uint64_t v) { return scale2(add2(v, nm), kh, kl); });
+  }
+  float s0, s1;
+  unpack2(add2(acc[0], acc[1]), s0, s1);
+  return s0 + s1;
+}
+// g exp(scale (y - m)) for a vector without the target, g folded into the exponent: lb = log2|g| - m k_hi, flip = its sign bit
+// in both halves of a word.
+__device__ __forceinline__ uint4 lean_grad_vec(const uint4& q, uint64_t kh, uint64_t lb, uint32_t flip) {
+  uint64_t p[4];
+  VecOf<bf16>::pairs(q, p);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x, y;
+    unpack2(fma2(p[i], kh, lb), x, y);
+    w[i] = pack_bf16x2(exp2_fast(x), exp2_fast(y)) ^ flip;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ld_cluster(const float* p, int rank) {
@@ -260,176 +346,189 @@ __device__ __forceinline__ float ld_cluster(const float* p, int rank) {
   return v;
 }
 
+// A block's view of one row's slice.  Vectors [lo, hi) of the slice lie in the row and under `vocab` whole, the one or two
+// others are moved element by element.
+template <typename T>
+struct Slice {
+  static constexpr int N = VecOf<T>::N;
+  const T* y;                   // the row
+  T* dY;
+  const uint4* src;             // vector 0 of the slice
+  uint4* dst;
+  int e0, lo, hi;               // column of vector 0's first element
+  __device__ __forceinline__ Slice(const Args& a, long long row, int v0) {
+    const size_t base = (size_t)row * a.width;
+    const int mis = (int)(base % N);
+    y = (const T*)a.y + base;
+    dY = (T*)a.dY + base;
+    src = reinterpret_cast<const uint4*>(y - mis) + v0;
+    dst = reinterpret_cast<uint4*>(dY - mis) + v0;
+    e0 = v0 * N - mis;
+    lo = e0 < 0 ? 1 : 0;
+    hi = max(lo, min(a.per, (a.vocab + mis) / N - v0));
+  }
+};
+
+// What the second pass over a row needs, from the warp that worked it out.
+struct RowResult { float m, g, cs, lb; };
+
 // One read of the logits, one write of the gradient: a.slices blocks of one cluster share a row, every thread holds up to
 // NV vectors of it in registers from the load to the store.  (max, sum) go through shuffles, shared memory and the cluster's
-// distributed shared memory.  kScore stops after the log probability.
+// distributed shared memory; one warp turns them into the row's coefficient.  kScore stops after the log probability.
+// What bounds it is issue slots next to DRAM: at 16 bytes in and out, an SM has 177 of them per vector and thread at
+// full bandwidth, and the arithmetic of a vector takes about 70.  So range checks are made for THREADS vectors at a time,
+// and what is done once per row is done by one warp.
 template <typename T, int MODE, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS)
-token_held_kernel(const Args a) {
-  constexpr int N = VecOf<T>::N, P = N / 2;
-  __shared__ float pair_ms[2];
+token_held_kernel(const __grid_constant__ Args a) {
+  constexpr int N = VecOf<T>::N, W = THREADS / 32;
+  constexpr bool LEAN = MODE == kPolicy && N == 8;
+  __shared__ float warp_m[W], warp_s[W], pair_ms[2];
+  __shared__ RowResult result;
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int row = blockIdx.x / a.slices, rank = blockIdx.x % a.slices;
-  const size_t base = (size_t)row * a.width;
-  const T* y = (const T*)a.y + base;
-  T* dY = (T*)a.dY + base;
+  const Slice<T> sl(a, row, rank * a.per);
   const int t = a.targets[row];
   const float w = a.weights != nullptr ? a.weights[row] : a.default_weight;
   const bool live = w != 0.0f && t >= 0 && t < a.vocab;
-  const int mis = (int)(base % N);
-  const int v0 = rank * a.per;
   if (live) {
     uint4 q[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int v = i * THREADS + threadIdx.x;
-      const int e0 = (v0 + v) * N - mis;
-      // out of the slice or the row: nothing but -inf
-      q[i] = load_vec<T>(y, e0, v < a.per ? a.vocab : 0);
-    }
-    const float yt = to_f32(y[t]);
-    RowTerms terms{};
-    if (MODE == kPolicy) terms = row_terms(a, row);
-    float m = VecOf<T>::max_of(q[0]);
-#pragma unroll
-    for (int i = 1; i < NV; ++i) m = fmaxf(m, VecOf<T>::max_of(q[i]));
-    float s;
-    {
-      const float ref = m == -INFINITY ? 0.0f : m;
-      const uint64_t nm = pack2(-ref, -ref), kh = pack2(a.k_hi, a.k_hi), kl = pack2(a.k_lo, a.k_lo);
-      uint64_t acc[2] = {pack2(0.0f, 0.0f), pack2(0.0f, 0.0f)};
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        uint64_t p[P];
-        VecOf<T>::pairs(q[i], p);
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-          float x0, x1;
-          unpack2(scale2(add2(p[j], nm), kh, kl), x0, x1);
-          acc[j & 1] = add2(acc[j & 1], pack2(exp2_fast(x0), exp2_fast(x1)));
-        }
+      const int v = i * THREADS + tid;
+      if (sl.lo == 0 && (i + 1) * THREADS <= sl.hi) {       // the same for the whole block
+        q[i] = __ldcs(sl.src + v);
+      } else {
+        q[i] = load_vec<T>(sl.y, sl.e0 + v * N, v < a.per ? a.vocab : 0);   // out of the slice or the row: nothing but -inf
       }
-      float s0, s1;
-      unpack2(add2(acc[0], acc[1]), s0, s1);
-      s = s0 + s1;
     }
-    block_max_sum(m, s, a);
-    if (a.slices > 1) {
-      if (threadIdx.x == 0) { pair_ms[0] = m; pair_ms[1] = s; }
+    float m = max_of_all<T>(q);
+    float s = add_terms<T, LEAN, NV>(q, m == -INFINITY ? 0.0f : m, 0.0f, a);
+    join_lanes<LEAN>(m, s, a);
+    if (lane == 0) { warp_m[wid] = m; warp_s[wid] = s; }
+    __syncthreads();
+    if (wid == 0) {
+      const float yt = to_f32(sl.y[t]);
+      RowTerms terms{};
+      if (MODE == kPolicy) terms = row_terms(a, row);
+      m = lane < W ? warp_m[lane] : -INFINITY;
+      s = lane < W ? warp_s[lane] : 0.0f;
+      join_lanes<LEAN>(m, s, a);
+      if (a.slices > 1) {
+        if (lane == 0) { pair_ms[0] = m; pair_ms[1] = s; }
+        __syncwarp();
+      }
+      if (a.slices > 1) {
+        cluster_arrive();
+        cluster_wait();
+        m = lane < a.slices ? ld_cluster(&pair_ms[0], lane) : -INFINITY;
+        s = lane < a.slices ? ld_cluster(&pair_ms[1], lane) : 0.0f;
+        join_lanes<LEAN>(m, s, a);
+        cluster_arrive();                                   // the pairs have been read; waited for at the end
+      }
+      const float lp = log_prob<LEAN>(yt, m, s, a);
+      const float inv = 1.0f / s;
+      const bool first = rank == 0 && lane == 0;
+      if (first) {
+        if (a.logp != nullptr) a.logp[row] = lp;
+        if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
+        if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
+      }
+      if (MODE == kPolicy) {
+        const float cs = policy_coef(a, terms, row, lp, w, first && a.parts != nullptr) * a.scale, g = -cs * inv;
+        if (lane == 0) result = RowResult{m, g, cs, log2f(fabsf(g)) - m * a.k_hi};
+      }
+    } else if (a.slices > 1) {                              // barriers of the cluster count every thread
       cluster_arrive();
       cluster_wait();
-      const int lane = threadIdx.x & 31;
-      const float om = lane < a.slices ? ld_cluster(&pair_ms[0], lane) : -INFINITY;
-      float os = lane < a.slices ? ld_cluster(&pair_ms[1], lane) : 0.0f;
-      cluster_arrive();                                     // all pairs have been read; waited for at the end
-      m = om;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (om != -INFINITY) os *= exp_diff(om - m, a);
-      s = warp_sum(os);
-    }
-    const float lp = fmaf(yt - m, a.scale, -logf(s));
-    const float inv = 1.0f / s;
-    const bool first = rank == 0 && threadIdx.x == 0;
-    float c = 0.0f;
-    if (MODE == kPolicy) {
-      double part[3];
-      c = policy_coef(a, terms, lp, w, part);
-      if (first && a.parts != nullptr)
-        for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = part[j];
-    }
-    if (first) {
-      if (a.logp != nullptr) a.logp[row] = lp;
-      if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
-      if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
+      cluster_arrive();
     }
     if (MODE == kPolicy && a.dY != nullptr) {
-      const float cs = c * a.scale, g = -cs * inv;
+      __syncthreads();
+      const RowResult r = result;
+      const uint64_t kh = pack2(a.k_hi, a.k_hi), lb = pack2(r.lb, r.lb);
+      const uint32_t flip = r.g < 0.0f ? 0x80008000u : 0u;
+      const bool lean = LEAN && fabsf(r.m) <= kLeanMax && r.g != 0.0f;
       // the packed words are what is kept: without this the compiler keeps the unpacked fp32 values too (98 registers
       // a thread where 60 do, half the resident blocks)
 #pragma unroll
       for (int i = 0; i < NV; ++i) asm volatile("" : "+r"(q[i].x), "+r"(q[i].y), "+r"(q[i].z), "+r"(q[i].w));
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int v = i * THREADS + threadIdx.x;
-        const int e0 = (v0 + v) * N - mis;
-        if (v < a.per && e0 < a.width) store_vec<T>(dY, e0, a.width, a.vocab, grad_vec<T>(q[i], m, g, cs, t - e0, a));
+        const int v = i * THREADS + tid, e0 = sl.e0 + v * N;
+        if constexpr (LEAN) {
+          if (lean && sl.lo == 0 && (i + 1) * THREADS <= sl.hi) {
+            uint4 o = lean_grad_vec(q[i], kh, lb, flip);
+            if ((unsigned)(t - e0) < (unsigned)N) o = grad_vec<T>(q[i], r.m, r.g, r.cs, t - e0, a);
+            __stcs(sl.dst + v, o);
+            continue;
+          }
+        }
+        if (v < a.per && e0 < a.width) store_vec<T>(sl.dY, e0, a.width, a.vocab, grad_vec<T>(q[i], r.m, r.g, r.cs, t - e0, a));
       }
     }
     if (a.slices > 1) cluster_wait();
   } else {
-    if (rank == 0 && threadIdx.x == 0) {
+    if (rank == 0 && tid == 0) {
       if (a.logp != nullptr) a.logp[row] = 0.0f;
       if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
       if (MODE == kPolicy && a.parts != nullptr)
         for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
     }
-    if (MODE == kPolicy && a.dY != nullptr)
-      for (int v = threadIdx.x; v < a.per; v += THREADS) {
-        const int e0 = (v0 + v) * N - mis;
-        if (e0 < a.width) store_vec<T>(dY, e0, a.width, a.width, make_uint4(0u, 0u, 0u, 0u));
+    if (MODE == kPolicy && a.dY != nullptr) {
+      const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+      for (int v = tid; v < a.per; v += THREADS) {
+        if (v >= sl.lo && v < sl.hi) __stcs(sl.dst + v, zero);
+        else store_vec<T>(sl.dY, sl.e0 + v * N, a.width, a.width, zero);
       }
+    }
   }
   if (MODE == kPolicy && a.parts != nullptr) policy_finish(a);
 }
 
-// Rows too long to be held: one block per row, two reads of the row ((max, sum) first, the gradient from the second).
+// One block per row of any length.  kScore: a stream over the logits.  kPolicy: rows too long to be held are read twice
+// ((max, sum) first, the gradient from the second read, which finds much of the row in L2).
+constexpr int kRowThreads = 512;
 template <typename T, int MODE>
-__global__ void __launch_bounds__(512)
-token_row_kernel(const Args a) {
-  constexpr int N = VecOf<T>::N, P = N / 2;
-  const int row = blockIdx.x;
-  const size_t base = (size_t)row * a.width;
-  const T* y = (const T*)a.y + base;
-  T* dY = (T*)a.dY + base;
+__global__ void __launch_bounds__(kRowThreads)
+token_row_kernel(const __grid_constant__ Args a) {
+  constexpr int N = VecOf<T>::N, B = 4;
+  const int row = blockIdx.x, tid = threadIdx.x;
+  const Slice<T> sl(a, row, 0);                             // a.per: the vectors of a row
   const int t = a.targets[row];
   const float w = a.weights != nullptr ? a.weights[row] : a.default_weight;
   const bool live = w != 0.0f && t >= 0 && t < a.vocab;
-  const int mis = (int)(base % N);
   float c = 0.0f, m = -INFINITY, inv = 0.0f;
   if (live) {
     float s = 0.0f;
-    const uint64_t kh = pack2(a.k_hi, a.k_hi), kl = pack2(a.k_lo, a.k_lo);
-    for (int v = threadIdx.x; v * N - mis < a.vocab; v += 4 * blockDim.x) {
-      uint4 q[4];
+    for (int i = 0; i < a.per; i += B * kRowThreads) {
+      uint4 q[B];
+      if (i >= sl.lo && i + B * kRowThreads <= sl.hi) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = load_vec<T>(y, (v + i * (int)blockDim.x) * N - mis, a.vocab);
-      const float cm = fmaxf(fmaxf(fmaxf(VecOf<T>::max_of(q[0]), VecOf<T>::max_of(q[1])),
-                                   fmaxf(VecOf<T>::max_of(q[2]), VecOf<T>::max_of(q[3]))), m);
-      if (cm != m) { s *= m == -INFINITY ? (s != s ? s : 0.0f) : exp_diff(m - cm, a); m = cm; }
-      const float ref = m == -INFINITY ? 0.0f : m;
-      const uint64_t nm = pack2(-ref, -ref);
-      uint64_t acc = pack2(0.0f, 0.0f);
+        for (int j = 0; j < B; ++j) q[j] = MODE == kScore ? __ldcs(sl.src + i + j * kRowThreads + tid) : sl.src[i + j * kRowThreads + tid];
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint64_t p[P];
-        VecOf<T>::pairs(q[i], p);
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-          float x0, x1;
-          unpack2(scale2(add2(p[j], nm), kh, kl), x0, x1);
-          acc = add2(acc, pack2(exp2_fast(x0), exp2_fast(x1)));
+        for (int j = 0; j < B; ++j) {
+          const int v = i + j * kRowThreads + tid;
+          q[j] = load_vec<T>(sl.y, sl.e0 + v * N, v < a.per ? a.vocab : 0);
         }
       }
-      float s0, s1;
-      unpack2(acc, s0, s1);
-      s += s0 + s1;
+      const float cm = fmaxf(max_of_all<T>(q), m);
+      if (m != -INFINITY) s *= rebase<false>(m, cm, a);
+      m = cm;
+      s = add_terms<T, false, B>(q, m == -INFINITY ? 0.0f : m, s, a);
     }
-    block_max_sum(m, s, a);
-    const float lp = fmaf(to_f32(y[t]) - m, a.scale, -logf(s));
+    block_max_sum<false>(m, s, a);
+    const float lp = log_prob<false>(to_f32(sl.y[t]), m, s, a);
     inv = 1.0f / s;
-    if (MODE == kPolicy) {
-      double part[3];
-      c = policy_coef(a, row_terms(a, row), lp, w, part);
-      if (threadIdx.x == 0 && a.parts != nullptr)
-        for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = part[j];
-    }
-    if (threadIdx.x == 0) {
+    if (MODE == kPolicy) c = policy_coef(a, row_terms(a, row), row, lp, w, tid == 0 && a.parts != nullptr);
+    if (tid == 0) {
       if (a.logp != nullptr) a.logp[row] = lp;
       if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
       if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
     }
     if (MODE == kPolicy && a.dY == a.y) __syncthreads();    // y[t] is read before it is overwritten
-  } else if (threadIdx.x == 0) {
+  } else if (tid == 0) {
     if (a.logp != nullptr) a.logp[row] = 0.0f;
     if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
     if (MODE == kPolicy && a.parts != nullptr)
@@ -437,10 +536,10 @@ token_row_kernel(const Args a) {
   }
   if (MODE == kPolicy && a.dY != nullptr) {
     const float cs = c * a.scale, g = -cs * inv;
-    for (int v = threadIdx.x; v * N - mis < a.width; v += blockDim.x) {
-      const int e0 = v * N - mis;
-      if (!live) store_vec<T>(dY, e0, a.width, a.width, make_uint4(0u, 0u, 0u, 0u));
-      else store_vec<T>(dY, e0, a.width, a.vocab, grad_vec<T>(load_vec<T>(y, e0, a.vocab), m, g, cs, t - e0, a));
+    for (int v = tid; v < a.per; v += kRowThreads) {
+      const int e0 = sl.e0 + v * N;
+      if (!live) store_vec<T>(sl.dY, e0, a.width, a.width, make_uint4(0u, 0u, 0u, 0u));
+      else store_vec<T>(sl.dY, e0, a.width, a.vocab, grad_vec<T>(load_vec<T>(sl.y, e0, a.vocab), m, g, cs, t - e0, a));
     }
   }
   if (MODE == kPolicy && a.parts != nullptr) policy_finish(a);

@@ -2361,11 +2361,49 @@ void token_args(const et_stack* s, et::tok::Args* a, const void* y, const int32_
   a->k_hi = hi;
   a->k_lo = std::max((float)(k - (double)hi), 1e-30f);                      // > 0: keeps -inf at -inf
   a->done = (uint32_t*)s->at(s->off_status) + kDoneWord;
+  a->ticket = a->done + 1;
+}
+// How many clusters of `slices` blocks of a kernel run at once on the current device.  Asked once per kernel, device and
+// cluster size.
+template <auto kern>
+et_status resident_clusters(int threads, int slices, int sms, int* out) {
+  static int cached[64][4] = {};                            // per device and log2(slices)
+  int dev = 0, lg = 0;
+  CU_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return ET_ERR_UNSUPPORTED;
+  while ((1 << lg) < slices) ++lg;
+  std::lock_guard<std::mutex> cache_lock(g_cache_mutex);
+  if (cached[dev][lg] == 0) {
+    int n = 0;
+    if (slices == 1) {
+      CU_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, threads, 0));
+      n *= sms;
+    } else {
+      cudaLaunchConfig_t cfg{};
+      cfg.gridDim = dim3((unsigned)(sms * slices));
+      cfg.blockDim = dim3((unsigned)threads);
+      cudaLaunchAttribute attr{};
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = (unsigned)slices;
+      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      CU_TRY(cudaOccupancyMaxActiveClusters(&n, kern, &cfg));
+    }
+    cached[dev][lg] = std::max(1, n);
+  }
+  *out = cached[dev][lg];
+  return ET_OK;
 }
 template <typename T, int MODE, int THREADS, int NV>
-et_status launch_held(const et::tok::Args& a, cudaStream_t st) {
+et_status launch_held(const et_stack* s, const et::tok::Args& a, cudaStream_t st) {
+  int clusters = a.rows;                                    // kScore: one row a block (or cluster)
+  if (MODE == et::tok::kPolicy) {
+    ET_TRY((resident_clusters<et::tok::token_held_kernel<T, MODE, THREADS, NV>>(THREADS, a.slices, s->sms, &clusters)));
+    clusters = std::min(clusters, a.rows);
+  }
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)a.rows * (unsigned)a.slices);
+  cfg.gridDim = dim3((unsigned)clusters * (unsigned)a.slices);
   cfg.blockDim = dim3(THREADS);
   cfg.stream = st;
   cudaLaunchAttribute attr{};
@@ -2383,10 +2421,15 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
   // 16-byte vectors of a row: the logits alone where nothing is written; one more where rows begin inside a vector
   const int cols = a.dY != nullptr ? a.width : a.vocab;
   const int vecs = ceil_div(cols, N) + (a.width % N != 0 ? 1 : 0);
-  const int cap = 512 * 8;                                                  // vectors a block can hold
-  int slices = 1;
-  while (slices < 8 && slices * cap < vecs) slices *= 2;
-  if (slices * cap < vecs || (MODE == et::tok::kScore && a.rows >= 2 * s->sms && vecs >= 1024)) {
+  // How a row is cut: one block where 512 threads x 8 vectors hold it, else the fewest blocks of 256 threads (four of them
+  // fit an SM, so more rows are in flight: 131072 bf16 columns 832 us in 8 x 256 threads, 866 us in 4 x 512), else of 512.
+  // Every thread takes the same number of rounds, as few as the slice needs: empty rounds cost as much as full ones.
+  int slices = 1, threads = vecs <= 256 ? 128 : vecs <= 2048 ? 256 : 512;
+  if (vecs > 512 * 8) {
+    threads = vecs <= 8 * 256 * 8 ? 256 : 512;
+    while (slices < 8 && slices * threads * 8 < vecs) slices *= 2;
+  }
+  if (slices * threads * 8 < vecs || (MODE == et::tok::kScore && a.rows >= 2 * s->sms && vecs >= 1024)) {
     a.slices = 1;
     a.per = vecs;
     et::tok::token_row_kernel<T, MODE><<<(unsigned)a.rows, et::tok::kRowThreads, 0, st>>>(a);
@@ -2394,10 +2437,25 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
   }
   a.slices = slices;
   a.per = ceil_div(vecs, slices);
-  if (a.per <= 128 * 2) return launch_held<T, MODE, 128, 2>(a, st);
-  if (a.per <= 256 * 4) return launch_held<T, MODE, 256, 4>(a, st);
-  if (a.per <= 256 * 8) return launch_held<T, MODE, 256, 8>(a, st);
-  return launch_held<T, MODE, 512, 8>(a, st);
+  const int rounds = ceil_div(a.per, threads);
+  if (threads == 128) return rounds == 1 ? launch_held<T, MODE, 128, 1>(s, a, st) : launch_held<T, MODE, 128, 2>(s, a, st);
+  if (threads == 256) {
+    switch (rounds) {
+      case 1: case 2: return launch_held<T, MODE, 256, 2>(s, a, st);
+      case 3: return launch_held<T, MODE, 256, 3>(s, a, st);
+      case 4: return launch_held<T, MODE, 256, 4>(s, a, st);
+      case 5: return launch_held<T, MODE, 256, 5>(s, a, st);
+      case 6: return launch_held<T, MODE, 256, 6>(s, a, st);
+      case 7: return launch_held<T, MODE, 256, 7>(s, a, st);
+      default: return launch_held<T, MODE, 256, 8>(s, a, st);
+    }
+  }
+  switch (rounds) {
+    case 5: return launch_held<T, MODE, 512, 5>(s, a, st);
+    case 6: return launch_held<T, MODE, 512, 6>(s, a, st);
+    case 7: return launch_held<T, MODE, 512, 7>(s, a, st);
+    default: return launch_held<T, MODE, 512, 8>(s, a, st);   // fewer rounds do not come up: slices of 512 threads are over 2048 vectors
+  }
 }
 template <int MODE>
 et_status launch_tokens(et_stack* s, const et::tok::Args& a, cudaStream_t st) {

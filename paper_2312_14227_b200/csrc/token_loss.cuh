@@ -55,7 +55,8 @@ struct Args {
   float2* stats;              // kScore writes, kGrad reads: (max of the row's y, 1 / sum exp(scale (y - max))); may be null
   float* coef;                // kGrad: c_i.  kScore sets it to 0 where it is not null
   double* parts;              // kPolicy: rows x 3: w * (-surrogate), w * kl, w * [clipped]; may be null
-  uint32_t* done;             // kPolicy with parts: blocks that have finished; 0 between calls
+  uint32_t* done;             // kPolicy: blocks that have finished; 0 between calls
+  uint32_t* ticket;           // kPolicy: rows handed out beyond the first two of each cluster; 0 between calls
   float* out;                 // kPolicy with parts: {loss, policy part, kl part, clipped share}
   int32_t rows, width, vocab;
   int32_t slices, per;        // blocks (of one cluster) that share a row, 16-byte vectors of each
@@ -160,9 +161,10 @@ __device__ __forceinline__ void policy_finish(const Args& a) {
   if (!last) return;
   __threadfence();
   double s[3] = {0.0, 0.0, 0.0};
-  for (int i = threadIdx.x; i < a.rows; i += blockDim.x)
+  if (a.out != nullptr)
+    for (int i = threadIdx.x; i < a.rows; i += blockDim.x)
 #pragma unroll
-    for (int q = 0; q < 3; ++q) s[q] += __ldcg(a.parts + (size_t)i * 3 + q);
+      for (int q = 0; q < 3; ++q) s[q] += __ldcg(a.parts + (size_t)i * 3 + q);
 #pragma unroll
   for (int q = 0; q < 3; ++q) {
 #pragma unroll
@@ -176,9 +178,12 @@ __device__ __forceinline__ void policy_finish(const Args& a) {
       r[q] = 0.0;
       for (int wq = 0; wq < (int)(blockDim.x >> 5); ++wq) r[q] += sh[q][wq];
     }
-    a.out[0] = (float)(r[0] + (double)a.kl_coef * r[1]);
-    a.out[1] = (float)r[0]; a.out[2] = (float)r[1]; a.out[3] = (float)r[2];
+    if (a.out != nullptr) {
+      a.out[0] = (float)(r[0] + (double)a.kl_coef * r[1]);
+      a.out[1] = (float)r[0]; a.out[2] = (float)r[1]; a.out[3] = (float)r[2];
+    }
     *a.done = 0u;
+    *a.ticket = 0u;
   }
 }
 
@@ -369,82 +374,138 @@ struct Slice {
   }
 };
 
+__device__ __forceinline__ void st_cluster(int* p, int rank, int v) {
+  uint32_t local = (uint32_t)__cvta_generic_to_shared(p), remote;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(rank));
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote), "r"(v) : "memory");
+}
+// Asks L2 for a slice: one instruction, nothing waits for it.
+template <typename T>
+__device__ __forceinline__ void prefetch_slice(const Slice<T>& sl) {
+  if (sl.hi > sl.lo)
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(sl.src + sl.lo), "r"((sl.hi - sl.lo) * 16) : "memory");
+}
 // What the second pass over a row needs, from the warp that worked it out.
-struct RowResult { float m, g, cs, lb; };
+struct RowResult { float m, g, cs, lb, hit; };     // hit: the target's gradient
 
 // One read of the logits, one write of the gradient: a.slices blocks of one cluster share a row, every thread holds up to
 // NV vectors of it in registers from the load to the store.  (max, sum) go through shuffles, shared memory and the cluster's
 // distributed shared memory; one warp turns them into the row's coefficient.  kScore stops after the log probability.
-// What bounds it is issue slots next to DRAM: at 16 bytes in and out, an SM has 177 of them per vector and thread at
-// full bandwidth, and the arithmetic of a vector takes about 70.  So range checks are made for THREADS vectors at a time,
-// and what is done once per row is done by one warp.
+//
+// What bounds it is issue slots and the exponential unit next to DRAM: at 16 bytes in and out, an SM has 177 issue slots per
+// vector and thread at full bandwidth and the exponentials alone take 128 cycles of their unit.  So range checks are made for
+// THREADS vectors at a time and what is done once per row is done by one warp.  For kPolicy the blocks are persistent and take
+// rows by ticket (rows that are left out cost less than others, so a fixed share would leave SMs idle at the end); a row is
+// known an iteration ahead and its slice is asked into L2 by one instruction while the row before is worked on.
 template <typename T, int MODE, int THREADS, int NV>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS)    // 64 registers a thread
 token_held_kernel(const __grid_constant__ Args a) {
   constexpr int N = VecOf<T>::N, W = THREADS / 32;
   constexpr bool LEAN = MODE == kPolicy && N == 8;
-  __shared__ float warp_m[W], warp_s[W], pair_ms[2];
+  __shared__ float warp_m[W], warp_s[W], pair_m[2], pair_s[2];
   __shared__ RowResult result;
+  __shared__ int rows_after[2];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int row = blockIdx.x / a.slices, rank = blockIdx.x % a.slices;
-  const Slice<T> sl(a, row, rank * a.per);
-  const int t = a.targets[row];
-  const float w = a.weights != nullptr ? a.weights[row] : a.default_weight;
-  const bool live = w != 0.0f && t >= 0 && t < a.vocab;
-  if (live) {
+  const int C = a.slices, rank = blockIdx.x % C, clusters = gridDim.x / C;
+  int row = blockIdx.x / C, next = MODE == kPolicy ? row + clusters : a.rows;
+  int t_next = 0;
+  float w_next = 0.0f;
+  auto head = [&](int r) {
+    t_next = a.targets[r];
+    w_next = a.weights != nullptr ? a.weights[r] : a.default_weight;
+  };
+  auto takes_part = [&](int t, float w) { return w != 0.0f && t >= 0 && t < a.vocab; };
+  if (row < a.rows) head(row);
+  for (int it = 0; row < a.rows; ++it) {                     // `row` is the same in all blocks of a cluster
+    const int b = it & 1;
+    const Slice<T> sl(a, row, rank * a.per);
+    const int t = t_next;
+    const float w = w_next;
+    const bool live = takes_part(t, w);
     uint4 q[NV];
+    // every round but the last is full: the same for the whole block, and so for all but slices that begin inside a vector or
+    // reach far beyond `vocab`
+    const bool regular = sl.lo == 0 && (NV - 1) * THREADS <= sl.hi;
+    if (live) {
+      if (regular) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int v = i * THREADS + tid;
-      if (sl.lo == 0 && (i + 1) * THREADS <= sl.hi) {       // the same for the whole block
-        q[i] = __ldcs(sl.src + v);
+        for (int i = 0; i < NV - 1; ++i) q[i] = __ldcs(sl.src + i * THREADS + tid);
       } else {
-        q[i] = load_vec<T>(sl.y, sl.e0 + v * N, v < a.per ? a.vocab : 0);   // out of the slice or the row: nothing but -inf
+#pragma unroll
+        for (int i = 0; i < NV - 1; ++i) {
+          const int v = i * THREADS + tid;
+          q[i] = load_vec<T>(sl.y, sl.e0 + v * N, v < a.per ? a.vocab : 0);   // out of the slice or the row: nothing but -inf
+        }
+      }
+      const int v = (NV - 1) * THREADS + tid;
+      q[NV - 1] = load_vec<T>(sl.y, sl.e0 + v * N, v < a.per ? a.vocab : 0);
+    }
+    if (MODE == kPolicy) {
+      if (rank == 0 && tid == 0) {                           // the row after the next one
+        const int after = 2 * clusters + (int)atomicAdd(a.ticket, 1u);
+        if (C == 1) rows_after[b] = after;
+        else for (int c = 0; c < C; ++c) st_cluster(&rows_after[b], c, after);
+      }
+      if (next < a.rows) {
+        head(next);
+        if (tid == THREADS - 1 && takes_part(t_next, w_next)) prefetch_slice(Slice<T>(a, next, rank * a.per));
       }
     }
-    float m = max_of_all<T>(q);
-    float s = add_terms<T, LEAN, NV>(q, m == -INFINITY ? 0.0f : m, 0.0f, a);
-    join_lanes<LEAN>(m, s, a);
-    if (lane == 0) { warp_m[wid] = m; warp_s[wid] = s; }
+    float m = -INFINITY, s = 0.0f, yt = 0.0f;
+    RowTerms terms{};
+    if (live) {
+      if (wid == 0) {                                        // what the row's coefficient needs besides the sums
+        yt = to_f32(sl.y[t]);
+        if (MODE == kPolicy) terms = row_terms(a, row);
+      }
+      m = max_of_all<T>(q);
+      s = add_terms<T, LEAN, NV>(q, m == -INFINITY ? 0.0f : m, 0.0f, a);
+      join_lanes<LEAN>(m, s, a);
+      if (lane == 0) { warp_m[wid] = m; warp_s[wid] = s; }
+    }
     __syncthreads();
     if (wid == 0) {
-      const float yt = to_f32(sl.y[t]);
-      RowTerms terms{};
-      if (MODE == kPolicy) terms = row_terms(a, row);
-      m = lane < W ? warp_m[lane] : -INFINITY;
-      s = lane < W ? warp_s[lane] : 0.0f;
-      join_lanes<LEAN>(m, s, a);
-      if (a.slices > 1) {
-        if (lane == 0) { pair_ms[0] = m; pair_ms[1] = s; }
-        __syncwarp();
+      if (live) {
+        m = lane < W ? warp_m[lane] : -INFINITY;
+        s = lane < W ? warp_s[lane] : 0.0f;
+        join_lanes<LEAN>(m, s, a);
       }
-      if (a.slices > 1) {
+      if (C > 1) {
+        if (lane == 0) { pair_m[b] = m; pair_s[b] = s; }
+        __syncwarp();
         cluster_arrive();
         cluster_wait();
-        m = lane < a.slices ? ld_cluster(&pair_ms[0], lane) : -INFINITY;
-        s = lane < a.slices ? ld_cluster(&pair_ms[1], lane) : 0.0f;
-        join_lanes<LEAN>(m, s, a);
-        cluster_arrive();                                   // the pairs have been read; waited for at the end
+        if (live) {
+          m = lane < C ? ld_cluster(&pair_m[b], lane) : -INFINITY;
+          s = lane < C ? ld_cluster(&pair_s[b], lane) : 0.0f;
+          join_lanes<LEAN>(m, s, a);
+        }
       }
-      const float lp = log_prob<LEAN>(yt, m, s, a);
-      const float inv = 1.0f / s;
       const bool first = rank == 0 && lane == 0;
-      if (first) {
-        if (a.logp != nullptr) a.logp[row] = lp;
-        if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
-        if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
+      if (live) {
+        const float lp = log_prob<LEAN>(yt, m, s, a), inv = 1.0f / s;
+        if (first) {
+          if (a.logp != nullptr) a.logp[row] = lp;
+          if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
+        }
+        if (MODE == kPolicy) {
+          const float cs = policy_coef(a, terms, row, lp, w, first && a.parts != nullptr) * a.scale, g = -cs * inv;
+          if (lane == 0) result = RowResult{m, g, cs, log2f(fabsf(g)) - m * a.k_hi, fmaf(g, exp_diff(yt - m, a), cs)};
+        }
+      } else if (first) {
+        if (a.logp != nullptr) a.logp[row] = 0.0f;
+        if (MODE == kPolicy && a.parts != nullptr)
+          for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
       }
-      if (MODE == kPolicy) {
-        const float cs = policy_coef(a, terms, row, lp, w, first && a.parts != nullptr) * a.scale, g = -cs * inv;
-        if (lane == 0) result = RowResult{m, g, cs, log2f(fabsf(g)) - m * a.k_hi};
-      }
-    } else if (a.slices > 1) {                              // barriers of the cluster count every thread
+      if (MODE == kScore && first && a.coef != nullptr) a.coef[row] = 0.0f;
+    } else if (C > 1) {                                      // barriers of the cluster count every thread
       cluster_arrive();
       cluster_wait();
-      cluster_arrive();
     }
-    if (MODE == kPolicy && a.dY != nullptr) {
-      __syncthreads();
+    if (MODE == kScore) break;                               // one row a block
+    __syncthreads();
+    const int after = rows_after[b];
+    if (a.dY != nullptr && live) {
       const RowResult r = result;
       const uint64_t kh = pack2(a.k_hi, a.k_hi), lb = pack2(r.lb, r.lb);
       const uint32_t flip = r.g < 0.0f ? 0x80008000u : 0u;
@@ -453,37 +514,41 @@ token_held_kernel(const __grid_constant__ Args a) {
       // a thread where 60 do, half the resident blocks)
 #pragma unroll
       for (int i = 0; i < NV; ++i) asm volatile("" : "+r"(q[i].x), "+r"(q[i].y), "+r"(q[i].z), "+r"(q[i].w));
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
+      auto out = [&](const uint4& x) -> uint4 {
+        if constexpr (LEAN) return lean_grad_vec(x, kh, lb, flip);
+        else return grad_vec<T>(x, r.m, r.g, 0.0f, -1, a);
+      };
+      // a vector that is not known to lie in the row, or of a row that takes the exact way
+      auto out_checked = [&](int i) {
         const int v = i * THREADS + tid, e0 = sl.e0 + v * N;
-        if constexpr (LEAN) {
-          if (lean && sl.lo == 0 && (i + 1) * THREADS <= sl.hi) {
-            uint4 o = lean_grad_vec(q[i], kh, lb, flip);
-            if ((unsigned)(t - e0) < (unsigned)N) o = grad_vec<T>(q[i], r.m, r.g, r.cs, t - e0, a);
-            __stcs(sl.dst + v, o);
-            continue;
-          }
-        }
-        if (v < a.per && e0 < a.width) store_vec<T>(sl.dY, e0, a.width, a.vocab, grad_vec<T>(q[i], r.m, r.g, r.cs, t - e0, a));
+        if (v < a.per && e0 < a.width) store_vec<T>(sl.dY, e0, a.width, a.vocab, grad_vec<T>(q[i], r.m, r.g, 0.0f, -1, a));
+      };
+      if (regular && (lean || !LEAN)) {
+#pragma unroll
+        for (int i = 0; i < NV - 1; ++i) __stcs(sl.dst + i * THREADS + tid, out(q[i]));
+        if ((NV - 1) * THREADS + tid < sl.hi) __stcs(sl.dst + (NV - 1) * THREADS + tid, out(q[NV - 1]));
+        else out_checked(NV - 1);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) out_checked(i);
       }
-    }
-    if (a.slices > 1) cluster_wait();
-  } else {
-    if (rank == 0 && tid == 0) {
-      if (a.logp != nullptr) a.logp[row] = 0.0f;
-      if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
-      if (MODE == kPolicy && a.parts != nullptr)
-        for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
-    }
-    if (MODE == kPolicy && a.dY != nullptr) {
+      const int tv = (t - sl.e0) >> (N == 8 ? 3 : 2);        // the target's element, by the thread that wrote its vector
+      if (tv >= 0 && tv < a.per && tv % THREADS == tid) sl.dY[t] = from_f32<T>(r.hit);
+    } else if (a.dY != nullptr) {
       const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
       for (int v = tid; v < a.per; v += THREADS) {
         if (v >= sl.lo && v < sl.hi) __stcs(sl.dst + v, zero);
         else store_vec<T>(sl.dY, sl.e0 + v * N, a.width, a.width, zero);
       }
     }
+    row = next;
+    next = after;
   }
-  if (MODE == kPolicy && a.parts != nullptr) policy_finish(a);
+  if (C > 1) {                                               // no block leaves while another reads its shared memory
+    cluster_arrive();
+    cluster_wait();
+  }
+  if (MODE == kPolicy) policy_finish(a);
 }
 
 // One block per row of any length.  kScore: a stream over the logits.  kPolicy: rows too long to be held are read twice
@@ -542,7 +607,7 @@ token_row_kernel(const __grid_constant__ Args a) {
       else store_vec<T>(sl.dY, e0, a.width, a.vocab, grad_vec<T>(load_vec<T>(sl.y, e0, a.vocab), m, g, cs, t - e0, a));
     }
   }
-  if (MODE == kPolicy && a.parts != nullptr) policy_finish(a);
+  if (MODE == kPolicy) policy_finish(a);
 }
 
 // The gradient from a row's (max, 1 / sum) and c, block (slice, row): nothing but a stream over the logits.

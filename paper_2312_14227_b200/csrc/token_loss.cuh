@@ -398,7 +398,7 @@ struct RowResult { float m, g, cs, lb, hit; };     // hit: the target's gradient
 // rows by ticket (rows that are left out cost less than others, so a fixed share would leave SMs idle at the end); a row is
 // known an iteration ahead and its slice is asked into L2 by one instruction while the row before is worked on.
 template <typename T, int MODE, int THREADS, int NV>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS)    // 64 registers a thread
+__global__ void __launch_bounds__(THREADS, (NV <= 4 ? 1536 : 1024) / THREADS)    // 40 or 64 registers a thread
 token_held_kernel(const __grid_constant__ Args a) {
   constexpr int N = VecOf<T>::N, W = THREADS / 32;
   constexpr bool LEAN = MODE == kPolicy && N == 8;

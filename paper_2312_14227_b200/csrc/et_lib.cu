@@ -205,7 +205,7 @@ struct LayerRT {
   int img_h = 0, img_w = 0, ksize = 0;   // patch gather: K = channels, N = ksize^2 * K
   bool trainable() const { return kind == ET_LAYER_DENSE || kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM || kind == ET_LAYER_EMBEDDING; }
   bool has_tensor(int k) const { return trainable() && (k == 0 || kind != ET_LAYER_EMBEDDING); }   // an embedding has no tensor 2l + 1
-  size_t off_keys[2] = {0, 0}, off_rows[2] = {0, 0}, off_hist = 0, off_epart = 0;   // embedding: sorting buffers, partial gradient rows
+  size_t off_keys[2] = {0, 0}, off_rows[2] = {0, 0}, off_hist = 0, off_epart = 0, off_named = 0;   // embedding: sorting buffers, partial gradient rows
   bool vector_params() const { return kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM; }   // gamma, beta: [N]
   size_t off_means = 0;     // batch norm: the two column means of the backward formula
   size_t w_count() const { return !trainable() ? 0 : vector_params() ? (size_t)N : (size_t)K * N; }   // elements of tensor 2l
@@ -336,17 +336,25 @@ TilePlan choose_tiles(int rows, int cols, int kb_total, int sms, bool allow_spli
 }
 
 // How the gradient of an embedding with `vocab` rows of `d` is cut up for `rows` tokens.
-struct EmbPlan { int tiles, bits, passes, chunks, threads, col_tiles; };
+struct EmbPlan {
+  bool one;                  // one block sorts all ids
+  int key_bits, tiles, bits, passes, chunks, threads, col_tiles, join_groups, join_tiles;
+  int imp_slots() const { return chunks * col_tiles + join_groups * join_tiles; }
+};
 EmbPlan emb_plan(long long rows, int vocab, int d) {
   EmbPlan p;
   int bits = 1;
   while (bits < 32 && ((unsigned long long)vocab >> bits) != 0) ++bits;    // keys 0 .. vocab (= left out)
+  p.key_bits = bits;
+  p.one = rows <= et::kSortOneMax;
   p.passes = ceil_div(bits, et::kSortMaxBits);
   p.bits = ceil_div(bits, p.passes);
   p.tiles = ceil_div(rows, et::kSortTile);
   p.chunks = ceil_div(rows, et::kEmbChunk);
   p.threads = std::min(256, ceil_div(ceil_div(d, et::kVec), 32) * 32);
   p.col_tiles = ceil_div(d, p.threads * et::kVec);
+  p.join_groups = ceil_div(p.chunks, et::kJoinChunks);
+  p.join_tiles = ceil_div(d, et::kJoinCols);
   return p;
 }
 constexpr int kClipTensors = 256;          // tensors named by one launch's table
@@ -920,7 +928,10 @@ et_status run_embed_forward(et_stack* s, void* y, cudaStream_t st) {
   const LayerRT& L = s->ly[0];
   T* out = s->L == 1 ? (T*)y : (T*)s->at(L.off_a_out);
   const int grid = std::min(ceil_div(s->M, 8), s->sms * 16);
-  et::embed_forward_kernel<T><<<grid, 256, 0, st>>>((const T*)L.W, (const int32_t*)s->x, out, s->M, L.K, L.N, s->emb_scale);
+  if (L.N % et::kVec == 0)
+    et::embed_forward_kernel<T, true><<<grid, 256, 0, st>>>((const T*)L.W, (const int32_t*)s->x, out, s->M, L.K, L.N, s->emb_scale);
+  else
+    et::embed_forward_kernel<T, false><<<grid, 256, 0, st>>>((const T*)L.W, (const int32_t*)s->x, out, s->M, L.K, L.N, s->emb_scale);
   return after_launch();
 }
 // The gradient of the table from G_1 (the caller's dY where the embedding is the only layer).
@@ -930,49 +941,82 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
   const LayerRT& L = s->ly[0];
   const EmbPlan p = emb_plan(s->M, L.K, L.N);
   const int n = (int)s->M;
-  const uint32_t *keys = nullptr, *rows = nullptr;
   const int32_t* ids = (const int32_t*)s->x;
-  uint32_t* hist = (uint32_t*)s->at(L.off_hist);
-  {
-    TimedLaunch tl(s, ET_K_WGRAD, st);
-    for (int pass = 0; pass < p.passes; ++pass) {
-      uint32_t* ko = (uint32_t*)s->at(L.off_keys[pass & 1]);
-      uint32_t* ro = (uint32_t*)s->at(L.off_rows[pass & 1]);
-      const int shift = pass * p.bits;
-      et::sort_hist_kernel<<<p.tiles, et::kSortThreads, 0, st>>>(ids, keys, n, L.K, shift, p.bits, hist);
-      ET_TRY(after_launch());
-      et::sort_scan_kernel<<<1, 1024, 0, st>>>(hist, p.tiles << p.bits);
-      ET_TRY(after_launch());
-      et::sort_scatter_kernel<<<p.tiles, et::kSortThreads, 0, st>>>(ids, keys, rows, n, L.K, shift, p.bits, hist, ko, ro);
-      ET_TRY(after_launch());
-      keys = ko; rows = ro;
-      *launches += 3;
-    }
-  }
   et::EmbSink<T> sink;
   sink.grad = grad; sink.delta = delta; sink.W = (T*)L.W; sink.master = L.W32; sink.m_state = L.st1[0]; sink.v_state = L.st2[0];
   sink.opt = opt_params(s, lr); sink.do_sgd = sgd ? 1 : 0; sink.delta_is_snapshot = s->delta_is_snapshot ? 1 : 0;
-  float* imp = delta != nullptr ? (float*)s->at(s->off_imp_parts) + s->imp_offs[0] : nullptr;
-  const int used = 2 * p.chunks * p.col_tiles;
-  if (imp != nullptr && used < L.imp_count_w) CU_TRY(cudaMemsetAsync(imp + used, 0, sizeof(float) * (L.imp_count_w - used), st));
-  float* part = (float*)s->at(L.off_epart);
-  const dim3 grid(p.chunks, p.col_tiles);
+  // rows that no token names have a gradient of 0 to export, or an optimiser step to take
+  const bool fills = grad != nullptr || (sgd && sink.opt.kind != et::kOptSgd);
+  uint32_t* named = fills ? (uint32_t*)s->at(L.off_named) : nullptr;
+  et::EmbFill<T> fill{sink, named, 0, 0, L.N};
+  fill.sink.delta = nullptr;                                // the importance sum has no term there
+  // blocks that fill, for a kernel of `threads` threads a block: enough to saturate memory, no more than there are rows for
+  const int fill_rows_max = ceil_div(L.K, 4);
+  const uint32_t *keys = nullptr, *rows = nullptr;
   {
     TimedLaunch tl(s, ET_K_WGRAD, st);
-    et::embed_grad_kernel<T><<<grid, p.threads, 0, st>>>(grad_act<T>(s, 1, dY), keys, rows, n, L.K, L.N, s->emb_scale, part, imp, sink);
-    ET_TRY(after_launch());
+    if (p.one) {
+      uint32_t* ko = (uint32_t*)s->at(L.off_keys[0]);
+      uint32_t* ro = (uint32_t*)s->at(L.off_rows[0]);
+      et::sort_one_kernel<<<1, 1024, 0, st>>>(ids, n, L.K, p.key_bits, ko, ro, named);
+      ET_TRY(after_launch());
+      keys = ko; rows = ro;
+      fill.v1 = fills ? L.K : 0;                            // all of it beside the gradient kernel
+      ++*launches;
+    } else {
+      uint32_t* hist = (uint32_t*)s->at(L.off_hist);
+      const size_t pass_words = (size_t)p.tiles << p.bits;
+      if (fills) CU_TRY(cudaMemsetAsync(named, 0, (size_t)ceil_div(L.K, 32) * sizeof(uint32_t), st));
+      et::sort_hist_kernel<<<p.tiles, et::kSortThreads, 0, st>>>(ids, n, L.K, p.bits, hist, p.passes, named);
+      ET_TRY(after_launch());
+      ++*launches;
+      for (int pass = 0; pass < p.passes; ++pass) {
+        uint32_t* ko = (uint32_t*)s->at(L.off_keys[pass & 1]);
+        uint32_t* ro = (uint32_t*)s->at(L.off_rows[pass & 1]);
+        // the passes share the filling
+        fill.v0 = fills ? (int)((long long)L.K * pass / p.passes) : 0;
+        fill.v1 = fills ? (int)((long long)L.K * (pass + 1) / p.passes) : 0;
+        const int fill_blocks = fills ? std::min(s->sms * 4, fill_rows_max) : 0;
+        et::sort_pass_kernel<T><<<p.tiles + fill_blocks, et::kSortThreads, 0, st>>>(
+            ids, keys, rows, n, L.K, pass * p.bits, p.bits, p.tiles, hist + pass * pass_words,
+            pass + 1 < p.passes ? hist + (pass + 1) * pass_words : nullptr, ko, ro, fill);
+        ET_TRY(after_launch());
+        keys = ko; rows = ro;
+        ++*launches;
+      }
+      fill.v0 = fill.v1 = 0;
+    }
   }
-  TimedLaunch tl(s, ET_K_WGRAD_REDUCE, st);
-  et::embed_join_kernel<T><<<grid, p.threads, 0, st>>>(keys, n, L.K, L.N, s->emb_scale, part,
-                                                       imp != nullptr ? imp + p.chunks * p.col_tiles : nullptr, sink);
-  ET_TRY(after_launch());
-  *launches += 2;
-  if (grad != nullptr || (sgd && sink.opt.kind != et::kOptSgd)) {
-    sink.delta = nullptr;                                   // the importance sum has no term there
-    et::embed_untouched_kernel<T><<<ceil_div(L.K, 8), 256, 0, st>>>(keys, n, L.K, L.N, sink);
-    ET_TRY(after_launch());
+  float* imp = delta != nullptr ? (float*)s->at(s->off_imp_parts) + s->imp_offs[0] : nullptr;
+  const int used = p.imp_slots();
+  if (imp != nullptr && used < L.imp_count_w) CU_TRY(cudaMemsetAsync(imp + used, 0, sizeof(float) * (L.imp_count_w - used), st));
+  float* part = (float*)s->at(L.off_epart);
+  const bool whole = L.N % et::kVec == 0;                    // rows are whole vectors
+  const bool plain_export = grad != nullptr && delta == nullptr && !sgd && ((uintptr_t)grad & 15) == 0;
+  {
+    TimedLaunch tl(s, ET_K_WGRAD, st);
+    const int fill_blocks = fill.v1 > fill.v0 ? std::min(ceil_div(s->sms * 8, p.col_tiles), fill_rows_max) : 0;
+    const dim3 grid(p.chunks + fill_blocks, p.col_tiles);
+    auto go = [&](auto kern) -> et_status {
+      kern<<<grid, p.threads, 0, st>>>(grad_act<T>(s, 1, dY), keys, rows, n, L.K, L.N, s->emb_scale, p.chunks, part, imp, sink, fill);
+      return after_launch();
+    };
+    if (whole && plain_export) ET_TRY(go(et::embed_grad_kernel<T, true, true>));
+    else if (whole) ET_TRY(go(et::embed_grad_kernel<T, true, false>));
+    else ET_TRY(go(et::embed_grad_kernel<T, false, false>));
     ++*launches;
   }
+  TimedLaunch tl(s, ET_K_WGRAD_REDUCE, st);
+  const dim3 grid(p.join_groups, p.join_tiles);
+  if (imp != nullptr) imp += p.chunks * p.col_tiles;
+  auto go = [&](auto kern) -> et_status {
+    kern<<<grid, 256, 0, st>>>(keys, n, L.K, L.N, s->emb_scale, p.chunks, part, imp, sink);
+    return after_launch();
+  };
+  if (whole && plain_export) ET_TRY(go(et::embed_join_kernel<T, true, true>));
+  else if (whole) ET_TRY(go(et::embed_join_kernel<T, true, false>));
+  else ET_TRY(go(et::embed_join_kernel<T, false, false>));
+  ++*launches;
   return ET_OK;
 }
 
@@ -1811,7 +1855,8 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
         y.off_keys[k] = take((size_t)M * sizeof(uint32_t));
         y.off_rows[k] = take((size_t)M * sizeof(uint32_t));
       }
-      y.off_hist = take(((size_t)p.tiles << p.bits) * sizeof(uint32_t));
+      y.off_hist = take((((size_t)p.tiles * p.passes) << p.bits) * sizeof(uint32_t));
+      y.off_named = take((size_t)ceil_div(y.K, 32) * sizeof(uint32_t));
       y.off_epart = take((size_t)p.chunks * 2 * y.N * sizeof(float));
     } else if (dtype == ET_BF16) {
       const int kb_n = ceil_div(y.Nw, et::tc::BK) * y.fold;
@@ -1861,7 +1906,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     if (y.kind == ET_LAYER_EMBEDDING) {                    // partial importances: those of et_importance or of the two gradient kernels
       const EmbPlan p = emb_plan(M, y.K, y.N);
       const long long n = std::max<long long>(((long long)y.K * y.N + et::kEltThreads * et::kVec - 1) / (et::kEltThreads * et::kVec),
-                                              2ll * p.chunks * p.col_tiles);
+                                              (long long)p.imp_slots());
       if (n + imp_total > (1ll << 30)) { delete s; return ET_ERR_UNSUPPORTED; }
       y.imp_count_w = (int)n; y.imp_count_b = 0;
       s->imp_offs[2 * l] = imp_total; s->imp_counts[2 * l] = y.imp_count_w; imp_total += y.imp_count_w;

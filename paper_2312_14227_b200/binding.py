@@ -146,9 +146,7 @@ def et_launch_count() -> int:
 
 def _ptr(t) -> Optional[int]:
     """Device / host pointer of a torch tensor, numpy array, int or None."""
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
     if isinstance(t, np.ndarray):
         return t.ctypes.data
@@ -159,10 +157,7 @@ def _ptr_array(seq: Optional[Sequence], n: int):
     if seq is None:
         return None
     assert len(seq) == n
-    arr = (C.c_void_p * n)()
-    for i, t in enumerate(seq):
-        arr[i] = _ptr(t)
-    return arr
+    return (C.c_void_p * n)(*map(_ptr, seq))
 
 
 def _stream_ptr(stream) -> Optional[int]:

@@ -100,6 +100,13 @@ __device__ __forceinline__ float2 gelu_tanh_grad_x2(float z0, float z1) {
   return __half22float2(__hfma2(b, du, a));
 }
 
+// First statement of a kernel that is launched with programmatic stream serialisation: waits until the stream's previous
+// kernel has finished (and its writes are visible), then lets the next one start its launch.  What overlaps is launch latency.
+__device__ __forceinline__ void chain_begin() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // ---- row segments: NV consecutive elements of one row, vectorised when aligned ----------
 // `n` = how many of the NV elements exist (ragged right edge); the rest read as 0.
 template <int NV>

@@ -44,6 +44,7 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(256)
 embed_forward_kernel(const T* __restrict__ table, const int32_t* __restrict__ ids, T* __restrict__ out, long long rows,
                      int vocab, int d, float scale) {
+  chain_begin();
   constexpr int U = 4;                                      // loads of a row that are on their way at once
   const int lane = threadIdx.x & 31;
   for (long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); r < rows; r += (long long)gridDim.x * 8) {
@@ -191,6 +192,7 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, int n) {
 static __global__ void __launch_bounds__(1024)
 sort_one_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uint32_t* __restrict__ keys_out,
                 uint32_t* __restrict__ rows_out, uint32_t* __restrict__ named) {
+  chain_begin();
   constexpr int E = kSortOneMax / 1024, BINS = 1 << kSortOneBits;
   __shared__ uint16_t cnt[32][BINS];
   __shared__ uint32_t sk[kSortOneMax];
@@ -256,6 +258,7 @@ sort_one_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uin
 static __global__ void __launch_bounds__(kSortThreads)
 sort_hist_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uint32_t* __restrict__ hist, int passes,
                  uint32_t* __restrict__ named) {
+  chain_begin();
   __shared__ uint32_t cnt[1 << kSortMaxBits];
   const int bins = 1 << bits;
   for (int i = threadIdx.x; i < bins; i += kSortThreads) cnt[i] = 0;
@@ -284,6 +287,7 @@ __global__ void __launch_bounds__(kSortThreads)
 sort_pass_kernel(const int32_t* __restrict__ ids, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows, int n,
                  int vocab, int shift, int bits, int tiles, const uint32_t* __restrict__ hist, uint32_t* __restrict__ hist_next,
                  uint32_t* __restrict__ keys_out, uint32_t* __restrict__ rows_out, const __grid_constant__ EmbFill<T> fill) {
+  chain_begin();
   constexpr int kWarps = kSortThreads / 32, E = kSortPerThread;
   if ((int)blockIdx.x >= tiles) {
     embed_fill(fill, blockIdx.x - tiles, gridDim.x - tiles);
@@ -347,6 +351,7 @@ __global__ void __launch_bounds__(256)
 embed_grad_kernel(const T* __restrict__ G, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows, int n, int vocab,
                   int d, float scale, int chunks, float* __restrict__ part, float* __restrict__ imp_part, const __grid_constant__ EmbSink<T> sink,
                   const __grid_constant__ EmbFill<T> fill) {
+  chain_begin();
   constexpr int U = 8;                                          // rows on their way at once
   if ((int)blockIdx.x >= chunks) {
     embed_fill(fill, (blockIdx.x - chunks) * gridDim.y + blockIdx.y, (gridDim.x - chunks) * gridDim.y);
@@ -409,6 +414,7 @@ template <typename T, bool VEC, bool EXPORT>
 __global__ void __launch_bounds__(256)
 embed_join_kernel(const uint32_t* __restrict__ keys, int n, int vocab, int d, float scale, int chunks, const float* __restrict__ part,
                   float* __restrict__ imp_part, const __grid_constant__ EmbSink<T> sink) {
+  chain_begin();
   __shared__ int count[kJoinChunks];                            // chunks that an id beginning in this one goes on in; 0: none does
   __shared__ float sm[8][kJoinCols];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;

@@ -55,6 +55,21 @@ inline et_status after_launch() {
   g_launches.fetch_add(1, std::memory_order_relaxed);
   return ET_OK;
 }
+// A launch whose latency overlaps the stream's previous kernel: the kernel begins with et::chain_begin().
+template <typename... P, typename... A>
+et_status launch_chained(void (*kern)(P...), dim3 grid, dim3 block, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  CU_TRY(cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...));
+  return after_launch();
+}
 inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
@@ -928,11 +943,8 @@ et_status run_embed_forward(et_stack* s, void* y, cudaStream_t st) {
   const LayerRT& L = s->ly[0];
   T* out = s->L == 1 ? (T*)y : (T*)s->at(L.off_a_out);
   const int grid = std::min(ceil_div(s->M, 8), s->sms * 16);
-  if (L.N % et::kVec == 0)
-    et::embed_forward_kernel<T, true><<<grid, 256, 0, st>>>((const T*)L.W, (const int32_t*)s->x, out, s->M, L.K, L.N, s->emb_scale);
-  else
-    et::embed_forward_kernel<T, false><<<grid, 256, 0, st>>>((const T*)L.W, (const int32_t*)s->x, out, s->M, L.K, L.N, s->emb_scale);
-  return after_launch();
+  return launch_chained(L.N % et::kVec == 0 ? et::embed_forward_kernel<T, true> : et::embed_forward_kernel<T, false>, grid, 256, st,
+                        (const T*)L.W, (const int32_t*)s->x, out, s->M, L.K, L.N, s->emb_scale);
 }
 // The gradient of the table from G_1 (the caller's dY where the embedding is the only layer).
 template <typename T>
@@ -958,8 +970,7 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
     if (p.one) {
       uint32_t* ko = (uint32_t*)s->at(L.off_keys[0]);
       uint32_t* ro = (uint32_t*)s->at(L.off_rows[0]);
-      et::sort_one_kernel<<<1, 1024, 0, st>>>(ids, n, L.K, p.key_bits, ko, ro, named);
-      ET_TRY(after_launch());
+      ET_TRY(launch_chained(et::sort_one_kernel, 1, 1024, st, ids, n, L.K, p.key_bits, ko, ro, named));
       keys = ko; rows = ro;
       fill.v1 = fills ? L.K : 0;                            // all of it beside the gradient kernel
       ++*launches;
@@ -967,8 +978,7 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
       uint32_t* hist = (uint32_t*)s->at(L.off_hist);
       const size_t pass_words = (size_t)p.tiles << p.bits;
       if (fills) CU_TRY(cudaMemsetAsync(named, 0, (size_t)ceil_div(L.K, 32) * sizeof(uint32_t), st));
-      et::sort_hist_kernel<<<p.tiles, et::kSortThreads, 0, st>>>(ids, n, L.K, p.bits, hist, p.passes, named);
-      ET_TRY(after_launch());
+      ET_TRY(launch_chained(et::sort_hist_kernel, p.tiles, et::kSortThreads, st, ids, n, L.K, p.bits, hist, p.passes, named));
       ++*launches;
       for (int pass = 0; pass < p.passes; ++pass) {
         uint32_t* ko = (uint32_t*)s->at(L.off_keys[pass & 1]);
@@ -977,10 +987,9 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
         fill.v0 = fills ? (int)((long long)L.K * pass / p.passes) : 0;
         fill.v1 = fills ? (int)((long long)L.K * (pass + 1) / p.passes) : 0;
         const int fill_blocks = fills ? std::min(s->sms * 4, fill_rows_max) : 0;
-        et::sort_pass_kernel<T><<<p.tiles + fill_blocks, et::kSortThreads, 0, st>>>(
-            ids, keys, rows, n, L.K, pass * p.bits, p.bits, p.tiles, hist + pass * pass_words,
-            pass + 1 < p.passes ? hist + (pass + 1) * pass_words : nullptr, ko, ro, fill);
-        ET_TRY(after_launch());
+        ET_TRY(launch_chained(et::sort_pass_kernel<T>, p.tiles + fill_blocks, et::kSortThreads, st, ids, keys, rows, n, L.K,
+                              pass * p.bits, p.bits, p.tiles, hist + pass * pass_words,
+                              pass + 1 < p.passes ? hist + (pass + 1) * pass_words : nullptr, ko, ro, fill));
         keys = ko; rows = ro;
         ++*launches;
       }
@@ -998,8 +1007,8 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
     const int fill_blocks = fill.v1 > fill.v0 ? std::min(ceil_div(s->sms * 8, p.col_tiles), fill_rows_max) : 0;
     const dim3 grid(p.chunks + fill_blocks, p.col_tiles);
     auto go = [&](auto kern) -> et_status {
-      kern<<<grid, p.threads, 0, st>>>(grad_act<T>(s, 1, dY), keys, rows, n, L.K, L.N, s->emb_scale, p.chunks, part, imp, sink, fill);
-      return after_launch();
+      return launch_chained(kern, grid, p.threads, st, grad_act<T>(s, 1, dY), keys, rows, n, L.K, L.N, s->emb_scale, p.chunks, part,
+                            imp, sink, fill);
     };
     if (whole && plain_export) ET_TRY(go(et::embed_grad_kernel<T, true, true>));
     else if (whole) ET_TRY(go(et::embed_grad_kernel<T, true, false>));
@@ -1010,8 +1019,7 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
   const dim3 grid(p.join_groups, p.join_tiles);
   if (imp != nullptr) imp += p.chunks * p.col_tiles;
   auto go = [&](auto kern) -> et_status {
-    kern<<<grid, 256, 0, st>>>(keys, n, L.K, L.N, s->emb_scale, p.chunks, part, imp, sink);
-    return after_launch();
+    return launch_chained(kern, grid, 256, st, keys, n, L.K, L.N, s->emb_scale, p.chunks, part, imp, sink);
   };
   if (whole && plain_export) ET_TRY(go(et::embed_join_kernel<T, true, true>));
   else if (whole) ET_TRY(go(et::embed_join_kernel<T, true, false>));
@@ -2319,9 +2327,9 @@ et_status run_sumsq(et_stack* s, const uint8_t* mask, int n_tensors, float* cons
   return for_each_clip_table(s, mask, n_tensors, grads, nullptr, false, [&](const auto& tab) -> et_status {
     constexpr int N = sizeof(tab.e) / sizeof(tab.e[0]);
     const int grid = clip_grid(s, tab.blocks);
-    et::sumsq_kernel<N><<<grid, et::kClipThreads, 0, st>>>(tab, parts + *n_parts);
+    double* out = parts + *n_parts;
     *n_parts += grid;
-    return after_launch();
+    return launch_chained(et::sumsq_kernel<N>, grid, et::kClipThreads, st, tab, out);
   });
 }
 }  // namespace
@@ -2334,8 +2342,8 @@ et_status et_grad_norm(et_stack* s, const uint8_t* mask, int32_t n_tensors, floa
   TimedLaunch tl(s, ET_K_OTHER, st);
   int n_parts = 0;
   ET_TRY(run_sumsq(s, mask, n_tensors, grads, &n_parts, st));
-  et::norm_finalize_kernel<<<1, et::kClipThreads, 0, st>>>((const double*)s->at(s->off_norm_parts), n_parts, INFINITY, norm_dev);
-  return after_launch();
+  return launch_chained(et::norm_finalize_kernel, 1, et::kClipThreads, st, (const double*)s->at(s->off_norm_parts), n_parts, INFINITY,
+                        norm_dev);
 }
 
 et_status et_clip_grads(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float* const* clipped,
@@ -2349,13 +2357,11 @@ et_status et_clip_grads(et_stack* s, const uint8_t* mask, int32_t n_tensors, flo
   const double* parts = (const double*)s->at(s->off_norm_parts);
   if (n_parts == 0) {                                       // nothing selected: the norm is 0, the factor 1
     if (norm_dev == nullptr) return ET_OK;
-    et::norm_finalize_kernel<<<1, et::kClipThreads, 0, st>>>(parts, 0, max_norm, norm_dev);
-    return after_launch();
+    return launch_chained(et::norm_finalize_kernel, 1, et::kClipThreads, st, parts, 0, max_norm, norm_dev);
   }
   return for_each_clip_table(s, mask, n_tensors, grads, clipped, false, [&](const auto& tab) -> et_status {
     constexpr int N = sizeof(tab.e) / sizeof(tab.e[0]);
-    et::clip_kernel<N><<<clip_grid(s, tab.blocks), et::kClipThreads, 0, st>>>(tab, parts, n_parts, max_norm, norm_dev);
-    return after_launch();
+    return launch_chained(et::clip_kernel<N>, clip_grid(s, tab.blocks), et::kClipThreads, st, tab, parts, n_parts, max_norm, norm_dev);
   });
 }
 
@@ -2370,18 +2376,15 @@ et_status et_update_clipped(et_stack* s, const uint8_t* mask, int32_t n_tensors,
   const double* parts = (const double*)s->at(s->off_norm_parts);
   if (n_parts == 0) {
     if (norm_dev == nullptr) return ET_OK;
-    et::norm_finalize_kernel<<<1, et::kClipThreads, 0, st>>>(parts, 0, max_norm, norm_dev);
-    return after_launch();
+    return launch_chained(et::norm_finalize_kernel, 1, et::kClipThreads, st, parts, 0, max_norm, norm_dev);
   }
   const et::OptParams o = opt_params(s, lr);
   return for_each_clip_table(s, mask, n_tensors, grads, nullptr, true, [&](const auto& tab) -> et_status {
     constexpr int N = sizeof(tab.e) / sizeof(tab.e[0]);
     const int grid = clip_grid(s, tab.blocks);
     if (s->dtype == ET_BF16)
-      et::update_clipped_kernel<bf16, N><<<grid, et::kClipThreads, 0, st>>>(tab, parts, n_parts, max_norm, norm_dev, o);
-    else
-      et::update_clipped_kernel<float, N><<<grid, et::kClipThreads, 0, st>>>(tab, parts, n_parts, max_norm, norm_dev, o);
-    return after_launch();
+      return launch_chained(et::update_clipped_kernel<bf16, N>, grid, et::kClipThreads, st, tab, parts, n_parts, max_norm, norm_dev, o);
+    return launch_chained(et::update_clipped_kernel<float, N>, grid, et::kClipThreads, st, tab, parts, n_parts, max_norm, norm_dev, o);
   });
 }
 
@@ -2451,12 +2454,14 @@ et_status launch_held(const et_stack* s, const et::tok::Args& a, cudaStream_t st
   cfg.gridDim = dim3((unsigned)clusters * (unsigned)a.slices);
   cfg.blockDim = dim3(THREADS);
   cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = (unsigned)a.slices;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = a.slices > 1 ? 1 : 0;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)a.slices;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.slices > 1 ? 2 : 1;
   CU_TRY(cudaLaunchKernelEx(&cfg, et::tok::token_held_kernel<T, MODE, THREADS, NV>, a));
   return after_launch();
 }
@@ -2477,8 +2482,7 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
   if (slices * threads * 8 < vecs || (MODE == et::tok::kScore && a.rows >= 2 * s->sms && vecs >= 1024)) {
     a.slices = 1;
     a.per = vecs;
-    et::tok::token_row_kernel<T, MODE><<<(unsigned)a.rows, et::tok::kRowThreads, 0, st>>>(a);
-    return after_launch();
+    return launch_chained(et::tok::token_row_kernel<T, MODE>, (unsigned)a.rows, et::tok::kRowThreads, st, a);
   }
   a.slices = slices;
   a.per = ceil_div(vecs, slices);
@@ -2566,8 +2570,7 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   p.pairs = pairs; p.vocab = a.vocab; p.kind = cfg->kind; p.beta = cfg->beta; p.smoothing = cfg->label_smoothing;
   {
     TimedLaunch tl(s, ET_K_OTHER, st);
-    et::tok::pair_kernel<<<pairs, 256, 0, st>>>(p);
-    ET_TRY(after_launch());
+    ET_TRY(launch_chained(et::tok::pair_kernel, pairs, 256, st, p));
   }
   if (dY == nullptr) return ET_OK;
   a.dY = dY;
@@ -2577,9 +2580,8 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   const long long blocks = (long long)a.rows * a.slices;
   if (blocks > 0x7fffffffll) return ET_ERR_TOO_LARGE;
   TimedLaunch tl(s, ET_K_OTHER, st);
-  if (s->dtype == ET_BF16) et::tok::token_grad_kernel<bf16><<<(unsigned)blocks, et::tok::kGradThreads, 0, st>>>(a);
-  else                     et::tok::token_grad_kernel<float><<<(unsigned)blocks, et::tok::kGradThreads, 0, st>>>(a);
-  return after_launch();
+  return launch_chained(s->dtype == ET_BF16 ? et::tok::token_grad_kernel<bf16> : et::tok::token_grad_kernel<float>, (unsigned)blocks,
+                        et::tok::kGradThreads, st, a);
 }
 
 et_status et_stack_set_optimizer(et_stack* s, const et_optimizer_config* cfg, float* const* state1,

@@ -58,6 +58,7 @@ __device__ __forceinline__ double block_sum64(double v) {
 template <int N>
 __global__ void __launch_bounds__(kClipThreads)
 sumsq_kernel(const __grid_constant__ ClipTable<N> tab, double* __restrict__ parts) {
+  chain_begin();
   double acc = 0.0;
   for (long long vb = blockIdx.x; vb < tab.blocks; vb += gridDim.x) {
     const ClipEntry& e = tab.e[clip_find(tab, vb)];
@@ -96,6 +97,7 @@ __device__ __forceinline__ float2 norm_and_factor(const double* __restrict__ par
 }
 static __global__ void __launch_bounds__(kClipThreads)
 norm_finalize_kernel(const double* __restrict__ parts, int n, float max_norm, float* __restrict__ out) {
+  chain_begin();
   const float2 nf = norm_and_factor(parts, n, max_norm);
   if (threadIdx.x == 0) { out[0] = nf.x; out[1] = nf.y; }
 }
@@ -104,10 +106,11 @@ template <int N>
 __global__ void __launch_bounds__(kClipThreads)
 clip_kernel(const __grid_constant__ ClipTable<N> tab, const double* __restrict__ parts, int n_parts, float max_norm,
             float* __restrict__ norm_out) {
+  chain_begin();
   const float2 nf = norm_and_factor(parts, n_parts, max_norm);
   const float f = nf.y;
   if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = nf.x; norm_out[1] = f; }
-  for (long long vb = blockIdx.x; vb < tab.blocks; vb += gridDim.x) {
+  for (long long vb = tab.blocks - 1 - blockIdx.x; vb >= 0; vb -= gridDim.x) {   // backwards: the end is still in L2
     const ClipEntry& e = tab.e[clip_find(tab, vb)];
     if (f == 1.0f && e.out == e.g) continue;                // in place and nothing to clip: nothing changes
     const size_t i0 = (size_t)(vb - e.block_begin) * kClipBlock;
@@ -136,11 +139,12 @@ template <typename T, int N>
 __global__ void __launch_bounds__(kClipThreads)
 update_clipped_kernel(const __grid_constant__ ClipTable<N> tab, const double* __restrict__ parts, int n_parts, float max_norm,
                       float* __restrict__ norm_out, const OptParams opt) {
+  chain_begin();
   const float2 nf = norm_and_factor(parts, n_parts, max_norm);
   const float f = nf.y;
   if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = nf.x; norm_out[1] = f; }
   if (!(nf.x <= 3.402823466e38f)) return;
-  for (long long vb = blockIdx.x; vb < tab.blocks; vb += gridDim.x) {
+  for (long long vb = tab.blocks - 1 - blockIdx.x; vb >= 0; vb -= gridDim.x) {   // backwards: the end is still in L2
     const ClipEntry& e = tab.e[clip_find(tab, vb)];
 #pragma unroll
     for (int q = 0; q < kClipVec / 8; ++q) {

@@ -400,6 +400,7 @@ struct RowResult { float m, g, cs, lb, hit; };     // hit: the target's gradient
 template <typename T, int MODE, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS, (NV <= 4 ? 1536 : 1024) / THREADS)    // 40 or 64 registers a thread
 token_held_kernel(const __grid_constant__ Args a) {
+  chain_begin();
   constexpr int N = VecOf<T>::N, W = THREADS / 32;
   constexpr bool LEAN = MODE == kPolicy && N == 8;
   __shared__ float warp_m[W], warp_s[W], pair_m[2], pair_s[2];
@@ -557,6 +558,7 @@ constexpr int kRowThreads = 512;
 template <typename T, int MODE>
 __global__ void __launch_bounds__(kRowThreads)
 token_row_kernel(const __grid_constant__ Args a) {
+  chain_begin();
   constexpr int N = VecOf<T>::N, B = 4;
   const int row = blockIdx.x, tid = threadIdx.x;
   const Slice<T> sl(a, row, 0);                             // a.per: the vectors of a row
@@ -615,6 +617,7 @@ constexpr int kGradThreads = 256, kGradVecs = 4;
 template <typename T>
 __global__ void __launch_bounds__(kGradThreads)
 token_grad_kernel(const Args a) {
+  chain_begin();
   constexpr int N = VecOf<T>::N;
   const int row = blockIdx.x / a.slices, v0 = (blockIdx.x % a.slices) * (kGradThreads * kGradVecs) + threadIdx.x;
   const size_t base = (size_t)row * a.width;
@@ -675,6 +678,7 @@ __device__ __forceinline__ double log1pexp(double x) {       // log(1 + exp(x))
 // One block per pair: both sums (64 bits, fixed order), the pair's loss, the rows' coefficients.
 static __global__ void __launch_bounds__(256)
 pair_kernel(const PairArgs a) {
+  chain_begin();
   __shared__ double sh[8];
   __shared__ double total[2];
   const int p = blockIdx.x;

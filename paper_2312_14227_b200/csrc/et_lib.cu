@@ -2563,6 +2563,7 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   a.logp = (float*)s->at(s->off_tok_logp);
   a.stats = (float2*)s->at(s->off_tok_stats);
   a.coef = (float*)s->at(s->off_tok_coef);                   // set to 0: rows of no sequence keep it
+  a.begin = seq_begin; a.n_begin = 2 * pairs;
   ET_TRY(launch_tokens<et::tok::kScore>(s, a, st));
   et::tok::PairArgs p{};
   p.logp = a.logp; p.weights = weights; p.targets = targets; p.begin = seq_begin; p.ref = ref_logp; p.seq_logp = seq_logp;
@@ -2577,6 +2578,7 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   const int vec_elems = s->dtype == ET_BF16 ? 8 : 4;
   const int vecs = ceil_div(a.width, vec_elems) + (a.width % vec_elems != 0 ? 1 : 0);
   a.slices = ceil_div(vecs, et::tok::kGradThreads * et::tok::kGradVecs);
+  a.per = et::tok::kGradThreads * et::tok::kGradVecs;
   const long long blocks = (long long)a.rows * a.slices;
   if (blocks > 0x7fffffffll) return ET_ERR_TOO_LARGE;
   TimedLaunch tl(s, ET_K_OTHER, st);

@@ -52,8 +52,11 @@ struct Args {
   const float* logp_old;      // kPolicy; null: the current log probability (ratio 1)
   const float* logp_ref;      // kPolicy; null: no KL term
   float* logp;                // lp of each row, 0 where the row is left out; may be null
-  float2* stats;              // kScore writes, kGrad reads: (max of the row's y, 1 / sum exp(scale (y - max))); may be null
+  float2* stats;              // kScore writes, kGrad reads: (max of the row's y, 1 / sum exp(scale (y - max))), (0, -1) for a
+                              // row that is left out; may be null
   float* coef;                // kGrad: c_i.  kScore sets it to 0 where it is not null
+  const int32_t* begin;       // kScore: null, or [n_begin + 1]: rows outside begin[0] .. begin[n_begin] - 1 are left out
+  int32_t n_begin;
   double* parts;              // kPolicy: rows x 3: w * (-surrogate), w * kl, w * [clipped]; may be null
   uint32_t* done;             // kPolicy: blocks that have finished; 0 between calls
   uint32_t* ticket;           // kPolicy: rows handed out beyond the first two of each cluster; 0 between calls
@@ -149,6 +152,12 @@ __device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, i
   return w * slope;
 }
 
+// Whether a row takes part.
+template <int MODE>
+__device__ __forceinline__ bool takes_part(const Args& a, int row, int t, float w) {
+  if (MODE == kScore && a.begin != nullptr && (row < a.begin[0] || row >= a.begin[a.n_begin])) return false;
+  return w != 0.0f && t >= 0 && t < a.vocab;
+}
 // Sums of the policy loss's row contributions by the block that finishes last, in a fixed order.
 __device__ __forceinline__ void policy_finish(const Args& a) {
   __shared__ bool last;
@@ -415,14 +424,13 @@ token_held_kernel(const __grid_constant__ Args a) {
     t_next = a.targets[r];
     w_next = a.weights != nullptr ? a.weights[r] : a.default_weight;
   };
-  auto takes_part = [&](int t, float w) { return w != 0.0f && t >= 0 && t < a.vocab; };
   if (row < a.rows) head(row);
   for (int it = 0; row < a.rows; ++it) {                     // `row` is the same in all blocks of a cluster
     const int b = it & 1;
     const Slice<T> sl(a, row, rank * a.per);
     const int t = t_next;
     const float w = w_next;
-    const bool live = takes_part(t, w);
+    const bool live = takes_part<MODE>(a, row, t, w);
     uint4 q[NV];
     // every round but the last is full: the same for the whole block, and so for all but slices that begin inside a vector or
     // reach far beyond `vocab`
@@ -449,7 +457,7 @@ token_held_kernel(const __grid_constant__ Args a) {
       }
       if (next < a.rows) {
         head(next);
-        if (tid == THREADS - 1 && takes_part(t_next, w_next)) prefetch_slice(Slice<T>(a, next, rank * a.per));
+        if (tid == THREADS - 1 && takes_part<MODE>(a, next, t_next, w_next)) prefetch_slice(Slice<T>(a, next, rank * a.per));
       }
     }
     float m = -INFINITY, s = 0.0f, yt = 0.0f;
@@ -495,6 +503,7 @@ token_held_kernel(const __grid_constant__ Args a) {
         }
       } else if (first) {
         if (a.logp != nullptr) a.logp[row] = 0.0f;
+        if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(0.0f, -1.0f);
         if (MODE == kPolicy && a.parts != nullptr)
           for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
       }
@@ -564,26 +573,33 @@ token_row_kernel(const __grid_constant__ Args a) {
   const Slice<T> sl(a, row, 0);                             // a.per: the vectors of a row
   const int t = a.targets[row];
   const float w = a.weights != nullptr ? a.weights[row] : a.default_weight;
-  const bool live = w != 0.0f && t >= 0 && t < a.vocab;
+  const bool live = takes_part<MODE>(a, row, t, w);
   float c = 0.0f, m = -INFINITY, inv = 0.0f;
   if (live) {
+    // a gradient will read the logits once more: they are not marked as read for the last time
+    const bool last_read = MODE == kScore && a.coef == nullptr;
     float s = 0.0f;
-    for (int i = 0; i < a.per; i += B * kRowThreads) {
-      uint4 q[B];
-      if (i >= sl.lo && i + B * kRowThreads <= sl.hi) {
-#pragma unroll
-        for (int j = 0; j < B; ++j) q[j] = MODE == kScore ? __ldcs(sl.src + i + j * kRowThreads + tid) : sl.src[i + j * kRowThreads + tid];
-      } else {
-#pragma unroll
-        for (int j = 0; j < B; ++j) {
-          const int v = i + j * kRowThreads + tid;
-          q[j] = load_vec<T>(sl.y, sl.e0 + v * N, v < a.per ? a.vocab : 0);
-        }
-      }
+    auto batch = [&](const auto& q) {
       const float cm = fmaxf(max_of_all<T>(q), m);
       if (m != -INFINITY) s *= rebase<false>(m, cm, a);
       m = cm;
-      s = add_terms<T, false, B>(q, m == -INFINITY ? 0.0f : m, s, a);
+      s = add_terms<T, false>(q, m == -INFINITY ? 0.0f : m, s, a);
+    };
+    int v = tid;
+    if (v < sl.lo) {
+      const uint4 q[1] = {load_vec<T>(sl.y, sl.e0 + v * N, a.vocab)};
+      batch(q);
+      v += kRowThreads;
+    }
+    for (; v + (B - 1) * kRowThreads < sl.hi; v += B * kRowThreads) {
+      uint4 q[B];
+#pragma unroll
+      for (int j = 0; j < B; ++j) q[j] = last_read ? __ldcs(sl.src + v + j * kRowThreads) : sl.src[v + j * kRowThreads];
+      batch(q);
+    }
+    for (; v < a.per; v += kRowThreads) {
+      const uint4 q[1] = {load_vec<T>(sl.y, sl.e0 + v * N, a.vocab)};
+      batch(q);
     }
     block_max_sum<false>(m, s, a);
     const float lp = log_prob<false>(to_f32(sl.y[t]), m, s, a);
@@ -597,6 +613,7 @@ token_row_kernel(const __grid_constant__ Args a) {
     if (MODE == kPolicy && a.dY == a.y) __syncthreads();    // y[t] is read before it is overwritten
   } else if (tid == 0) {
     if (a.logp != nullptr) a.logp[row] = 0.0f;
+    if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(0.0f, -1.0f);
     if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
     if (MODE == kPolicy && a.parts != nullptr)
       for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
@@ -612,40 +629,59 @@ token_row_kernel(const __grid_constant__ Args a) {
   if (MODE == kPolicy) policy_finish(a);
 }
 
-// The gradient from a row's (max, 1 / sum) and c, block (slice, row): nothing but a stream over the logits.
+// The gradient from a row's (max, 1 / sum) and c, block (row, slice): nothing but a stream over the logits.
 constexpr int kGradThreads = 256, kGradVecs = 4;
 template <typename T>
 __global__ void __launch_bounds__(kGradThreads)
-token_grad_kernel(const Args a) {
+token_grad_kernel(const __grid_constant__ Args a) {
   chain_begin();
-  constexpr int N = VecOf<T>::N;
-  const int row = blockIdx.x / a.slices, v0 = (blockIdx.x % a.slices) * (kGradThreads * kGradVecs) + threadIdx.x;
-  const size_t base = (size_t)row * a.width;
-  const T* y = (const T*)a.y + base;
-  T* dY = (T*)a.dY + base;
-  const int mis = (int)(base % N);
+  constexpr int N = VecOf<T>::N, STEP = kGradThreads;
+  const int row = (int)(blockIdx.x / a.slices);
+  const Slice<T> sl(a, row, (blockIdx.x % a.slices) * (kGradThreads * kGradVecs));   // a.per: vectors of a slice
+  const int tid = threadIdx.x;
   const float c = a.coef[row];
-  if (c == 0.0f) {                                          // left out, or of no weight: the logits are not read
+  const float2 st = a.stats[row];
+  const int t = a.targets[row];
+  const bool regular = sl.lo == 0 && kGradVecs * STEP <= sl.hi;                       // the same for the whole block
+  if (c == 0.0f || st.y < 0.0f) {                           // left out, or of no weight: the logits are not read
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
     for (int i = 0; i < kGradVecs; ++i) {
-      const int e0 = (v0 + i * kGradThreads) * N - mis;
-      if (e0 < a.width) store_vec<T>(dY, e0, a.width, a.width, make_uint4(0u, 0u, 0u, 0u));
+      const int v = i * STEP + tid;
+      if (regular) __stcs(sl.dst + v, zero);
+      else if (sl.e0 + v * N < a.width) store_vec<T>(sl.dY, sl.e0 + v * N, a.width, a.width, zero);
     }
     return;
   }
-  uint4 q[kGradVecs];
-#pragma unroll
-  for (int i = 0; i < kGradVecs; ++i) {
-    const int e0 = (v0 + i * kGradThreads) * N - mis;
-    q[i] = load_vec<T>(y, e0, a.vocab);
-  }
-  const float2 st = a.stats[row];
-  const int t = a.targets[row];
   const float cs = c * a.scale, g = -cs * st.y;
+  const bool lean = N == 8 && fabsf(st.x) <= kLeanMax && g != 0.0f;
+  uint4 q[kGradVecs];
+  if (regular && (lean || N == 4)) {
+#pragma unroll
+    for (int i = 0; i < kGradVecs; ++i) q[i] = __ldcs(sl.src + i * STEP + tid);
+    const float b = log2f(fabsf(g)) - st.x * a.k_hi;
+    const uint64_t kh = pack2(a.k_hi, a.k_hi), lb = pack2(b, b);
+    const uint32_t flip = g < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int i = 0; i < kGradVecs; ++i) {
+      if constexpr (N == 8) __stcs(sl.dst + i * STEP + tid, lean_grad_vec(q[i], kh, lb, flip));
+      else __stcs(sl.dst + i * STEP + tid, grad_vec<T>(q[i], st.x, g, 0.0f, -1, a));
+    }
+    const int tv = (t - sl.e0) >> (N == 8 ? 3 : 2);          // the target's vector once more, by the thread that wrote it
+    if (t >= sl.e0 && tv < kGradVecs * STEP && tv % STEP == tid) {
+      // its words are in a register that a constant index names
+#pragma unroll
+      for (int i = 0; i < kGradVecs; ++i)
+        if (tv / STEP == i) __stcs(sl.dst + tv, grad_vec<T>(q[i], st.x, g, cs, t - (sl.e0 + tv * N), a));
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kGradVecs; ++i) q[i] = load_vec<T>(sl.y, sl.e0 + (i * STEP + tid) * N, a.vocab);
 #pragma unroll
   for (int i = 0; i < kGradVecs; ++i) {
-    const int e0 = (v0 + i * kGradThreads) * N - mis;
-    if (e0 < a.width) store_vec<T>(dY, e0, a.width, a.vocab, grad_vec<T>(q[i], st.x, g, cs, t - e0, a));
+    const int e0 = sl.e0 + (i * STEP + tid) * N;
+    if (e0 < a.width) store_vec<T>(sl.dY, e0, a.width, a.vocab, grad_vec<T>(q[i], st.x, g, cs, t - e0, a));
   }
 }
 

@@ -1,6 +1,7 @@
 """ctypes binding of include/et.h.  Function names and argument order follow the C ABI."""
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import Optional, Sequence
@@ -157,7 +158,11 @@ def _ptr_array(seq: Optional[Sequence], n: int):
     if seq is None:
         return None
     assert len(seq) == n
-    return (C.c_void_p * n)(*map(_ptr, seq))
+    try:                                             # tensors and None: the usual case, hundreds of them a step
+        ptrs = array.array("Q", [0 if t is None else t.data_ptr() for t in seq])
+    except AttributeError:
+        ptrs = array.array("Q", [_ptr(t) or 0 for t in seq])
+    return (C.c_void_p * n).from_buffer(ptrs)
 
 
 def _stream_ptr(stream) -> Optional[int]:
@@ -167,6 +172,8 @@ def _stream_ptr(stream) -> Optional[int]:
 
 
 def _mask_arr(mask) -> np.ndarray:
+    if type(mask) is np.ndarray and mask.dtype == np.uint8 and mask.flags.c_contiguous:
+        return mask
     return np.ascontiguousarray(np.asarray(mask, dtype=np.uint8))
 
 

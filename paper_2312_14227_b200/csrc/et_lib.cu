@@ -1469,7 +1469,9 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
       }
     }
     if (!done_by_list) {
-    const bool two = !s->timing && s->opt_two_streams && setup_two_streams(s);   // per-kernel timing wants kernels one at a time
+    // per-kernel timing wants kernels one at a time; an embedding by itself has no error-gradient chain to run beside
+    const bool alone = L == 1 && s->ly[0].kind == ET_LAYER_EMBEDDING;
+    const bool two = !s->timing && !alone && s->opt_two_streams && setup_two_streams(s);
     // Sharing the GPU with the higher-priority error-gradient chain: when few kernels are selected
     // the weight gradients are filler work and should hand their SMs back after every unit; when
     // they are as much work as the chain itself, persistent CTAs (epilogue overlap) pay more (ViT-B step:

@@ -198,6 +198,7 @@ sort_one_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uin
   __shared__ uint32_t sk[kSortOneMax];
   __shared__ uint16_t sr[kSortOneMax];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int warps = (n + E * 32 - 1) / (E * 32);            // warps that hold ids
   if (named != nullptr)
     for (int i = tid; i < (vocab + 31) / 32; i += 1024) named[i] = 0;
   // a warp owns E * 32 consecutive positions; few ids: the first warps hold them all
@@ -217,20 +218,20 @@ sort_one_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uin
       if (in[q] && key[q] < (uint32_t)vocab) atomicOr(&named[key[q] >> 5], 1u << (key[q] & 31));
   }
   for (int shift = 0; shift < bits; shift += kSortOneBits) {
-    for (int i = tid; i < 32 * BINS / 2; i += 1024) reinterpret_cast<uint32_t*>(&cnt[0][0])[i] = 0;
+    for (int i = tid; i < warps * BINS / 2; i += 1024) reinterpret_cast<uint32_t*>(&cnt[0][0])[i] = 0;
     __syncthreads();
-    warp_ranks<E>(key, in, shift, BINS - 1, cnt[wid], rank);
+    if (wid < warps) warp_ranks<E>(key, in, shift, BINS - 1, cnt[wid], rank);
     __syncthreads();
     uint32_t total = 0;
     if (tid < BINS)
-      for (int w = 0; w < 32; ++w) {
+      for (int w = 0; w < warps; ++w) {
         const uint32_t c = cnt[w][tid];
         cnt[w][tid] = (uint16_t)total;
         total += c;
       }
     const uint32_t at = block_scan(tid < BINS ? total : 0u, 1024);
     if (tid < BINS)
-      for (int w = 0; w < 32; ++w) cnt[w][tid] = (uint16_t)(cnt[w][tid] + at);
+      for (int w = 0; w < warps; ++w) cnt[w][tid] = (uint16_t)(cnt[w][tid] + at);
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < E; ++q)

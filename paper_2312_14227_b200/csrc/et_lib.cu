@@ -2445,12 +2445,20 @@ et_status resident_clusters(int threads, int slices, int sms, int* out) {
   *out = cached[dev][lg];
   return ET_OK;
 }
+// The reported numbers of a policy loss where its kernel's last block does not add them up.
+et_status policy_total(const et::tok::Args& a, cudaStream_t st) {
+  if (a.finish != 0) return ET_OK;
+  return launch_chained(et::tok::policy_finish_kernel, 1, 1024, st, a);
+}
 template <typename T, int MODE, int THREADS, int NV>
-et_status launch_held(const et_stack* s, const et::tok::Args& a, cudaStream_t st) {
+et_status launch_held(const et_stack* s, et::tok::Args a, cudaStream_t st) {
   int clusters = a.rows;                                    // kScore: one row a block (or cluster)
   if (MODE == et::tok::kPolicy) {
     ET_TRY((resident_clusters<et::tok::token_held_kernel<T, MODE, THREADS, NV>>(THREADS, a.slices, s->sms, &clusters)));
     clusters = std::min(clusters, a.rows);
+    a.n_parts = THREADS >= et::tok::kTicketThreads ? a.rows : clusters;
+    // a few loads a thread for the last block, else a kernel of its own (32 threads took 150 us over 16384 rows)
+    a.finish = a.out == nullptr || a.n_parts <= 16 * THREADS ? 1 : 0;
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)clusters * (unsigned)a.slices);
@@ -2465,7 +2473,29 @@ et_status launch_held(const et_stack* s, const et::tok::Args& a, cudaStream_t st
   cfg.attrs = attr;
   cfg.numAttrs = a.slices > 1 ? 2 : 1;
   CU_TRY(cudaLaunchKernelEx(&cfg, et::tok::token_held_kernel<T, MODE, THREADS, NV>, a));
-  return after_launch();
+  ET_TRY(after_launch());
+  return MODE == et::tok::kPolicy ? policy_total(a, st) : ET_OK;
+}
+template <typename T, int MODE, int THREADS>
+et_status held_by_rounds(const et_stack* s, const et::tok::Args& a, int rounds, cudaStream_t st) {
+  switch (rounds) {                                         // below 5 only where 32 threads are too many or a cluster splits evenly
+    case 1: case 2: return launch_held<T, MODE, THREADS, 2>(s, a, st);
+    case 3: case 4: return launch_held<T, MODE, THREADS, 4>(s, a, st);
+    case 5: return launch_held<T, MODE, THREADS, 5>(s, a, st);
+    case 6: return launch_held<T, MODE, THREADS, 6>(s, a, st);
+    case 7: return launch_held<T, MODE, THREADS, 7>(s, a, st);
+    default: return launch_held<T, MODE, THREADS, 8>(s, a, st);
+  }
+}
+template <typename T, int MODE>
+et_status held_by_threads(const et_stack* s, const et::tok::Args& a, int threads, int rounds, cudaStream_t st) {
+  switch (threads) {
+    case 32: return held_by_rounds<T, MODE, 32>(s, a, rounds, st);
+    case 64: return held_by_rounds<T, MODE, 64>(s, a, rounds, st);
+    case 128: return held_by_rounds<T, MODE, 128>(s, a, rounds, st);
+    case 256: return held_by_rounds<T, MODE, 256>(s, a, rounds, st);
+    default: return held_by_rounds<T, MODE, 512>(s, a, rounds, st);
+  }
 }
 template <typename T, int MODE>
 et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
@@ -2473,10 +2503,12 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
   // 16-byte vectors of a row: the logits alone where nothing is written; one more where rows begin inside a vector
   const int cols = a.dY != nullptr ? a.width : a.vocab;
   const int vecs = ceil_div(cols, N) + (a.width % N != 0 ? 1 : 0);
-  // How a row is cut: one block where 512 threads x 8 vectors hold it, else the fewest blocks of 256 threads (four of them
-  // fit an SM, so more rows are in flight: 131072 bf16 columns 832 us in 8 x 256 threads, 866 us in 4 x 512), else of 512.
-  // Every thread takes the same number of rounds, as few as the slice needs: empty rounds cost as much as full ones.
-  int slices = 1, threads = vecs <= 256 ? 128 : vecs <= 2048 ? 256 : 512;
+  // How a row is cut: one block, the smallest whose threads hold it in 8 vectors each, up to 512 threads; beyond that the fewest
+  // blocks of 256 threads (four of them fit an SM, so more rows are in flight: 131072 bf16 columns 832 us in 8 x 256 threads,
+  // 866 us in 4 x 512), else of 512.  Every thread takes the same number of rounds, as few as the slice needs: empty rounds cost
+  // as much as full ones.
+  int slices = 1, threads = 32;
+  while (threads < 512 && vecs > threads * 8) threads *= 2;
   if (vecs > 512 * 8) {
     threads = vecs <= 8 * 256 * 8 ? 256 : 512;
     while (slices < 8 && slices * threads * 8 < vecs) slices *= 2;
@@ -2484,29 +2516,14 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
   if (slices * threads * 8 < vecs || (MODE == et::tok::kScore && a.rows >= 2 * s->sms && vecs >= 1024)) {
     a.slices = 1;
     a.per = vecs;
-    return launch_chained(et::tok::token_row_kernel<T, MODE>, (unsigned)a.rows, et::tok::kRowThreads, st, a);
+    a.n_parts = a.rows;
+    a.finish = a.rows <= 16 * et::tok::kRowThreads ? 1 : 0;
+    ET_TRY(launch_chained(et::tok::token_row_kernel<T, MODE>, (unsigned)a.rows, et::tok::kRowThreads, st, a));
+    return MODE == et::tok::kPolicy ? policy_total(a, st) : ET_OK;
   }
   a.slices = slices;
   a.per = ceil_div(vecs, slices);
-  const int rounds = ceil_div(a.per, threads);
-  if (threads == 128) return rounds == 1 ? launch_held<T, MODE, 128, 1>(s, a, st) : launch_held<T, MODE, 128, 2>(s, a, st);
-  if (threads == 256) {
-    switch (rounds) {
-      case 1: case 2: return launch_held<T, MODE, 256, 2>(s, a, st);
-      case 3: return launch_held<T, MODE, 256, 3>(s, a, st);
-      case 4: return launch_held<T, MODE, 256, 4>(s, a, st);
-      case 5: return launch_held<T, MODE, 256, 5>(s, a, st);
-      case 6: return launch_held<T, MODE, 256, 6>(s, a, st);
-      case 7: return launch_held<T, MODE, 256, 7>(s, a, st);
-      default: return launch_held<T, MODE, 256, 8>(s, a, st);
-    }
-  }
-  switch (rounds) {
-    case 5: return launch_held<T, MODE, 512, 5>(s, a, st);
-    case 6: return launch_held<T, MODE, 512, 6>(s, a, st);
-    case 7: return launch_held<T, MODE, 512, 7>(s, a, st);
-    default: return launch_held<T, MODE, 512, 8>(s, a, st);   // fewer rounds do not come up: slices of 512 threads are over 2048 vectors
-  }
+  return held_by_threads<T, MODE>(s, a, threads, ceil_div(a.per, threads), st);
 }
 template <int MODE>
 et_status launch_tokens(et_stack* s, const et::tok::Args& a, cudaStream_t st) {

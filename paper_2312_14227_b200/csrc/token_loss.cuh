@@ -57,7 +57,9 @@ struct Args {
   float* coef;                // kGrad: c_i.  kScore sets it to 0 where it is not null
   const int32_t* begin;       // kScore: null, or [n_begin + 1]: rows outside begin[0] .. begin[n_begin] - 1 are left out
   int32_t n_begin;
-  double* parts;              // kPolicy: rows x 3: w * (-surrogate), w * kl, w * [clipped]; may be null
+  double* parts;              // kPolicy: 3 x n_parts: w * (-surrogate), w * kl, w * [clipped], of a row or of a block's rows; may be null
+  int32_t n_parts;
+  int32_t finish;             // kPolicy: the block that finishes last adds the parts up (else policy_finish_kernel does)
   uint32_t* done;             // kPolicy: blocks that have finished; 0 between calls
   uint32_t* ticket;           // kPolicy: rows handed out beyond the first two of each cluster; 0 between calls
   float* out;                 // kPolicy with parts: {loss, policy part, kl part, clipped share}
@@ -139,8 +141,8 @@ __device__ __forceinline__ RowTerms row_terms(const Args& a, int row) {
   r.ref = a.logp_ref != nullptr ? a.logp_ref[row] : 0.0f;
   return r;
 }
-// `report`: this thread writes the contributions (64-bit arithmetic, so one thread's work, not a block's).
-__device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, int row, float lp, float w, bool report) {
+// `sums`: the contributions are added here (64-bit arithmetic, so one thread's work, not a block's); may be null.
+__device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, float lp, float w, double* sums) {
   const float r = a.logp_old != nullptr ? expf(lp - t.old) : 1.0f;
   const float rc = fminf(fmaxf(r, 1.0f - a.clip_low), 1.0f + a.clip_high);
   const bool clipped = r * t.adv > rc * t.adv;
@@ -151,11 +153,10 @@ __device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, i
     kl = e - d;
     slope -= a.kl_coef * e;
   }
-  if (report) {
-    double* part = a.parts + (size_t)row * 3;
-    part[0] = -(double)w * (double)((clipped ? rc : r) * t.adv);
-    part[1] = (double)w * (double)kl;
-    part[2] = clipped ? (double)w : 0.0;
+  if (sums != nullptr) {
+    sums[0] -= (double)w * (double)((clipped ? rc : r) * t.adv);
+    sums[1] += (double)w * (double)kl;
+    if (clipped) sums[2] += (double)w;
   }
   return w * slope;
 }
@@ -166,10 +167,47 @@ __device__ __forceinline__ bool takes_part(const Args& a, int row, int t, float 
   if (MODE == kScore && a.begin != nullptr && (row < a.begin[0] || row >= a.begin[a.n_begin])) return false;
   return w != 0.0f && t >= 0 && t < a.vocab;
 }
-// Sums of the policy loss's row contributions by the block that finishes last, in a fixed order.
-__device__ __forceinline__ void policy_finish(const Args& a) {
-  __shared__ bool last;
+__device__ __forceinline__ void put_parts(const Args& a, int at, const double (&s)[3]) {
+#pragma unroll
+  for (int q = 0; q < 3; ++q) a.parts[(size_t)q * a.n_parts + at] = s[q];
+}
+// The parts added up by one block, in a fixed order; counters back to 0 for the next call.
+__device__ __forceinline__ void policy_total(const Args& a) {
   __shared__ double sh[3][32];
+  if (a.out != nullptr) {
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+      double s = 0.0;
+#pragma unroll 4
+      for (int i = threadIdx.x; i < a.n_parts; i += blockDim.x) s += __ldcg(a.parts + (size_t)q * a.n_parts + i);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      if ((threadIdx.x & 31) == 0) sh[q][threadIdx.x >> 5] = s;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    if (a.out != nullptr) {
+      double r[3];
+      for (int q = 0; q < 3; ++q) {
+        r[q] = 0.0;
+        for (int wq = 0; wq < (int)((blockDim.x + 31) >> 5); ++wq) r[q] += sh[q][wq];
+      }
+      a.out[0] = (float)(r[0] + (double)a.kl_coef * r[1]);
+      a.out[1] = (float)r[0]; a.out[2] = (float)r[1]; a.out[3] = (float)r[2];
+    }
+    *a.done = 0u;
+    *a.ticket = 0u;
+  }
+}
+static __global__ void __launch_bounds__(1024) policy_finish_kernel(const __grid_constant__ Args a) {
+  chain_begin();
+  policy_total(a);
+}
+// The same by the block that finishes last.
+__device__ __forceinline__ void policy_finish(const Args& a) {
+  if (a.finish == 0) return;
+  __shared__ bool last;
   if (threadIdx.x == 0) {
     __threadfence();
     last = atomicAdd(a.done, 1u) == gridDim.x - 1;
@@ -177,31 +215,7 @@ __device__ __forceinline__ void policy_finish(const Args& a) {
   __syncthreads();
   if (!last) return;
   __threadfence();
-  double s[3] = {0.0, 0.0, 0.0};
-  if (a.out != nullptr)
-    for (int i = threadIdx.x; i < a.rows; i += blockDim.x)
-#pragma unroll
-      for (int q = 0; q < 3; ++q) s[q] += __ldcg(a.parts + (size_t)i * 3 + q);
-#pragma unroll
-  for (int q = 0; q < 3; ++q) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s[q] += __shfl_xor_sync(0xffffffffu, s[q], o);
-    if ((threadIdx.x & 31) == 0) sh[q][threadIdx.x >> 5] = s[q];
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    double r[3];
-    for (int q = 0; q < 3; ++q) {
-      r[q] = 0.0;
-      for (int wq = 0; wq < (int)(blockDim.x >> 5); ++wq) r[q] += sh[q][wq];
-    }
-    if (a.out != nullptr) {
-      a.out[0] = (float)(r[0] + (double)a.kl_coef * r[1]);
-      a.out[1] = (float)r[0]; a.out[2] = (float)r[1]; a.out[3] = (float)r[2];
-    }
-    *a.done = 0u;
-    *a.ticket = 0u;
-  }
+  policy_total(a);
 }
 
 // ---- 16-byte vectors of a row ------------------------------------------------------------------
@@ -412,14 +426,16 @@ struct RowResult { float m, g, cs, lb, hit; };     // hit: the target's gradient
 // What bounds it is issue slots and the exponential unit next to DRAM: at 16 bytes in and out, an SM has 177 issue slots per
 // vector and thread at full bandwidth and the exponentials alone take 128 cycles of their unit.  So range checks are made for
 // THREADS vectors at a time and what is done once per row is done by one warp.  For kPolicy the blocks are persistent and take
-// rows by ticket (rows that are left out cost less than others, so a fixed share would leave SMs idle at the end); a row is
-// known an iteration ahead and its slice is asked into L2 by one instruction while the row before is worked on.
+// long rows by ticket (rows that are left out cost less than others, so a fixed share would leave SMs idle at the end; short ones
+// even out, and one counter would not serve them all); a row is known an iteration ahead and its slice is asked into L2 by one instruction while the row before is worked on.
+constexpr int kTicketThreads = 128;
 template <typename T, int MODE, int THREADS, int NV>
-__global__ void __launch_bounds__(THREADS, (NV <= 4 ? 1536 : 1024) / THREADS)    // 40 or 64 registers a thread
+__global__ void __launch_bounds__(THREADS, THREADS < 64 ? 32 : (NV <= 4 ? 1536 : 1024) / THREADS)    // 40 or 64 registers a thread
 token_held_kernel(const __grid_constant__ Args a) {
   chain_begin();
   constexpr int N = VecOf<T>::N, W = THREADS / 32;
   constexpr bool LEAN = MODE == kPolicy && N == 8;
+  constexpr bool TICKETS = MODE == kPolicy && THREADS >= kTicketThreads;      // else every block takes each gridDim.x-th row
   __shared__ float warp_m[W], warp_s[W], pair_m[2], pair_s[2];
   __shared__ RowResult result;
   __shared__ int rows_after[2];
@@ -432,6 +448,7 @@ token_held_kernel(const __grid_constant__ Args a) {
     t_next = a.targets[r];
     w_next = a.weights != nullptr ? a.weights[r] : a.default_weight;
   };
+  double sums[3] = {0.0, 0.0, 0.0};                          // without tickets: of all the rows of the block
   if (row < a.rows) head(row);
   for (int it = 0; row < a.rows; ++it) {                     // `row` is the same in all blocks of a cluster
     const int b = it & 1;
@@ -458,7 +475,7 @@ token_held_kernel(const __grid_constant__ Args a) {
       q[NV - 1] = load_vec<T>(sl.y, sl.e0 + v * N, v < a.per ? a.vocab : 0);
     }
     if (MODE == kPolicy) {
-      if (rank == 0 && tid == 0) {                           // the row after the next one
+      if (TICKETS && rank == 0 && tid == 0) {         // the row after the next one
         const int after = 2 * clusters + (int)atomicAdd(a.ticket, 1u);
         if (C == 1) rows_after[b] = after;
         else for (int c = 0; c < C; ++c) st_cluster(&rows_after[b], c, after);
@@ -507,14 +524,15 @@ token_held_kernel(const __grid_constant__ Args a) {
           if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
         }
         if (MODE == kPolicy) {
-          const float cs = policy_coef(a, terms, row, lp, w, first && a.parts != nullptr) * a.scale, g = -cs * inv;
+          double one[3] = {0.0, 0.0, 0.0};
+          const float cs = policy_coef(a, terms, lp, w, first && a.parts != nullptr ? (TICKETS ? one : sums) : nullptr) * a.scale, g = -cs * inv;
+          if (TICKETS && first && a.parts != nullptr) put_parts(a, row, one);
           if (lane == 0) result = RowResult{m, g, cs, log2f(fabsf(g)) - m * a.k_hi, fmaf(g, exp_diff(yt - m, a), cs)};
         }
       } else if (first) {
         if (a.logp != nullptr) a.logp[row] = 0.0f;
         if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(0.0f, -1.0f);
-        if (MODE == kPolicy && a.parts != nullptr)
-          for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
+        if (TICKETS && a.parts != nullptr) put_parts(a, row, {0.0, 0.0, 0.0});
       }
       if (MODE == kScore && first && a.coef != nullptr) a.coef[row] = 0.0f;
     } else if (C > 1) {                                      // barriers of the cluster count every thread
@@ -523,7 +541,7 @@ token_held_kernel(const __grid_constant__ Args a) {
     }
     if (MODE == kScore) break;                               // one row a block
     __syncthreads();
-    const int after = rows_after[b];
+    const int after = TICKETS ? rows_after[b] : next + clusters;
     if (a.dY != nullptr && live) {
       const RowResult r = result;
       const uint64_t kh = pack2(a.k_hi, a.k_hi), lb = pack2(r.lb, r.lb);
@@ -563,6 +581,7 @@ token_held_kernel(const __grid_constant__ Args a) {
     row = next;
     next = after;
   }
+  if (MODE == kPolicy && !TICKETS && a.parts != nullptr && rank == 0 && tid == 0) put_parts(a, blockIdx.x / C, sums);
   if (C > 1) {                                               // no block leaves while another reads its shared memory
     cluster_arrive();
     cluster_wait();
@@ -614,7 +633,11 @@ token_row_kernel(const __grid_constant__ Args a) {
     const float yt = to_f32(sl.y[t]);
     const float lp = MODE == kPolicy ? log_prob<false>(yt, m, s, a) : tid == 0 ? log_prob_summed(yt, m, s, a) : 0.0f;
     inv = 1.0f / s;
-    if (MODE == kPolicy) c = policy_coef(a, row_terms(a, row), row, lp, w, tid == 0 && a.parts != nullptr);
+    if (MODE == kPolicy) {
+      double sums[3] = {0.0, 0.0, 0.0};
+      c = policy_coef(a, row_terms(a, row), lp, w, tid == 0 && a.parts != nullptr ? sums : nullptr);
+      if (tid == 0 && a.parts != nullptr) put_parts(a, row, sums);
+    }
     if (tid == 0) {
       if (a.logp != nullptr) a.logp[row] = lp;
       if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(m, inv);
@@ -625,8 +648,7 @@ token_row_kernel(const __grid_constant__ Args a) {
     if (a.logp != nullptr) a.logp[row] = 0.0f;
     if (MODE == kScore && a.stats != nullptr) a.stats[row] = make_float2(0.0f, -1.0f);
     if (MODE == kScore && a.coef != nullptr) a.coef[row] = 0.0f;
-    if (MODE == kPolicy && a.parts != nullptr)
-      for (int j = 0; j < 3; ++j) a.parts[(size_t)row * 3 + j] = 0.0;
+    if (MODE == kPolicy && a.parts != nullptr) put_parts(a, row, {0.0, 0.0, 0.0});
   }
   if (MODE == kPolicy && a.dY != nullptr) {
     const float cs = c * a.scale, g = -cs * inv;

@@ -22,15 +22,19 @@ constexpr int kSortOneBits = 8;
 // VEC kernels take widths that are multiples of kVec with 16-byte aligned bases: eight elements move as whole vectors without a
 // test, so that the compiler can put the loads of several rows on their way together (behind load_seg's tests it cannot: 103
 // against 60 us for the gradient kernel of 32768 x 2048).
-template <bool VEC, typename T>
-__device__ __forceinline__ void emb_load(const T* p, int n, float (&v)[kVec]) {
-  if constexpr (!VEC) {
-    load_seg<kVec>(p, n, v);
-  } else if constexpr (sizeof(T) == 4) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+// Eight elements as they lie in memory: what is held while loads are on their way (four registers for bf16, not eight).
+template <typename T, bool VEC> struct EmbRaw;
+template <> struct EmbRaw<float, true> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p, int) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
+  __device__ __forceinline__ void get(float (&v)[kVec]) const {
     v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  } else {
-    const uint4 q = *reinterpret_cast<const uint4*>(p);
+  }
+};
+template <> struct EmbRaw<bf16, true> {
+  uint4 q;
+  __device__ __forceinline__ void load(const bf16* p, int) { q = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&v)[kVec]) const {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -38,6 +42,20 @@ __device__ __forceinline__ void emb_load(const T* p, int n, float (&v)[kVec]) {
       v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
   }
+};
+template <typename T> struct EmbRaw<T, false> {
+  float f[kVec];
+  __device__ __forceinline__ void load(const T* p, int n) { load_seg<kVec>(p, n, f); }
+  __device__ __forceinline__ void get(float (&v)[kVec]) const {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = f[i];
+  }
+};
+template <bool VEC, typename T>
+__device__ __forceinline__ void emb_load(const T* p, int n, float (&v)[kVec]) {
+  EmbRaw<T, VEC> r;
+  r.load(p, n);
+  r.get(v);
 }
 // ---- lookup: one warp per row -----------------------------------------------------------------
 template <typename T, bool VEC>
@@ -89,6 +107,13 @@ struct EmbSink {
   OptParams opt;
   int do_sgd, delta_is_snapshot;
 };
+template <typename T>
+__device__ __forceinline__ void emb_sgd(const EmbSink<T>& k, size_t i0, float (&w)[kVec], const float (&g)[kVec]) {
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) w[i] = fmaf(-k.opt.lr, g[i], w[i]);        // opt_update's plain SGD
+  if (k.master != nullptr) store_seg<kVec>(k.master + i0, kVec, w);
+  store_seg<kVec>(k.W + i0, kVec, w);
+}
 // Importance, optimisers and ragged widths: called, not inlined.  Eight inlined copies of the optimisers in the gradient kernel's
 // unrolled loop cost it more in instruction fetches than a call does (28 against 7 us for 300 rows).
 struct Eight { float v[kVec]; };
@@ -99,13 +124,27 @@ __device__ __noinline__ float emb_finish_call(const EmbSink<T>& k, size_t i0, in
   for (int i = 0; i < kVec; ++i) g[i] = e.v[i];
   return consume_grad<T>(i0, n, g, k.grad, k.delta, k.W, k.opt, k.do_sgd, k.delta_is_snapshot, k.master, k.m_state, k.v_state);
 }
-// EXPORT: the gradient is written and nothing else is wanted (whole vectors only).
-template <bool EXPORT, typename T>
+// Ways a finished row is consumed.  Export: it is written and nothing else is wanted.  Sgd, SgdMaster: w <- w - lr g and nothing else,
+// on the table or on its fp32 master.  General: all the rest, and ragged widths.
+enum EmbWay { kEmbGeneral = 0, kEmbExport = 1, kEmbSgd = 2, kEmbSgdMaster = 3 };
+template <int WAY, typename T> struct EmbWeight { using type = T; };          // where the current weight is read
+template <typename T> struct EmbWeight<kEmbSgdMaster, T> { using type = float; };
+template <int WAY, typename T>
+__device__ __forceinline__ const typename EmbWeight<WAY, T>::type* emb_weight(const EmbSink<T>& k) {
+  if constexpr (WAY == kEmbSgdMaster) return k.master;
+  else return k.W;
+}
+template <int WAY, typename T>
 __device__ __forceinline__ float emb_finish(const EmbSink<T>& k, size_t i0, int n, const float (&g)[kVec]) {
-  if constexpr (EXPORT) {
+  if constexpr (WAY == kEmbExport) {
     float4* p = reinterpret_cast<float4*>(k.grad + i0);
     __stcs(p, make_float4(g[0], g[1], g[2], g[3]));
     __stcs(p + 1, make_float4(g[4], g[5], g[6], g[7]));
+    return 0.0f;
+  } else if constexpr (WAY >= kEmbSgd) {
+    float w[kVec];
+    emb_load<true>(emb_weight<WAY>(k) + i0, kVec, w);
+    emb_sgd(k, i0, w, g);
     return 0.0f;
   } else {
     Eight e;
@@ -140,7 +179,7 @@ __device__ __forceinline__ void embed_fill(const EmbFill<T>& f, int block, int b
         float g[kVec];
 #pragma unroll
         for (int i = 0; i < kVec; ++i) g[i] = 0.0f;
-        emb_finish<false>(f.sink, (size_t)v * f.d + c, min(kVec, c1 - c), g);
+        emb_finish<kEmbGeneral>(f.sink, (size_t)v * f.d + c, min(kVec, c1 - c), g);
       }
     }
   }
@@ -347,55 +386,77 @@ sort_pass_kernel(const int32_t* __restrict__ ids, const uint32_t* __restrict__ k
 // Block (chunk, column tile): sums of the chunk's rows, id by id.  part: [chunks][2][d]; slot 0 = the id the chunk
 // continues from the one before, slot 1 = the id it hands on to the next.  imp_part: one number per block.
 // Blocks behind the last chunk fill table rows that no token names.
-template <typename T, bool VEC, bool EXPORT>
-__global__ void __launch_bounds__(256)
+template <typename T, bool VEC, int WAY>
+__global__ void __launch_bounds__(256, WAY == kEmbGeneral || sizeof(T) == 4 ? 2 : 3)
 embed_grad_kernel(const T* __restrict__ G, const uint32_t* __restrict__ keys, const uint32_t* __restrict__ rows, int n, int vocab,
                   int d, float scale, int chunks, float* __restrict__ part, float* __restrict__ imp_part, const __grid_constant__ EmbSink<T> sink,
                   const __grid_constant__ EmbFill<T> fill) {
   chain_begin();
-  constexpr int U = 8;                                          // rows on their way at once
+  constexpr bool SGD = WAY >= kEmbSgd;
+  constexpr int U = sizeof(T) == 2 && WAY != kEmbSgdMaster ? 8 : 4;   // rows on their way at once
   if ((int)blockIdx.x >= chunks) {
     embed_fill(fill, (blockIdx.x - chunks) * gridDim.y + blockIdx.y, (gridDim.x - chunks) * gridDim.y);
     return;
   }
-  __shared__ uint32_t sk[kEmbChunk + 2], sr[kEmbChunk];
+  // What happens after a row has been added: nothing (more of its id follows), the id is finished here, or its sum goes to one
+  // of the chunk's two slots: 0 for an id that began in an earlier chunk, 1 for one that goes on in the next.
+  enum { kMore = 0, kFinish = 1, kSlot0 = 2, kSlot1 = 3 };
+  __shared__ uint32_t sk[kEmbChunk], sr[kEmbChunk];
+  __shared__ uint8_t then[kEmbChunk];
+  __shared__ int count;                                         // rows that take part: left-out ones are behind all others
   const int chunk = blockIdx.x, p0 = chunk * kEmbChunk, len = min(kEmbChunk, n - p0);
-  for (int i = threadIdx.x; i < kEmbChunk + 2; i += blockDim.x) {   // sk[0]: the key before, sk[len + 1]: the one behind
-    const int p = p0 + i - 1;
-    sk[i] = p >= 0 && p < n ? keys[p] : 0xffffffffu;
-    if (i < kEmbChunk) sr[i] = i < len ? rows[p0 + i] : 0u;
+  if (threadIdx.x < 32) {                                       // kEmbChunk = 32: one lane per row
+    const int i = threadIdx.x, p = p0 + i;
+    const uint32_t key = i < len ? keys[p] : 0xffffffffu;
+    const uint32_t behind = i < len && p + 1 < n ? keys[p + 1] : 0xffffffffu;
+    const uint32_t before = p0 > 0 ? keys[p0 - 1] : 0xffffffffu;
+    const bool in = key < (uint32_t)vocab;
+    const uint32_t ins = __ballot_sync(0xffffffffu, in);
+    sk[i] = key;
+    sr[i] = in ? rows[p] : 0u;
+    const bool last = i + 1 == len, ends = last || behind != key;
+    then[i] = !in || !ends ? kMore : key == before ? kSlot0 : last && behind == key ? kSlot1 : kFinish;
+    if (i == 0) count = __popc(ins);
   }
   __syncthreads();
   const int c = (blockIdx.y * blockDim.x + threadIdx.x) * kVec;
-  const int nc = min(kVec, d - c);
+  const int nc = min(kVec, d - c), rows_in = count;
   float dot = 0.0f;
   if (nc > 0) {
     float acc[kVec];
-    bool head = sk[1] == sk[0];                                 // the first id began in an earlier chunk
 #pragma unroll
     for (int i = 0; i < kVec; ++i) acc[i] = 0.0f;
-    for (int q0 = 0; q0 < len && sk[q0 + 1] < (uint32_t)vocab; q0 += U) {
-      float v[U][kVec];
+    for (int q0 = 0; q0 < rows_in; q0 += U) {
+      EmbRaw<T, VEC> raw[U];
+      EmbRaw<typename EmbWeight<WAY, T>::type, true> weight[SGD ? U : 1];
 #pragma unroll
-      for (int u = 0; u < U; ++u)                               // behind the last row: row 0 again, or nothing; not added
-        emb_load<VEC>(G + (size_t)sr[(q0 + u) % kEmbChunk] * d + c, q0 + u < len && sk[q0 + u + 1] < (uint32_t)vocab ? nc : 0, v[u]);
+      for (int u = 0; u < U; ++u) {                             // behind the last row: row 0 again, or nothing; not added
+        const int q = min(q0 + u, kEmbChunk - 1);
+        raw[u].load(G + (size_t)sr[q] * d + c, q0 + u < rows_in ? nc : 0);
+        if constexpr (SGD) {
+          if (q0 + u < rows_in && then[q] == kFinish) weight[u].load(emb_weight<WAY>(sink) + (size_t)sk[q] * d + c, kVec);
+        }
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int q = q0 + u;
-        const uint32_t key = q < len ? sk[q + 1] : 0xffffffffu;
-        if (key >= (uint32_t)vocab) break;
+        if (q >= rows_in) break;
+        float v[kVec];
+        raw[u].get(v);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) acc[i] += v[u][i];
-        if (q + 1 < len && sk[q + 2] == key) continue;          // more of this id in the chunk
-        const bool tail = q + 1 == len && sk[q + 2] == key;     // ... or in the next one
-        if (head || tail) {
-          store_seg<kVec>(part + ((size_t)chunk * 2 + (head ? 0 : 1)) * d + c, nc, acc);
-        } else {
+        for (int i = 0; i < kVec; ++i) acc[i] += v[i];
+        const int what = then[q];
+        if (what == kMore) continue;
+        if (what == kFinish) {
 #pragma unroll
           for (int i = 0; i < kVec; ++i) acc[i] *= scale;
-          dot += emb_finish<EXPORT>(sink, (size_t)key * d + c, nc, acc);
+          if constexpr (SGD) {
+            weight[u].get(v);
+            emb_sgd(sink, (size_t)sk[q] * d + c, v, acc);
+          } else dot += emb_finish<WAY>(sink, (size_t)sk[q] * d + c, nc, acc);
+        } else {
+          store_seg<kVec>(part + ((size_t)chunk * 2 + (what - kSlot0)) * d + c, nc, acc);
         }
-        head = false;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) acc[i] = 0.0f;
       }
@@ -406,12 +467,13 @@ embed_grad_kernel(const T* __restrict__ G, const uint32_t* __restrict__ keys, co
     if (threadIdx.x == 0) imp_part[blockIdx.y * chunks + chunk] = dot;
   }
 }
+static_assert(kEmbChunk == 32, "the gradient kernel's first warp looks at one row a lane");
 
 // Block (group of kJoinChunks chunks, tile of 256 columns): the ids that begin in one of the chunks and go on in the next ones: adds
 // their partial rows.  Warp j takes chunk j's id where it crosses few borders; the others are added by all warps, eight
 // lanes of rows side by side, joined in a fixed order.
 constexpr int kJoinChunks = 8, kJoinCols = 32 * kVec, kJoinAlone = 4;
-template <typename T, bool VEC, bool EXPORT>
+template <typename T, bool VEC, int WAY>
 __global__ void __launch_bounds__(256)
 embed_join_kernel(const uint32_t* __restrict__ keys, int n, int vocab, int d, float scale, int chunks, const float* __restrict__ part,
                   float* __restrict__ imp_part, const __grid_constant__ EmbSink<T> sink) {
@@ -455,7 +517,7 @@ embed_join_kernel(const uint32_t* __restrict__ keys, int n, int vocab, int d, fl
         }
 #pragma unroll
       for (int i = 0; i < kVec; ++i) acc[i] *= scale;
-      dot += emb_finish<EXPORT>(sink, (size_t)keys[(size_t)(chunk + 1) * kEmbChunk] * d + c, nc, acc);
+      dot += emb_finish<WAY>(sink, (size_t)keys[(size_t)(chunk + 1) * kEmbChunk] * d + c, nc, acc);
     }
   }
   for (int j = 0; j < kJoinChunks; ++j) {
@@ -487,7 +549,7 @@ embed_join_kernel(const uint32_t* __restrict__ keys, int n, int vocab, int d, fl
         acc[i] = s * scale;
       }
       const uint32_t key = keys[(size_t)(chunk + 1) * kEmbChunk];
-      dot += emb_finish<EXPORT>(sink, (size_t)key * d + c, nc, acc);
+      dot += emb_finish<WAY>(sink, (size_t)key * d + c, nc, acc);
     }
     __syncthreads();
   }

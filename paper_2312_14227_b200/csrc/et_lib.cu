@@ -1002,6 +1002,7 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
   float* part = (float*)s->at(L.off_epart);
   const bool whole = L.N % et::kVec == 0;                    // rows are whole vectors
   const bool plain_export = grad != nullptr && delta == nullptr && !sgd && ((uintptr_t)grad & 15) == 0;
+  const bool plain_sgd = sgd && sink.opt.kind == et::kOptSgd && delta == nullptr && grad == nullptr;
   {
     TimedLaunch tl(s, ET_K_WGRAD, st);
     const int fill_blocks = fill.v1 > fill.v0 ? std::min(ceil_div(s->sms * 8, p.col_tiles), fill_rows_max) : 0;
@@ -1010,9 +1011,11 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
       return launch_chained(kern, grid, p.threads, st, grad_act<T>(s, 1, dY), keys, rows, n, L.K, L.N, s->emb_scale, p.chunks, part,
                             imp, sink, fill);
     };
-    if (whole && plain_export) ET_TRY(go(et::embed_grad_kernel<T, true, true>));
-    else if (whole) ET_TRY(go(et::embed_grad_kernel<T, true, false>));
-    else ET_TRY(go(et::embed_grad_kernel<T, false, false>));
+    if (whole && plain_export) ET_TRY(go(et::embed_grad_kernel<T, true, et::kEmbExport>));
+    else if (whole && plain_sgd && sink.master == nullptr) ET_TRY(go(et::embed_grad_kernel<T, true, et::kEmbSgd>));
+    else if (whole && plain_sgd) ET_TRY(go(et::embed_grad_kernel<T, true, et::kEmbSgdMaster>));
+    else if (whole) ET_TRY(go(et::embed_grad_kernel<T, true, et::kEmbGeneral>));
+    else ET_TRY(go(et::embed_grad_kernel<T, false, et::kEmbGeneral>));
     ++*launches;
   }
   TimedLaunch tl(s, ET_K_WGRAD_REDUCE, st);
@@ -1021,9 +1024,11 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
   auto go = [&](auto kern) -> et_status {
     return launch_chained(kern, grid, 256, st, keys, n, L.K, L.N, s->emb_scale, p.chunks, part, imp, sink);
   };
-  if (whole && plain_export) ET_TRY(go(et::embed_join_kernel<T, true, true>));
-  else if (whole) ET_TRY(go(et::embed_join_kernel<T, true, false>));
-  else ET_TRY(go(et::embed_join_kernel<T, false, false>));
+  if (whole && plain_export) ET_TRY(go(et::embed_join_kernel<T, true, et::kEmbExport>));
+  else if (whole && plain_sgd && sink.master == nullptr) ET_TRY(go(et::embed_join_kernel<T, true, et::kEmbSgd>));
+  else if (whole && plain_sgd) ET_TRY(go(et::embed_join_kernel<T, true, et::kEmbSgdMaster>));
+  else if (whole) ET_TRY(go(et::embed_join_kernel<T, true, et::kEmbGeneral>));
+  else ET_TRY(go(et::embed_join_kernel<T, false, et::kEmbGeneral>));
   ++*launches;
   return ET_OK;
 }
@@ -2458,7 +2463,7 @@ et_status launch_held(const et_stack* s, et::tok::Args a, cudaStream_t st) {
     clusters = std::min(clusters, a.rows);
     a.n_parts = THREADS >= et::tok::kTicketThreads ? a.rows : clusters;
     // a few loads a thread for the last block, else a kernel of its own (32 threads took 150 us over 16384 rows)
-    a.finish = a.out == nullptr || a.n_parts <= 16 * THREADS ? 1 : 0;
+    a.finish = a.out == nullptr || a.n_parts <= 2 * THREADS ? 1 : 0;
   }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)clusters * (unsigned)a.slices);
@@ -2517,7 +2522,7 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
     a.slices = 1;
     a.per = vecs;
     a.n_parts = a.rows;
-    a.finish = a.rows <= 16 * et::tok::kRowThreads ? 1 : 0;
+    a.finish = a.rows <= 2 * et::tok::kRowThreads ? 1 : 0;
     ET_TRY(launch_chained(et::tok::token_row_kernel<T, MODE>, (unsigned)a.rows, et::tok::kRowThreads, st, a));
     return MODE == et::tok::kPolicy ? policy_total(a, st) : ET_OK;
   }

@@ -2414,7 +2414,8 @@ void token_args(const et_stack* s, et::tok::Args* a, const void* y, const int32_
   float hi = (float)k;
   if ((double)hi > k) hi = std::nextafterf(hi, 0.0f);
   a->k_hi = hi;
-  a->k_lo = std::max((float)(k - (double)hi), 1e-30f);                      // > 0: keeps -inf at -inf
+  const float lo = (float)(k - (double)hi);
+  a->k_lo = lo > 0.f ? lo : std::max(hi * 1e-12f, 1.2e-38f);                // > 0: keeps -inf at -inf
   a->done = (uint32_t*)s->at(s->off_status) + kDoneWord;
   a->ticket = a->done + 1;
 }

@@ -143,7 +143,7 @@ update_clipped_kernel(const __grid_constant__ ClipTable<N> tab, const double* __
   const float2 nf = norm_and_factor(parts, n_parts, max_norm);
   const float f = nf.y;
   if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = nf.x; norm_out[1] = f; }
-  if (!(nf.x <= 3.402823466e38f)) return;
+  if (f == 0.0f) return;
   for (long long vb = tab.blocks - 1 - blockIdx.x; vb >= 0; vb -= gridDim.x) {   // backwards: the end is still in L2
     const ClipEntry& e = tab.e[clip_find(tab, vb)];
 #pragma unroll

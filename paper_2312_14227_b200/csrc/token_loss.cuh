@@ -542,8 +542,8 @@ token_held_kernel(const __grid_constant__ Args a) {
     if (MODE == kScore) break;                               // one row a block
     __syncthreads();
     const int after = TICKETS ? rows_after[b] : next + clusters;
-    if (a.dY != nullptr && live) {
-      const RowResult r = result;
+    const RowResult r = result;
+    if (a.dY != nullptr && live && r.cs != 0.0f) {           // a clipped row without a KL term has no gradient either
       const uint64_t kh = pack2(a.k_hi, a.k_hi), lb = pack2(r.lb, r.lb);
       const uint32_t flip = r.g < 0.0f ? 0x80008000u : 0u;
       const bool lean = LEAN && fabsf(r.m) <= kLeanMax && r.g != 0.0f;

@@ -360,3 +360,61 @@ def test_profile_costs(dtype):
     n.check()
     assert t_dw[0] > 0 and t_dw[1] == 0 and t_dy[0] == 0 and t_dy[1] == 0 and t_fwd > 0
     assert all(torch.equal(a, b) for a, b in zip(before, n.params))
+
+
+@pytest.mark.parametrize("dtype,master", [(F, False), (B, False), (B, True)])
+@pytest.mark.parametrize("opt", ["sgd", "sgdw", "adam"])
+@pytest.mark.parametrize("M,V,d", [(4096, 700, 64), (4097, 700, 64), (9000, 5000, 40), (6000, 300, 1032)])
+def test_fused_step_is_the_exported_gradients_step(dtype, master, opt, M, V, d):
+    """Both ways of sorting, rows without a token filled beside either; with and without masters."""
+    a, b = (Emb(M, V, d, dtype, "zipf", seed=21, master=master) for _ in range(2))
+    states = []
+    for c in (a, b):
+        st = [torch.full((V, d), v, device=DEV) for v in (1e-2, 1e-4)]
+        if opt == "sgdw":
+            et.et_stack_set_optimizer(c.s, et.ET_OPT_SGDW, [st[0], None], momentum=0.9, weight_decay=1e-2)
+        elif opt == "adam":
+            et.et_stack_set_optimizer(c.s, et.ET_OPT_ADAM, [st[0], None], [st[1], None])
+        states.append(st)
+        c.forward()
+    et.et_backward_elastic(a.s, a.dY, [1, 0], flags=et.ET_FLAG_FUSE_SGD, lr=0.01)
+    grad = torch.full((V, d), float("nan"), device=DEV)
+    et.et_backward_elastic(b.s, b.dY, [1, 0], [grad, None])
+    et.et_update_masked(b.s, [1, 0], [grad, None], 0.01)
+    a.check()
+    b.check()
+    assert torch.equal(a.T, b.T) and all(torch.equal(x, y) for x, y in zip(*states))
+    if master:
+        assert torch.equal(a.T32, b.T32)
+    both = torch.full((V, d), float("nan"), device=DEV)             # exported and applied in one call
+    c = Emb(M, V, d, dtype, "zipf", seed=21, master=master)
+    c.forward()
+    et.et_backward_elastic(c.s, c.dY, [1, 0], [both, None], flags=et.ET_FLAG_FUSE_SGD, lr=0.01)
+    c.check()
+    assert torch.equal(both, grad)
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+def test_gradient_at_any_address(dtype):
+    c = Emb(5000, 300, 64, dtype, "zipf", seed=22)
+    c.forward()
+    g, tol = c.grad_tol()
+    raw = torch.full((300 * 64 + 8,), 7.0, device=DEV)
+    for off in (1, 2, 3, 4):
+        raw.fill_(7.0)
+        view = raw[off:off + 300 * 64]
+        et.et_backward_elastic(c.s, c.dY, [1, 0], [view, None])
+        c.check()
+        assert (np.abs(view.double().cpu().numpy().reshape(300, 64) - g) <= tol).all()
+        assert (raw[:off] == 7).all() and (raw[off + 300 * 64:] == 7).all()
+
+
+def test_host_resident_gradient():
+    c = Emb(400, 90, 64, B, "zipf", seed=23)
+    c.forward()
+    grad, want = torch.empty(90, 64, device=DEV), torch.empty(90, 64, device=DEV)
+    et.et_backward_elastic(c.s, c.dY, [1, 0], [want, None])
+    host = c.dY.cpu().pin_memory()
+    et.et_backward_elastic_host(c.s, host, [1, 0], [grad, None])
+    c.check()
+    assert torch.equal(grad, want)

@@ -396,3 +396,46 @@ def test_captured_and_replayed_on_another_stream():
     for a, b in zip(got, (d1, d2, s1, s2, lp)):
         assert torch.equal(a, b) or torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
     del g
+
+
+@pytest.mark.parametrize("width,vocab,dtype", [(4096, 100, F), (4096, 100, B), (40000, 3001, B), (9000, 4, F), (300000, 70, B)])
+def test_few_logits_in_a_wide_row(width, vocab, dtype):
+    """Whole vectors, whole rounds and whole slices of padding behind the vocabulary."""
+    c = Case(24, width, vocab, dtype, seed=41, edge=False)
+    _check_policy(c, _policy(c, 0.05))
+    begin = [0, 6, 11, 17, 22]
+    _check_pref(c, begin, _near(c, begin, 8), 0)
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("rows", [1, 3, 147, 149, 300, 1000, 5000])
+def test_any_number_of_rows(dtype, rows):
+    """Fewer rows than blocks, one more, many rounds; one or two warps a row and one block a row."""
+    for width in (200, 1504, 3000):
+        c = Case(rows, width, width - 3, dtype, seed=42 + rows, edge=rows > 6, masked=0.5)
+        _check_policy(c, _policy(c, 0.05))
+
+
+@pytest.mark.parametrize("scale", [1e-6, 1e-3, 30.0])
+def test_logit_scales(scale):
+    s = float(np.float32(scale))
+    c = Case(30, 1000, 997, F, scale=s, seed=43, spread=2.0 / max(s, 1.0))
+    _check_policy(c, _policy(c, 0.05))
+
+
+def test_values_far_from_zero():
+    """Rows whose largest value is large either way: the terms go by differences."""
+    for dtype in (F, B):
+        for off in (-3e4, 3e4, 1e30, -1e30):
+            c = Case(12, 2056, 2056, dtype, seed=44, edge=False, masked=0.0)
+            c.y += off
+            c.y[:, 5] = off
+            c.targets[:] = 5
+            c.y_host = c.y.to(torch.float64).cpu().numpy()
+            out = torch.empty(12, device=DEV)
+            et.et_token_logp(c.st.s, c.y, c.dev(c.targets, np.int32), out)
+            c.st.check()
+            want, _ = tok.log_probs(c.y_host, c.targets, 2056, 1.0, c.live)
+            c.check_logp(out, want)
+            if abs(off) < 1e6:
+                _check_policy(c, _policy(c, 0.05))

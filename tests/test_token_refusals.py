@@ -103,3 +103,19 @@ def test_clip_arguments():
         assert _status(et.et_update_clipped, s, m, [P, P], 0.1, bad) == et.ET_ERR_INVALID_ARG
     assert _status(et.et_clip_grads, s, m, [P, P], [P, P], 1.0) == et.ET_ERR_STATE
     assert _status(et.et_update_clipped, s, m, [P, P], 0.1, float("inf")) == et.ET_ERR_STATE
+
+
+def test_tensors_of_another_type_or_layout():
+    torch = pytest.importorskip("torch")
+    s = _stack(dtype=et.ET_BF16)
+    y, ids = torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    f = torch.zeros(4)
+    assert _status(et.et_token_logp, s, y, ids.long(), f) == et.ET_ERR_DTYPE
+    assert _status(et.et_token_logp, s, y.float(), ids, f) == et.ET_ERR_DTYPE
+    assert _status(et.et_token_logp, s, y, ids, f.double()) == et.ET_ERR_DTYPE
+    assert _status(et.et_loss_policy_grad, s, y, ids, f.half(), y) == et.ET_ERR_DTYPE
+    assert _status(et.et_loss_policy_grad, s, torch.zeros(16, 4, dtype=torch.bfloat16).t(), ids, f, y) == et.ET_ERR_INVALID_ARG
+    assert _status(et.et_loss_preference_grad, s, y, ids, torch.zeros(3, dtype=torch.int64), y) == et.ET_ERR_DTYPE
+    e = et.et_stack_create([(11, 8, 0, 1, -1, EMB)], 4, et.ET_F32)
+    assert _status(et.et_forward_stack, e, torch.zeros(4, dtype=torch.int64), f) == et.ET_ERR_DTYPE
+    assert _status(et.et_forward_stack, e, torch.zeros(4), f) == et.ET_ERR_DTYPE

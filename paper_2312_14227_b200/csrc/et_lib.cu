@@ -2596,7 +2596,7 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   p.pairs = pairs; p.vocab = a.vocab; p.kind = cfg->kind; p.beta = cfg->beta; p.smoothing = cfg->label_smoothing;
   {
     TimedLaunch tl(s, ET_K_OTHER, st);
-    ET_TRY(launch_chained(et::tok::pair_kernel, pairs, 256, st, p));
+    ET_TRY(launch_chained(et::tok::pair_kernel, pairs, et::tok::kPairThreads, st, p));
   }
   if (dY == nullptr) return ET_OK;
   a.dY = dY;

@@ -740,62 +740,67 @@ __device__ __forceinline__ float pair_weight(const PairArgs& a, int row) {
   const int t = a.targets[row];
   return t >= 0 && t < a.vocab ? (a.weights != nullptr ? a.weights[row] : 1.0f) : 0.0f;
 }
-__device__ __forceinline__ double log1pexp(double x) {       // log(1 + exp(x))
-  return fmax(x, 0.0) + log1p(exp(-fabs(x)));
-}
-// One block per pair: both sums (64 bits, fixed order), the pair's loss, the rows' coefficients.
-static __global__ void __launch_bounds__(256)
-pair_kernel(const PairArgs a) {
+// One block per pair, half its threads for each sequence: both sums (64 bits, fixed order), the pair's loss, the rows'
+// coefficients.  What takes its time is latency: the loads of four rows a thread go out together, one thread does the loss.
+constexpr int kPairThreads = 512, kPairHalf = kPairThreads / 2;
+static __global__ void __launch_bounds__(kPairThreads)
+pair_kernel(const __grid_constant__ PairArgs a) {
   chain_begin();
-  __shared__ double sh[8];
-  __shared__ double total[2];
-  const int p = blockIdx.x;
-  int b[2], e[2];
-  for (int q = 0; q < 2; ++q) {
-    b[q] = min(max(a.begin[2 * p + q], 0), a.rows);
-    e[q] = max(b[q], min(max(a.begin[2 * p + q + 1], 0), a.rows));
-    double s = 0.0;
-    for (int i = b[q] + (int)threadIdx.x; i < e[q]; i += blockDim.x) {
-      const float w = pair_weight(a, i);
-      if (w != 0.0f) s += (double)w * (double)a.logp[i];
+  __shared__ double sh[kPairThreads / 32];
+  __shared__ double slope_sh;
+  const int p = blockIdx.x, side = threadIdx.x / kPairHalf, at = threadIdx.x % kPairHalf;
+  const int b = min(max(a.begin[2 * p + side], 0), a.rows);
+  const int e = max(b, min(max(a.begin[2 * p + side + 1], 0), a.rows));
+  double s = 0.0;
+  for (int i = b + at; i < e; i += 4 * kPairHalf) {
+    float w[4], lp[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = i + k * kPairHalf;
+      w[k] = r < e ? pair_weight(a, r) : 0.0f;
+      lp[k] = r < e ? a.logp[r] : 0.0f;
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      double r = 0.0;
-      for (int wq = 0; wq < (int)(blockDim.x >> 5); ++wq) r += sh[wq];
-      total[q] = r;
-    }
-    __syncthreads();
+    for (int k = 0; k < 4; ++k)
+      if (w[k] != 0.0f) s += (double)w[k] * (double)lp[k];
   }
-  const double beta = a.beta, eps = a.smoothing;
-  const double rc = beta * (total[0] - (a.ref != nullptr ? (double)a.ref[2 * p] : 0.0));
-  const double rr = beta * (total[1] - (a.ref != nullptr ? (double)a.ref[2 * p + 1] : 0.0));
-  const double x = rc - rr;
-  double loss, dx;
-  if (a.kind == kPrefSigmoid) {
-    loss = (1.0 - eps) * log1pexp(-x) + eps * log1pexp(x);
-    dx = eps / (1.0 + exp(-x)) - (1.0 - eps) / (1.0 + exp(x));
-  } else if (a.kind == kPrefIpo) {
-    const double h = x / beta - 0.5 / beta;
-    loss = h * h;
-    dx = 2.0 * h / beta;
-  } else {
-    loss = fmax(0.0, 1.0 - x);
-    if (x != x) loss = x;
-    dx = x < 1.0 ? -1.0 : (x != x ? x : 0.0);
-  }
-  const double slope = dx * beta / (double)a.pairs;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+  __syncthreads();
   if (threadIdx.x == 0) {
+    double total[2] = {0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < kPairThreads / 32; ++k) total[k / (kPairHalf / 32)] += sh[k];
+    const double beta = a.beta, eps = a.smoothing;
+    const double rc = beta * (total[0] - (a.ref != nullptr ? (double)a.ref[2 * p] : 0.0));
+    const double rr = beta * (total[1] - (a.ref != nullptr ? (double)a.ref[2 * p + 1] : 0.0));
+    const double x = rc - rr;
+    double loss, dx;
+    if (a.kind == kPrefSigmoid) {
+      // t = exp(-|x|): log(1 + exp(+-x)) = max(0, +-x) + log(1 + t), sigmoid(-|x|) = t / (1 + t)
+      const double t = exp(-fabs(x)), l = log1p(t), small = t / (1.0 + t), large = 1.0 / (1.0 + t);
+      loss = l + (1.0 - eps) * fmax(-x, 0.0) + eps * fmax(x, 0.0);
+      dx = eps * (x < 0.0 ? small : large) - (1.0 - eps) * (x < 0.0 ? large : small);
+      if (x != x) loss = dx = x;
+    } else if (a.kind == kPrefIpo) {
+      const double h = x / beta - 0.5 / beta;
+      loss = h * h;
+      dx = 2.0 * h / beta;
+    } else {
+      loss = fmax(0.0, 1.0 - x);
+      dx = x < 1.0 ? -1.0 : 0.0;
+      if (x != x) loss = dx = x;
+    }
+    slope_sh = dx * beta / (double)a.pairs;
     if (a.seq_logp != nullptr) { a.seq_logp[2 * p] = (float)total[0]; a.seq_logp[2 * p + 1] = (float)total[1]; }
     double* out = a.parts + (size_t)p * 4;
     out[0] = loss; out[1] = rc; out[2] = rr; out[3] = x > 0.0 ? 1.0 : 0.0;
   }
-  for (int q = 0; q < 2; ++q)
-    for (int i = b[q] + (int)threadIdx.x; i < e[q]; i += blockDim.x)
-      a.coef[i] = (float)((double)pair_weight(a, i) * (q == 0 ? slope : -slope));
+  __syncthreads();
+  const double slope = side == 0 ? slope_sh : -slope_sh;
+#pragma unroll 4
+  for (int i = b + at; i < e; i += kPairHalf) a.coef[i] = (float)((double)pair_weight(a, i) * slope);
   if (a.out == nullptr) return;
   // the block that finishes last adds the pairs up, in a fixed order
   __shared__ bool last;
@@ -806,16 +811,16 @@ pair_kernel(const PairArgs a) {
   __syncthreads();
   if (!last || threadIdx.x >= 32) return;
   __threadfence();
-  double s[4] = {0.0, 0.0, 0.0, 0.0};
+  double mean[4] = {0.0, 0.0, 0.0, 0.0};
   for (int i = threadIdx.x; i < a.pairs; i += 32)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) s[q] += __ldcg(a.parts + (size_t)i * 4 + q);
+    for (int q = 0; q < 4; ++q) mean[q] += __ldcg(a.parts + (size_t)i * 4 + q);
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s[q] += __shfl_xor_sync(0xffffffffu, s[q], o);
+    for (int o = 16; o > 0; o >>= 1) mean[q] += __shfl_xor_sync(0xffffffffu, mean[q], o);
   if (threadIdx.x == 0) {
-    for (int q = 0; q < 4; ++q) a.out[q] = (float)(s[q] / (double)a.pairs);
+    for (int q = 0; q < 4; ++q) a.out[q] = (float)(mean[q] / (double)a.pairs);
     *a.done = 0u;
   }
 }

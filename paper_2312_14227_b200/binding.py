@@ -166,21 +166,21 @@ def _ptr_array(seq: Optional[Sequence], n: int):
     return (C.c_void_p * n).from_buffer(ptrs)
 
 
-def _typed(where: str, **tensors):
-    """Refuses torch tensors of another type or layout than the call reads: name=(tensor, type).  Addresses and None pass."""
+def _typed(where: str, storage: int, stored=(), ints=(), floats=()):
+    """Refuses torch tensors of another type or layout than the call reads: `stored` in the stack's storage type, int32,
+    float32.  Addresses, arrays and None pass."""
     torch = sys.modules.get("torch")
     if torch is None:
         return
-    for name, (t, kind) in tensors.items():
-        if isinstance(t, torch.Tensor):
-            if t.dtype is not getattr(torch, kind):
-                raise EtError(ET_ERR_DTYPE, f"{where}: {name} is {t.dtype}, not {kind}")
-            if not t.is_contiguous():
-                raise EtError(ET_ERR_INVALID_ARG, f"{where}: {name} is not contiguous")
-
-
-def _storage(s) -> str:
-    return "bfloat16" if s.dtype == ET_BF16 else "float32"
+    tensor = torch.Tensor
+    for group, dtype in ((stored, torch.bfloat16 if storage == ET_BF16 else torch.float32), (ints, torch.int32),
+                         (floats, torch.float32)):
+        for i, t in enumerate(group):
+            if isinstance(t, tensor):
+                if t.dtype is not dtype:
+                    raise EtError(ET_ERR_DTYPE, f"{where}: a tensor of {t.dtype} where {dtype} is read (number {i} of these)")
+                if not t.is_contiguous():
+                    raise EtError(ET_ERR_INVALID_ARG, f"{where}: a tensor of {dtype} that is not contiguous (number {i} of these)")
 
 
 def _stream_ptr(stream) -> Optional[int]:
@@ -345,7 +345,7 @@ def et_stack_bind_master(s: Stack, W32, b32):
 
 def et_forward_stack(s: Stack, x, y, stream=None):
     if s.takes_ids:
-        _typed("et_forward_stack", x=(x, "int32"))
+        _typed("et_forward_stack", s.dtype, ints=(x,))
     _check(_lib.et_forward_stack(s.handle, _ptr(x), _ptr(y), _stream_ptr(stream)), "et_forward_stack")
 
 
@@ -359,7 +359,7 @@ def et_stack_set_embedding_scale(s: Stack, scale: float):
 
 
 def et_token_logp(s: Stack, y, targets, logp, vocab: int = 0, logit_scale: float = 1.0, stream=None):
-    _typed("et_token_logp", y=(y, _storage(s)), targets=(targets, "int32"), logp=(logp, "float32"))
+    _typed("et_token_logp", s.dtype, (y,), (targets,), (logp,))
     _check(_lib.et_token_logp(s.handle, _ptr(y), _ptr(targets), vocab, logit_scale, _ptr(logp), _stream_ptr(stream)),
            "et_token_logp")
 
@@ -367,9 +367,7 @@ def et_token_logp(s: Stack, y, targets, logp, vocab: int = 0, logit_scale: float
 def et_loss_policy_grad(s: Stack, y, targets, advantages, dY=None, weights=None, logp_old=None, logp_ref=None, logp=None,
                         loss_dev=None, vocab: int = 0, logit_scale: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2,
                         kl_coef: float = 0.0, stream=None):
-    _typed("et_loss_policy_grad", y=(y, _storage(s)), targets=(targets, "int32"), advantages=(advantages, "float32"),
-           dY=(dY, _storage(s)), weights=(weights, "float32"), logp_old=(logp_old, "float32"), logp_ref=(logp_ref, "float32"),
-           logp=(logp, "float32"), loss_dev=(loss_dev, "float32"))
+    _typed("et_loss_policy_grad", s.dtype, (y, dY), (targets,), (advantages, weights, logp_old, logp_ref, logp, loss_dev))
     cfg = et_policy_config(vocab, logit_scale, clip_low, clip_high, kl_coef)
     _check(_lib.et_loss_policy_grad(s.handle, _ptr(y), _ptr(targets), _ptr(weights), _ptr(advantages), _ptr(logp_old),
                                     _ptr(logp_ref), C.addressof(cfg), _ptr(dY), _ptr(logp), _ptr(loss_dev),
@@ -380,9 +378,7 @@ def et_loss_preference_grad(s: Stack, y, targets, seq_begin, dY=None, weights=No
                             kind: int = ET_PREF_SIGMOID, vocab: int = 0, logit_scale: float = 1.0, beta: float = 0.1,
                             label_smoothing: float = 0.0, pairs: Optional[int] = None, stream=None):
     """`pairs`: taken from the length of seq_begin (2 pairs + 1) unless given."""
-    _typed("et_loss_preference_grad", y=(y, _storage(s)), targets=(targets, "int32"), seq_begin=(seq_begin, "int32"),
-           dY=(dY, _storage(s)), weights=(weights, "float32"), ref_logp=(ref_logp, "float32"), seq_logp=(seq_logp, "float32"),
-           loss_dev=(loss_dev, "float32"))
+    _typed("et_loss_preference_grad", s.dtype, (y, dY), (targets, seq_begin), (weights, ref_logp, seq_logp, loss_dev))
     cfg = et_preference_config(kind, vocab, logit_scale, beta, label_smoothing)
     if pairs is None:
         pairs = (len(seq_begin) - 1) // 2

@@ -236,6 +236,7 @@ sort_one_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uin
   __shared__ uint16_t cnt[32][BINS];
   __shared__ uint32_t sk[kSortOneMax];
   __shared__ uint16_t sr[kSortOneMax];
+  __shared__ uint32_t base[BINS];
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int warps = (n + E * 32 - 1) / (E * 32);            // warps that hold ids
   if (named != nullptr)
@@ -263,19 +264,23 @@ sort_one_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uin
     __syncthreads();
     uint32_t total = 0;
     if (tid < BINS)
-      for (int w = 0; w < warps; ++w) {
-        const uint32_t c = cnt[w][tid];
-        cnt[w][tid] = (uint16_t)total;
-        total += c;
+      for (int w0 = 0; w0 < warps; w0 += 8) {               // eight warps' counts at a time: one shared-memory latency for them
+        uint32_t c[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c[k] = w0 + k < warps ? cnt[w0 + k][tid] : 0u;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (w0 + k < warps) cnt[w0 + k][tid] = (uint16_t)total;
+          total += c[k];
+        }
       }
     const uint32_t at = block_scan(tid < BINS ? total : 0u, 1024);
-    if (tid < BINS)
-      for (int w = 0; w < warps; ++w) cnt[w][tid] = (uint16_t)(cnt[w][tid] + at);
+    if (tid < BINS) base[tid] = at;
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < E; ++q)
       if (in[q]) {
-        const uint32_t pos = cnt[wid][(key[q] >> shift) & (BINS - 1)] + rank[q];
+        const uint32_t dig = (key[q] >> shift) & (BINS - 1), pos = base[dig] + cnt[wid][dig] + rank[q];
         sk[pos] = key[q];
         sr[pos] = (uint16_t)row[q];
       }

@@ -76,29 +76,8 @@ struct Args {
 __device__ __forceinline__ uint64_t scale2(uint64_t d, uint64_t k_hi, uint64_t k_lo) { return fma2(d, k_lo, mul2(d, k_hi)); }
 __device__ __forceinline__ float exp_diff(float d, const Args& a) { return exp2_fast(fmaf(d, a.k_lo, d * a.k_hi)); }
 
-// Two ways to form a term exp(scale (y - m)) = exp2(u):
-//   exact   u = (y - m) (k_hi + k_lo): three packed operations.  fp32 rows, and log probabilities that are to be summed.
-//   lean    u = y k_hi + b, b = fl(-m k_hi): one.  For bf16 rows of a loss: the FMA pipe, at 4 scalar operations an element and pass,
-//           was what bounded the kernel.  b's rounding is common to all terms of the row and to the target's; without k_lo the
-//           log of the sum is off by k_lo ln 2 E_p[m - y], some 1e-8 absolute.
-// Lean needs m k_hi inside fp32's range: rows whose largest value is beyond +-1e37 (rows of nothing but the type's lowest
-// value among them) take the exact way.
-constexpr float kLeanMax = 1e37f;
-template <bool LEAN>
-__device__ __forceinline__ float rebase(float from, float to, const Args& a) {      // factor of a sum that moves from max `from` to `to`
-  if (LEAN && fabsf(from) <= kLeanMax && fabsf(to) <= kLeanMax) return exp2_fast(__fmul_rn(from, a.k_hi) - __fmul_rn(to, a.k_hi));
-  return exp_diff(from - to, a);
-}
 // lp of the target's logit from the row's (max, sum).
-template <bool LEAN>
-__device__ __forceinline__ float log_prob(float yt, float m, float s, const Args& a) {
-  if (LEAN && fabsf(m) <= kLeanMax) {
-    constexpr float kLn2 = 0.6931471805599453f;
-    return fmaf(fmaf(yt, a.k_hi, -(m * a.k_hi)) + (yt - m) * a.k_lo, kLn2, -logf(s));
-  }
-  return fmaf(yt - m, a.scale, -logf(s));
-}
-
+__device__ __forceinline__ float log_prob(float yt, float m, float s, const Args& a) { return fmaf(yt - m, a.scale, -logf(s)); }
 // The same for a log probability that is reported and summed (one thread's work): the log in 64 bits, and ex2.approx's mean
 // relative error taken off.  It is low by 5.0e-8 on average wherever in its range (measured over 2^22 arguments against
 // 64-bit values: -4.97e-8 on [-1, 0], -5.08e-8 on [-20, 0]), which moves the log of every sum the same way; over the rows of a
@@ -108,26 +87,24 @@ __device__ __forceinline__ float log_prob_summed(float yt, float m, float s, con
 }
 
 // (max, sum) over the lanes of a warp.  fmaxf drops NaN; the sum carries it.
-template <bool LEAN>
 __device__ __forceinline__ void join_lanes(float& m, float& s, const Args& a) {
   const float own = m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (own != -INFINITY) s *= rebase<LEAN>(own, m, a);
+  if (own != -INFINITY) s *= exp_diff(own - m, a);
   s = warp_sum(s);
 }
 // (max, sum) over a block: all threads get the pair.  A thread without elements holds (-inf, 0).
-template <bool LEAN>
 __device__ __forceinline__ void block_max_sum(float& m, float& s, const Args& a) {
   __shared__ float sm[32], ss[32];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, nw = (blockDim.x + 31) >> 5;
-  join_lanes<LEAN>(m, s, a);
+  join_lanes(m, s, a);
   __syncthreads();
   if (lane == 0) { sm[wid] = m; ss[wid] = s; }
   __syncthreads();
   m = lane < nw ? sm[lane] : -INFINITY;
   s = lane < nw ? ss[lane] : 0.0f;
-  join_lanes<LEAN>(m, s, a);
+  join_lanes(m, s, a);
 }
 
 // d loss / d lp of a row of the policy loss, and its contributions to the reported sums.
@@ -327,51 +304,26 @@ __device__ __forceinline__ uint4 grad_vec(const uint4& q, float m, float g, floa
 }
 
 // Sum of the terms of B vectors over the reference `ref` (finite), added to s.
-template <typename T, bool LEAN, int B>
+template <typename T, int B>
 __device__ __forceinline__ float add_terms(const uint4 (&x)[B], float ref, float s, const Args& a) {
   constexpr int P = VecOf<T>::N / 2;
-  const uint64_t kh = pack2(a.k_hi, a.k_hi);
+  const uint64_t nm = pack2(-ref, -ref), kh = pack2(a.k_hi, a.k_hi), kl = pack2(a.k_lo, a.k_lo);
   uint64_t acc[2] = {pack2(s, 0.0f), pack2(0.0f, 0.0f)};
-  auto all = [&](auto&& arg) {
 #pragma unroll
-    for (int i = 0; i < B; ++i) {
-      uint64_t p[P];
-      VecOf<T>::pairs(x[i], p);
+  for (int i = 0; i < B; ++i) {
+    uint64_t p[P];
+    VecOf<T>::pairs(x[i], p);
 #pragma unroll
-      for (int j = 0; j < P; ++j) {
-        float x0, x1;
-        unpack2(arg(p[j]), x0, x1);
-        acc[j & 1] = add2(acc[j & 1], pack2(exp2_fast(x0), exp2_fast(x1)));
-      }
+    for (int j = 0; j < P; ++j) {
+      float x0, x1;
+      unpack2(scale2(add2(p[j], nm), kh, kl), x0, x1);
+      acc[j & 1] = add2(acc[j & 1], pack2(exp2_fast(x0), exp2_fast(x1)));
     }
-  };
-  if (LEAN && fabsf(ref) <= kLeanMax) {
-    const float b = -(ref * a.k_hi);
-    const uint64_t bb = pack2(b, b);
-    all([&](uint64_t v) { return fma2(v, kh, bb); });
-  } else {
-    const uint64_t nm = pack2(-ref, -ref), kl = pack2(a.k_lo, a.k_lo);
-    all([&](uint64_t v) { return scale2(add2(v, nm), kh, kl); });
   }
   float s0, s1;
   unpack2(add2(acc[0], acc[1]), s0, s1);
   return s0 + s1;
 }
-// g exp(scale (y - m)) for a vector without the target, g folded into the exponent: lb = log2|g| - m k_hi, flip = its sign bit
-// in both halves of a word.
-__device__ __forceinline__ uint4 lean_grad_vec(const uint4& q, uint64_t kh, uint64_t lb, uint32_t flip) {
-  uint64_t p[4];
-  VecOf<bf16>::pairs(q, p);
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x, y;
-    unpack2(fma2(p[i], kh, lb), x, y);
-    w[i] = pack_bf16x2(exp2_fast(x), exp2_fast(y)) ^ flip;
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ld_cluster(const float* p, int rank) {
@@ -417,7 +369,7 @@ __device__ __forceinline__ void prefetch_slice(const Slice<T>& sl) {
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(sl.src + sl.lo), "r"((sl.hi - sl.lo) * 16) : "memory");
 }
 // What the second pass over a row needs, from the warp that worked it out.
-struct RowResult { float m, g, cs, lb, hit; };     // hit: the target's gradient
+struct RowResult { float m, g, cs, hit; };       // hit: the target's gradient
 
 // One read of the logits, one write of the gradient: a.slices blocks of one cluster share a row, every thread holds up to
 // NV vectors of it in registers from the load to the store.  (max, sum) go through shuffles, shared memory and the cluster's
@@ -434,7 +386,6 @@ __global__ void __launch_bounds__(THREADS, THREADS < 64 ? 32 : (NV <= 4 ? 1536 :
 token_held_kernel(const __grid_constant__ Args a) {
   chain_begin();
   constexpr int N = VecOf<T>::N, W = THREADS / 32;
-  constexpr bool LEAN = MODE == kPolicy && N == 8;
   constexpr bool TICKETS = MODE == kPolicy && THREADS >= kTicketThreads;      // else every block takes each gridDim.x-th row
   __shared__ float warp_m[W], warp_s[W], pair_m[2], pair_s[2];
   __shared__ RowResult result;
@@ -493,8 +444,8 @@ token_held_kernel(const __grid_constant__ Args a) {
         if (MODE == kPolicy) terms = row_terms(a, row);
       }
       m = max_of_all<T>(q);
-      s = add_terms<T, LEAN, NV>(q, m == -INFINITY ? 0.0f : m, 0.0f, a);
-      join_lanes<LEAN>(m, s, a);
+      s = add_terms<T>(q, m == -INFINITY ? 0.0f : m, 0.0f, a);
+      join_lanes(m, s, a);
       if (lane == 0) { warp_m[wid] = m; warp_s[wid] = s; }
     }
     __syncthreads();
@@ -502,7 +453,7 @@ token_held_kernel(const __grid_constant__ Args a) {
       if (live) {
         m = lane < W ? warp_m[lane] : -INFINITY;
         s = lane < W ? warp_s[lane] : 0.0f;
-        join_lanes<LEAN>(m, s, a);
+        join_lanes(m, s, a);
       }
       if (C > 1) {
         if (lane == 0) { pair_m[b] = m; pair_s[b] = s; }
@@ -512,12 +463,12 @@ token_held_kernel(const __grid_constant__ Args a) {
         if (live) {
           m = lane < C ? ld_cluster(&pair_m[b], lane) : -INFINITY;
           s = lane < C ? ld_cluster(&pair_s[b], lane) : 0.0f;
-          join_lanes<LEAN>(m, s, a);
+          join_lanes(m, s, a);
         }
       }
       const bool first = rank == 0 && lane == 0;
       if (live) {
-        const float lp = MODE == kPolicy ? log_prob<LEAN>(yt, m, s, a) : first ? log_prob_summed(yt, m, s, a) : 0.0f;
+        const float lp = MODE == kPolicy ? log_prob(yt, m, s, a) : first ? log_prob_summed(yt, m, s, a) : 0.0f;
         const float inv = 1.0f / s;
         if (first) {
           if (a.logp != nullptr) a.logp[row] = lp;
@@ -527,7 +478,7 @@ token_held_kernel(const __grid_constant__ Args a) {
           double one[3] = {0.0, 0.0, 0.0};
           const float cs = policy_coef(a, terms, lp, w, first && a.parts != nullptr ? (TICKETS ? one : sums) : nullptr) * a.scale, g = -cs * inv;
           if (TICKETS && first && a.parts != nullptr) put_parts(a, row, one);
-          if (lane == 0) result = RowResult{m, g, cs, log2f(fabsf(g)) - m * a.k_hi, fmaf(g, exp_diff(yt - m, a), cs)};
+          if (lane == 0) result = RowResult{m, g, cs, fmaf(g, exp_diff(yt - m, a), cs)};
         }
       } else if (first) {
         if (a.logp != nullptr) a.logp[row] = 0.0f;
@@ -544,23 +495,12 @@ token_held_kernel(const __grid_constant__ Args a) {
     const int after = TICKETS ? rows_after[b] : next + clusters;
     const RowResult r = result;
     if (a.dY != nullptr && live && r.cs != 0.0f) {           // a clipped row without a KL term has no gradient either
-      const uint64_t kh = pack2(a.k_hi, a.k_hi), lb = pack2(r.lb, r.lb);
-      const uint32_t flip = r.g < 0.0f ? 0x80008000u : 0u;
-      const bool lean = LEAN && fabsf(r.m) <= kLeanMax && r.g != 0.0f;
-      // the packed words are what is kept: without this the compiler keeps the unpacked fp32 values too (98 registers
-      // a thread where 60 do, half the resident blocks)
-#pragma unroll
-      for (int i = 0; i < NV; ++i) asm volatile("" : "+r"(q[i].x), "+r"(q[i].y), "+r"(q[i].z), "+r"(q[i].w));
-      auto out = [&](const uint4& x) -> uint4 {
-        if constexpr (LEAN) return lean_grad_vec(x, kh, lb, flip);
-        else return grad_vec<T>(x, r.m, r.g, 0.0f, -1, a);
-      };
-      // a vector that is not known to lie in the row, or of a row that takes the exact way
-      auto out_checked = [&](int i) {
+      auto out = [&](const uint4& x) { return grad_vec<T>(x, r.m, r.g, 0.0f, -1, a); };
+      auto out_checked = [&](int i) {                        // a vector that is not known to lie in the row
         const int v = i * THREADS + tid, e0 = sl.e0 + v * N;
-        if (v < a.per && e0 < a.width) store_vec<T>(sl.dY, e0, a.width, a.vocab, grad_vec<T>(q[i], r.m, r.g, 0.0f, -1, a));
+        if (v < a.per && e0 < a.width) store_vec<T>(sl.dY, e0, a.width, a.vocab, out(q[i]));
       };
-      if (regular && (lean || !LEAN)) {
+      if (regular) {
 #pragma unroll
         for (int i = 0; i < NV - 1; ++i) __stcs(sl.dst + i * THREADS + tid, out(q[i]));
         if ((NV - 1) * THREADS + tid < sl.hi) __stcs(sl.dst + (NV - 1) * THREADS + tid, out(q[NV - 1]));
@@ -609,9 +549,9 @@ token_row_kernel(const __grid_constant__ Args a) {
     float s = 0.0f;
     auto batch = [&](const auto& q) {
       const float cm = fmaxf(max_of_all<T>(q), m);
-      if (m != -INFINITY) s *= rebase<false>(m, cm, a);
+      if (m != -INFINITY) s *= exp_diff(m - cm, a);
       m = cm;
-      s = add_terms<T, false>(q, m == -INFINITY ? 0.0f : m, s, a);
+      s = add_terms<T>(q, m == -INFINITY ? 0.0f : m, s, a);
     };
     int v = tid;
     if (v < sl.lo) {
@@ -629,9 +569,9 @@ token_row_kernel(const __grid_constant__ Args a) {
       const uint4 q[1] = {load_vec<T>(sl.y, sl.e0 + v * N, a.vocab)};
       batch(q);
     }
-    block_max_sum<false>(m, s, a);
+    block_max_sum(m, s, a);
     const float yt = to_f32(sl.y[t]);
-    const float lp = MODE == kPolicy ? log_prob<false>(yt, m, s, a) : tid == 0 ? log_prob_summed(yt, m, s, a) : 0.0f;
+    const float lp = MODE == kPolicy ? log_prob(yt, m, s, a) : tid == 0 ? log_prob_summed(yt, m, s, a) : 0.0f;
     inv = 1.0f / s;
     if (MODE == kPolicy) {
       double sums[3] = {0.0, 0.0, 0.0};
@@ -686,19 +626,12 @@ token_grad_kernel(const __grid_constant__ Args a) {
     return;
   }
   const float cs = c * a.scale, g = -cs * st.y;
-  const bool lean = N == 8 && fabsf(st.x) <= kLeanMax && g != 0.0f;
   uint4 q[kGradVecs];
-  if (regular && (lean || N == 4)) {
+  if (regular) {
 #pragma unroll
     for (int i = 0; i < kGradVecs; ++i) q[i] = __ldcs(sl.src + i * STEP + tid);
-    const float b = log2f(fabsf(g)) - st.x * a.k_hi;
-    const uint64_t kh = pack2(a.k_hi, a.k_hi), lb = pack2(b, b);
-    const uint32_t flip = g < 0.0f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int i = 0; i < kGradVecs; ++i) {
-      if constexpr (N == 8) __stcs(sl.dst + i * STEP + tid, lean_grad_vec(q[i], kh, lb, flip));
-      else __stcs(sl.dst + i * STEP + tid, grad_vec<T>(q[i], st.x, g, 0.0f, -1, a));
-    }
+    for (int i = 0; i < kGradVecs; ++i) __stcs(sl.dst + i * STEP + tid, grad_vec<T>(q[i], st.x, g, 0.0f, -1, a));
     const int tv = (t - sl.e0) >> (N == 8 ? 3 : 2);          // the target's vector once more, by the thread that wrote it
     if (t >= sl.e0 && tv < kGradVecs * STEP && tv % STEP == tid) {
       // its words are in a register that a constant index names

@@ -605,7 +605,7 @@ token_row_kernel(const __grid_constant__ Args a) {
   if (MODE == kPolicy) policy_finish(a);
 }
 
-// The gradient from a row's (max, 1 / sum) and c, block (row, slice): nothing but a stream over the logits.  2.3 GB in
+// The gradient from a row's (max, 1 / sum) and c, block (row, slice): nothing but a stream over the logits.  0.82 GB in
 // and out of 8192 rows of 32000 bf16 columns in 124 us: at the copy bandwidth.
 constexpr int kGradThreads = 256, kGradVecs = 4;
 template <typename T>

@@ -418,3 +418,72 @@ def test_host_resident_gradient():
     et.et_backward_elastic_host(c.s, host, [1, 0], [grad, None])
     c.check()
     assert torch.equal(grad, want)
+
+
+@pytest.mark.parametrize("gemm_list", [0, 1])
+@pytest.mark.parametrize("sel", [[2, 4, 7], [0, 2, 3, 4, 5, 6, 7], [0], [5]])
+def test_dense_layers_above_a_table(gemm_list, sel):
+    """Widths the one-launch backward takes: with it and without, the table selected or not, as on the looked-up rows."""
+    layers = [wl.embedding_layer(300, 128, 0.5), wl.Layer(128, 256, act=wl.ACT_GELU_TANH), wl.Layer(256, 128, residual_src=1), wl.Layer(128, 320)]
+    n = TokenNet(B, M=700, seed=6, layers=layers)
+    et.et_stack_set_option(n.s, et.ET_OPTION_GEMM_LIST, gemm_list)
+    et.et_forward_stack(n.s, n.x, n.y)
+    n.dY.normal_()
+    mask = _mask(n.L, sel)
+    g1 = [torch.full(p.shape, float("nan"), device=DEV) if m else None for p, m in zip(n.params, mask)]
+    et.et_backward_elastic(n.s, n.dY, mask, g1)
+    n.check()
+    host = n.host(n.params)
+    saved = orc.forward(n.layers, host[0::2], host[1::2], n.ids)
+    want, _ = orc.backward_masked(n.layers, host[0::2], saved, n.dY.double().cpu().numpy(), mask)
+    for t in sel:
+        got = g1[t].double().cpu().numpy()
+        assert np.abs(got - want[t]).max() <= 3e-2 * np.abs(want[t]).max(), t
+
+
+def test_tables_beyond_32_bit_offsets():
+    V, d, M = 300000, 8200, 4200                       # 2.46e9 elements
+    c_ids = np.random.default_rng(1).integers(0, V, M).astype(np.int32)
+    c_ids[:3] = [V - 1, 0, V - 1]
+    s = et.et_stack_create([(V, d, 0, 1, -1, et.ET_LAYER_EMBEDDING)], M, B)
+    T = torch.zeros(V, d, dtype=torch.bfloat16, device=DEV)
+    T[V - 1] = 3.0
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, [T], [None], ws)
+    x = torch.from_numpy(c_ids).to(DEV)
+    y = torch.empty(M, d, dtype=torch.bfloat16, device=DEV)
+    et.et_forward_stack(s, x, y)
+    assert (y[0] == 3).all() and (y[1] == 0).all() and (y[2] == 3).all()
+    dY = torch.ones(M, d, dtype=torch.bfloat16, device=DEV)
+    grad = torch.full((V, d), float("nan"), device=DEV)
+    et.et_backward_elastic(s, dY, [1, 0], [grad, None])
+    count = torch.zeros(V, device=DEV).index_add_(0, x.long(), torch.ones(M, device=DEV))
+    assert torch.equal(grad.amax(1), count) and torch.equal(grad.amin(1), count)
+    before = T[V - 1].clone()
+    et.et_backward_elastic(s, dY, [1, 0], flags=et.ET_FLAG_FUSE_SGD, lr=0.5)
+    torch.cuda.synchronize()
+    k = float(count[V - 1])
+    assert (T[V - 1].float() == before.float() - 0.5 * k).all() and (T[0].float() == -0.5 * float(count[0])).all()
+
+
+def test_two_stacks_at_once():
+    """Two stacks, each on a stream of its own, at the same time: what they give one after the other."""
+    a, b = Emb(9000, 3000, 264, B, "zipf", seed=31), Emb(3000, 900, 520, F, "zipf", seed=32)
+    out = {}
+    for c in (a, b):
+        c.grad = torch.empty(c.V, c.d, device=DEV)
+        c.forward()
+        et.et_backward_elastic(c.s, c.dY, [1, 0], [c.grad, None])
+        c.check()
+        out[c] = c.grad.clone()
+        c.grad.fill_(float("nan"))
+    streams = {c: torch.cuda.Stream() for c in (a, b)}
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c in (a, b):
+            et.et_forward_stack(c.s, c.x, c.y, stream=streams[c])
+            et.et_backward_elastic(c.s, c.dY, [1, 0], [c.grad, None], stream=streams[c])
+    torch.cuda.synchronize()
+    for c in (a, b):
+        c.check()
+        assert torch.equal(out[c], c.grad)

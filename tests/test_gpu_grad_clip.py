@@ -232,3 +232,21 @@ def test_same_inputs_same_bits_and_replay():
     n.check()
     assert all(torch.equal(a, b) for a, b in zip(first[:-1], outs)) and float(n.norm[0]) == 2 * float(first[-1][0])
     del g
+
+
+def test_a_tensor_beyond_32_bit_offsets():
+    k = 47000                                            # 2.2e9 elements
+    s = et.et_stack_create([(k, k, 0, 1, -1)], 1, et.ET_F32)
+    W, b = torch.zeros(k * k, device=DEV), torch.zeros(k, device=DEV)
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, [W], [b], ws)
+    g = torch.zeros(k * k, device=DEV)
+    g[-1], g[0], g[2 ** 31] = 3.0, 4.0, 12.0
+    norm = torch.empty(2, device=DEV)
+    et.et_update_clipped(s, [1, 0], [g, None], 1.0, 6.5, norm)
+    torch.cuda.synchronize()
+    assert norm.tolist() == [13.0, 0.5]
+    assert float(W[-1]) == -1.5 and float(W[0]) == -2.0 and float(W[2 ** 31]) == -6.0 and int((W != 0).sum()) == 3
+    et.et_clip_grads(s, [1, 0], [g, None], [g, None], 6.5, norm)
+    torch.cuda.synchronize()
+    assert float(g[-1]) == 1.5 and float(g[0]) == 2.0 and float(g[2 ** 31]) == 6.0 and int((g != 0).sum()) == 3

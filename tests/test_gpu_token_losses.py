@@ -439,3 +439,57 @@ def test_values_far_from_zero():
             c.check_logp(out, want)
             if abs(off) < 1e6:
                 _check_policy(c, _policy(c, 0.05))
+
+
+def test_logits_beyond_32_bit_offsets():
+    M, V = 20000, 131072                                # 2.6e9 logits
+    st = Stack(M, V, B)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    y = torch.randn(M, V, generator=g, device=DEV, dtype=torch.bfloat16)
+    t = torch.randint(0, V, (M,), generator=g, device=DEV, dtype=torch.int32)
+    adv = torch.randn(M, generator=g, device=DEV)
+    lp, lp2, dY = torch.empty(M, device=DEV), torch.empty(M, device=DEV), torch.empty_like(y)
+    et.et_loss_policy_grad(st.s, y, t, adv, dY, logp=lp)
+    et.et_token_logp(st.s, y, t, lp2)
+    st.check()
+    for i in (0, 1, 16383, 16384, M - 1):
+        z = y[i].double()
+        want = z[t[i].long()] - torch.logsumexp(z, 0)
+        for got in (lp[i], lp2[i]):
+            assert abs(float(got) - float(want)) <= 64 * E * abs(float(want))
+        p = torch.softmax(z, 0)
+        p[t[i].long()] -= 1
+        w = float(adv[i]) / M * p
+        assert ((dY[i].double() - w).abs() <= (2.0 ** -8 + 1e-5) * w.abs() + TINY).all()
+    begin = torch.tensor([0, M // 2, M - 1], dtype=torch.int32, device=DEV)
+    et.et_loss_preference_grad(st.s, y, t, begin, dY, beta=1e-6)
+    st.check()
+    i, j = M - 2, M - 1
+    p = torch.softmax(y[i].double(), 0)
+    p[t[i].long()] -= 1
+    ratio = (dY[i].double() / p)[p.abs() > 1e-7]
+    assert (dY[j] == 0).all() and float(ratio.std() / ratio.mean().abs()) < 2.0 ** -8
+
+
+def test_two_stacks_at_once():
+    """Two stacks, each on a stream of its own, at the same time: what they give one after the other."""
+    cs = [Case(700, 8200, 8195, B, seed=51), Case(300, 4099, 4099, F, seed=52)]
+    want, args = [], []
+    for c in cs:
+        t, w, adv = c.dev(c.targets, np.int32), c.dev(c.weights), c.dev(c.rng.normal(size=c.M))
+        old = c.dev(c.rng.normal(size=c.M) - 8)
+        dY, stats = torch.empty_like(c.y), torch.empty(4, device=DEV)
+        args.append((t, w, adv, old, dY, stats))
+        et.et_loss_policy_grad(c.st.s, c.y, t, adv, dY, weights=w, logp_old=old, loss_dev=stats, vocab=c.vocab)
+        c.st.check()
+        want.append((dY.clone(), stats.clone()))
+    streams = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, (t, w, adv, old, dY, stats), s in zip(cs, args, streams):
+            et.et_loss_policy_grad(c.st.s, c.y, t, adv, dY, weights=w, logp_old=old, loss_dev=stats, vocab=c.vocab, stream=s)
+    torch.cuda.synchronize()
+    for c, a, (dY, stats) in zip(cs, args, want):
+        c.st.check()
+        assert torch.equal(a[4], dY) and torch.equal(a[5], stats)

@@ -67,9 +67,9 @@
  *   d gamma = column sums of g * xhat and d beta = column sums of g for selected tensors.
  *
  *   Storage type (et_dtype) applies to weights, biases, activations, error gradients
- *   and delta-W; accumulation is always fp32.  Exported gradients and importances are
+ *   and delta-W; accumulation is fp32 or wider.  Exported gradients and importances are
  *   fp32.  ET_BF16 stacks run on tcgen05 tensor cores and need every feature count to
- *   be a multiple of 8, and out_features/fold a multiple of 256 when fold > 1.
+ *   be a multiple of 8 (an embedding's vocabulary excepted), and out_features/fold a multiple of 256 when fold > 1.
  *
  * Memory and errors
  *   Every "device" pointer is caller-owned CUDA device memory, 16-byte aligned, valid
@@ -136,6 +136,7 @@ typedef struct {
   int32_t kind;           /* et_layer_kind.  ET_LAYER_NORM: in_features == out_features (a multiple of 8,
                              at most 2048), act = ET_ACT_NONE, fold = 1, residual_src = -1 */
   float eps;              /* ET_LAYER_NORM: added to the variance, > 0 or 0 */
+  /* ET_LAYER_EMBEDDING: in_features = vocabulary, out_features = width of a row, act = ET_ACT_NONE, fold = 1, residual_src = -1 */
   int32_t heads;          /* ET_LAYER_ATTENTION: in_features = 3 * out_features, out_features = 64 * heads;   */
   int32_t seq_len;        /*   rows form sequences of seq_len (<= 256) consecutive rows, M a multiple of it;  */
                           /*   ET_BF16 only; not the first or last layer; the layer below has no activation;   */

@@ -159,6 +159,8 @@ def _ptr_array(seq: Optional[Sequence], n: int):
     if seq is None:
         return None
     assert len(seq) == n
+    if n == 0:
+        return (C.c_void_p * 0)()
     try:                                             # tensors and None: the usual case, hundreds of them a step
         ptrs = array.array("Q", [0 if t is None else t.data_ptr() for t in seq])
     except AttributeError:

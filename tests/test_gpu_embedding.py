@@ -487,3 +487,22 @@ def test_two_stacks_at_once():
     for c in (a, b):
         c.check()
         assert torch.equal(out[c], c.grad)
+
+
+@pytest.mark.parametrize("M", [200, 6000])
+def test_reported_launches_and_timing(M):
+    c = Emb(M, 900, 64, B, "zipf", seed=41)
+    c.forward()
+    grad = torch.empty(900, 64, device=DEV)
+    before, rep = et.et_launch_count(), et.Report(1)
+    et.et_backward_elastic(c.s, c.dY, [1, 0], [grad, None], report=rep)
+    assert et.et_launch_count() - before == rep.launches > 0 and rep.flops_executed == 0.0
+    want = grad.clone()
+    et.et_timing_enable(c.s, True)
+    et.et_forward_stack(c.s, c.x, c.y)
+    et.et_backward_elastic(c.s, c.dY, [1, 0], [grad, None])
+    t = et.et_timing_read(c.s)
+    et.et_timing_enable(c.s, False)
+    c.check()
+    assert t["forward"][1] == 1 and t["wgrad"][1] >= 2 and t["wgrad_reduce"][1] == 1 and t["dgrad"][1] == 0
+    assert all(ms > 0 for ms, n in t.values() if n) and torch.equal(want, grad)

@@ -190,6 +190,11 @@ __device__ __forceinline__ void embed_fill(const EmbFill<T>& f, int block, int b
 // Ids outside [0, vocab) become `vocab` and end up behind all others.
 __device__ __forceinline__ uint32_t emb_key(int32_t id, int vocab) { return id >= 0 && id < vocab ? (uint32_t)id : (uint32_t)vocab; }
 
+// Sets an id's bit.  Frequent ids find it set and leave the word alone: 60000 tokens of 300 ids would queue up at ten words.
+__device__ __forceinline__ void emb_name(uint32_t* named, uint32_t key) {
+  const uint32_t bit = 1u << (key & 31);
+  if ((__ldcg(named + (key >> 5)) & bit) == 0) atomicOr(&named[key >> 5], bit);
+}
 // Ranks a warp's keys, 32 at a time in order: rank = keys of the same digit the warp has met before.  cnt: the warp's counters.
 template <int E, typename Cnt>
 __device__ __forceinline__ void warp_ranks(const uint32_t (&key)[E], const bool (&in)[E], int shift, int mask, Cnt* cnt,
@@ -256,7 +261,7 @@ sort_one_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, uin
   if (named != nullptr) {
 #pragma unroll
     for (int q = 0; q < E; ++q)
-      if (in[q] && key[q] < (uint32_t)vocab) atomicOr(&named[key[q] >> 5], 1u << (key[q] & 31));
+      if (in[q] && key[q] < (uint32_t)vocab) emb_name(named, key[q]);
   }
   for (int shift = 0; shift < bits; shift += kSortOneBits) {
     for (int i = tid; i < warps * BINS / 2; i += 1024) reinterpret_cast<uint32_t*>(&cnt[0][0])[i] = 0;
@@ -316,7 +321,7 @@ sort_hist_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, ui
     if (i >= n) continue;
     const uint32_t key = emb_key(ids[i], vocab);
     atomicAdd(&cnt[key & (bins - 1)], 1u);
-    if (named != nullptr && key < (uint32_t)vocab) atomicOr(&named[key >> 5], 1u << (key & 31));
+    if (named != nullptr && key < (uint32_t)vocab) emb_name(named, key);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < bins; i += kSortThreads) {
@@ -489,21 +494,21 @@ embed_join_kernel(const uint32_t* __restrict__ keys, int n, int vocab, int d, fl
   __shared__ float sm[8][kJoinCols];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int c = blockIdx.y * kJoinCols + lane * kVec, nc = min(kVec, d - c);
-  if (threadIdx.x < kJoinChunks) {
-    const long long p0 = ((long long)blockIdx.x * kJoinChunks + threadIdx.x) * kEmbChunk, p1 = p0 + kEmbChunk;
+  {                                                             // a warp a chunk: how many chunks the id goes on in, 32 at a look
+    const long long first = (long long)blockIdx.x * kJoinChunks + wid, p0 = first * kEmbChunk, p1 = p0 + kEmbChunk;
     int k = 0;
     if (p1 < n) {
       const uint32_t key = keys[p1 - 1];
       if (key < (uint32_t)vocab && keys[p1] == key && !(p0 > 0 && keys[p0 - 1] == key)) {
-        int lo = (int)p1, hi = n;                               // first position behind the id
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (keys[mid] == key) lo = mid + 1; else hi = mid;
+        for (;;) {
+          const long long p = p1 + (long long)(k + lane) * kEmbChunk;
+          const uint32_t same = __ballot_sync(0xffffffffu, p < n && keys[p] == key);
+          k += __popc(same);                                    // sorted: the ones come first
+          if (same != 0xffffffffu) break;
         }
-        k = (lo - 1) / kEmbChunk - (int)(p0 / kEmbChunk);
       }
     }
-    count[threadIdx.x] = k;
+    if (lane == 0) count[wid] = k;
   }
   __syncthreads();
   float dot = 0.0f;
@@ -536,7 +541,7 @@ embed_join_kernel(const uint32_t* __restrict__ keys, int n, int vocab, int d, fl
 #pragma unroll
     for (int i = 0; i < kVec; ++i) acc[i] = 0.0f;
     if (nc > 0) {
-#pragma unroll 4
+#pragma unroll 8
       for (int r = wid; r <= k; r += 8) {
         float v[kVec];
         emb_load<VEC>(part + ((size_t)(chunk + r) * 2 + (r == 0 ? 1 : 0)) * d + c, nc, v);

@@ -41,7 +41,7 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-enum Mode { kScore = 0, kPolicy = 1, kGrad = 2 };
+enum Mode { kScore = 0, kPolicy = 1 };
 
 struct Args {
   const void* y;              // [rows x width]
@@ -52,9 +52,9 @@ struct Args {
   const float* logp_old;      // kPolicy; null: the current log probability (ratio 1)
   const float* logp_ref;      // kPolicy; null: no KL term
   float* logp;                // lp of each row, 0 where the row is left out; may be null
-  float2* stats;              // kScore writes, kGrad reads: (max of the row's y, 1 / sum exp(scale (y - max))), (0, -1) for a
+  float2* stats;              // kScore writes, token_grad_kernel reads: (max of the row's y, 1 / sum exp(scale (y - max))), (0, -1) for a
                               // row that is left out; may be null
-  float* coef;                // kGrad: c_i.  kScore sets it to 0 where it is not null
+  float* coef;                // token_grad_kernel: c_i.  kScore sets it to 0 where it is not null
   const int32_t* begin;       // kScore: null, or [n_begin + 1]: rows outside begin[0] .. begin[n_begin] - 1 are left out
   int32_t n_begin;
   double* parts;              // kPolicy: 3 x n_parts: w * (-surrogate), w * kl, w * [clipped], of a row or of a block's rows; may be null
@@ -403,6 +403,10 @@ token_held_kernel(const __grid_constant__ Args a) {
     w_next = a.weights != nullptr ? a.weights[r] : a.default_weight;
   };
   double sums[3] = {0.0, 0.0, 0.0};                          // without tickets: of all the rows of the block
+  if (C > 1) {                                               // every block of the cluster runs before one writes another's shared memory
+    cluster_arrive();
+    cluster_wait();
+  }
   if (row < a.rows) head(row);
   for (int it = 0; row < a.rows; ++it) {                     // `row` is the same in all blocks of a cluster
     const int b = it & 1;

@@ -63,7 +63,7 @@ def pair_loss(x, kind, beta, eps):
     """Loss of one pair and its slope in x."""
     if kind == 0:
         up, down = np.logaddexp(0, -x), np.logaddexp(0, x)       # -log sigmoid(x), -log sigmoid(-x)
-        return (1 - eps) * up + eps * down, -(1 - eps) * np.exp(-np.logaddexp(0, x)) + eps * np.exp(-np.logaddexp(0, -x))
+        return (1 - eps) * up + (eps * down if eps else 0.0), -(1 - eps) * np.exp(-np.logaddexp(0, x)) + eps * np.exp(-np.logaddexp(0, -x))
     if kind == 1:
         h = x / beta - 1 / (2 * beta)
         return h * h, 2 * h / beta

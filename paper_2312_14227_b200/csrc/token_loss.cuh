@@ -722,7 +722,8 @@ pair_kernel(const __grid_constant__ PairArgs a) {
     if (a.kind == kPrefSigmoid) {
       // t = exp(-|x|): log(1 + exp(+-x)) = max(0, +-x) + log(1 + t), sigmoid(-|x|) = t / (1 + t)
       const double t = exp(-fabs(x)), l = log1p(t), small = t / (1.0 + t), large = 1.0 / (1.0 + t);
-      loss = l + (1.0 - eps) * fmax(-x, 0.0) + eps * fmax(x, 0.0);
+      loss = l + (1.0 - eps) * fmax(-x, 0.0);
+      if (eps > 0.0) loss += eps * fmax(x, 0.0);           // x = inf (a rejected token of probability 0) times no smoothing is nothing
       dx = eps * (x < 0.0 ? small : large) - (1.0 - eps) * (x < 0.0 ? large : small);
       if (x != x) loss = dx = x;
     } else if (a.kind == kPrefIpo) {

@@ -1,0 +1,51 @@
+"""Token losses, clipping and the table's gradient at the ends of their ranges, through the C ABI.  Expected values are closed forms."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2312_14227_b200 as et
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+E = 2.0 ** -24
+F, B = et.ET_F32, et.ET_BF16
+INF = float("inf")
+
+
+def _stack(M, width, dtype):
+    s = et.et_stack_create([(8, width, 0, 1, -1)], M, dtype)
+    tdt = torch.bfloat16 if dtype == B else torch.float32
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, [torch.zeros(8, width, dtype=tdt, device=DEV)], [torch.zeros(width, dtype=tdt, device=DEV)], ws)
+    return s, tdt
+
+
+def _dev(a, dt):
+    return torch.tensor(a, dtype=dt, device=DEV)
+
+
+# widths: rows held by one block, rows read twice
+@pytest.mark.parametrize("dtype,width", [(F, 1024), (B, 1024), (B, 300000)])
+def test_rejected_token_of_probability_zero(dtype, width):
+    """x = inf: the pair's sigmoid loss and gradient are 0 and leave the batch's mean alone."""
+    s, tdt = _stack(4, width, dtype)
+    y = torch.zeros(4, width, dtype=tdt, device=DEV)     # every token's log probability is -log(width)
+    y[1, 2] = -INF                                       # the rejected answer of pair 0
+    t, begin = _dev([0, 2, 1, 1], torch.int32), _dev([0, 1, 2, 3, 4], torch.int32)
+    for dY in (torch.full_like(y, float("nan")), None):
+        stats, seq = torch.full((4,), float("nan"), device=DEV), torch.full((4,), float("nan"), device=DEV)
+        et.et_loss_preference_grad(s, y, t, begin, dY, seq_logp=seq, loss_dev=stats, beta=0.5)
+        torch.cuda.synchronize()
+        # pair 1: x = 0, loss log 2; one rounding of the mean to 32 bits
+        assert abs(float(stats[0]) - 0.5 * math.log(2)) <= 2 * E * math.log(2)
+        assert float(stats[2]) == -INF and float(stats[3]) == 0.5 and float(seq[1]) == -INF
+        if dY is not None:
+            assert (dY[:2] == 0).all()
+            # c = -1/2 beta / pairs = -1/8: -1/8 (1 - p) at the target; p itself and the product round, then the storage type
+            want, half = -0.125 * (1 - 1 / width), torch.finfo(tdt).eps / 2
+            assert abs(float(dY[2, 1]) - want) <= (half + 32 * E) * abs(want)
+    stats = torch.empty(4, device=DEV)
+    et.et_loss_preference_grad(s, y, t, begin, None, loss_dev=stats, beta=0.5, label_smoothing=0.1)
+    assert float(stats[0]) == INF                        # with smoothing the loss of that pair is infinite

@@ -291,6 +291,8 @@ typedef struct {
  *     kl_i = exp(d_i) - 1 - d_i,   d_i = logp_ref_i - lp_i          logp_ref NULL: 0
  *     loss = sum_i w_i ( -min(r_i A_i, clip(r_i, 1 - clip_low, 1 + clip_high) A_i) + kl_coef kl_i )
  *   weights NULL: w_i = 1 / M.  advantages, logp_old, logp_ref: device float[M].
+ *   r_i and exp(d_i) are formed in fp32: infinite where lp_i is more than 88 above logp_old_i or below logp_ref_i.
+ *   kl_coef = 0: kl_i is reported (it may be infinite) and is no part of the loss or the gradient.
  *   logp      device float[M] or NULL: lp_i
  *   loss_dev  device float[4] or NULL: the loss, its first part, sum w_i kl_i, sum of the w_i whose ratio is clipped
  * Where both arguments of the min are equal the first one's slope counts. */

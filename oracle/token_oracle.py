@@ -52,10 +52,13 @@ def policy(y, targets, weights, adv, old, ref, vocab, scale, lo, hi, beta):
         kl, dkl = np.zeros_like(lp), np.zeros_like(lp)
     else:
         d = np.where(live, ref - lp, 0.0)
-        kl, dkl = np.exp(d) - 1 - d, 1 - np.exp(d)
-    coef = w * (np.where(clipped, 0.0, -first) + beta * dkl)
-    part1, part2 = -(w * np.minimum(first, second)).sum(), (w * kl).sum()
-    stats = np.array([part1 + beta * part2, part1, part2, (w * clipped).sum()])
+        kl, dkl = np.where(d == np.inf, np.inf, np.exp(d) - 1 - np.where(d == np.inf, 0.0, d)), 1 - np.exp(d)
+    slope = np.where(clipped, 0.0, -first)
+    if beta:                                     # a divergence that is reported only may be infinite
+        slope = slope + beta * dkl
+    coef = w * slope
+    part1, part2 = -(w * np.minimum(first, second)).sum(), np.where(w != 0, w * np.where(w != 0, kl, 0.0), 0.0).sum()
+    stats = np.array([part1 + beta * part2 if beta else part1, part1, part2, (w * clipped).sum()])
     return stats, lp, logit_grad(y, targets, vocab, scale, live, p, coef), coef
 
 

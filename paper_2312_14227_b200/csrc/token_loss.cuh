@@ -127,8 +127,8 @@ __device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, f
   float kl = 0.0f;
   if (a.logp_ref != nullptr) {
     const float d = t.ref - lp, e = expm1f(d);
-    kl = e - d;
-    slope -= a.kl_coef * e;
+    kl = e < INFINITY ? e - d : e;                         // d = inf (a token of probability 0): inf, not inf - inf; NaN stays
+    if (a.kl_coef != 0.0f) slope -= a.kl_coef * e;         // a divergence that is reported only may be infinite
   }
   if (sums != nullptr) {
     sums[0] -= (double)w * (double)((clipped ? rc : r) * t.adv);
@@ -170,7 +170,7 @@ __device__ __forceinline__ void policy_total(const Args& a) {
         r[q] = 0.0;
         for (int wq = 0; wq < (int)((blockDim.x + 31) >> 5); ++wq) r[q] += sh[q][wq];
       }
-      a.out[0] = (float)(r[0] + (double)a.kl_coef * r[1]);
+      a.out[0] = (float)(a.kl_coef != 0.0f ? r[0] + (double)a.kl_coef * r[1] : r[0]);
       a.out[1] = (float)r[0]; a.out[2] = (float)r[1]; a.out[3] = (float)r[2];
     }
     *a.done = 0u;

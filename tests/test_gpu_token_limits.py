@@ -49,3 +49,36 @@ def test_rejected_token_of_probability_zero(dtype, width):
     stats = torch.empty(4, device=DEV)
     et.et_loss_preference_grad(s, y, t, begin, None, loss_dev=stats, beta=0.5, label_smoothing=0.1)
     assert float(stats[0]) == INF                        # with smoothing the loss of that pair is infinite
+
+
+def _policy(s, y, t, adv, w, old=None, ref=None, **k):
+    dY = torch.full_like(y, float("nan"))
+    lp, stats = torch.full((len(y),), float("nan"), device=DEV), torch.full((4,), float("nan"), device=DEV)
+    f = lambda a: None if a is None else _dev(a, torch.float32)  # noqa: E731
+    et.et_loss_policy_grad(s, y, _dev(t, torch.int32), f(adv), dY, weights=f(w), logp_old=f(old), logp_ref=f(ref), logp=lp, loss_dev=stats, **k)
+    torch.cuda.synchronize()
+    return dY, lp, stats
+
+
+@pytest.mark.parametrize("gap", [200.0, 1e4, INF])
+@pytest.mark.parametrize("rows", [3, 700])               # the sums by the last block, or by a kernel of their own
+@pytest.mark.parametrize("dtype,width", [(F, 1024), (B, 1024), (B, 300000)])
+def test_divergence_that_is_reported_only(dtype, width, rows, gap):
+    """kl_coef = 0: a reference far above the policy, or a taken token of probability 0, leaves loss and gradient alone."""
+    if rows == 700 and width == 300000:
+        rows = 1100                                      # rows read twice: 1024 and more take the kernel
+    s, tdt = _stack(rows, width, dtype)
+    y = torch.zeros(rows, width, dtype=tdt, device=DEV)
+    y[0, 1] = -gap                                       # the taken token of row 0
+    t, old = [1] * rows, [-math.log(width)] * rows
+    w = [0.5, 0.5] + [0.0] * (rows - 2)
+    for adv in ([1.0, 2.0] + [0.0] * (rows - 2), [-1.0, 2.0] + [0.0] * (rows - 2)):
+        dY, lp, stats = _policy(s, y, t, adv, w, old, [-1.0] * rows, kl_coef=0.0)
+        # row 0: r = 0; with A < 0 the clipped side counts, 0.8 A: surrogate -0.8 and no slope.  Row 1: r = 1 but for lp's roundings
+        first = 0.5 * (0.0 if adv[0] > 0 else 0.8) - 1.0
+        tol = 64 * E * (1 + math.log(width))
+        assert abs(float(stats[0]) - first) <= tol and float(stats[0]) == float(stats[1])
+        assert float(stats[2]) == INF and float(stats[3]) == (0.0 if adv[0] > 0 else 0.5)
+        assert float(lp[0]) < -150 and (dY[0] == 0).all()
+        want = -1.0 * (1 - 1 / width)
+        assert abs(float(dY[1, 1]) - want) <= (torch.finfo(tdt).eps / 2 + tol) * abs(want) and torch.isfinite(dY[1]).all()

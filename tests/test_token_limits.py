@@ -23,3 +23,15 @@ def test_oracle_rejected_token_of_probability_zero():
     assert S[1] == -INF and math.isclose(stats[0], 0.5 * math.log(2), rel_tol=1e-15)      # pair 1: x = 0
     assert coef[0] == 0 and coef[1] == 0 and not dY[:2].any() and coef[2] == -0.125 and coef[3] == 0.125
     assert tok.preference(y, t, None, [0, 1, 2, 3, 4], None, 4, 1.0, 0, 0.5, 0.1)[0][0] == INF
+
+
+@pytest.mark.parametrize("gap", [1e4, INF])
+def test_oracle_divergence_that_is_reported_only(gap):
+    """kl_coef = 0: a reference far above the policy, or a taken token of probability 0, leaves loss and gradient alone."""
+    y = _logits(2)
+    y[0, 1] = -gap
+    t, w, adv = np.array([1, 2]), np.full(2, 0.5), np.array([1.0, 2.0])
+    old, ref = np.full(2, -math.log(4)), np.full(2, -1.0)
+    stats, lp, dY, coef = tok.policy(y, t, w, adv, old, ref, 4, 1.0, 0.2, 0.2, 0.0)
+    assert coef[0] == 0 and not dY[0].any() and coef[1] == -1.0                  # r = 0, r = 1
+    assert math.isclose(stats[0], -1.0, rel_tol=1e-15) and stats[1] == stats[0] and stats[2] == INF

@@ -122,8 +122,10 @@ __device__ __forceinline__ RowTerms row_terms(const Args& a, int row) {
 __device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, float lp, float w, double* sums) {
   const float r = a.logp_old != nullptr ? expf(lp - t.old) : 1.0f;
   const float rc = fminf(fmaxf(r, 1.0f - a.clip_low), 1.0f + a.clip_high);
-  const bool clipped = r * t.adv > rc * t.adv;
-  float slope = clipped ? 0.0f : -t.adv * r;
+  const bool nothing = t.adv == 0.0f && r == INFINITY;       // no advantage: nothing, however far the ratio has gone
+  const float first = nothing ? 0.0f : r * t.adv, second = nothing ? 0.0f : rc * t.adv;
+  const bool clipped = first > second;
+  float slope = clipped ? 0.0f : -first;
   float kl = 0.0f;
   if (a.logp_ref != nullptr) {
     const float d = t.ref - lp, e = expm1f(d);
@@ -131,7 +133,7 @@ __device__ __forceinline__ float policy_coef(const Args& a, const RowTerms& t, f
     if (a.kl_coef != 0.0f) slope -= a.kl_coef * e;         // a divergence that is reported only may be infinite
   }
   if (sums != nullptr) {
-    sums[0] -= (double)w * (double)((clipped ? rc : r) * t.adv);
+    sums[0] -= (double)w * (double)(clipped ? second : first);
     sums[1] += (double)w * (double)kl;
     if (clipped) sums[2] += (double)w;
   }

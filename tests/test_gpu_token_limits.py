@@ -82,3 +82,20 @@ def test_divergence_that_is_reported_only(dtype, width, rows, gap):
         assert float(lp[0]) < -150 and (dY[0] == 0).all()
         want = -1.0 * (1 - 1 / width)
         assert abs(float(dY[1, 1]) - want) <= (torch.finfo(tdt).eps / 2 + tol) * abs(want) and torch.isfinite(dY[1]).all()
+
+
+@pytest.mark.parametrize("clip_high", [0.2, INF])
+@pytest.mark.parametrize("dtype,width", [(F, 1024), (B, 1024), (B, 300000)])
+def test_no_advantage_and_a_ratio_beyond_fp32(dtype, width, clip_high):
+    """A = 0 takes the row out of the loss, whatever the ratio; any other advantage keeps its row."""
+    s, tdt = _stack(3, width, dtype)
+    y = torch.zeros(3, width, dtype=tdt, device=DEV)
+    lp0 = -math.log(width)
+    dY, lp, stats = _policy(s, y, [1, 1, 1], [0.0, 2.0, 0.0], [0.5, 0.5, 0.5], [lp0 - 100, lp0, lp0 - 1e4], clip_high=clip_high)
+    tol = 64 * E * (1 + math.log(width))
+    assert (dY[0] == 0).all() and (dY[2] == 0).all() and abs(float(stats[0]) + 1.0) <= tol and float(stats[3]) == 0.0
+    want = -1.0 * (1 - 1 / width)
+    assert abs(float(dY[1, 1]) - want) <= (torch.finfo(tdt).eps / 2 + tol) * abs(want)
+    y[0, 0] = float("nan")                               # a row with a NaN still gives NaN
+    dY, _, stats = _policy(s, y, [1, 1, 1], [0.0, 2.0, 0.0], [0.5, 0.5, 0.5], [lp0 - 100, lp0, lp0 - 1e4], clip_high=clip_high)
+    assert torch.isnan(dY[0]).any() and math.isnan(float(stats[0])) and (dY[2] == 0).all()

@@ -16,8 +16,8 @@ from . import binding as et
 
 class ElasticLoop:
     """loss: None for the mean-squared error against `target`, else a callable (y, dY, loss_out, stream) that enqueues
-    calls which write dL/dy into dY and the loss into loss_out (a device float), for instance et_loss_policy_grad; `target` is
-    then not used.  max_norm: clip the selected gradients by their global norm before each update (et_update_clipped, with the
+    calls which write dL/dy into dY and the loss into loss_out[0]; loss_out is a device float[4], what the token losses
+    (et_loss_policy_grad, et_loss_preference_grad) take as loss_dev.  `target` is then not used.  max_norm: clip the selected gradients by their global norm before each update (et_update_clipped, with the
     optimiser the stack is set to); the gradients then take buffers of their own.  x of a stack with an embedding: int32 ids."""
 
     def __init__(self, stack, W, b, x, target, lr, period, window, rho, t_dw, t_dy, t_fwd=0.0, Tq=1000,
@@ -53,7 +53,7 @@ class ElasticLoop:
         """Runs `steps` training steps.  elastic=False trains every tensor at every step (full
         backprop, no evaluation).  Returns losses, the mask used at each step, the importances
         of each evaluation and, with time_steps, the mean device time per step in ms."""
-        losses = torch.zeros(steps, dtype=torch.float32, device=self.x.device)
+        losses = torch.zeros((steps, 4), dtype=torch.float32, device=self.x.device)    # a row a step: the token losses report four numbers
         masks, evaluations, dp_ms = [], [], []
         e0 = e1 = None
         if time_steps:
@@ -68,9 +68,9 @@ class ElasticLoop:
                     s_.copy_(p_)
             et.et_forward_stack(self.stack, self.x, self.y, stream=self.stream)
             if self.loss is None:
-                et.et_loss_mse_grad(self.stack, self.y, self.target, self.dY, losses[step:step + 1], stream=self.stream)
+                et.et_loss_mse_grad(self.stack, self.y, self.target, self.dY, losses[step], stream=self.stream)
             else:
-                self.loss(self.y, self.dY, losses[step:step + 1], self.stream)
+                self.loss(self.y, self.dY, losses[step], self.stream)
             mask = self.mask.copy()
             masks.append(mask)
             if elastic and phase == self.window - 1:
@@ -95,6 +95,6 @@ class ElasticLoop:
             e1.record(self.stream)
             torch.cuda.synchronize()
             out["ms_per_step"] = e0.elapsed_time(e1) / steps
-        out["losses"] = losses.cpu().numpy().astype(np.float64)
+        out["losses"] = losses[:, 0].cpu().numpy().astype(np.float64)
         return out
 

@@ -99,3 +99,27 @@ def test_no_advantage_and_a_ratio_beyond_fp32(dtype, width, clip_high):
     y[0, 0] = float("nan")                               # a row with a NaN still gives NaN
     dY, _, stats = _policy(s, y, [1, 1, 1], [0.0, 2.0, 0.0], [0.5, 0.5, 0.5], [lp0 - 100, lp0, lp0 - 1e4], clip_high=clip_high)
     assert torch.isnan(dY[0]).any() and math.isnan(float(stats[0])) and (dY[2] == 0).all()
+
+
+def test_elastic_loop_with_a_token_loss_handed_its_buffer():
+    """loss_out goes straight to the call that writes four numbers; the losses are those of a buffer of its own."""
+    from paper_2312_14227_b200.elastic_loop import ElasticLoop
+    out = []
+    for own in (False, True):
+        s, _ = _stack(6, 64, F)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(1)
+        W, b = [torch.randn(8, 64, generator=g, device=DEV)], [torch.zeros(64, device=DEV)]
+        ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+        et.et_stack_bind(s, W, b, ws)
+        t, adv, spare = _dev([1, 2, 3, 4, 5, 6], torch.int32), torch.randn(6, generator=g, device=DEV), torch.zeros(4, device=DEV)
+
+        def loss(y, dY, loss_out, stream):
+            et.et_loss_policy_grad(s, y, t, adv, dY, loss_dev=spare if own else loss_out, stream=stream)
+            if own:
+                loss_out[:1].copy_(spare[:1])
+
+        x = torch.randn(6, 8, generator=g, device=DEV)
+        loop = ElasticLoop(s, W, b, x, None, lr=0.5, period=4, window=2, rho=0.5, t_dw=np.ones(2), t_dy=np.ones(2), loss=loss)
+        out.append(loop.run(5, elastic=False)["losses"])
+    assert (out[0] == out[1]).all() and np.isfinite(out[0]).all() and (out[0] != 0).any()

@@ -35,3 +35,32 @@ def test_oracle_divergence_that_is_reported_only(gap):
     stats, lp, dY, coef = tok.policy(y, t, w, adv, old, ref, 4, 1.0, 0.2, 0.2, 0.0)
     assert coef[0] == 0 and not dY[0].any() and coef[1] == -1.0                  # r = 0, r = 1
     assert math.isclose(stats[0], -1.0, rel_tol=1e-15) and stats[1] == stats[0] and stats[2] == INF
+
+
+def test_elastic_loop_hands_a_token_loss_room_for_its_numbers(monkeypatch):
+    """The token losses write four floats: each step's loss_out takes them, and the steps' losses are the first of each."""
+    torch = pytest.importorskip("torch")
+    from paper_2312_14227_b200 import elastic_loop as el
+
+    class Stack:
+        L, M, out_width = 1, 4, 8
+
+    for name in ("et_forward_stack", "et_backward_elastic"):
+        monkeypatch.setattr(el.et, name, lambda *a, **k: None)
+    given = []
+
+    def loss(y, dY, out, stream):
+        assert out.dtype == torch.float32 and out.is_contiguous() and out.numel() == 4
+        given.append(out)
+        out.copy_(torch.arange(4.0) + 10 * len(given))
+
+    W, b = [torch.zeros(8, 8)], [torch.zeros(8)]
+    loop = el.ElasticLoop(Stack, W, b, torch.zeros(4, 8), None, 0.1, 4, 2, 0.5, np.ones(2), np.ones(2), loss=loss)
+    assert loop.run(3, elastic=False)["losses"].tolist() == [10.0, 20.0, 30.0]
+    store = given[0].untyped_storage()
+    assert all(g.storage_offset() * 4 + 16 <= store.nbytes() for g in given)
+    assert [g.tolist() for g in given] == [[10.0, 11.0, 12.0, 13.0], [20.0, 21.0, 22.0, 23.0], [30.0, 31.0, 32.0, 33.0]]
+    # without a loss of its own the mean-squared error's number
+    monkeypatch.setattr(el.et, "et_loss_mse_grad", lambda s, y, t, dY, out, stream: out[:1].fill_(7.0))
+    loop = el.ElasticLoop(Stack, W, b, torch.zeros(4, 8), torch.zeros(4, 8), 0.1, 4, 2, 0.5, np.ones(2), np.ones(2))
+    assert loop.run(2, elastic=False)["losses"].tolist() == [7.0, 7.0]

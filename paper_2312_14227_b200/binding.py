@@ -168,21 +168,58 @@ def _ptr_array(seq: Optional[Sequence], n: int):
     return (C.c_void_p * n).from_buffer(ptrs)
 
 
-def _typed(where: str, storage: int, stored=(), ints=(), floats=()):
-    """Refuses torch tensors of another type or layout than the call reads: `stored` in the stack's storage type, int32,
-    float32.  Addresses, arrays and None pass."""
+_types = {}
+
+
+def _torch_types(storage: int):
+    """(storage type, int32, float32) as torch types; three Nones, which no tensor has, while torch is not loaded."""
+    if not _types:
+        torch = sys.modules.get("torch")
+        if torch is None:
+            return None, None, None
+        _types.update({ET_F32: (torch.float32, torch.int32, torch.float32), ET_BF16: (torch.bfloat16, torch.int32, torch.float32)})
+    return _types[storage]
+
+
+def _operands(where: str, s: "Stack", args):
+    """Addresses of a call's device operands, each given as (operand, type, elements that the call reads or writes).  Refuses
+    torch tensors of another type or layout, with fewer elements, or on another device than the stack's workspace.  Addresses,
+    arrays and None pass."""
+    dev, out = s.device, []
+    for t, dtype, need in args:
+        if t is None or type(t) is int:
+            out.append(t)
+            continue
+        try:
+            if t.dtype is dtype and t.numel() >= need and t.get_device() == dev and t.is_contiguous():
+                out.append(t.data_ptr())
+                continue
+        except AttributeError:
+            pass
+        return _operands_checked(where, s, args)
+    return out
+
+
+def _operands_checked(where: str, s: "Stack", args):
+    """The same, slowly: says what is wrong, types first, and lets pass what the short way does not know (arrays, pinned host
+    memory, a workspace given by its address)."""
     torch = sys.modules.get("torch")
-    if torch is None:
-        return
-    tensor = torch.Tensor
-    for group, dtype in ((stored, torch.bfloat16 if storage == ET_BF16 else torch.float32), (ints, torch.int32),
-                         (floats, torch.float32)):
-        for i, t in enumerate(group):
-            if isinstance(t, tensor):
-                if t.dtype is not dtype:
-                    raise EtError(ET_ERR_DTYPE, f"{where}: a tensor of {t.dtype} where {dtype} is read (number {i} of these)")
-                if not t.is_contiguous():
-                    raise EtError(ET_ERR_INVALID_ARG, f"{where}: a tensor of {dtype} that is not contiguous (number {i} of these)")
+    tensors = [(i, t, dtype, need) for i, (t, dtype, need) in enumerate(args) if torch is not None and isinstance(t, torch.Tensor)]
+    for i, t, dtype, need in tensors:
+        if t.dtype is not dtype:
+            raise EtError(ET_ERR_DTYPE, f"{where}: a tensor of {t.dtype} where {dtype} is read (number {i})")
+    for i, t, dtype, need in tensors:
+        if not t.is_contiguous():
+            raise EtError(ET_ERR_INVALID_ARG, f"{where}: a tensor of {dtype} that is not contiguous (number {i})")
+        if t.numel() < need:
+            raise EtError(ET_ERR_INVALID_ARG, f"{where}: a tensor of {t.numel()} elements where {need} are read or written (number {i})")
+    for i, t, dtype, need in tensors:
+        if t.is_cuda:
+            if s.device is not None and t.get_device() != s.device:
+                raise EtError(ET_ERR_INVALID_ARG, f"{where}: a tensor on {t.device}, the workspace is on device {s.device} (number {i})")
+        elif s.bound and not t.is_pinned():
+            raise EtError(ET_ERR_INVALID_ARG, f"{where}: a tensor on {t.device} where device memory is read or written (number {i})")
+    return [_ptr(t) for t, _, _ in args]
 
 
 def _stream_ptr(stream) -> Optional[int]:
@@ -299,6 +336,7 @@ class Stack:
         _check(_lib.et_stack_create(descs, self.L, self.M, dtype, C.byref(h)), "et_stack_create")
         self.handle = h
         self._keep = []
+        self.bound, self.device = False, None        # device: number of the device that a bound workspace tensor is on
 
     def close(self):
         if getattr(self, "handle", None):
@@ -337,6 +375,7 @@ def et_stack_bind(s: Stack, W, b, workspace, workspace_bytes: Optional[int] = No
     s._keep = [list(W), list(b), workspace]          # keep the tensors alive while bound
     _check(_lib.et_stack_bind(s.handle, _ptr_array(W, s.L), _ptr_array(b, s.L), _ptr(workspace),
                               workspace_bytes, _stream_ptr(stream)), "et_stack_bind")
+    s.bound, s.device = True, workspace.get_device() if getattr(workspace, "is_cuda", False) else None
 
 
 def et_stack_bind_master(s: Stack, W32, b32):
@@ -347,7 +386,8 @@ def et_stack_bind_master(s: Stack, W32, b32):
 
 def et_forward_stack(s: Stack, x, y, stream=None):
     if s.takes_ids:
-        _typed("et_forward_stack", s.dtype, ints=(x,))
+        st, i32, _ = _torch_types(s.dtype)
+        x, y = _operands("et_forward_stack", s, ((x, i32, s.M), (y, st, s.M * s.out_width)))
     _check(_lib.et_forward_stack(s.handle, _ptr(x), _ptr(y), _stream_ptr(stream)), "et_forward_stack")
 
 
@@ -361,32 +401,41 @@ def et_stack_set_embedding_scale(s: Stack, scale: float):
 
 
 def et_token_logp(s: Stack, y, targets, logp, vocab: int = 0, logit_scale: float = 1.0, stream=None):
-    _typed("et_token_logp", s.dtype, (y,), (targets,), (logp,))
-    _check(_lib.et_token_logp(s.handle, _ptr(y), _ptr(targets), vocab, logit_scale, _ptr(logp), _stream_ptr(stream)),
-           "et_token_logp")
+    st, i32, f32 = _torch_types(s.dtype)
+    M = s.M
+    y, targets, logp = _operands("et_token_logp", s, ((y, st, M * s.out_width), (targets, i32, M), (logp, f32, M)))
+    _check(_lib.et_token_logp(s.handle, y, targets, vocab, logit_scale, logp, _stream_ptr(stream)), "et_token_logp")
 
 
 def et_loss_policy_grad(s: Stack, y, targets, advantages, dY=None, weights=None, logp_old=None, logp_ref=None, logp=None,
                         loss_dev=None, vocab: int = 0, logit_scale: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2,
                         kl_coef: float = 0.0, stream=None):
-    _typed("et_loss_policy_grad", s.dtype, (y, dY), (targets,), (advantages, weights, logp_old, logp_ref, logp, loss_dev))
+    st, i32, f32 = _torch_types(s.dtype)
+    M = s.M
+    n = M * s.out_width
+    y, dY, targets, advantages, weights, logp_old, logp_ref, logp, loss_dev = _operands(
+        "et_loss_policy_grad", s, ((y, st, n), (dY, st, n), (targets, i32, M), (advantages, f32, M), (weights, f32, M),
+                                   (logp_old, f32, M), (logp_ref, f32, M), (logp, f32, M), (loss_dev, f32, 4)))
     cfg = et_policy_config(vocab, logit_scale, clip_low, clip_high, kl_coef)
-    _check(_lib.et_loss_policy_grad(s.handle, _ptr(y), _ptr(targets), _ptr(weights), _ptr(advantages), _ptr(logp_old),
-                                    _ptr(logp_ref), C.addressof(cfg), _ptr(dY), _ptr(logp), _ptr(loss_dev),
-                                    _stream_ptr(stream)), "et_loss_policy_grad")
+    _check(_lib.et_loss_policy_grad(s.handle, y, targets, weights, advantages, logp_old, logp_ref, C.addressof(cfg), dY, logp,
+                                    loss_dev, _stream_ptr(stream)), "et_loss_policy_grad")
 
 
 def et_loss_preference_grad(s: Stack, y, targets, seq_begin, dY=None, weights=None, ref_logp=None, seq_logp=None, loss_dev=None,
                             kind: int = ET_PREF_SIGMOID, vocab: int = 0, logit_scale: float = 1.0, beta: float = 0.1,
                             label_smoothing: float = 0.0, pairs: Optional[int] = None, stream=None):
     """`pairs`: taken from the length of seq_begin (2 pairs + 1) unless given."""
-    _typed("et_loss_preference_grad", s.dtype, (y, dY), (targets, seq_begin), (weights, ref_logp, seq_logp, loss_dev))
-    cfg = et_preference_config(kind, vocab, logit_scale, beta, label_smoothing)
+    st, i32, f32 = _torch_types(s.dtype)
     if pairs is None:
         pairs = (len(seq_begin) - 1) // 2
-    _check(_lib.et_loss_preference_grad(s.handle, _ptr(y), _ptr(targets), _ptr(weights), _ptr(seq_begin), pairs, _ptr(ref_logp),
-                                        C.addressof(cfg), _ptr(dY), _ptr(seq_logp), _ptr(loss_dev), _stream_ptr(stream)),
-           "et_loss_preference_grad")
+    M = s.M
+    n, q = M * s.out_width, 2 * pairs
+    y, dY, targets, seq_begin, weights, ref_logp, seq_logp, loss_dev = _operands(
+        "et_loss_preference_grad", s, ((y, st, n), (dY, st, n), (targets, i32, M), (seq_begin, i32, q + 1), (weights, f32, M),
+                                       (ref_logp, f32, q), (seq_logp, f32, q), (loss_dev, f32, 4)))
+    cfg = et_preference_config(kind, vocab, logit_scale, beta, label_smoothing)
+    _check(_lib.et_loss_preference_grad(s.handle, y, targets, weights, seq_begin, pairs, ref_logp, C.addressof(cfg), dY, seq_logp,
+                                        loss_dev, _stream_ptr(stream)), "et_loss_preference_grad")
 
 
 def et_grad_norm(s: Stack, mask, grads, norm_dev, stream=None):

@@ -64,3 +64,47 @@ def test_elastic_loop_hands_a_token_loss_room_for_its_numbers(monkeypatch):
     monkeypatch.setattr(el.et, "et_loss_mse_grad", lambda s, y, t, dY, out, stream: out[:1].fill_(7.0))
     loop = el.ElasticLoop(Stack, W, b, torch.zeros(4, 8), torch.zeros(4, 8), 0.1, 4, 2, 0.5, np.ones(2), np.ones(2))
     assert loop.run(2, elastic=False)["losses"].tolist() == [7.0, 7.0]
+
+
+def _short(fn, *a, **k):
+    with pytest.raises(et.EtError) as e:
+        fn(*a, **k)
+    return e.value.status
+
+
+@pytest.mark.parametrize("bound", [False, True])
+def test_token_calls_refuse_tensors_shorter_than_they_read(bound):
+    torch = pytest.importorskip("torch")
+    M, width = 4, 16
+    s = et.et_stack_create([(8, width, 0, 1, -1)], M, et.ET_F32)
+    s.bound = bound                                      # what the binding knows; the library still refuses the call by itself
+    y, ids = torch.zeros(M, width), torch.zeros(M, dtype=torch.int32)
+    f, four = torch.zeros(M), torch.zeros(4)
+    begin = torch.zeros(5, dtype=torch.int32)
+    cut = lambda t: t.reshape(-1)[:-1].clone()  # noqa: E731
+    bad = et.ET_ERR_INVALID_ARG
+    if not bound:                                        # all in order but the stack
+        assert _short(et.et_token_logp, s, y, ids, f) == et.ET_ERR_STATE
+        assert _short(et.et_loss_policy_grad, s, y, ids, f, y, f, f, f, f, four) == et.ET_ERR_STATE
+        assert _short(et.et_loss_preference_grad, s, y, ids, begin, y, f, four, four, four) == et.ET_ERR_STATE
+    else:                                                # ordinary host memory where the device reads
+        assert _short(et.et_token_logp, s, y, ids, f) == bad
+    for args in ((cut(y), ids, f), (y, cut(ids), f), (y, ids, cut(f))):
+        assert _short(et.et_token_logp, s, *args) == bad
+    good = [y, ids, f, y, f, f, f, f, four]
+    for i, t in enumerate(good):
+        assert _short(et.et_loss_policy_grad, s, *[cut(t) if i == j else u for j, u in enumerate(good)]) == bad, i
+    good = [y, ids, begin, y, f, four, four, four]
+    for i, t in enumerate(good):
+        k = {"pairs": 2} if i == 2 else {}
+        assert _short(et.et_loss_preference_grad, s, *[cut(t) if i == j else u for j, u in enumerate(good)], **k) == bad, i
+
+
+def test_lookup_refuses_tensors_shorter_than_it_reads():
+    torch = pytest.importorskip("torch")
+    s = et.et_stack_create([(11, 8, 0, 1, -1, et.ET_LAYER_EMBEDDING)], 4, et.ET_F32)
+    ids, y = torch.zeros(4, dtype=torch.int32), torch.zeros(4, 8)
+    assert _short(et.et_forward_stack, s, ids, y) == et.ET_ERR_STATE
+    assert _short(et.et_forward_stack, s, ids[:3].clone(), y) == et.ET_ERR_INVALID_ARG
+    assert _short(et.et_forward_stack, s, ids, y[:3].clone()) == et.ET_ERR_INVALID_ARG
+    assert _short(et.et_forward_stack, s, ids, y.double()) == et.ET_ERR_DTYPE

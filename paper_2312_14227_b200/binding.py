@@ -222,6 +222,44 @@ def _operands_checked(where: str, s: "Stack", args):
     return [_ptr(t) for t, _, _ in args]
 
 
+def _load_helper():
+    """The module that checks a list of tensors in one call, where it was built for the torch that runs; else None."""
+    import importlib
+    torch = sys.modules["torch"]
+    try:
+        helper = importlib.import_module(__package__ + "._operands")
+    except ImportError:
+        return None
+    return helper if torch.__version__.split("+")[0] == helper.torch_version.split("+")[0] else None
+
+
+_helper = []                                             # filled at the first list of tensors: torch is loaded then
+
+
+def _grad_array(where: str, s: "Stack", seq, mask: bytes, f32):
+    """Addresses of the selected tensors of a list of fp32 gradients (0 for the others), checked as _operands does."""
+    if seq is None:
+        return None
+    assert len(seq) == len(mask)
+    if f32 is not None and s.device is not None:
+        if not _helper:
+            _helper.append(_load_helper())
+        if _helper[0] is not None:
+            out = _helper[0].addresses(seq, mask, s.counts_i64, s.device)
+            if out is not None:
+                return out
+    args = [(t if m else None, f32, need) for t, m, need in zip(seq, mask, s.counts)]
+    return array.array("Q", [p or 0 for p in _operands(where, s, args)]).tobytes()
+
+
+def _norm_address(where: str, s: "Stack", t, f32):
+    if t is None:
+        return None
+    if f32 is not None and getattr(t, "dtype", None) is f32 and t.numel() >= 2 and t.get_device() == s.device and t.is_contiguous():
+        return t.data_ptr()
+    return _operands_checked(where, s, ((t, f32, 2),))[0]
+
+
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
         return None
@@ -313,6 +351,15 @@ class Report:
     flops_executed = property(lambda self: self.c.flops_executed)
 
 
+def _tensor_counts(d: et_layer_desc):
+    """Elements of the two tensors of a layer."""
+    if d.kind in (ET_LAYER_ATTENTION, ET_LAYER_IM2COL):
+        return 0, 0
+    if d.kind in (ET_LAYER_NORM, ET_LAYER_BATCHNORM):
+        return d.out_features, d.out_features
+    return d.in_features * d.out_features, 0 if d.kind == ET_LAYER_EMBEDDING else d.out_features
+
+
 class Stack:
     """Owns the opaque et_stack handle.  Layers: sequence of objects / tuples with
     in_features, out_features, act, fold, residual_src."""
@@ -330,6 +377,9 @@ class Stack:
                                          getattr(ly, "kind", ET_LAYER_DENSE), getattr(ly, "eps", 0.0),
                                          getattr(ly, "heads", 0), getattr(ly, "seq", 0), getattr(ly, "height", 0),
                                          getattr(ly, "width", 0), getattr(ly, "ksize", 0))
+        # elements of every tensor (0 where a layer has none): what a gradient holds
+        self.counts = [c for d in descs[:self.L] for c in _tensor_counts(d)]
+        self.counts_i64 = array.array("q", self.counts).tobytes()
         self.takes_ids = self.L > 0 and descs[0].kind == ET_LAYER_EMBEDDING
         self.out_width = (descs[self.L - 1].out_features // max(descs[self.L - 1].fold, 1)) if self.L else 0
         h = C.c_void_p()
@@ -439,20 +489,27 @@ def et_loss_preference_grad(s: Stack, y, targets, seq_begin, dY=None, weights=No
 
 
 def et_grad_norm(s: Stack, mask, grads, norm_dev, stream=None):
-    m = _mask_arr(mask)
-    _check(_lib.et_grad_norm(s.handle, _ptr(m), len(m), _ptr_array(grads, len(m)), _ptr(norm_dev), _stream_ptr(stream)),
+    f32 = _torch_types(s.dtype)[2]
+    m = _mask_arr(mask).tobytes()
+    g = _grad_array("et_grad_norm", s, grads, m, f32)
+    _check(_lib.et_grad_norm(s.handle, m, len(m), g, _norm_address("et_grad_norm", s, norm_dev, f32), _stream_ptr(stream)),
            "et_grad_norm")
 
 
 def et_clip_grads(s: Stack, mask, grads, clipped, max_norm: float, norm_dev=None, stream=None):
-    m = _mask_arr(mask)
-    _check(_lib.et_clip_grads(s.handle, _ptr(m), len(m), _ptr_array(grads, len(m)), _ptr_array(clipped, len(m)), max_norm,
-                              _ptr(norm_dev), _stream_ptr(stream)), "et_clip_grads")
+    f32 = _torch_types(s.dtype)[2]
+    m = _mask_arr(mask).tobytes()
+    g = _grad_array("et_clip_grads", s, grads, m, f32)
+    out = g if clipped is grads else _grad_array("et_clip_grads", s, clipped, m, f32)
+    _check(_lib.et_clip_grads(s.handle, m, len(m), g, out, max_norm,
+                              _norm_address("et_clip_grads", s, norm_dev, f32), _stream_ptr(stream)), "et_clip_grads")
 
 
 def et_update_clipped(s: Stack, mask, grads, lr: float, max_norm: float, norm_dev=None, stream=None):
-    m = _mask_arr(mask)
-    _check(_lib.et_update_clipped(s.handle, _ptr(m), len(m), _ptr_array(grads, len(m)), lr, max_norm, _ptr(norm_dev),
+    f32 = _torch_types(s.dtype)[2]
+    m = _mask_arr(mask).tobytes()
+    g = _grad_array("et_update_clipped", s, grads, m, f32)
+    _check(_lib.et_update_clipped(s.handle, m, len(m), g, lr, max_norm, _norm_address("et_update_clipped", s, norm_dev, f32),
                                   _stream_ptr(stream)), "et_update_clipped")
 
 

@@ -123,3 +123,36 @@ def test_elastic_loop_with_a_token_loss_handed_its_buffer():
         loop = ElasticLoop(s, W, b, x, None, lr=0.5, period=4, window=2, rho=0.5, t_dw=np.ones(2), t_dy=np.ones(2), loss=loss)
         out.append(loop.run(5, elastic=False)["losses"])
     assert (out[0] == out[1]).all() and np.isfinite(out[0]).all() and (out[0] != 0).any()
+
+
+@pytest.mark.parametrize("helper", [False, True])
+def test_clipping_calls_refuse_gradients_they_would_misread(helper, monkeypatch):
+    """A list of bf16 gradients of a bf16 stack is half of what would be read; with the helper module and without it."""
+    from paper_2312_14227_b200 import binding
+    monkeypatch.setattr(binding, "_helper", [binding._load_helper() if helper else None])
+    layers = [(8, 8, 0, 1, -1, et.ET_LAYER_NORM, 1e-5), (8, 16, 0, 1, -1)]
+    s = et.et_stack_create(layers, 4, B)
+    shapes = [(8,), (8,), (8, 16), (16,)]
+    params = [torch.zeros(n, dtype=torch.bfloat16, device=DEV) for n in shapes]
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, params[0::2], params[1::2], ws)
+    g, norm = [torch.full(n, 2.0, device=DEV) for n in shapes], torch.zeros(2, device=DEV)
+    bad = [(2, g[2].bfloat16(), et.ET_ERR_DTYPE), (2, torch.zeros(16, 8, device=DEV).t(), et.ET_ERR_INVALID_ARG),
+           (3, torch.zeros(15, device=DEV), et.ET_ERR_INVALID_ARG), (1, torch.zeros(1, device=DEV).expand(8), et.ET_ERR_INVALID_ARG),
+           (0, torch.zeros(8), et.ET_ERR_INVALID_ARG), (3, None, et.ET_ERR_INVALID_ARG)]
+    for i, t, status in bad:
+        lst = [t if i == j else u for j, u in enumerate(g)]
+        for call in (lambda: et.et_grad_norm(s, [1] * 4, lst, norm), lambda: et.et_clip_grads(s, [1] * 4, g, lst, 1.0),
+                     lambda: et.et_clip_grads(s, [1] * 4, lst, g, 1.0), lambda: et.et_update_clipped(s, [1] * 4, lst, 0.1, 1.0)):
+            with pytest.raises(et.EtError) as e:
+                call()
+            assert e.value.status == status, (i, status)
+        mask = [int(i != j) for j in range(4)]           # not selected: ignored, whatever it is
+        et.et_grad_norm(s, mask, lst, norm)
+        assert float(norm[0]) == np.float32(math.sqrt(4.0 * sum(math.prod(n) for n, m in zip(shapes, mask) if m)))
+    et.et_clip_grads(s, [1] * 4, g, g, 1.0, norm)
+    n = math.sqrt(4.0 * 160)
+    assert float(norm[0]) == np.float32(n) and all(((u - 2 / n).abs() <= 4 * E / n * 2).all() for u in g)
+    by_address = [u.data_ptr() for u in g]
+    et.et_grad_norm(s, [1] * 4, by_address, norm.data_ptr())
+    assert abs(float(norm[0]) - 1.0) <= 8 * E

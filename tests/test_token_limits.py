@@ -108,3 +108,49 @@ def test_lookup_refuses_tensors_shorter_than_it_reads():
     assert _short(et.et_forward_stack, s, ids[:3].clone(), y) == et.ET_ERR_INVALID_ARG
     assert _short(et.et_forward_stack, s, ids, y[:3].clone()) == et.ET_ERR_INVALID_ARG
     assert _short(et.et_forward_stack, s, ids, y.double()) == et.ET_ERR_DTYPE
+
+
+@pytest.mark.parametrize("bound", [False, True])
+def test_clipping_calls_refuse_gradients_of_another_type_layout_or_size(bound):
+    """A list of bf16 gradients of a bf16 stack is half of what would be read."""
+    torch = pytest.importorskip("torch")
+    s = et.et_stack_create([(8, 8, 0, 1, -1, et.ET_LAYER_NORM, 1e-5), (8, 16, 0, 1, -1)], 4, et.ET_BF16)
+    s.bound = bound
+    shapes = [(8,), (8,), (8, 16), (16,)]
+    good, m, norm = [torch.zeros(n) for n in shapes], [1, 1, 1, 1], torch.zeros(2)
+    bad = [(2, good[2].bfloat16(), et.ET_ERR_DTYPE), (2, torch.zeros(16, 8).t(), et.ET_ERR_INVALID_ARG),
+           (2, torch.zeros(127), et.ET_ERR_INVALID_ARG), (3, torch.zeros(15), et.ET_ERR_INVALID_ARG),
+           (0, torch.zeros(7), et.ET_ERR_INVALID_ARG), (1, torch.zeros(1).expand(8), et.ET_ERR_INVALID_ARG), (3, None, et.ET_ERR_INVALID_ARG)]
+    calls = [lambda g, n=norm, k=m: et.et_grad_norm(s, k, g, n), lambda g, n=norm, k=m: et.et_clip_grads(s, k, g, g, 1.0, n),
+             lambda g, n=norm, k=m: et.et_clip_grads(s, k, good, g, 1.0, n), lambda g, n=norm, k=m: et.et_clip_grads(s, k, g, good, 1.0, n),
+             lambda g, n=norm, k=m: et.et_update_clipped(s, k, g, 0.1, 1.0, n)]
+    for call in calls:
+        if bound:
+            assert _short(call, good) == et.ET_ERR_INVALID_ARG           # ordinary host memory
+        else:
+            assert _short(call, good) == et.ET_ERR_STATE
+            for i, t, status in bad:
+                assert _short(call, [t if i == j else g for j, g in enumerate(good)]) == status, i
+                if call not in (calls[2], calls[3]):                     # not selected: ignored, whatever it is
+                    off = [int(i != j) for j in range(4)]
+                    assert _short(call, [t if i == j else g for j, g in enumerate(good)], k=off) == et.ET_ERR_STATE
+            assert _short(call, good, torch.zeros(1)) == et.ET_ERR_INVALID_ARG
+            assert _short(call, good, norm.double()) == et.ET_ERR_DTYPE
+
+
+def test_helper_module_knows_nothing_but_device_tensors():
+    """The list check in one call is there wherever torch is, and leaves everything it does not know to the slow way."""
+    import array
+    torch = pytest.importorskip("torch")
+    from paper_2312_14227_b200 import binding
+    h = binding._load_helper()
+    assert h is not None
+    need = lambda *n: array.array("q", n).tobytes()  # noqa: E731
+    t = torch.zeros(4)
+    assert h.addresses([None, t], b"\0\0", need(4, 4), 0) == bytes(16) and h.addresses((), b"", need(), 0) == b""
+    for seq in ([t], [None], [7], ["x"], [np.zeros(4)], [torch.zeros(4, device="meta")], [t.to_sparse()]):
+        assert h.addresses(seq, b"\1", need(4), 0) is None and h.addresses(seq, b"\1", need(4), -1) is None
+    assert h.addresses([t], b"\0\0", need(4), 0) is None and h.addresses([t], b"\0", need(4, 4), 0) is None
+    for args in (([t], "x", need(4), 0), ([t], b"\0"), (7, b"\0", need(4), 0), ([t], b"\0", need(4), None)):
+        with pytest.raises(TypeError):
+            h.addresses(*args)

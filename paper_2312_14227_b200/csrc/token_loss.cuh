@@ -70,20 +70,24 @@ struct Args {
   float default_weight;
   float clip_low, clip_high, kl_coef;
 };
-// exp(scale d) for two differences d <= 0.  One fp32 constant for scale * log2(e) would be off by up to 2^-24 of it, the same
-// way in every term of every row: a bias of the log of the sum that sums over rows do not average out.  k_lo > 0 keeps
-// d = -inf at -inf (a negative or zero k_lo would make it NaN).
-__device__ __forceinline__ uint64_t scale2(uint64_t d, uint64_t k_hi, uint64_t k_lo) { return fma2(d, k_lo, mul2(d, k_hi)); }
-__device__ __forceinline__ float exp_diff(float d, const Args& a) { return exp2_fast(fmaf(d, a.k_lo, d * a.k_hi)); }
+// exp(scale d) for differences d <= 0, as 2^(d k_hi + (d k_lo + kExpUp)) with one rounding of the exponent.  What errs the same way in
+// every term moves the log of every sum the same way, which sums over rows do not average out, so:
+//  - one fp32 constant for scale * log2(e) would be off by up to 2^-23 of it.  The small product goes into the fused one: added
+//    to a rounded d k_hi it would vanish below half a step of it
+//  - ex2.approx is low by 5.0e-8 on average (measured in every octave of [-22, -1], 2^20 arguments each against 64-bit values:
+//    -4.96e-8 .. -5.11e-8; -2.88e-8 on [-1, 0]): kExpUp = 5.0e-8 / ln 2 raises the exponent by that.  It is below half a step
+//    of the exponents that count, and rounding to nearest carries it on average.  2^kExpUp itself comes out as 1: the largest term
+//    of a row is exact
+// k_lo > 0 keeps d = -inf at -inf (a negative or zero k_lo would make it NaN).
+constexpr float kExpUp = 7.2e-8f;
+__device__ __forceinline__ uint64_t scale2(uint64_t d, uint64_t k_hi, uint64_t k_lo) {
+  return fma2(d, k_hi, fma2(d, k_lo, pack2(kExpUp, kExpUp)));
+}
+__device__ __forceinline__ float exp_diff(float d, const Args& a) { return exp2_fast(fmaf(d, a.k_hi, fmaf(d, a.k_lo, kExpUp))); }
 
-// lp of the target's logit from the row's (max, sum).
-__device__ __forceinline__ float log_prob(float yt, float m, float s, const Args& a) { return fmaf(yt - m, a.scale, -logf(s)); }
-// The same for a log probability that is reported and summed (one thread's work): the log in 64 bits, and ex2.approx's mean
-// relative error taken off.  It is low by 5.0e-8 on average wherever in its range (measured over 2^22 arguments against
-// 64-bit values: -4.97e-8 on [-1, 0], -5.08e-8 on [-20, 0]), which moves the log of every sum the same way; over the rows of a
-// long sequence that is ten times what the rows' roundings leave.
-__device__ __forceinline__ float log_prob_summed(float yt, float m, float s, const Args& a) {
-  return (float)((double)(yt - m) * (double)a.scale - (log((double)s) + 5.0e-8));
+// lp of the target's logit from the row's (max, sum), the log in 64 bits (an fp32 log rounds by more than the sum's own error).
+__device__ __forceinline__ float log_prob(float yt, float m, float s, const Args& a) {
+  return (float)((double)(yt - m) * (double)a.scale - log((double)s));
 }
 
 // (max, sum) over the lanes of a warp.  fmaxf drops NaN; the sum carries it.
@@ -477,7 +481,7 @@ token_held_kernel(const __grid_constant__ Args a) {
       }
       const bool first = rank == 0 && lane == 0;
       if (live) {
-        const float lp = MODE == kPolicy ? log_prob(yt, m, s, a) : first ? log_prob_summed(yt, m, s, a) : 0.0f;
+        const float lp = MODE == kPolicy || first ? log_prob(yt, m, s, a) : 0.0f;
         const float inv = 1.0f / s;
         if (first) {
           if (a.logp != nullptr) a.logp[row] = lp;
@@ -581,7 +585,7 @@ token_row_kernel(const __grid_constant__ Args a) {
     }
     block_max_sum(m, s, a);
     const float yt = to_f32(sl.y[t]);
-    const float lp = MODE == kPolicy ? log_prob(yt, m, s, a) : tid == 0 ? log_prob_summed(yt, m, s, a) : 0.0f;
+    const float lp = MODE == kPolicy || tid == 0 ? log_prob(yt, m, s, a) : 0.0f;
     inv = 1.0f / s;
     if (MODE == kPolicy) {
       double sums[3] = {0.0, 0.0, 0.0};

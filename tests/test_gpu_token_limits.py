@@ -156,3 +156,55 @@ def test_clipping_calls_refuse_gradients_they_would_misread(helper, monkeypatch)
     by_address = [u.data_ptr() for u in g]
     et.et_grad_norm(s, [1] * 4, by_address, norm.data_ptr())
     assert abs(float(norm[0]) - 1.0) <= 8 * E
+
+
+@pytest.mark.parametrize("dtype,width", [(F, 1), (F, 100), (F, 8200), (B, 8), (B, 264), (B, 8200), (F, 140003), (B, 300000)])
+@pytest.mark.parametrize("call", ["logp", "policy"])
+def test_rows_with_all_their_mass_on_one_token(dtype, width, call):
+    """p = 1 to within e^-80: the log probability is 0, to the last bit."""
+    M = 600 if width < 20000 else 5
+    s, tdt = _stack(M, width, dtype)
+    y = torch.full((M, width), -100.0, dtype=tdt, device=DEV)
+    t = torch.randint(0, width, (M,), device=DEV, dtype=torch.int32)
+    y[torch.arange(M, device=DEV), t.long()] = 3.0
+    lp = torch.full((M,), float("nan"), device=DEV)
+    if call == "logp":
+        et.et_token_logp(s, y, t, lp)
+    else:
+        et.et_loss_policy_grad(s, y, t, torch.ones(M, device=DEV), None, logp=lp)
+    assert (lp == 0).all()
+
+
+# logit scales: 1, and one whose product with log2(e) is far from an fp32 number (1e-7 of it)
+@pytest.mark.parametrize("scale", [1.0, 0.9])
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("low,high", [(0.9, 1.0), (0.3, 0.9), (1e-4, 0.05)])
+@pytest.mark.parametrize("call", ["logp", "policy"])
+def test_errors_of_log_probabilities_have_no_sign(dtype, low, high, call, scale):
+    """The mean error over many rows: a log probability is added up over sequences, where errors of one sign do not cancel."""
+    M, width, scale = 32768, 264, float(np.float32(scale))
+    s, tdt = _stack(M, width, dtype)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    y = torch.randn(M, width, generator=g, device=DEV)
+    t = torch.randint(0, width, (M,), generator=g, device=DEV, dtype=torch.int32)
+    at = torch.arange(M, device=DEV)
+    p = low + (high - low) * torch.rand(M, generator=g, device=DEV).double()
+    y[at, t.long()] = -float("inf")
+    y[at, t.long()] = ((torch.logsumexp(scale * y.double(), 1) + torch.log(p / (1 - p))) / scale).float()      # the wanted share
+    y = y.to(tdt)
+    lp = torch.empty(M, device=DEV)
+    if call == "logp":
+        et.et_token_logp(s, y, t, lp, logit_scale=scale)
+    else:
+        et.et_loss_policy_grad(s, y, t, torch.ones(M, device=DEV), None, logp=lp, logit_scale=scale)
+    z = scale * y.double()
+    total = torch.logsumexp(z, 1)
+    want = z[at, t.long()] - total
+    err = lp.double() - want
+    # Roundings to nearest have no sign: of the sum (about 16 of them at e of it, independent), of lp itself (e |lp|): six standard
+    # deviations of their mean over M rows.  A term passes up to three exponentials (its own, the lanes' join, the warps' join); the
+    # unit's mean error is within 0.2e-8 of what is taken off, but 2.2e-8 for exponents in [-1, 0].  The largest term is exact.
+    spread = E * (4 + float(want.abs().max())) / math.sqrt(3)
+    share = float((1 - torch.exp(z.amax(1) - total)).mean())
+    assert abs(float(err.mean())) <= 6 * spread / math.sqrt(M) + 3 * 2.2e-8 * share, (float(err.mean()), share)

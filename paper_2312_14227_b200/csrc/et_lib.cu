@@ -6,6 +6,7 @@
 #include <cstdlib>
 #include <cmath>
 #include <cstring>
+#include <limits>
 #include <mutex>
 #include <new>
 #include <type_traits>
@@ -2415,7 +2416,7 @@ void token_args(const et_stack* s, et::tok::Args* a, const void* y, const int32_
   if ((double)hi > k) hi = std::nextafterf(hi, 0.0f);
   a->k_hi = hi;
   const float lo = (float)(k - (double)hi);
-  a->k_lo = lo > 0.f ? lo : std::max(hi * 1e-12f, 1.2e-38f);                // > 0: keeps -inf at -inf
+  a->k_lo = lo > 0.f ? lo : std::max(hi * 1e-12f, std::numeric_limits<float>::denorm_min());   // > 0: keeps -inf at -inf
   a->done = (uint32_t*)s->at(s->off_status) + kDoneWord;
   a->ticket = a->done + 1;
 }

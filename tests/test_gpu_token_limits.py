@@ -208,3 +208,25 @@ def test_errors_of_log_probabilities_have_no_sign(dtype, low, high, call, scale)
     spread = E * (4 + float(want.abs().max())) / math.sqrt(3)
     share = float((1 - torch.exp(z.amax(1) - total)).mean())
     assert abs(float(err.mean())) <= 6 * spread / math.sqrt(M) + 3 * 2.2e-8 * share, (float(err.mean()), share)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-33, 1e-35, 1.5e-38, 3e-38])
+def test_logit_scales_near_the_end_of_fp32(scale):
+    """Logits of 1e30 and more under a scale that brings them back to ordinary ones, down to where d scale leaves fp32."""
+    scale = float(np.float32(scale))
+    M, width = 9, 1000
+    s, _ = _stack(M, width, F)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    y = torch.randn(M, width, generator=g, device=DEV) * min(2 / scale, 5e37)
+    y[1, 3] = -INF
+    y[2, 5:] = -INF
+    t = torch.randint(0, 5, (M,), generator=g, device=DEV, dtype=torch.int32)
+    lp = torch.empty(M, device=DEV)
+    et.et_token_logp(s, y, t, lp, logit_scale=scale)
+    z = scale * y.double()
+    want = z[torch.arange(M, device=DEV), t.long()] - torch.logsumexp(z, 1)
+    # exponents up to 20: e (3 x 20 + 4 + a few levels of the sum) and lp's own rounding; scale log2(e) is good to 2^-24 of itself and the
+    # smallest number
+    tol = E * (64 + 40 + 2 * want.abs()) + 20 * 1.5e-45 / scale
+    assert ((lp.double() - want).abs() <= tol).all(), (lp, want)

@@ -396,6 +396,8 @@ et_status et_update_masked(et_stack* s, const uint8_t* mask, int32_t n_tensors, 
  *     norm = sqrt( sum over selected k of sum_i grads[k]_i^2 ),   factor = max_norm / norm where norm > max_norm, else 1
  * (squares and sums in 64 bits, in an order that does not depend on scheduling).  With a norm that is not finite the factor is 0.
  *   norm_dev  device float[2]: norm, factor (the clipping calls take NULL).  Nothing selected: 0, 1.
+ *             Both are rounded to fp32 there: a norm beyond it is reported as infinity, a factor below it as its smallest number;
+ *             the calls use the 64-bit values
  * et_grad_norm reports the norm alone (its factor is 1, or 0 for a norm that is not finite).
  * et_clip_grads writes clipped[k] = factor * grads[k] for selected k; clipped[k] may be grads[k] itself (then nothing is
  * written where the factor is 1), else it must not overlap any gradient.  A factor of 0 writes zeros.

@@ -98,9 +98,15 @@ sumsq_kernel(const __grid_constant__ ClipTable<N> tab, double* __restrict__ part
   if (threadIdx.x == 0) parts[blockIdx.x] = acc;
 }
 
-// Every block sums the partials itself, in the same order: (norm, factor).  A norm that is not finite gives factor 0.
-__device__ __forceinline__ float2 norm_and_factor(const double* __restrict__ parts, int n, float max_norm) {
-  __shared__ float2 sh;
+// Every block sums the partials itself, in the same order.  A clipped gradient is g * pre * factor: pre is 1, but 2^-126 where
+// the factor itself is below fp32's normal numbers (a norm of 1e35 clipped to 1e-4; its product with a gradient is an ordinary number
+// all the same).  A norm that is not finite gives finite = 0 and factor 0.
+struct ClipFactor {
+  float norm, factor, pre, reported;
+  int finite;
+};
+__device__ __forceinline__ ClipFactor norm_and_factor(const double* __restrict__ parts, int n, float max_norm) {
+  __shared__ ClipFactor sh;
   double s = 0.0;
   for (int i = threadIdx.x; i < n; i += blockDim.x) s += parts[i];
   s = block_sum64(s);
@@ -108,7 +114,12 @@ __device__ __forceinline__ float2 norm_and_factor(const double* __restrict__ par
     const double norm = sqrt(s);
     const bool finite = norm <= 1.7976931348623157e308;     // false for NaN too
     const double f = !finite ? 0.0 : norm > (double)max_norm ? (double)max_norm / norm : 1.0;
-    sh = make_float2((float)norm, (float)f);
+    const bool small = finite && f < 0x1p-126;
+    sh.norm = (float)norm;
+    sh.factor = (float)(small ? f * 0x1p126 : f);
+    sh.pre = small ? 0x1p-126f : 1.0f;
+    sh.reported = finite ? fmaxf((float)f, 0x1p-149f) : 0.0f;            // 0 says that the norm was not finite
+    sh.finite = finite;
   }
   __syncthreads();
   return sh;
@@ -116,8 +127,8 @@ __device__ __forceinline__ float2 norm_and_factor(const double* __restrict__ par
 static __global__ void __launch_bounds__(kClipThreads)
 norm_finalize_kernel(const double* __restrict__ parts, int n, float max_norm, float* __restrict__ out) {
   chain_begin();
-  const float2 nf = norm_and_factor(parts, n, max_norm);
-  if (threadIdx.x == 0) { out[0] = nf.x; out[1] = nf.y; }
+  const ClipFactor c = norm_and_factor(parts, n, max_norm);
+  if (threadIdx.x == 0) { out[0] = c.norm; out[1] = c.reported; }
 }
 
 template <int N>
@@ -125,9 +136,9 @@ __global__ void __launch_bounds__(kClipThreads)
 clip_kernel(const __grid_constant__ ClipTable<N> tab, const double* __restrict__ parts, int n_parts, float max_norm,
             float* __restrict__ norm_out) {
   chain_begin();
-  const float2 nf = norm_and_factor(parts, n_parts, max_norm);
-  const float f = nf.y;
-  if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = nf.x; norm_out[1] = f; }
+  const ClipFactor c = norm_and_factor(parts, n_parts, max_norm);
+  const float f = c.factor, pre = c.pre;
+  if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = c.norm; norm_out[1] = c.reported; }
   for (long long vb = tab.blocks - 1 - blockIdx.x; vb >= 0; vb -= gridDim.x) {   // backwards: the end is still in L2
     const ClipEntry& e = tab.e[clip_find(tab, vb)];
     if (f == 1.0f && e.out == e.g) continue;                // in place and nothing to clip: nothing changes
@@ -139,13 +150,13 @@ clip_kernel(const __grid_constant__ ClipTable<N> tab, const double* __restrict__
       const size_t i = i0 + ((size_t)q * kClipThreads + threadIdx.x) * 4;
       const long long l = (long long)e.count - (long long)i;
       left[q] = l < 0 ? 0 : (int)min(l, 4ll);
-      if (f != 0.0f) clip_load(e.g + i, left[q], true, v[q]);
+      if (c.finite) clip_load(e.g + i, left[q], true, v[q]);
     }
 #pragma unroll
     for (int q = 0; q < kClipVec / 4; ++q) {
       const size_t i = i0 + ((size_t)q * kClipThreads + threadIdx.x) * 4;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[q][j] = f != 0.0f ? v[q][j] * f : 0.0f;
+      for (int j = 0; j < 4; ++j) v[q][j] = c.finite ? v[q][j] * pre * f : 0.0f;
       if (left[q] == 4 && (reinterpret_cast<uintptr_t>(e.out + i) & 15) == 0)
         __stcs(reinterpret_cast<float4*>(e.out + i), make_float4(v[q][0], v[q][1], v[q][2], v[q][3]));
       else
@@ -161,10 +172,10 @@ __global__ void __launch_bounds__(kClipThreads)
 update_clipped_kernel(const __grid_constant__ ClipTable<N> tab, const double* __restrict__ parts, int n_parts, float max_norm,
                       float* __restrict__ norm_out, const OptParams opt) {
   chain_begin();
-  const float2 nf = norm_and_factor(parts, n_parts, max_norm);
-  const float f = nf.y;
-  if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = nf.x; norm_out[1] = f; }
-  if (f == 0.0f) return;
+  const ClipFactor c = norm_and_factor(parts, n_parts, max_norm);
+  const float f = c.factor, pre = c.pre;
+  if (norm_out != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { norm_out[0] = c.norm; norm_out[1] = c.reported; }
+  if (!c.finite) return;
   for (long long vb = tab.blocks - 1 - blockIdx.x; vb >= 0; vb -= gridDim.x) {   // backwards: the end is still in L2
     const ClipEntry& e = tab.e[clip_find(tab, vb)];
 #pragma unroll
@@ -177,7 +188,7 @@ update_clipped_kernel(const __grid_constant__ ClipTable<N> tab, const double* __
       if (e.master != nullptr) load_seg<8>(e.master + i0, n, w);
       else load_seg<8>((const T*)e.W + i0, n, w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] *= f;
+      for (int i = 0; i < 8; ++i) g[i] = g[i] * pre * f;
       opt_update_seg(w, g, opt, e.m_state, e.v_state, i0, n);
       if (e.master != nullptr) store_seg<8>(e.master + i0, n, w);
       store_seg<8>((T*)e.W + i0, n, w);

@@ -230,3 +230,32 @@ def test_logit_scales_near_the_end_of_fp32(scale):
     # smallest number
     tol = E * (64 + 40 + 2 * want.abs()) + 20 * 1.5e-45 / scale
     assert ((lp.double() - want).abs() <= tol).all(), (lp, want)
+
+
+@pytest.mark.parametrize("value,max_norm", [(1e30, 1e-9), (1e35, 1e-4), (3e38, 1e-3), (3e38, 1e-8), (1e38, 1e-38), (1e-38, 1e-44)])
+def test_factors_below_fp32(value, max_norm):
+    """max_norm / norm below fp32's normal numbers (and below all of them): the clipped gradients are ordinary numbers."""
+    d = 64
+    s = et.et_stack_create([(d, d, 0, 1, -1)], 8, F)
+    W, b = torch.zeros(d, d, device=DEV), torch.zeros(d, device=DEV)
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, [W], [b], ws)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(4)
+    g = [torch.rand(d, d, generator=gen, device=DEV) * value, torch.rand(d, generator=gen, device=DEV) * value]
+    out, norm = [torch.full_like(x, float("nan")) for x in g], torch.empty(2, device=DEV)
+    n = math.sqrt(sum(float((x.double() ** 2).sum()) for x in g))
+    mx = float(np.float32(max_norm))
+    et.et_clip_grads(s, [1, 1], g, out, mx, norm)
+    assert (float(norm[0]) == INF) if n > 3.41e38 else abs(float(norm[0]) - n) <= 2 * E * n
+    assert float(norm[1]) > 0 and abs(float(norm[1]) - mx / n) <= E * mx / n + 1.5e-45
+    for x, o in zip(g, out):
+        want = x.double() * (mx / n)                     # the factor and two products round; results below 2^-126 to the step there
+        assert ((o.double() - want).abs() <= 4 * E * want + 2.9e-45).all()
+    et.et_update_clipped(s, [1, 1], g, -1.0, mx)         # W <- W + clipped
+    assert torch.equal(W, out[0]) and torch.equal(b, out[1])
+    # Adam's state moves too: a finite norm is a step
+    st = [[torch.ones_like(W), torch.ones_like(b)], [torch.ones_like(W), torch.ones_like(b)]]
+    et.et_stack_set_optimizer(s, et.ET_OPT_ADAM, st[0], st[1])
+    et.et_update_clipped(s, [1, 1], g, 0.0, mx)
+    assert all((x != 1).all() for x in st[0] + st[1])

@@ -447,7 +447,10 @@ et_status et_bias_grad_noalloc(const void* dZ, int64_t M, int32_t width, et_dtyp
  * and fills per-TENSOR cost vectors of length 2L following Section 5.1: kernel tensor:
  * t_dw = weight-gradient time, t_dy = error-gradient time (with the fused backward of the
  * non-trainable work below it, Section 5.3); bias tensor: t_dw = bias-gradient time,
- * t_dy = 0.  An embedding layer's gradient goes to t_dw of its table.  A normalisation layer is one black box (Section 5.2): the time of its whole
+ * t_dy = 0.  An embedding layer's gradient goes to t_dw of its table, as an exported gradient: every row of the table is
+ * written (of a table beyond 256 MB of gradient, over and over into a scratch of that size).  That is what a step with exported
+ * gradients pays, and nearest to one whose optimiser moves every row; plain SGD in the backward call touches named rows only and
+ * pays less.  A normalisation layer is one black box (Section 5.2): the time of its whole
  * backward kernel (error gradient and d gamma together) plus its two finishing kernels goes
  * to t_dy of beta; t_dw of gamma and beta and t_dy of gamma are 0.  An attention layer is a
  * non-trainable layer (Section 5.3): its backward time is added to t_dy of the bias of the layer below.

@@ -107,6 +107,7 @@ struct EmbSink {
   float* v_state;
   OptParams opt;
   int do_sgd, delta_is_snapshot;
+  size_t wrap;               // not 0: `grad` is a scratch of so many elements (whole rows), written over and over (et_profile_costs)
 };
 template <typename T>
 __device__ __forceinline__ void emb_sgd(const EmbSink<T>& k, size_t i0, float (&w)[kVec], const float (&g)[kVec]) {
@@ -123,7 +124,8 @@ __device__ __noinline__ float emb_finish_call(const EmbSink<T>& k, size_t i0, in
   float g[kVec];
 #pragma unroll
   for (int i = 0; i < kVec; ++i) g[i] = e.v[i];
-  return consume_grad<T>(i0, n, g, k.grad, k.delta, k.W, k.opt, k.do_sgd, k.delta_is_snapshot, k.master, k.m_state, k.v_state);
+  float* grad = k.wrap == 0 ? k.grad : k.grad + (i0 % k.wrap) - i0;
+  return consume_grad<T>(i0, n, g, grad, k.delta, k.W, k.opt, k.do_sgd, k.delta_is_snapshot, k.master, k.m_state, k.v_state);
 }
 // Ways a finished row is consumed.  Export: it is written and nothing else is wanted.  Sgd, SgdMaster: w <- w - lr g and nothing else,
 // on the table or on its fp32 master.  General: all the rest, and ragged widths.
@@ -173,7 +175,9 @@ __device__ __forceinline__ void embed_fill(const EmbFill<T>& f, int block, int b
     const int v = f.v0 + (int)(u / segs), c0 = (int)(u % segs) * kFillCols, c1 = min(f.d, c0 + kFillCols);
     if ((f.named[v >> 5] >> (v & 31)) & 1u) continue;
     if (zeros) {                                            // a gradient that is exported and not applied
-      float4* g = reinterpret_cast<float4*>(f.sink.grad + (size_t)v * f.d);
+      size_t at = (size_t)v * f.d;
+      if (f.sink.wrap != 0) at %= f.sink.wrap;
+      float4* g = reinterpret_cast<float4*>(f.sink.grad + at);
       for (int c = c0 / 4 + lane; c < c1 / 4; c += 32) __stcs(g + c, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
     } else {
       for (int c = c0 + lane * kVec; c < c1; c += 32 * kVec) {

@@ -373,6 +373,11 @@ EmbPlan emb_plan(long long rows, int vocab, int d) {
   p.join_tiles = ceil_div(d, et::kJoinCols);
   return p;
 }
+// Rows of a table that et_profile_costs has room to write a gradient to: all of a table up to 256 MB, else as many as that takes (twice
+// what L2 holds, so that writing them over and over goes to DRAM like the whole).
+inline size_t emb_scratch_rows(int vocab, int d) {
+  return std::min<size_t>(vocab, std::max<size_t>(1, ((size_t)256 << 20) / ((size_t)d * sizeof(float))));
+}
 constexpr int kClipTensors = 256;          // tensors named by one launch's table
 inline int clip_launches(int n_tensors) { return ceil_div(n_tensors, kClipTensors); }
 
@@ -950,7 +955,7 @@ et_status run_embed_forward(et_stack* s, void* y, cudaStream_t st) {
 // The gradient of the table from G_1 (the caller's dY where the embedding is the only layer).
 template <typename T>
 et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* delta, bool sgd, float lr, int* launches,
-                             cudaStream_t st) {
+                             cudaStream_t st, size_t wrap = 0) {
   const LayerRT& L = s->ly[0];
   const EmbPlan p = emb_plan(s->M, L.K, L.N);
   const int n = (int)s->M;
@@ -958,6 +963,7 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
   et::EmbSink<T> sink;
   sink.grad = grad; sink.delta = delta; sink.W = (T*)L.W; sink.master = L.W32; sink.m_state = L.st1[0]; sink.v_state = L.st2[0];
   sink.opt = opt_params(s, lr); sink.do_sgd = sgd ? 1 : 0; sink.delta_is_snapshot = s->delta_is_snapshot ? 1 : 0;
+  sink.wrap = wrap;
   // rows that no token names have a gradient of 0 to export, or an optimiser step to take
   const bool fills = grad != nullptr || (sgd && sink.opt.kind != et::kOptSgd);
   uint32_t* named = fills ? (uint32_t*)s->at(L.off_named) : nullptr;
@@ -1002,7 +1008,7 @@ et_status run_embed_backward(et_stack* s, const void* dY, float* grad, const T* 
   if (imp != nullptr && used < L.imp_count_w) CU_TRY(cudaMemsetAsync(imp + used, 0, sizeof(float) * (L.imp_count_w - used), st));
   float* part = (float*)s->at(L.off_epart);
   const bool whole = L.N % et::kVec == 0;                    // rows are whole vectors
-  const bool plain_export = grad != nullptr && delta == nullptr && !sgd && ((uintptr_t)grad & 15) == 0;
+  const bool plain_export = grad != nullptr && wrap == 0 && delta == nullptr && !sgd && ((uintptr_t)grad & 15) == 0;
   const bool plain_sgd = sgd && sink.opt.kind == et::kOptSgd && delta == nullptr && grad == nullptr;
   {
     TimedLaunch tl(s, ET_K_WGRAD, st);
@@ -1874,6 +1880,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       y.off_hist = take((((size_t)p.tiles * p.passes) << p.bits) * sizeof(uint32_t));
       y.off_named = take((size_t)ceil_div(y.K, 32) * sizeof(uint32_t));
       y.off_epart = take((size_t)p.chunks * 2 * y.N * sizeof(float));
+      max_partial = std::max(max_partial, emb_scratch_rows(y.K, y.N) * y.N * sizeof(float));
     } else if (dtype == ET_BF16) {
       const int kb_n = ceil_div(y.Nw, et::tc::BK) * y.fold;
       const TilePlan f = choose_tiles((int)M, y.Nw, ceil_div(y.K, et::tc::BK) * y.fold, s->sms, false, false, 0);
@@ -2715,12 +2722,14 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
         ~AddCarried() { *slot += v; }
       } add_carried{&t_dy[2 * l + (s->ly[l].has_tensor(1) ? 1 : 0)], carried};
       if (s->ly[l].kind == ET_LAYER_EMBEDDING) {
-        // nothing lies below it: all of its backward time is the gradient of the table
+        // nothing lies below it: all of its backward time is the gradient of the table, every row of it written
         t_dw[2 * l + 1] = 0.0;
+        const LayerRT& y = s->ly[l];
+        const size_t rows = emb_scratch_rows(y.K, y.N), wrap = rows < (size_t)y.K ? rows * y.N : 0;
         if (s->dtype == ET_BF16)
-          ET_TRY(timed([&]() { return run_embed_backward<bf16>(s, dY, nullptr, nullptr, false, 0.f, &dummy, st); }, &t_dw[2 * l]));
+          ET_TRY(timed([&]() { return run_embed_backward<bf16>(s, dY, scratch_grad, nullptr, false, 0.f, &dummy, st, wrap); }, &t_dw[2 * l]));
         else
-          ET_TRY(timed([&]() { return run_embed_backward<float>(s, dY, nullptr, nullptr, false, 0.f, &dummy, st); }, &t_dw[2 * l]));
+          ET_TRY(timed([&]() { return run_embed_backward<float>(s, dY, scratch_grad, nullptr, false, 0.f, &dummy, st, wrap); }, &t_dw[2 * l]));
         continue;
       }
       if (s->ly[l].kind == ET_LAYER_BATCHNORM) {

@@ -259,3 +259,28 @@ def test_factors_below_fp32(value, max_norm):
     et.et_stack_set_optimizer(s, et.ET_OPT_ADAM, st[0], st[1])
     et.et_update_clipped(s, [1, 1], g, 0.0, mx)
     assert all((x != 1).all() for x in st[0] + st[1])
+
+
+@pytest.mark.parametrize("dtype,d", [(F, 512), (B, 512), (F, 510)])
+def test_cost_of_a_table_counts_every_row(dtype, d):
+    """The profiled time of a table's gradient is that of writing all of it, tables beyond the scratch included; nothing else changes."""
+    M, tdt = 64, torch.bfloat16 if dtype == B else torch.float32
+    for V in (1000, 100000, 400000):
+        et.et_debug_guard_regions(True)
+        s = et.et_stack_create([(V, d, 0, 1, -1, et.ET_LAYER_EMBEDDING)], M, dtype)
+        et.et_debug_guard_regions(False)
+        T = torch.full((V, d), 0.5, dtype=tdt, device=DEV)
+        ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+        et.et_stack_bind(s, [T], [None], ws)
+        x = torch.arange(M, device=DEV, dtype=torch.int32) * 7 % V
+        y, dY = torch.empty(M, d, dtype=tdt, device=DEV), torch.ones(M, d, dtype=tdt, device=DEV)
+        t_dw, t_dy, _ = et.et_profile_costs(s, x, y, dY, 5)
+        # the device's memory takes 8 TB/s at the most; what stays in L2 (126 MB) need not have reached it yet
+        assert t_dw[0] * 1e-3 >= (V * d * 4 - 140e6) / 8e12 and t_dw[1] == 0 and t_dy[0] == 0 and t_dy[1] == 0
+        st, bad = et.et_debug_check_guards(s)
+        assert st == et.ET_OK, bad
+        assert (T == 0.5).all() and (y == 0.5).all()
+        grad = torch.full((V, d), float("nan"), device=DEV)
+        et.et_backward_elastic(s, dY, [1, 0], [grad, None])
+        want = torch.zeros(V, device=DEV).index_add_(0, x.long(), torch.ones(M, device=DEV))
+        assert torch.equal(grad, want[:, None].expand(V, d))

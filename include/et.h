@@ -453,7 +453,8 @@ et_status et_bias_grad_noalloc(const void* dZ, int64_t M, int32_t width, et_dtyp
  * pays less.  A normalisation layer is one black box (Section 5.2): the time of its whole
  * backward kernel (error gradient and d gamma together) plus its two finishing kernels goes
  * to t_dy of beta; t_dw of gamma and beta and t_dy of gamma are 0.  An attention layer is a
- * non-trainable layer (Section 5.3): its backward time is added to t_dy of the bias of the layer below.
+ * non-trainable layer (Section 5.3): its backward time is added to t_dy of the bias of the layer below (an embedding: to that of
+ * the tensor it does not have, which a selection of its table is charged with).
  * t_fwd receives the forward time.  Milliseconds.  Synchronous.  Runs a forward
  * pass from x (writing y) and a full backward from dY first; weights are not changed. */
 et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, int32_t iters,

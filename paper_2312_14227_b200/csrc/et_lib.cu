@@ -2720,7 +2720,7 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
       struct AddCarried {
         double* slot; double v;
         ~AddCarried() { *slot += v; }
-      } add_carried{&t_dy[2 * l + (s->ly[l].has_tensor(1) ? 1 : 0)], carried};
+      } add_carried{&t_dy[2 * l + 1], carried};              // an embedding has no tensor there: its table pays for what lies above
       if (s->ly[l].kind == ET_LAYER_EMBEDDING) {
         // nothing lies below it: all of its backward time is the gradient of the table, every row of it written
         t_dw[2 * l + 1] = 0.0;

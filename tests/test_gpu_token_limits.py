@@ -284,3 +284,68 @@ def test_cost_of_a_table_counts_every_row(dtype, d):
         et.et_backward_elastic(s, dY, [1, 0], [grad, None])
         want = torch.zeros(V, device=DEV).index_add_(0, x.long(), torch.ones(M, device=DEV))
         assert torch.equal(grad, want[:, None].expand(V, d))
+
+
+def _above_a_table(kind):
+    import workloads as wl
+    if kind == "attention":
+        return B, 120, [wl.embedding_layer(50, 384, 2.0), wl.attention_layer(128, 2, 40), wl.Layer(128, 72)]
+    if kind == "gather":                                 # the gathered matrix is formed
+        return F, 60, [wl.embedding_layer(50, 8, 2.0)] + wl.conv_layers(8, 24, 5, 6) + [wl.Layer(24, 16)]
+    if kind == "convolution":                            # the convolution's GEMMs fetch the patches themselves
+        return B, 144, [wl.embedding_layer(50, 128, 2.0)] + wl.conv_layers(128, 64, 6, 12) + [wl.Layer(64, 72)]
+    return B, 150, [wl.embedding_layer(50, 64, 2.0), wl.batchnorm_layer(64, act=wl.ACT_RELU), wl.Layer(64, 72)]
+
+
+@pytest.mark.parametrize("kind", ["attention", "gather", "convolution", "batchnorm"])
+def test_layers_without_tensors_directly_above_a_table(kind):
+    """The table's gradient through them; and their backward time is charged to a selection of the table."""
+    import workloads as wl
+    from oracle import elastic_oracle as orc
+    dtype, M, layers = _above_a_table(kind)
+    tdt = torch.bfloat16 if dtype == B else torch.float32
+    rng, L = np.random.default_rng(6), len(layers)
+    W, b = [], []
+    for ly in layers:
+        k = ly.kind
+        if k in (wl.KIND_ATTENTION, wl.KIND_IM2COL):
+            w_, b_ = np.zeros(0), np.zeros(0)
+        elif k == wl.KIND_EMBEDDING:
+            w_, b_ = rng.normal(size=(ly.in_features, ly.out_features)) * 0.4, np.zeros(0)
+        elif k == wl.KIND_BATCHNORM:
+            w_, b_ = 1 + 0.1 * rng.normal(size=ly.out_features), 0.3 * rng.normal(size=ly.out_features)
+        else:
+            w_, b_ = rng.normal(size=(ly.in_features, ly.out_features)) / np.sqrt(ly.in_features), 0.1 * rng.normal(size=ly.out_features)
+        W.append(torch.from_numpy(w_).to(tdt).to(DEV))
+        b.append(torch.from_numpy(b_).to(tdt).to(DEV))
+    s = et.et_stack_create(layers, M, dtype)
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, W, b, ws)
+    et.et_stack_set_embedding_scale(s, 2.0)
+    ids = rng.integers(0, 50, M).astype(np.int32)
+    x = torch.from_numpy(ids).to(DEV)
+    y = torch.empty(M, layers[-1].out_width, dtype=tdt, device=DEV)
+    dY = torch.from_numpy(rng.normal(size=y.shape)).to(tdt).to(DEV)
+    et.et_forward_stack(s, x, y)
+    mask = np.zeros(2 * L, dtype=np.uint8)
+    mask[0] = mask[-1] = 1
+    grads = [None] * (2 * L)
+    grads[0], grads[-1] = torch.full(W[0].shape, float("nan"), device=DEV), torch.full(b[-1].shape, float("nan"), device=DEV)
+    et.et_backward_elastic(s, dY, mask, grads)
+    torch.cuda.synchronize()
+    assert et.et_device_status(s) == et.ET_OK
+    host = lambda ts: [t.double().cpu().numpy() for t in ts]  # noqa: E731
+    saved = orc.forward(layers, host(W), host(b), ids)
+    want, _ = orc.backward_masked(layers, host(W), saved, dY.double().cpu().numpy(), mask)
+    rel = lambda a, o: np.abs(a.double().cpu().numpy() - o).max() / np.abs(o).max()  # noqa: E731
+    tol = 3e-2 if dtype == B else 1e-4                   # the bars of the other whole-stack tests
+    assert rel(y, saved.a[-1]) <= tol and rel(grads[0], want[0]) <= tol and rel(grads[-1], want[2 * L - 1]) <= tol
+    t_dw, t_dy, _ = et.et_profile_costs(s, x, y, dY, 3)
+    assert t_dw[0] > 0 and t_dy[0] == 0 and t_dw[1] == 0
+    if kind in ("attention", "gather"):
+        only = np.zeros(2 * L, dtype=np.uint8)
+        only[0] = 1
+        assert t_dy[1] > 0                               # charged: a strict selection pays t_dy of everything above its deepest tensor
+        assert et.et_time_selective(only, t_dw, t_dy) >= t_dw[0] + t_dy[1]
+    else:
+        assert t_dy[1] == 0

@@ -2590,6 +2590,13 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   if (cfg->label_smoothing > 0.f && cfg->kind != ET_PREF_SIGMOID) return ET_ERR_UNSUPPORTED;
   if (dY == nullptr && seq_logp == nullptr && loss_dev == nullptr) return ET_ERR_INVALID_ARG;
   if (s != nullptr && pairs > s->M) return ET_ERR_TOO_LARGE;
+  int grad_slices = 0;                                       // blocks that share a row's gradient
+  if (s != nullptr) {
+    const int vec_elems = s->dtype == ET_BF16 ? 8 : 4;
+    const int vecs = ceil_div(s->out_width(), vec_elems) + (s->out_width() % vec_elems != 0 ? 1 : 0);
+    grad_slices = ceil_div(vecs, et::tok::kGradThreads * et::tok::kGradVecs);
+    if (dY != nullptr && (long long)s->M * grad_slices > 0x7fffffffll) return ET_ERR_TOO_LARGE;
+  }
   et::tok::Args a{};
   ET_TRY(check_tokens(s, y, targets, cfg->vocab, cfg->logit_scale, dY, &a.vocab));
   cudaStream_t st = (cudaStream_t)stream;
@@ -2611,14 +2618,10 @@ et_status et_loss_preference_grad(et_stack* s, const void* y, const int32_t* tar
   }
   if (dY == nullptr) return ET_OK;
   a.dY = dY;
-  const int vec_elems = s->dtype == ET_BF16 ? 8 : 4;
-  const int vecs = ceil_div(a.width, vec_elems) + (a.width % vec_elems != 0 ? 1 : 0);
-  a.slices = ceil_div(vecs, et::tok::kGradThreads * et::tok::kGradVecs);
+  a.slices = grad_slices;
   a.per = et::tok::kGradThreads * et::tok::kGradVecs;
-  const long long blocks = (long long)a.rows * a.slices;
-  if (blocks > 0x7fffffffll) return ET_ERR_TOO_LARGE;
   TimedLaunch tl(s, ET_K_OTHER, st);
-  return launch_chained(s->dtype == ET_BF16 ? et::tok::token_grad_kernel<bf16> : et::tok::token_grad_kernel<float>, (unsigned)blocks,
+  return launch_chained(s->dtype == ET_BF16 ? et::tok::token_grad_kernel<bf16> : et::tok::token_grad_kernel<float>, (unsigned)(s->M * grad_slices),
                         et::tok::kGradThreads, st, a);
 }
 

@@ -154,3 +154,11 @@ def test_helper_module_knows_nothing_but_device_tensors():
     for args in (([t], "x", need(4), 0), ([t], b"\0"), (7, b"\0", need(4), 0), ([t], b"\0", need(4), None)):
         with pytest.raises(TypeError):
             h.addresses(*args)
+
+
+def test_preference_loss_refuses_before_it_launches():
+    """More blocks than a grid holds: refused with the other arguments (on a stack that is not bound: before that is looked at)."""
+    s = et.et_stack_create([(8, 1 << 22, 0, 1, -1)], 65535 * 128, et.ET_BF16)
+    p = 1 << 20                                          # an address: refused before it is used
+    assert _short(et.et_loss_preference_grad, s, p, p, p, p, pairs=2) == et.ET_ERR_TOO_LARGE
+    assert _short(et.et_loss_preference_grad, s, p, p, p, None, loss_dev=p, pairs=2) == et.ET_ERR_STATE

@@ -349,3 +349,68 @@ def test_layers_without_tensors_directly_above_a_table(kind):
         assert et.et_time_selective(only, t_dw, t_dy) >= t_dw[0] + t_dy[1]
     else:
         assert t_dy[1] == 0
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("loss", ["policy", "preference"])
+def test_whole_step_captured_and_replayed(dtype, loss):
+    """Lookup, layers, token loss, masked backward and clipped update in one graph: the eager steps, bit for bit, on new ids each time."""
+    import workloads as wl
+    M, V, OUT = 600, 300, 264
+    layers = [wl.embedding_layer(V, 128, 0.5), wl.Layer(128, 256, act=wl.ACT_GELU_TANH), wl.Layer(256, 128, residual_src=1), wl.Layer(128, OUT)]
+    tdt = torch.bfloat16 if dtype == B else torch.float32
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(8)
+    W0 = [torch.randn(V if ly.kind == wl.KIND_EMBEDDING else ly.in_features, ly.out_features, generator=gen, device=DEV) / math.sqrt(ly.in_features)
+          for ly in layers]
+    b0 = [torch.zeros(0 if ly.kind == wl.KIND_EMBEDDING else ly.out_features, device=DEV) for ly in layers]
+    batches = [torch.randint(-1, V + 1, (M,), generator=gen, device=DEV, dtype=torch.int32) for _ in range(4)]
+    t = torch.randint(0, OUT, (M,), generator=gen, device=DEV, dtype=torch.int32)
+    adv, begin = torch.randn(M, generator=gen, device=DEV), _dev([0, 100, 250, 400, 590], torch.int32)
+    mask = np.array([1, 0, 1, 1, 0, 1, 1, 1], dtype=np.uint8)
+    results = []
+    for captured in (False, True):
+        s = et.et_stack_create(layers, M, dtype)
+        W, b = [w.clone().to(tdt) for w in W0], [v.clone().to(tdt) for v in b0]
+        ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+        et.et_stack_bind(s, W, b, ws)
+        et.et_stack_set_embedding_scale(s, 0.5)
+        params = [p for pair in zip(W, b) for p in pair]
+        st = [[torch.zeros(p.shape, device=DEV) for p in params] for _ in range(2)]
+        et.et_stack_set_optimizer(s, et.ET_OPT_ADAM, st[0], st[1])
+        et.et_stack_set_optimizer_step(s, 1)
+        x, y = batches[0].clone(), torch.empty(M, OUT, dtype=tdt, device=DEV)
+        dY, stats, norm = torch.empty_like(y), torch.zeros(4, device=DEV), torch.zeros(2, device=DEV)
+        grads = [torch.zeros(p.shape, device=DEV) if m else None for p, m in zip(params, mask)]
+
+        def step(stream):
+            et.et_forward_stack(s, x, y, stream=stream)
+            if loss == "policy":
+                et.et_loss_policy_grad(s, y, t, adv, dY, loss_dev=stats, stream=stream)
+            else:
+                et.et_loss_preference_grad(s, y, t, begin, dY, loss_dev=stats, stream=stream)
+            et.et_backward_elastic(s, dY, mask, grads, stream=stream)
+            et.et_update_clipped(s, mask, grads, 0.01, 1e-3, norm, stream=stream)
+
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        seen, graph = [], None
+        for i, ids in enumerate(batches):
+            torch.cuda.synchronize()
+            x.copy_(ids)
+            torch.cuda.synchronize()
+            if i == 0 or not captured:
+                step(side)
+            else:
+                if graph is None:
+                    graph = torch.cuda.CUDAGraph()
+                    with torch.cuda.graph(graph, stream=side):
+                        step(side)
+                graph.replay()
+            torch.cuda.synchronize()
+            seen += [stats.clone(), norm.clone(), y.clone()]
+        assert et.et_device_status(s) == et.ET_OK
+        results.append(seen + [p.clone() for p in params] + [v for ts in st for v in ts])
+        del graph
+    assert all(torch.equal(a, c) for a, c in zip(*results))
+    assert not torch.equal(results[0][2], results[0][5])             # the batches differ

@@ -27,7 +27,9 @@
  *   and head  P = softmax(q k^T / 8),  a_{l+1} = [P v] with the heads side by side.  It has no
  *   trainable tensors: its W and b pointers may be NULL, its two mask bits must be 0 and its two
  *   slots in gradient / importance / state arrays are ignored.  Its backward (above the deepest
- *   selected layer only) recomputes P from the saved per-row log-sum-exp.
+ *   selected layer only) recomputes P from the saved per-row log-sum-exp.  Every row of a sequence sees all of it (there
+ *   is no causal mask): a stack from token ids to logits that uses it is not an autoregressive model, and the token losses
+ *   below are for stacks without it or above features that are causal already.
  *
  *   A layer of kind ET_LAYER_BATCHNORM is a batch normalisation in training mode, the layer Section 5.2
  *   is written about: like ET_LAYER_NORM with the mean and the biased variance of each feature taken
@@ -269,7 +271,7 @@ et_status et_loss_mse_grad(et_stack* s, const void* y, const void* target, void*
  *            not read (it may hold anything), its gradient is 0, its log probability is reported as 0
  *   weights  device float[M], or NULL (see the call)
  *   dY       device, shape and type of y: d loss / d y.  May be y itself (the logits are overwritten), otherwise it must not
- *            overlap it; NULL: no gradient is formed
+ *            overlap it; NULL: no gradient is formed.  Nothing else that a call writes may overlap what it reads
  * Logits of -inf (or the type's lowest value) are tokens of probability 0; a row without a finite logit, with one of
  * +inf or with a NaN gives NaN.  Reported numbers are added up in 64 bits and a fixed order.  They use rows of the workspace:
  * two of these calls on one stack must not overlap.  Asynchronous on `stream`. */

@@ -42,12 +42,16 @@ def build_operands(force: bool = False, verbose: bool = False):
     cmd = [os.environ.get("CXX", "g++"), "-shared", "-fPIC", "-std=c++17", "-O2", "-o", OPERANDS, OPERANDS_SOURCE, "-I", python,
            "-I", os.path.join(torch, "include"), "-I", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
            "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        print("_operands was not built, the binding checks lists of tensors in Python:\n" + res.stdout + res.stderr, file=sys.stderr)
+    try:
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        failed, said = res.returncode != 0, res.stdout + res.stderr
+    except OSError as e:
+        failed, said = True, str(e)
+    if failed:
+        print("_operands was not built, the binding checks lists of tensors in Python:\n" + said, file=sys.stderr)
         return None
     if verbose:
-        print(res.stdout + res.stderr)
+        print(said)
     return OPERANDS
 
 

@@ -4,7 +4,10 @@
 // The rows are sorted by id (stable radix sort: rows of one id stay in order), the sorted positions are cut into
 // chunks of kEmbChunk, and a block adds up the rows of one chunk, id by id.  An id whose rows lie within one chunk is
 // finished there; an id that crosses chunk borders leaves one fp32 partial row per chunk, which a second kernel adds
-// in order.  Work per block is the same whatever the ids' frequencies, and the sums' order depends on the ids alone.
+// in order.  The sums' order depends on the ids alone.  Work per block of the gradient kernel is the same whatever the ids'
+// frequencies.  Not so in the second kernel: one block per 256 columns adds all partial rows of an id, a 32nd of its tokens, so an id
+// with half of the batch shows (plain SGD on a bf16 table of 65536 rows: 32768 tokens x 2048 columns 81 -> 96 us, 65536 x 1024
+// 81 -> 121 us, 262144 x 256 105 -> 284 us).
 #pragma once
 
 #include "kernels.cuh"
@@ -335,7 +338,9 @@ sort_hist_kernel(const int32_t* __restrict__ ids, int n, int vocab, int bits, ui
   }
 }
 // One pass: places every key of a tile where its digit begins for this tile plus its rank among the tile's keys of that digit, and
-// counts the next pass's digits by the tile they land in.  Blocks behind the last tile fill table rows that no token names (the
+// counts the next pass's digits by the tile they land in.  Every tile reads all tiles' counts, so a pass reads tiles^2 * bins words
+// from L2: nothing at 16 tiles, most of the time beyond a million ids (plain SGD on 64 columns: 65536 ids 44 us, 262144 83, 1 M
+// 259, 4 M 1821).  Blocks behind the last tile fill table rows that no token names (the
 // passes of few blocks would leave the GPU idle otherwise).
 template <typename T>
 __global__ void __launch_bounds__(kSortThreads)

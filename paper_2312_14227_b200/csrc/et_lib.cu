@@ -2518,9 +2518,9 @@ et_status launch_tokens_t(et_stack* s, et::tok::Args a, cudaStream_t st) {
   const int cols = a.dY != nullptr ? a.width : a.vocab;
   const int vecs = ceil_div(cols, N) + (a.width % N != 0 ? 1 : 0);
   // How a row is cut: one block, the smallest whose threads hold it in 8 vectors each, up to 512 threads; beyond that the fewest
-  // blocks of 256 threads (four of them fit an SM, so more rows are in flight: 131072 bf16 columns 692 us in 8 x 256 threads,
-  // 746 us in 4 x 512), else of 512.  Every thread takes the same number of rounds, as few as the slice needs: empty rounds cost
-  // as much as full ones.
+  // blocks of 256 threads (four of them fit an SM, so more rows are in flight: 131072 bf16 columns, side by side at full clocks,
+  // 692 us in 8 x 256 threads, 746 us in 4 x 512), else of 512.  Every thread takes the same number of rounds, as few as the
+  // slice needs: empty rounds cost as much as full ones.
   // Few rows leave SMs idle and a row's latency counts: two rounds a thread where 512 threads get by with that (200 rows of 4096
   // bf16 columns 11.2 -> 8.7 us a call).
   const int rounds = a.rows <= 2 * s->sms ? 2 : 8;

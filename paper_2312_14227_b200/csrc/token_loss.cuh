@@ -387,8 +387,9 @@ struct RowResult { float m, g, cs, hit; };       // hit: the target's gradient
 // For kPolicy the blocks are persistent and take long rows by ticket (rows that are left out cost less than others, so a fixed share
 // leaves SMs idle at the end: 100 against 93 us; short ones even out, and one counter would not serve them all); a row is known an
 // iteration ahead and its slice is asked into L2 by one instruction while the row before is worked on (without: 98 us).
-// Measured, of the copy bandwidth (6558 GB/s): 8192 rows of 131072 bf16 columns 701 us (86 %), 4096 rows of 32003, 15 % of them
-// left out, 95 us (78 %), the same in fp32 170 us (87 %).
+// Measured, of the copy bandwidth (6558 GB/s): 8192 rows of 131072 bf16 columns 718 us at full clocks (84 %) and 760 us in
+// seconds-long runs, whose clocks the power limit lowers (80 %); 4096 rows of 32003, 15 % of them left out, 95 us (78 %) and 98 us, the
+// same in fp32 174 us (85 %).
 constexpr int kTicketThreads = 128;
 template <typename T, int MODE, int THREADS, int NV>
 __global__ void __launch_bounds__(THREADS, THREADS < 64 ? 32 : (NV <= 4 ? 1536 : 1024) / THREADS)    // 40 or 64 registers a thread
@@ -542,8 +543,8 @@ token_held_kernel(const __grid_constant__ Args a) {
   if (MODE == kPolicy) policy_finish(a);
 }
 
-// One block per row of any length.  kScore: a stream over the logits (2048 rows of 50257 bf16 columns 39 us, 81 % of the copy
-// bandwidth; the exponential unit is 57 % busy).  kPolicy: rows too long to be held are read twice
+// One block per row of any length.  kScore: a stream over the logits (2048 rows of 50257 bf16 columns 40 us, 78 % of the copy
+// bandwidth, 42 us in seconds-long runs; the exponential unit is 57 % busy).  kPolicy: rows too long to be held are read twice
 // ((max, sum) first, the gradient from the second read, which finds much of the row in L2).
 constexpr int kRowThreads = 512;
 template <typename T, int MODE>

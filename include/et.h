@@ -82,7 +82,8 @@
  *   Arguments are validated on the host before anything is launched; a call that
  *   returns an error has enqueued nothing.  Calls are asynchronous on `stream`
  *   (a cudaStream_t passed as void*, NULL = default stream) unless stated otherwise.
- *   Calls on one stack must not overlap on the GPU (they share the workspace).
+ *   Calls on one stack must not overlap on the GPU (they share the workspace).  While a stack is bound its workspace is its
+ *   own: it holds counters that every call has to find as the call before left them.
  */
 #ifndef ET_H_
 #define ET_H_

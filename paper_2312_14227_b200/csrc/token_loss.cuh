@@ -441,7 +441,8 @@ token_held_kernel(const __grid_constant__ Args a) {
     }
     if (MODE == kPolicy) {
       if (TICKETS && rank == 0 && tid == 0) {         // the row after the next one
-        const int after = 2 * clusters + (int)atomicAdd(a.ticket, 1u);
+        // a counter that something else has written to must not lead out of the rows (they are left undone then)
+        const int after = (int)min(2u * (uint32_t)clusters + min(atomicAdd(a.ticket, 1u), (uint32_t)a.rows), (uint32_t)a.rows);
         if (C == 1) rows_after[b] = after;
         else for (int c = 0; c < C; ++c) st_cluster(&rows_after[b], c, after);
       }

@@ -414,3 +414,34 @@ def test_whole_step_captured_and_replayed(dtype, loss):
         del graph
     assert all(torch.equal(a, c) for a, c in zip(*results))
     assert not torch.equal(results[0][2], results[0][5])             # the batches differ
+
+
+@pytest.mark.parametrize("value", [0x7fffffff, 0x80000000, 0xfffffff0, 5000])
+def test_a_foreign_row_counter_leads_to_no_row_outside(value):
+    """The counter that hands out rows, overwritten by something else: no row outside the logits is read or written, and binding
+    again puts it right."""
+    M, width = 1000, 32008
+    s, tdt = _stack(M, width, B)
+    ws, W, b = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV), s._keep[0], s._keep[1]
+    et.et_stack_bind(s, W, b, ws)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(7)
+    room = torch.full((M + 4, width), 7.0, dtype=tdt, device=DEV)
+    dY = room[2:M + 2]
+    y = torch.randn(M, width, generator=g, device=DEV).to(tdt)
+    t, adv = torch.randint(0, width, (M,), generator=g, device=DEV, dtype=torch.int32), torch.ones(M, device=DEV)
+    want = torch.empty_like(y)
+    et.et_loss_policy_grad(s, y, t, adv, want)
+    torch.cuda.synchronize()
+    word = ws[33 * 4:34 * 4].view(torch.int32)           # the status region's word 33
+    assert int(word[0]) == 0
+    word.fill_(value - (1 << 32) if value >= 1 << 31 else value)
+    et.et_loss_policy_grad(s, y, t, adv, dY)
+    torch.cuda.synchronize()
+    assert (room[:2] == 7).all() and (room[-2:] == 7).all()
+    done = (dY == want).all(1) | (dY == 7.0).all(1)
+    assert done.all() and (dY[0] == want[0]).all()       # each row is right or was not come to
+    et.et_stack_bind(s, W, b, ws)
+    et.et_loss_policy_grad(s, y, t, adv, dY)
+    torch.cuda.synchronize()
+    assert torch.equal(dY, want)

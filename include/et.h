@@ -298,7 +298,9 @@ typedef struct {
  *   kl_coef = 0: kl_i is reported (it may be infinite) and is no part of the loss or the gradient.
  *   logp      device float[M] or NULL: lp_i
  *   loss_dev  device float[4] or NULL: the loss, its first part, sum w_i kl_i, sum of the w_i whose ratio is clipped
- * Where both arguments of the min are equal the first one's slope counts. */
+ * Where both arguments of the min are equal the first one's slope counts.  lp_i and the same number from et_token_logp agree to
+ * their last bits, not always in them (the order of a sum goes by the launch): where r_i = 1 is meant, as with clip_low =
+ * clip_high = 0 on the policy that sampled, logp_old is NULL. */
 et_status et_loss_policy_grad(et_stack* s, const void* y, const int32_t* targets, const float* weights, const float* advantages,
                               const float* logp_old, const float* logp_ref, const et_policy_config* cfg, void* dY,
                               float* logp, float* loss_dev, void* stream);

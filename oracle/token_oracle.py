@@ -52,7 +52,9 @@ def policy(y, targets, weights, adv, old, ref, vocab, scale, lo, hi, beta):
         kl, dkl = np.zeros_like(lp), np.zeros_like(lp)
     else:
         d = np.where(live, ref - lp, 0.0)
-        kl, dkl = np.where(d == np.inf, np.inf, np.exp(d) - 1 - np.where(d == np.inf, 0.0, d)), 1 - np.exp(d)
+        with np.errstate(over="ignore"):
+            grown = np.exp(d)
+        kl, dkl = np.where(d == np.inf, np.inf, grown - 1 - np.where(d == np.inf, 0.0, d)), 1 - grown
     slope = np.where(clipped, 0.0, -first)
     if beta:                                     # a divergence that is reported only may be infinite
         slope = slope + beta * dkl

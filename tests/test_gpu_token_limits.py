@@ -445,3 +445,41 @@ def test_a_foreign_row_counter_leads_to_no_row_outside(value):
     et.et_loss_policy_grad(s, y, t, adv, dY)
     torch.cuda.synchronize()
     assert torch.equal(dY, want)
+
+
+@pytest.mark.parametrize("opt", ["sgd", "adam"])
+def test_elastic_schedule_of_a_table_with_masters_and_clipping(opt):
+    """Token ids, fp32 masters of bf16 tensors, clipped updates and re-selection together: the stored tensors stay the rounded masters,
+    tensors that a step does not select stay as they are."""
+    import workloads as wl
+    from paper_2312_14227_b200.elastic_loop import ElasticLoop
+    M, V, D, OUT = 96, 61, 48, 72
+    layers = [wl.embedding_layer(V, D, 1.5), wl.Layer(D, 80, act=wl.ACT_GELU_TANH), wl.Layer(80, OUT)]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    W = [(torch.randn(ly.in_features, ly.out_features, generator=g, device=DEV) * 0.2).bfloat16() for ly in layers]
+    b = [torch.zeros(0 if ly.kind == wl.KIND_EMBEDDING else ly.out_features, dtype=torch.bfloat16, device=DEV) for ly in layers]
+    s = et.et_stack_create(layers, M, B)
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, W, b, ws)
+    et.et_stack_set_embedding_scale(s, 1.5)
+    params = [p for pair in zip(W, b) for p in pair]
+    st = [[torch.zeros(p.shape, device=DEV) for p in params] for _ in range(2)]
+    ids = torch.randint(0, V, (M,), generator=g, device=DEV, dtype=torch.int32)
+    t, adv = torch.randint(0, OUT, (M,), generator=g, device=DEV, dtype=torch.int32), torch.randn(M, generator=g, device=DEV)
+    loss = lambda y, dY, out, stream: et.et_loss_policy_grad(s, y, t, adv, dY, loss_dev=out, stream=stream)  # noqa: E731
+    loop = ElasticLoop(s, W, b, ids, None, lr=0.05, period=6, window=2, rho=0.4, t_dw=np.ones(6), t_dy=np.ones(6), master=True,
+                       loss=loss, max_norm=0.01)
+    if opt == "adam":
+        et.et_stack_set_optimizer(s, et.ET_OPT_ADAM, st[0], st[1])
+        et.et_stack_set_optimizer_step(s, 1)
+    first = [p.clone() for p in params]
+    out = loop.run(2)
+    assert out["masks"][0].tolist() == [1, 0, 1, 1, 1, 1] and len(out["importances"]) == 1
+    assert all(not torch.equal(p, q) for p, q, m in zip(params, first, out["masks"][0]) if m)
+    loop.mask = np.array([0, 0, 0, 0, 1, 1], dtype=np.uint8)
+    before = [p.clone() for p in loop.master]
+    out = loop.run(1, elastic=False)
+    assert out["masks"][0].tolist() == [0, 0, 0, 0, 1, 1] and np.isfinite(out["losses"]).all()
+    for i, (p, m, q) in enumerate(zip(params, loop.master, before)):
+        assert torch.equal(p, m.bfloat16()) and torch.equal(m, q) == (i < 4)

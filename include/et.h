@@ -29,7 +29,37 @@
  *   slots in gradient / importance / state arrays are ignored.  Its backward (above the deepest
  *   selected layer only) recomputes P from the saved per-row log-sum-exp.  Every row of a sequence sees all of it (there
  *   is no causal mask): a stack from token ids to logits that uses it is not an autoregressive model, and the token losses
- *   below are for stacks without it or above features that are causal already.
+ *   below are for stacks without it (ET_LAYER_MASKED_ATTENTION has the masks) or above features that are causal already.
+ *
+ *   A layer of kind ET_LAYER_MASKED_ATTENTION is softmax attention over sequences of any length, without tensors like
+ *   ET_LAYER_ATTENTION.  a_l = [q of `heads` | k of `kv_heads` | v of `kv_heads`] blocks of `head_dim` columns; query head h reads key and
+ *   value head h / (heads / kv_heads):
+ *       s_ij = softcap tanh(scale q_i.k_j / softcap)      (softcap 0: scale q_i.k_j)   - slope_h |i - j|
+ *       a_{l+1}[i] = sum_j softmax_j(s_ij) v_j            over the keys j that row i sees, the heads side by side
+ *   Row i sees rows of its own sequence only (et_stack_set_sequences; else runs of seq_len rows, 0: all M rows are one sequence); with
+ *   ET_MASK_CAUSAL those up to itself, and the first prefix[q] rows of its sequence q whatever their place.  slope_h: 0, or
+ *   et_stack_set_distance_bias.  A row of no sequence gives 0 and gets gradient 0, and may hold anything; rows of sequences are meant to be
+ *   finite: an infinity or a NaN of one row can reach rows that do not see it.  scale 0: 1 / sqrt(head_dim).  P and the scores'
+ *   gradients are rounded to bf16 before they are multiplied; scores, softmax and sums are fp32.  Runs of the same inputs give the same bits.
+ *
+ *   A layer of kind ET_LAYER_ROTARY turns the query and key heads of such rows by their positions, and leaves the value heads as they are.
+ *   The first 2 R columns of a head are R = sections[0] + .. pairs: columns k and R + k (ET_ROTARY_HALVES) or 2 k and 2 k + 1
+ *   (ET_ROTARY_ADJACENT); columns from 2 R on stay.  Pair k of axis a (sections[a] pairs belong to axis a, in order) turns by the angle
+ *       position_a theta^(-k / R)      (ET_ROTARY_ONE_SPECTRUM)      or      position_a theta^(-k_a / sections[a])
+ *   with k_a counted from the section's start (ET_ROTARY_OWN_SPECTRUM): (x, y) -> (x cos - y sin, y cos + x sin).  Positions:
+ *   et_stack_set_positions, else (one axis) a row's number within runs of seq_len rows (0: its number).  Angles are exact to 2^-24 of a half
+ *   turn at any int32 position.  No tensors.  Behind a dense layer and in front of another layer it works in place.
+ *
+ *   A layer of kind ET_LAYER_GATED is a dense layer whose two halves are multiplied, the first behind its activation:
+ *       Z_l = a_l W_l + b_l  (out_features = 2 h columns: gate | up),   a_{l+1} = act_l(Z_l[:, :h]) * Z_l[:, h:]
+ *   fold = 2; act_l is ET_ACT_GELU_TANH, ET_ACT_RELU or ET_ACT_SILU, residual_src = -1.  Tensors 2l and 2l+1 are W_l and b_l, whole.  Costed
+ *   like a dense layer; the time in which dZ_l is formed from the gradient of a_{l+1} goes to t_dy of b_l (Section 5.3).
+ *
+ *   A layer of kind ET_LAYER_DROPOUT sets elements to 0 with probability p = drop and divides the others by 1 - p:
+ *       a_{l+1} = keep * a_l / (1 - p)  (+ a_j if residual_src = j)
+ *   while a seed is set (et_stack_set_dropout_seed); without one it passes a_l through.  No mask is stored: element e of the [M x width]
+ *   matrix is kept where word e % 4 of Philox4x32-10 with counter (e / 4 low, e / 4 high, step low, l) and key (seed low, seed high) is at
+ *   least p 2^32, p taken to the nearest multiple of 2^-32.  Dropped elements are not looked at (they may be NaN).  No tensors.
  *
  *   A layer of kind ET_LAYER_BATCHNORM is a batch normalisation in training mode, the layer Section 5.2
  *   is written about: like ET_LAYER_NORM with the mean and the biased variance of each feature taken
@@ -110,11 +140,14 @@ typedef enum {
 } et_status;
 
 typedef enum { ET_F32 = 0, ET_BF16 = 1 } et_dtype;
-typedef enum { ET_ACT_NONE = 0, ET_ACT_GELU_TANH = 1, ET_ACT_RELU = 2 } et_act;
+typedef enum { ET_ACT_NONE = 0, ET_ACT_GELU_TANH = 1, ET_ACT_RELU = 2, ET_ACT_SILU = 3 /* ET_LAYER_GATED only */ } et_act;
 typedef enum {
   ET_LAYER_DENSE = 0, ET_LAYER_NORM = 1, ET_LAYER_ATTENTION = 2, ET_LAYER_IM2COL = 3, ET_LAYER_BATCHNORM = 4,
-  ET_LAYER_EMBEDDING = 5
+  ET_LAYER_EMBEDDING = 5, ET_LAYER_MASKED_ATTENTION = 6, ET_LAYER_ROTARY = 7, ET_LAYER_GATED = 8, ET_LAYER_DROPOUT = 9
 } et_layer_kind;
+typedef enum { ET_MASK_NONE = 0, ET_MASK_CAUSAL = 1 } et_attention_mask;
+typedef enum { ET_ROTARY_HALVES = 0, ET_ROTARY_ADJACENT = 1 } et_rotary_pairing;
+typedef enum { ET_ROTARY_ONE_SPECTRUM = 0, ET_ROTARY_OWN_SPECTRUM = 1 } et_rotary_spectrum;
 
 /* Cost-model reading for the selector (Section 2.2 / Eq. 7 versus the example after Eq. 3). */
 typedef enum {
@@ -147,6 +180,19 @@ typedef struct {
   int32_t height;         /* ET_LAYER_IM2COL: rows are images of height x width pixels, NHWC (M a multiple of  */
   int32_t width;          /*   height * width); in_features = channels (a multiple of 8), out_features =        */
   int32_t ksize;          /*   ksize^2 * channels, ksize odd and <= 7; act, fold, residual_src as for attention. */
+  /* ET_LAYER_MASKED_ATTENTION, ET_LAYER_ROTARY: in_features = (heads + 2 kv_heads) head_dim; the layer below has no activation and
+     no residual reads a_l; act, fold, residual_src as for attention; seq_len 0 or a divisor of M.  All fields 0 for other kinds. */
+  int32_t kv_heads;       /* attention: a divisor of heads */
+  int32_t head_dim;       /* attention: a multiple of 8, at most 128, out_features = heads * head_dim, ET_BF16 only */
+  int32_t mask;           /* attention: et_attention_mask */
+  float scale;            /* attention: factor of the scores, finite, 0: 1 / sqrt(head_dim) */
+  float softcap;          /* attention: >= 0 and finite, 0: scores are not capped */
+  int32_t axes;           /* rotary: 1, 2 or 3; out_features = in_features */
+  int32_t sections[3];    /* rotary: pairs of each axis, >= 1 for a < axes, together at most head_dim / 2 and 128 */
+  int32_t pairing;        /* rotary: et_rotary_pairing */
+  int32_t spectrum;       /* rotary: et_rotary_spectrum */
+  float theta;            /* rotary: > 0, finite */
+  float drop;             /* ET_LAYER_DROPOUT: p in [0, 1); in_features = out_features, act = ET_ACT_NONE, fold = 1 */
 } et_layer_desc;
 
 /* What one et_backward_elastic call executed.  The four arrays are caller-owned host
@@ -250,12 +296,38 @@ et_status et_stack_set_optimizer_step(et_stack* s, int32_t step, float weight_de
  * backward calls that follow; a backward call has to find the scale of its forward pass). */
 et_status et_stack_set_embedding_scale(et_stack* s, float scale);
 
+/* What layers without tensors read besides their input.  All of it is host state of the stack (et_stack_bind leaves it as it is) that
+ * names caller-owned device memory; calls that follow read that memory when they run, so that its contents may change between them
+ * and between replays of a captured call, but a backward call has to find what its forward pass found.
+ *
+ * Bounds of the sequences of every ET_LAYER_MASKED_ATTENTION layer: sequence q is the rows seq_begin[q] .. seq_begin[q+1]-1.
+ *   seq_begin  device int32[seqs + 1], non-decreasing, in [0, M]; rows before the first and behind the last bound are of no sequence.  (Bounds
+ *              outside that range are clamped; for bounds that are not non-decreasing no more is said than that nothing out of
+ *              range is read or written.)  NULL: back to runs of the layers' seq_len
+ *   prefix     device int32[seqs] or NULL: rows at each sequence's start that all of its rows see (ET_MASK_CAUSAL; clamped to the sequence) */
+et_status et_stack_set_sequences(et_stack* s, const int32_t* seq_begin, int32_t seqs, const int32_t* prefix);
+/* Slopes of the distance bias of one ET_LAYER_MASKED_ATTENTION layer: device float[heads], finite, or NULL: none. */
+et_status et_stack_set_distance_bias(et_stack* s, int32_t layer, const float* slopes);
+/* Positions for every ET_LAYER_ROTARY layer: device int32[axes][M], with as many axes as the layer of most axes has (ET_ERR_SHAPE for
+ * fewer), or NULL.  A stack with a layer of several axes needs them (ET_ERR_STATE from the forward pass). */
+et_status et_stack_set_positions(et_stack* s, const int32_t* positions, int32_t axes);
+/* Seed of every ET_LAYER_DROPOUT layer: device uint64[2], {seed, step}, or NULL: nothing is dropped (evaluation).  A training loop counts
+ * the step up between steps; of the step the low 32 bits count. */
+et_status et_stack_set_dropout_seed(et_stack* s, const uint64_t* seed);
+/* The gradient of the stack's input, for a stack that is part of something larger.  dX: device [M x in_features(0)], storage dtype,
+ * 16-byte aligned, not overlapping what a backward call reads; NULL (the default): it is not formed.  While set, every backward call passes the
+ * error gradient through all layers, whatever is selected (d = -1 in the terms above: dgrad of every layer is reported, an empty
+ * mask runs them, too), and writes it to dX.  Not for stacks that begin with an embedding (ET_ERR_INVALID_ARG), nor where
+ * several layers' residual_src is 0 (ET_ERR_UNSUPPORTED). */
+et_status et_stack_set_input_gradient(et_stack* s, void* dX);
+
 /* ---- forward and loss (precede the hot path; Eq. 3's T_forward) -------------------- */
 
 /* x: device [M x in_features(0)], y: device [M x width(a_L)], storage dtype.  Saves every
  * a_l and the pre-activations of activated layers in the workspace.  x itself is
  * referenced, not copied: it must stay valid and unchanged until the backward call that
- * uses this forward pass has finished. */
+ * uses this forward pass has finished.  (So must y where the last layer is ET_LAYER_MASKED_ATTENTION, whose backward pass reads it; dY is
+ * then another buffer.) */
 et_status et_forward_stack(et_stack* s, const void* x, void* y, void* stream);
 
 /* Mean-squared error over all M*D elements and its gradient dY = 2 (y - target) / (M*D).
@@ -528,9 +600,9 @@ typedef enum {
   ET_K_WGRAD = 2,          /* weight-gradient GEMM writing split partials (T3)          */
   ET_K_WGRAD_REDUCE = 3,   /* split reduction + gradient export + importance + SGD      */
   ET_K_BGRAD = 4,          /* bias gradient: column sums + finish (T2)                  */
-  ET_K_OTHER = 5,          /* loss gradient, top-layer activation backward, importance finalise */
+  ET_K_OTHER = 5,          /* loss gradient, top-layer activation backward, dZ of gated layers, importance finalise */
   ET_K_NORM = 6,           /* normalisation layers: forward, backward (error gradient + d gamma), gamma finish */
-  ET_K_ATTENTION = 7,      /* layers without tensors: attention core, patch gather; forward, backward */
+  ET_K_ATTENTION = 7,      /* layers without tensors: attention, rotary, dropout, patch gather; forward, backward */
   ET_K_LIST = 8,           /* the one-launch backward: every dgrad and wgrad GEMM of a call in one kernel */
   ET_K_CLASSES = 9
 } et_kernel_class;

@@ -20,7 +20,7 @@ _lib = C.CDLL(LIB_PATH)
 
 ET_OK = 0
 ET_F32, ET_BF16 = 0, 1
-ET_ACT_NONE, ET_ACT_GELU_TANH, ET_ACT_RELU = 0, 1, 2
+ET_ACT_NONE, ET_ACT_GELU_TANH, ET_ACT_RELU, ET_ACT_SILU = 0, 1, 2, 3
 ET_COST_STRICT, ET_COST_INCLUSIVE = 0, 1
 ET_FLAG_FUSE_SGD = 1
 ET_FLAG_DELTA_IS_SNAPSHOT = 2
@@ -35,11 +35,16 @@ class et_layer_desc(C.Structure):
     _fields_ = [("in_features", C.c_int32), ("out_features", C.c_int32), ("act", C.c_int32),
                 ("fold", C.c_int32), ("residual_src", C.c_int32), ("kind", C.c_int32), ("eps", C.c_float),
                 ("heads", C.c_int32), ("seq_len", C.c_int32), ("height", C.c_int32), ("width", C.c_int32),
-                ("ksize", C.c_int32)]
+                ("ksize", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("mask", C.c_int32), ("scale", C.c_float),
+                ("softcap", C.c_float), ("axes", C.c_int32), ("sections", C.c_int32 * 3), ("pairing", C.c_int32),
+                ("spectrum", C.c_int32), ("theta", C.c_float), ("drop", C.c_float)]
 
 
 ET_LAYER_DENSE, ET_LAYER_NORM, ET_LAYER_ATTENTION, ET_LAYER_IM2COL, ET_LAYER_BATCHNORM = 0, 1, 2, 3, 4
-ET_LAYER_EMBEDDING = 5
+ET_LAYER_EMBEDDING, ET_LAYER_MASKED_ATTENTION, ET_LAYER_ROTARY, ET_LAYER_GATED, ET_LAYER_DROPOUT = 5, 6, 7, 8, 9
+ET_MASK_NONE, ET_MASK_CAUSAL = 0, 1
+ET_ROTARY_HALVES, ET_ROTARY_ADJACENT = 0, 1
+ET_ROTARY_ONE_SPECTRUM, ET_ROTARY_OWN_SPECTRUM = 0, 1
 
 
 class et_policy_config(C.Structure):
@@ -95,6 +100,11 @@ _SIGS = {
     "et_clip_grads": [_vp, _vp, _i32, _vp, _vp, _f32, _vp, _vp],
     "et_update_clipped": [_vp, _vp, _i32, _vp, _f32, _f32, _vp, _vp],
     "et_stack_set_embedding_scale": [_vp, _f32],
+    "et_stack_set_sequences": [_vp, _vp, _i32, _vp],
+    "et_stack_set_distance_bias": [_vp, _i32, _vp],
+    "et_stack_set_positions": [_vp, _vp, _i32],
+    "et_stack_set_dropout_seed": [_vp, _vp],
+    "et_stack_set_input_gradient": [_vp, _vp],
     "et_importance": [_vp, _vp, _i32, _vp, _vp, _vp, _vp],
     "et_tensor_metric": [_vp, _vp, _i32, _i32, _vp, _vp, _vp],
     "et_sgd_masked": [_vp, _vp, _i32, _vp, _f32, _vp],
@@ -353,7 +363,7 @@ class Report:
 
 def _tensor_counts(d: et_layer_desc):
     """Elements of the two tensors of a layer."""
-    if d.kind in (ET_LAYER_ATTENTION, ET_LAYER_IM2COL):
+    if d.kind in (ET_LAYER_ATTENTION, ET_LAYER_IM2COL, ET_LAYER_MASKED_ATTENTION, ET_LAYER_ROTARY, ET_LAYER_DROPOUT):
         return 0, 0
     if d.kind in (ET_LAYER_NORM, ET_LAYER_BATCHNORM):
         return d.out_features, d.out_features
@@ -361,7 +371,7 @@ def _tensor_counts(d: et_layer_desc):
 
 
 class Stack:
-    """Owns the opaque et_stack handle.  Layers: sequence of objects / tuples with
+    """Owns the opaque et_stack handle.  Layers: sequence of et_layer_desc, or of objects / tuples with
     in_features, out_features, act, fold, residual_src."""
 
     def __init__(self, layers, M: int, dtype: int):
@@ -370,7 +380,9 @@ class Stack:
         self.dtype = dtype
         descs = (et_layer_desc * max(self.L, 1))()
         for i, ly in enumerate(layers):
-            if isinstance(ly, (tuple, list)):
+            if isinstance(ly, et_layer_desc):
+                descs[i] = ly
+            elif isinstance(ly, (tuple, list)):
                 descs[i] = et_layer_desc(*ly)
             else:
                 descs[i] = et_layer_desc(ly.in_features, ly.out_features, ly.act, ly.fold, ly.residual_src,
@@ -381,6 +393,9 @@ class Stack:
         self.counts = [c for d in descs[:self.L] for c in _tensor_counts(d)]
         self.counts_i64 = array.array("q", self.counts).tobytes()
         self.takes_ids = self.L > 0 and descs[0].kind == ET_LAYER_EMBEDDING
+        self.in_width = descs[0].in_features if self.L else 0
+        self.heads = [d.heads for d in descs[:self.L]]
+        self._keep_state = {}                        # tensors that the stack reads besides its input, kept alive
         self.out_width = (descs[self.L - 1].out_features // max(descs[self.L - 1].fold, 1)) if self.L else 0
         h = C.c_void_p()
         _check(_lib.et_stack_create(descs, self.L, self.M, dtype, C.byref(h)), "et_stack_create")
@@ -448,6 +463,54 @@ def et_loss_mse_grad(s: Stack, y, target, dY, loss_dev=None, stream=None):
 
 def et_stack_set_embedding_scale(s: Stack, scale: float):
     _check(_lib.et_stack_set_embedding_scale(s.handle, float(scale)), "et_stack_set_embedding_scale")
+
+
+def _set_state(s: Stack, name: str, *tensors):
+    s._keep_state[name] = tensors
+
+
+def et_stack_set_sequences(s: Stack, seq_begin, prefix=None, seqs: Optional[int] = None):
+    """`seqs`: taken from the length of seq_begin (seqs + 1) unless given.  seq_begin None: back to runs of the layers' seq_len."""
+    _, i32, _ = _torch_types(s.dtype)
+    if seqs is None:
+        seqs = len(seq_begin) - 1 if seq_begin is not None else 0
+    begin, pre = _operands("et_stack_set_sequences", s, ((seq_begin, i32, max(seqs, 0) + 1), (prefix, i32, seqs)))
+    _check(_lib.et_stack_set_sequences(s.handle, begin, seqs, pre), "et_stack_set_sequences")
+    _set_state(s, "sequences", seq_begin, prefix)
+
+
+def et_stack_set_distance_bias(s: Stack, layer: int, slopes):
+    _, _, f32 = _torch_types(s.dtype)
+    at, = _operands("et_stack_set_distance_bias", s, ((slopes, f32, s.heads[layer] if 0 <= layer < s.L else 0),))
+    _check(_lib.et_stack_set_distance_bias(s.handle, layer, at), "et_stack_set_distance_bias")
+    _set_state(s, ("slopes", layer), slopes)
+
+
+def et_stack_set_positions(s: Stack, positions, axes: Optional[int] = None):
+    """positions: [axes][M].  `axes`: taken from its shape unless given."""
+    _, i32, _ = _torch_types(s.dtype)
+    if axes is None:
+        axes = 0 if positions is None else positions.shape[0] if positions.ndim > 1 else 1
+    at, = _operands("et_stack_set_positions", s, ((positions, i32, max(axes, 0) * s.M),))
+    _check(_lib.et_stack_set_positions(s.handle, at, axes), "et_stack_set_positions")
+    _set_state(s, "positions", positions)
+
+
+def et_stack_set_dropout_seed(s: Stack, seed):
+    """seed: {seed, step} as int64[2] (its bits are taken as unsigned) or uint64[2]."""
+    torch = sys.modules.get("torch")
+    kind = seed.dtype if torch is not None and isinstance(seed, torch.Tensor) and seed.dtype in (torch.int64, torch.uint64) else \
+        torch.int64 if torch is not None else None
+    at, = _operands("et_stack_set_dropout_seed", s, ((seed, kind, 2),))
+    _check(_lib.et_stack_set_dropout_seed(s.handle, at), "et_stack_set_dropout_seed")
+    _set_state(s, "seed", seed)
+
+
+def et_stack_set_input_gradient(s: Stack, dX):
+    st, _, _ = _torch_types(s.dtype)
+    at, = _operands("et_stack_set_input_gradient", s, ((dX, st, s.M * s.in_width),))
+    _check(_lib.et_stack_set_input_gradient(s.handle, at), "et_stack_set_input_gradient")
+    _set_state(s, "dX", dX)
 
 
 def et_token_logp(s: Stack, y, targets, logp, vocab: int = 0, logit_scale: float = 1.0, stream=None):

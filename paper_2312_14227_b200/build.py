@@ -18,7 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libet.so")
-SOURCES = ["et_lib.cu", "et_noalloc.cu", "select.cpp"]
+SOURCES = ["et_lib.cu", "seq_attn.cu", "et_noalloc.cu", "select.cpp"]
 
 
 def _newest_source_mtime() -> float:
@@ -65,7 +65,7 @@ def build_library(force: bool = False, verbose: bool = False, debug_hooks: bool 
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [
-        nvcc, "-shared", "-o", LIB, "-std=c++17", "-O3", "-lineinfo",
+        nvcc, "-shared", "-o", LIB, "-std=c++17", "-O3", "-lineinfo", "--threads", "0",
         "-gencode", "arch=compute_100a,code=sm_100a",
         "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=default",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC,

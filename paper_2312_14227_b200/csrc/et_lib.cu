@@ -27,6 +27,10 @@
 #include "embedding.cuh"
 #include "grad_clip.cuh"
 #include "token_loss.cuh"
+#include "seq_attn.h"
+#include "rotary.cuh"
+#include "dropout.cuh"
+#include "gated.cuh"
 
 namespace {
 
@@ -165,6 +169,55 @@ et_status make_im2col_map(CUtensorMap* m, const void* ptr, int channels, int wid
   }
   return ET_OK;
 }
+// A matrix of `inner` columns that are part of rows of `stride` elements: boxes of 64 columns x 128 rows, or (chunks > 0, inner a multiple
+// of 64) [inner/64][outer][64] with boxes of 64 rows x `chunks` pieces; chunks < 0: 64 x 64.
+et_status make_part_map(CUtensorMap* m, const void* ptr, int inner, long long outer, int stride, int chunks) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (fn == nullptr) return ET_ERR_CUDA;
+  const bool three = chunks > 0;
+  cuuint64_t dims[3] = {three ? 64u : (cuuint64_t)inner, (cuuint64_t)outer, (cuuint64_t)(inner / 64)};
+  cuuint64_t strides[2] = {(cuuint64_t)stride * 2, 128};
+  cuuint32_t box[3] = {64, chunks == 0 ? 128u : 64u, (cuuint32_t)chunks};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, three ? 3 : 2, const_cast<void*>(ptr), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    g_last_cuda = (int)cudaErrorInvalidValue;
+    return ET_ERR_CUDA;
+  }
+  return ET_OK;
+}
+// Rows of `blocks` head blocks of `dim` columns: one box is 64 columns of one block x box_rows rows, columns past the block zero.
+et_status make_head_map(CUtensorMap* m, const void* ptr, int dim, int blocks, long long rows, int box_rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (fn == nullptr) return ET_ERR_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)blocks, (cuuint64_t)rows};
+  cuuint64_t strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)dim * blocks * 2};
+  cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    g_last_cuda = (int)cudaErrorInvalidValue;
+    return ET_ERR_CUDA;
+  }
+  return ET_OK;
+}
+// The same matrix by heads, made again when its address has changed.
+struct HeadMaps {
+  CUtensorMap b128, b64;
+  const void* ptr = nullptr;
+};
+et_status head_maps(HeadMaps* h, const void* ptr, int dim, int blocks, long long rows) {
+  if (h->ptr == ptr) return ET_OK;
+  h->ptr = nullptr;
+  ET_TRY(make_head_map(&h->b128, ptr, dim, blocks, rows, 128));
+  ET_TRY(make_head_map(&h->b64, ptr, dim, blocks, rows, 64));
+  h->ptr = ptr;
+  return ET_OK;
+}
 // All the views of one bf16 activation / gradient / weight matrix that the GEMMs use.
 struct TMaps {
   CUtensorMap b64;     // 64 x 64 boxes: MN-major operand fetched chunk by chunk
@@ -219,7 +272,29 @@ struct LayerRT {
   bool big_gemm = false;    // its GEMMs run for tens of microseconds (10 GFLOP and more)
   int imp_count_w = 0, imp_count_b = 0;
   int img_h = 0, img_w = 0, ksize = 0;   // patch gather: K = channels, N = ksize^2 * K
-  bool trainable() const { return kind == ET_LAYER_DENSE || kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM || kind == ET_LAYER_EMBEDDING; }
+  bool trainable() const {
+    return kind == ET_LAYER_DENSE || kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM || kind == ET_LAYER_EMBEDDING || kind == ET_LAYER_GATED;
+  }
+  bool gemms() const { return kind == ET_LAYER_DENSE || kind == ET_LAYER_GATED; }       // error and weight gradient are GEMMs
+  // A gated layer: N = 2 Nw columns of W, Z and dZ (fold = 1 here); its activation is not part of `act`, which the layer above applies
+  // the slope of: what arrives is the gradient of its output, and a kernel of its own forms dZ.
+  int gate_act = 0;
+  int dz_width() const { return kind == ET_LAYER_GATED ? N : Nw; }
+  bool own_dz() const { return act != ET_ACT_NONE || kind == ET_LAYER_GATED; }          // dZ_l is not G_{l+1} itself
+  int bn_gated = 128;       // output columns of a tile
+  et::gated::Maps gmaps;    // its tensor maps (input and, as the last layer, output: filled in per call)
+  // ET_LAYER_MASKED_ATTENTION (heads, seq; off_lse: log-sum-exp and D) and ET_LAYER_ROTARY
+  int kv = 0, dim = 0;
+  bool causal = false;
+  float scale = 0.f, cap = 0.f;
+  const float* slopes = nullptr;                 // et_stack_set_distance_bias
+  HeadMaps in_heads, out_heads, g_heads, dx_heads;
+  int axes = 0, pairs = 0;
+  bool adjacent = false;
+  bool in_place = false;    // rotary: a_{l+1} and G_{l+1} are the buffers of a_l and G_l
+  et::RotaryTable table;
+  uint32_t drop_limit = 0;  // ET_LAYER_DROPOUT: p 2^32
+  float drop_scale = 1.f;
   bool has_tensor(int k) const { return trainable() && (k == 0 || kind != ET_LAYER_EMBEDDING); }   // an embedding has no tensor 2l + 1
   size_t off_keys[2] = {0, 0}, off_rows[2] = {0, 0}, off_hist = 0, off_epart = 0, off_named = 0;   // embedding: sorting buffers, partial gradient rows
   bool vector_params() const { return kind == ET_LAYER_NORM || kind == ET_LAYER_BATCHNORM; }   // gamma, beta: [N]
@@ -260,6 +335,16 @@ struct et_stack {
   size_t off_tok_stats = 0, off_tok_logp = 0, off_tok_coef = 0, off_tok_parts = 0;   // token losses: per row
   size_t off_norm_parts = 0;           // global gradient norm: one 64-bit partial per block
   float emb_scale = 1.0f;              // ET_LAYER_EMBEDDING
+  const int32_t* seq_begin = nullptr;  // et_stack_set_sequences
+  const int32_t* seq_prefix = nullptr;
+  int n_seqs = 0;
+  const int32_t* positions = nullptr;  // et_stack_set_positions
+  int position_axes = 0;
+  const uint64_t* drop_seed = nullptr; // et_stack_set_dropout_seed
+  void* dX = nullptr;                  // et_stack_set_input_gradient
+  TMaps map_dx;
+  const void* map_dx_ptr = nullptr;
+  const void* y = nullptr;             // of the last forward pass
   int imp_total = 0;
   char* ws = nullptr;
   bool bound = false, forwarded = false;
@@ -414,12 +499,30 @@ template <typename T> T* grad_act(const et_stack* s, int i, const void* dY) {   
 }
 template <typename T> const T* dz_src(const et_stack* s, int l, const void* dY) {   // dZ_l (width Nw)
   const LayerRT& y = s->ly[l];
-  return y.act != ET_ACT_NONE ? (const T*)s->at(y.off_dZ) : grad_act<T>(s, l + 1, dY);
+  return y.own_dz() ? (const T*)s->at(y.off_dZ) : grad_act<T>(s, l + 1, dY);
+}
+// Where the error gradient through layer l goes: G_l, and dZ_{l-1} where the layer below has an activation (G_l itself is then only
+// needed for a residual).  Below layer 0 lies the caller's input gradient.
+struct Below {
+  bool act, G;
+  int act_kind;
+  void* g_out;
+  const void* z;
+  void* dz;
+};
+Below below(const et_stack* s, int l) {
+  if (l == 0) return {false, true, ET_ACT_NONE, s->dX, nullptr, nullptr};
+  const LayerRT& P = s->ly[l - 1];
+  const bool act = P.act != ET_ACT_NONE;
+  return {act, !act || P.residual_src >= 0, P.act, s->at(P.off_G_out), act ? s->at(P.off_Z) : nullptr, act ? s->at(P.off_dZ) : nullptr};
+}
+template <typename T> T* act_out(const et_stack* s, int l, void* y) {   // a_{l+1}
+  return l == s->L - 1 ? (T*)y : (T*)s->at(s->ly[l].off_a_out);
 }
 const TMaps& a_map(const et_stack* s, int l) { return l == 0 ? s->map_x : s->ly[l - 1].map_aout; }   // a_l
 const TMaps& g_map(const et_stack* s, int i) { return i == s->L ? s->map_dy : s->ly[i - 1].map_Gout; }  // G_i
 const TMaps& dz_map(const et_stack* s, int l) {                                                         // dZ_l
-  return s->ly[l].act != ET_ACT_NONE ? s->ly[l].map_dZ : g_map(s, l + 1);
+  return s->ly[l].own_dz() ? s->ly[l].map_dZ : g_map(s, l + 1);
 }
 
 // ---- GEMM launches ---------------------------------------------------------------------------
@@ -599,7 +702,7 @@ et_status run_forward_layer(et_stack* s, int l, void* y, cudaStream_t st) {
   }
 }
 
-// G_l = dZ_l W_l^T (+ skip gradient), dZ_{l-1} = G_l * act'(Z_{l-1});  l >= 1
+// G_l = dZ_l W_l^T (+ skip gradient), dZ_{l-1} = G_l * act'(Z_{l-1})
 // Row blocks of 32 that the dgrad GEMM of layer l writes fused column sums for.
 int dgrad_row_blocks(const et_stack* s, int l) {
   const bool pair = s->shared_plan ? s->ly[l].pair_dgrad_sh : s->ly[l].pair_dgrad;
@@ -615,16 +718,18 @@ et_status run_dgrad_layer(et_stack* s, int l, const void* dY, cudaStream_t st, b
   const LayerRT& L = s->ly[l];
   // Above a patch gather that is never materialised this GEMM is the convolution's error gradient: it goes
   // straight to the gather's input (layer l - 1's), reading dZ_l's patches with the kernel turned by 180 degrees.
-  const bool conv = is_bf16<T>::value && s->ly[l - 1].implicit;
+  const bool conv = is_bf16<T>::value && l >= 1 && s->ly[l - 1].implicit;
   const int lo = conv ? l - 1 : l;                          // G_lo is what this GEMM produces
   const LayerRT& Lc = s->ly[lo];
-  const LayerRT& P = s->ly[lo - 1];
+  const Below B = below(s, lo);
   const bool need_skip = Lc.consumer >= 0;
-  const bool need_act = P.act != ET_ACT_NONE;
-  const bool need_G = !need_act || P.residual_src >= 0;     // G_lo itself is read later
+  const bool need_act = B.act;
+  const bool need_G = B.G;                                  // G_lo itself is read later
+  if (lo == 0) want_colsum = false;
+  float* colsum = want_colsum ? (float*)s->at(s->ly[lo - 1].off_biaspart) : nullptr;
   if constexpr (is_bf16<T>::value) {
     et::tc::Params p = conv ? tc_params(s, (int)s->M, Lc.K, L.Nw, Lc.ksize * Lc.ksize, 1)
-                            : tc_params(s, (int)s->M, L.K, L.Nw, L.fold, 1);
+                            : tc_params(s, (int)s->M, L.K, L.dz_width(), L.fold, 1);
     p.b_k_seg_stride = L.Nw;
     if (conv) {
       LayerRT& G = s->ly[lo];
@@ -637,10 +742,10 @@ et_status run_dgrad_layer(et_stack* s, int l, const void* dY, cudaStream_t st, b
       p.a_tap_flip = 1;
       p.b_k_seg_stride = 0;
       p.b_mn_seg_stride = G.K;                              // W's rows are (tap, channel): one tap per segment
-      want_colsum = false;                                  // the bias below a gather takes the column-sum kernel
+      colsum = nullptr;                                     // the bias below a gather takes the column-sum kernel
     }
     et::tc::EpiMaps em;
-    const CUtensorMap& gout = P.map_Gout.b128;                // G_l lives in layer l-1's buffer
+    const CUtensorMap& gout = lo == 0 ? s->map_dx.b128 : s->ly[lo - 1].map_Gout.b128;   // G_l lives in layer l-1's buffer
     // Two tile plans: alone on the GPU whole waves count (768-wide outputs on 12608 rows: 192-wide pair
     // tiles, 200 units in 3 waves at 90 %); beside the weight-gradient stream the idle SMs of a last wave are
     // not lost, and the wider tile with less operand traffic per flop wins (256-wide: 150 units; measured on
@@ -652,47 +757,41 @@ et_status run_dgrad_layer(et_stack* s, int l, const void* dY, cudaStream_t st, b
     const CUtensorMap& amap = conv ? s->ly[lo].im_dg : dz_map(s, l).b128;
     const int ld_out = Lc.K;
     const CUtensorMap& skip = need_skip ? g_map(s, Lc.consumer + 1).b128 : gout;
-    const CUtensorMap& zmap = P.map_Z.b128;
-    const CUtensorMap& dzout = P.map_dZ.b128;
+    const CUtensorMap& zmap = need_act ? s->ly[lo - 1].map_Z.b128 : gout;
+    const CUtensorMap& dzout = need_act ? s->ly[lo - 1].map_dZ.b128 : gout;
     if (!need_act) {                                          // G_l = acc (+ skip)
       et::DgradEpiS<1> epi;
       epi.has_in[0] = need_skip; epi.has_in[1] = false; epi.has_out[0] = true; epi.has_out[1] = false;
-      epi.mul_act = false; epi.act_prev = P.act;
-      epi.colsum = want_colsum ? (float*)s->at(P.off_biaspart) : nullptr; epi.ld = ld_out;
+      epi.mul_act = false; epi.act_prev = B.act_kind;
+      epi.colsum = colsum; epi.ld = ld_out;
       em.in[0] = skip; em.out[0] = gout; em.in[1] = gout; em.out[1] = gout;
       return launch_tc<false, false>(bn_d, pair_d, amap, wmap, em, p, epi, s->sms, st, false, s->overlap_launch && !s->chain_shares_gpu);
     }
     if (!need_skip && !need_G) {                              // dZ_{l-1} = acc * act'(Z_{l-1})
       et::DgradEpiS<1> epi;
       epi.has_in[0] = true; epi.has_in[1] = false; epi.has_out[0] = true; epi.has_out[1] = false;
-      epi.mul_act = true; epi.act_prev = P.act;
-      epi.colsum = want_colsum ? (float*)s->at(P.off_biaspart) : nullptr; epi.ld = ld_out;
+      epi.mul_act = true; epi.act_prev = B.act_kind;
+      epi.colsum = colsum; epi.ld = ld_out;
       em.in[0] = zmap; em.out[0] = dzout; em.in[1] = zmap; em.out[1] = dzout;
       return launch_tc<false, false>(bn_d, pair_d, amap, wmap, em, p, epi, s->sms, st, false, s->overlap_launch && !s->chain_shares_gpu);
     }
     et::DgradEpiS<2> epi;                                     // both G_l and dZ_{l-1}
     epi.has_in[0] = need_skip; epi.has_in[1] = true; epi.has_out[0] = need_G; epi.has_out[1] = true;
-    epi.mul_act = false; epi.act_prev = P.act;
-    epi.colsum = want_colsum ? (float*)s->at(P.off_biaspart) : nullptr; epi.ld = ld_out;
+    epi.mul_act = false; epi.act_prev = B.act_kind;
+    epi.colsum = colsum; epi.ld = ld_out;
     em.in[0] = skip; em.out[0] = gout; em.in[1] = zmap; em.out[1] = dzout;
     return launch_tc<false, false>(bn_d, pair_d, amap, wmap, em, p, epi, s->sms, st, false, s->overlap_launch && !s->chain_shares_gpu);
   } else {
     et::DgradEpi<T> epi;
     epi.skip = need_skip ? grad_act<T>(s, L.consumer + 1, dY) : nullptr;
-    epi.act_prev = P.act;
+    epi.act_prev = B.act_kind;
     epi.ld = L.K;
-    if (!need_act) {
-      epi.Zprev = nullptr;
-      epi.outG = (T*)s->at(P.off_G_out);
-      epi.outdZ = nullptr;
-    } else {
-      epi.Zprev = (const T*)s->at(P.off_Z);
-      epi.outdZ = (T*)s->at(P.off_dZ);
-      epi.outG = need_G ? (T*)s->at(P.off_G_out) : nullptr;
-    }
+    epi.Zprev = (const T*)B.z;
+    epi.outdZ = (T*)B.dz;
+    epi.outG = need_G ? (T*)B.g_out : nullptr;
     et::simt::Params p;
-    p.rows = (int)s->M; p.cols = L.K; p.kc = L.Nw; p.segs = L.fold;
-    p.sa_i = L.Nw; p.sa_k = 1;
+    p.rows = (int)s->M; p.cols = L.K; p.kc = L.dz_width(); p.segs = L.fold;
+    p.sa_i = L.dz_width(); p.sa_k = 1;
     p.sb_k = 1; p.sb_seg = L.Nw; p.sb_j = L.N; p.b_wrap = 0;
     return launch_simt<T>(dz_src<T>(s, l, dY), (const T*)L.W, p, epi, st);
   }
@@ -776,12 +875,10 @@ et_status run_norm_backward(et_stack* s, int l, const void* dY, bool want_dx, bo
   T* dz_prev = nullptr;
   int act_prev = ET_ACT_NONE;
   if (want_dx) {
-    const LayerRT& P = s->ly[l - 1];
-    const bool need_act = P.act != ET_ACT_NONE;
-    const bool need_G = !need_act || P.residual_src >= 0;
+    const Below B = below(s, l);
     if (L.consumer >= 0) skip = grad_act<T>(s, L.consumer + 1, dY);
-    if (need_G) G_in = (T*)s->at(P.off_G_out);
-    if (need_act) { z_prev = (const T*)s->at(P.off_Z); dz_prev = (T*)s->at(P.off_dZ); act_prev = P.act; }
+    if (B.G) G_in = (T*)B.g_out;
+    if (B.act) { z_prev = (const T*)B.z; dz_prev = (T*)B.dz; act_prev = B.act_kind; }
   }
   float* gpart = (float*)s->at(L.off_gpart);
   int grid = 0;                       // blocks launched = rows of gpart written (at most L.norm_blocks)
@@ -851,17 +948,14 @@ et_status run_bn_backward(et_stack* s, int l, const void* dY, bool want_dx, bool
   ET_TRY(after_launch());
   ++*launches;
   if (want_dx) {
-    const LayerRT& P = s->ly[l - 1];
-    const bool need_act = P.act != ET_ACT_NONE;
-    const bool need_G = !need_act || P.residual_src >= 0;
+    const Below B = below(s, l);
     et::bn_finalize_kernel<<<ceil_div(C, 32), dim3(32, 32), 0, st>>>(part0, part1, chunks, C, (float)(1.0 / (double)M),
                                                                    L.eps, 2, nullptr, means);
     ET_TRY(after_launch());
     const long long total = (long long)M * (C / 8);
     et::bn_backward_kernel<T><<<ceil_div(total, et::kBnEltThreads), et::kBnEltThreads, 0, st>>>(
         dz, x, stats, means, (const T*)L.W, L.consumer >= 0 ? grad_act<T>(s, L.consumer + 1, dY) : nullptr,
-        need_G ? (T*)s->at(P.off_G_out) : nullptr, need_act ? (const T*)s->at(P.off_Z) : nullptr,
-        need_act ? (T*)s->at(P.off_dZ) : nullptr, P.act, s->M, C);
+        B.G ? (T*)B.g_out : nullptr, (const T*)B.z, (T*)B.dz, B.act_kind, s->M, C);
     ET_TRY(after_launch());
     *launches += 2;
   }
@@ -925,22 +1019,195 @@ et_status run_im2col_forward(et_stack* s, int l, cudaStream_t st) {
       act_in<T>(s, l), (T*)s->at(L.off_a_out), s->M, L.img_h, L.img_w, L.K, L.ksize);
   return after_launch();
 }
-// G_l (with the skip gradient) and dZ_{l-1} from the gradient of the gathered rows; l >= 1.
+// G_l (with the skip gradient) and dZ_{l-1} from the gradient of the gathered rows.
 template <typename T>
 et_status run_im2col_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
   TimedLaunch tl(s, ET_K_ATTENTION, st);
   const LayerRT& L = s->ly[l];
-  const LayerRT& P = s->ly[l - 1];
-  const bool need_act = P.act != ET_ACT_NONE;
-  const bool need_G = !need_act || P.residual_src >= 0;
+  const Below B = below(s, l);
   const T* skip = L.consumer >= 0 ? grad_act<T>(s, L.consumer + 1, dY) : nullptr;
   const long long total = (long long)s->M * (L.K / 8);
   et::col2im_kernel<T><<<ceil_div(total, et::kGatherThreads), et::kGatherThreads, 0, st>>>(
-      grad_act<T>(s, l + 1, dY), skip, need_G ? (T*)s->at(P.off_G_out) : nullptr,
-      need_act ? (const T*)s->at(P.off_Z) : nullptr, need_act ? (T*)s->at(P.off_dZ) : nullptr, P.act, s->M, L.img_h,
+      grad_act<T>(s, l + 1, dY), skip, B.G ? (T*)B.g_out : nullptr, (const T*)B.z, (T*)B.dz, B.act_kind, s->M, L.img_h,
       L.img_w, L.K, L.ksize);
   return after_launch();
 }
+
+// ---- masked attention -----------------------------------------------------------------------------
+et_status cuda_status(cudaError_t e, int launches) {
+  if (e != cudaSuccess) {
+    g_last_cuda = (int)e;
+    return ET_ERR_CUDA;
+  }
+  g_launches.fetch_add(launches, std::memory_order_relaxed);
+  return ET_OK;
+}
+et::seqattn::Args seq_args(const et_stack* s, int l) {
+  const LayerRT& L = s->ly[l];
+  et::seqattn::Args a{};
+  a.mask = {s->seq_begin, s->seq_prefix, s->n_seqs, L.seq > 0 ? L.seq : (int)s->M, (int)s->M, L.causal};
+  a.ld = ceil_div(s->M, 128) * 128;
+  a.lse = (float*)s->at(L.off_lse);
+  a.D = a.lse + (size_t)L.heads * a.ld;
+  a.slopes = L.slopes;
+  a.status = (uint32_t*)s->at(s->off_status);
+  a.heads = L.heads; a.kv = L.kv; a.dim = L.dim;
+  a.scale = L.scale; a.cap = L.cap;
+  return a;
+}
+et_status run_seq_forward(et_stack* s, int l, void* y, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_ATTENTION, st);
+  LayerRT& L = s->ly[l];
+  ET_TRY(head_maps(&L.in_heads, act_in<bf16>(s, l), L.dim, L.heads + 2 * L.kv, s->M));
+  ET_TRY(head_maps(&L.out_heads, act_out<bf16>(s, l, y), L.dim, L.heads, s->M));
+  return cuda_status(et::seqattn::forward(L.in_heads.b128, L.out_heads.b128, seq_args(s, l), s->sms, st), et::seqattn::kForwardLaunches);
+}
+// G_l (gradient of [q | k | v]) from G_{l+1}; the layer below has no activation, so G_l is its dZ.
+et_status run_seq_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_ATTENTION, st);
+  LayerRT& L = s->ly[l];
+  const bf16* out = l == s->L - 1 ? (const bf16*)s->y : (const bf16*)s->at(L.off_a_out);
+  const bf16* dout = grad_act<bf16>(s, l + 1, dY);
+  const void* dx = below(s, l).g_out;
+  ET_TRY(head_maps(&L.in_heads, act_in<bf16>(s, l), L.dim, L.heads + 2 * L.kv, s->M));
+  ET_TRY(head_maps(&L.g_heads, dout, L.dim, L.heads, s->M));
+  ET_TRY(head_maps(&L.dx_heads, dx, L.dim, L.heads + 2 * L.kv, s->M));
+  return cuda_status(et::seqattn::backward(L.in_heads.b128, L.in_heads.b64, L.g_heads.b128, L.g_heads.b64, L.dx_heads.b128, out, dout,
+                                           seq_args(s, l), s->sms, st), et::seqattn::kBackwardLaunches);
+}
+
+// ---- rotary positions -----------------------------------------------------------------------------
+template <typename T>
+et_status run_rotary(et_stack* s, int l, const T* in, T* out, bool back, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_ATTENTION, st);
+  const LayerRT& L = s->ly[l];
+  et::RotaryArgs a{};
+  a.positions = s->positions;
+  a.M = s->M; a.len = L.seq > 0 ? L.seq : (int)s->M;
+  a.dim = L.dim; a.pairs = L.pairs; a.heads = L.heads + L.kv; a.all = L.heads + 2 * L.kv;
+  a.adjacent = L.adjacent; a.copy = in != out; a.back = back;
+  const bool vec = L.dim % 8 == 0 && L.pairs % (L.adjacent ? 4 : 8) == 0;
+  const int per = vec ? (L.adjacent ? 4 : 8) : 1;
+  const long long items = (long long)s->M * ceil_div(L.pairs, per);
+  const int blocks = ceil_div(items, 256);
+  // rows alone that give less than two blocks an SM: the heads are cut, too
+  const int cut = std::max(1, std::min(a.all, ceil_div(2 * s->sms, blocks)));
+  return launch_chained(vec ? et::rotary_kernel<T, true> : et::rotary_kernel<T, false>, dim3(blocks, cut), 256, st, in, out, L.table, a);
+}
+template <typename T>
+et_status run_rotary_forward(et_stack* s, int l, void* y, cudaStream_t st) {
+  return run_rotary<T>(s, l, act_in<T>(s, l), act_out<T>(s, l, y), false, st);
+}
+template <typename T>
+et_status run_rotary_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+  return run_rotary<T>(s, l, grad_act<T>(s, l + 1, dY), (T*)below(s, l).g_out, true, st);
+}
+
+// ---- dropout --------------------------------------------------------------------------------------
+et::DropArgs drop_args(const et_stack* s, int l, int act) {
+  const LayerRT& L = s->ly[l];
+  return {L.drop_limit != 0 ? s->drop_seed : nullptr, (size_t)s->M * L.N, L.drop_limit, (uint32_t)l, L.drop_scale, act};
+}
+template <typename T>
+et_status run_dropout_forward(et_stack* s, int l, void* y, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_ATTENTION, st);
+  const LayerRT& L = s->ly[l];
+  const et::DropArgs a = drop_args(s, l, 0);
+  return launch_chained(et::dropout_kernel<T>, ceil_div(a.count, et::kDropThreads * 8), et::kDropThreads, st, act_in<T>(s, l),
+                        L.residual_src >= 0 ? act_in<T>(s, L.residual_src) : nullptr, act_out<T>(s, l, y), nullptr, nullptr, a);
+}
+template <typename T>
+et_status run_dropout_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_ATTENTION, st);
+  const LayerRT& L = s->ly[l];
+  const Below B = below(s, l);
+  const et::DropArgs a = drop_args(s, l, B.act_kind);
+  return launch_chained(et::dropout_kernel<T>, ceil_div(a.count, et::kDropThreads * 8), et::kDropThreads, st, grad_act<T>(s, l + 1, dY),
+                        L.consumer >= 0 ? grad_act<T>(s, L.consumer + 1, dY) : nullptr, B.G ? (T*)B.g_out : nullptr, (const T*)B.z,
+                        (T*)B.dz, a);
+}
+
+// ---- gated layer ----------------------------------------------------------------------------------
+template <int H>
+et_status launch_gated(const et_stack* s, const LayerRT& L, et::gated::Params p, cudaStream_t st) {
+  using C = et::gated::Cfg<H>;
+  auto kern = et::gated::gated_forward_kernel<H>;
+  static int clusters_dev[64] = {};
+  int dev = 0;
+  CU_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return ET_ERR_UNSUPPORTED;
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(et::gated::THREADS);
+  cfg.dynamicSmemBytes = C::SMEM;
+  cfg.stream = st;
+  int clusters;
+  {
+    std::lock_guard<std::mutex> cache_lock(g_cache_mutex);
+    if (clusters_dev[dev] == 0) {
+      CU_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM));
+      cfg.gridDim = dim3(s->sms & ~1);
+      int n = 0;
+      if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+        (void)cudaGetLastError();
+        n = std::max(1, s->sms / 2);
+      }
+      clusters_dev[dev] = n;
+    }
+    clusters = clusters_dev[dev];
+  }
+  p.tiles_m = ceil_div(p.rows, 2 * et::tc::BM);
+  p.tiles_n = ceil_div(p.h, H);
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3(2 * std::min(p.tiles_m * p.tiles_n, clusters));
+  CU_TRY(cudaLaunchKernelEx(&cfg, kern, L.gmaps, p));
+  return after_launch();
+}
+template <typename T>
+et_status run_gated_forward(et_stack* s, int l, void* y, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_FORWARD, st);
+  LayerRT& L = s->ly[l];
+  if constexpr (is_bf16<T>::value) {
+    et::gated::Params p{};
+    p.rows = (int)s->M; p.h = L.Nw; p.kb = ceil_div(L.K, et::tc::BK);
+    p.b_3d = L.Nw % 64 == 0; p.act = L.gate_act;
+    p.bias = (const bf16*)L.b;
+    p.status = (uint32_t*)s->at(s->off_status);
+    L.gmaps.a = a_map(s, l).b128;
+    L.gmaps.out[2] = (l == s->L - 1 ? s->map_y : L.map_aout).b128;
+    return L.bn_gated == 128 ? launch_gated<128>(s, L, p, st) : launch_gated<64>(s, L, p, st);
+  } else {
+    const dim3 grid(ceil_div(L.Nw, et::kGatedSimtN), ceil_div(s->M, et::kGatedSimtM));
+    et::gated_forward_simt_kernel<<<grid, 256, 0, st>>>(act_in<T>(s, l), (const T*)L.W, (const T*)L.b, (T*)s->at(L.off_Z),
+                                                        act_out<T>(s, l, y), (int)s->M, L.K, L.Nw, L.gate_act);
+    return after_launch();
+  }
+}
+// dZ_l from G_{l+1}
+template <typename T>
+et_status run_gated_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+  TimedLaunch tl(s, ET_K_OTHER, st);
+  const LayerRT& L = s->ly[l];
+  const long long items = s->M * ceil_div(L.Nw, 8);
+  return launch_chained(et::gated_backward_kernel<T>, ceil_div(items, 256), 256, st, grad_act<T>(s, l + 1, dY), (const T*)s->at(L.off_Z),
+                        (T*)s->at(L.off_dZ), s->M, L.Nw, L.gate_act);
+}
+
+// The backward pass of a layer without tensors.
+template <typename T>
+et_status run_plain_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+  switch (s->ly[l].kind) {
+    case ET_LAYER_ATTENTION: return run_attn_backward(s, l, dY, st);
+    case ET_LAYER_MASKED_ATTENTION: return run_seq_backward(s, l, dY, st);
+    case ET_LAYER_ROTARY: return run_rotary_backward<T>(s, l, dY, st);
+    case ET_LAYER_DROPOUT: return run_dropout_backward<T>(s, l, dY, st);
+    default: return run_im2col_backward<T>(s, l, dY, st);
+  }
+}
+int plain_backward_launches(const LayerRT& L) { return L.kind == ET_LAYER_MASKED_ATTENTION ? et::seqattn::kBackwardLaunches : 1; }
 
 // ---- embedding ------------------------------------------------------------------------------------
 template <typename T>
@@ -1074,7 +1341,7 @@ et_status run_wgrad_layer(et_stack* s, int l, const void* dY, float* grad, const
       et::simt::Params p;
       p.rows = L.K; p.cols = L.N; p.kc = (int)s->M; p.segs = 1;
       p.sa_i = 1; p.sa_k = L.K;
-      p.sb_k = L.Nw; p.sb_seg = 0; p.sb_j = 1; p.b_wrap = L.fold > 1 ? L.Nw : 0;
+      p.sb_k = L.dz_width(); p.sb_seg = 0; p.sb_j = 1; p.b_wrap = L.fold > 1 ? L.Nw : 0;
       ET_TRY(launch_simt<T>(act_in<T>(s, l), dz_src<T>(s, l, dY), p, epi, st));
     }
   }
@@ -1102,13 +1369,13 @@ et_status run_bgrad_layer(et_stack* s, int l, const void* dY, float* grad, const
   int chunks = fused_chunks;
   if (fused_chunks == 0) {
     chunks = ceil_div(s->M, et::kColsumRows);
-    dim3 grid(ceil_div(L.Nw, 256), chunks), block(32, 8);
-    et::colsum_partial_kernel<T><<<grid, block, 0, st>>>(dz_src<T>(s, l, dY), (int)s->M, L.Nw, part);
+    dim3 grid(ceil_div(L.dz_width(), 256), chunks), block(32, 8);
+    et::colsum_partial_kernel<T><<<grid, block, 0, st>>>(dz_src<T>(s, l, dY), (int)s->M, L.dz_width(), part);
     ET_TRY(after_launch());
     ++*launches;
   }
   float* imp = (float*)s->at(s->off_imp_parts) + s->imp_offs[2 * l + 1];
-  et::bias_finish_kernel<T><<<L.imp_count_b, dim3(et::kBiasCols, et::kBiasLanes), 0, st>>>(part, chunks, L.Nw, L.N, grad, delta, imp,
+  et::bias_finish_kernel<T><<<L.imp_count_b, dim3(et::kBiasCols, et::kBiasLanes), 0, st>>>(part, chunks, L.dz_width(), L.N, grad, delta, imp,
                                                                        (T*)L.b, opt_params(s, lr), sgd ? 1 : 0, s->delta_is_snapshot ? 1 : 0, L.b32,
                                                                        L.st1[1], L.st2[1]);
   ++*launches;
@@ -1200,7 +1467,7 @@ bool list_dgrad_form(const et_stack* s, int l, bool* has_in, bool* mul_act) {
   return false;
 }
 bool list_eligible(const et_stack* s, int d) {
-  if (s->dtype != ET_BF16 || !s->opt_gemm_list || s->list_state < 0) return false;
+  if (s->dtype != ET_BF16 || !s->opt_gemm_list || s->list_state < 0 || s->dX != nullptr) return false;
   for (int l = d; l < s->L; ++l)
     if (!s->ly[l].list_ok) return false;
   for (int l = d + 1; l < s->L; ++l) {
@@ -1450,7 +1717,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
 
   if (report != nullptr) {
     for (int l = 0; l < L; ++l) {
-      if (report->dgrad) report->dgrad[l] = l > d;
+      if (report->dgrad) report->dgrad[l] = l > d || s->dX != nullptr;
       if (report->wgrad) report->wgrad[l] = mask[2 * l] != 0;
       if (report->bgrad) report->bgrad[l] = mask[2 * l + 1] != 0;
       if (report->updated) {
@@ -1461,13 +1728,19 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
     report->deepest = d;
   }
 
-  if (d == L) {
+  const int to = s->dX != nullptr ? -1 : d;              // the error gradient passes through the layers above this one
+  const int from = s->dX != nullptr ? 0 : d;             // lowest layer that the pass comes to
+  if (d == L && to == d) {
     if (delta != nullptr) CU_TRY(cudaMemsetAsync(importance_dev, 0, sizeof(float) * 2 * L, st));
   } else {
     if constexpr (is_bf16<T>::value) {
       if (s->map_dy_ptr != dY) {
         ET_TRY(make_tmaps(&s->map_dy, dY, s->out_width(), s->M));
         s->map_dy_ptr = dY;
+      }
+      if (to < 0 && s->ly[0].gemms() && s->map_dx_ptr != s->dX) {
+        ET_TRY(make_tmaps(&s->map_dx, s->dX, s->ly[0].K, s->M));
+        s->map_dx_ptr = s->dX;
       }
     }
     // Stacks of plain dense layers take the one-launch path: all GEMMs of the pass in one cooperative kernel,
@@ -1482,18 +1755,18 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
     }
     if (!done_by_list) {
     // per-kernel timing wants kernels one at a time; an embedding by itself has no error-gradient chain to run beside
-    const bool alone = L == 1 && s->ly[0].kind == ET_LAYER_EMBEDDING;
+    const bool alone = d == L || (L == 1 && s->ly[0].kind == ET_LAYER_EMBEDDING);
     const bool two = !s->timing && !alone && s->opt_two_streams && setup_two_streams(s);
     // Sharing the GPU with the higher-priority error-gradient chain: when few kernels are selected
     // the weight gradients are filler work and should hand their SMs back after every unit; when
     // they are as much work as the chain itself, persistent CTAs (epilogue overlap) pay more (ViT-B step:
     // 2.33 ms with one-unit CTAs against 2.46 ms persistent; full backprop 4.0 ms persistent against 4.5 ms).
     int n_w = 0;
-    for (int l = d; l < L; ++l) n_w += mask[2 * l] ? 1 : 0;
+    for (int l = d; l < L; ++l) n_w += mask[2 * l] ? 1 : 0;      // (d == L: none)
     // Tile plan: the one made for a shared GPU whenever the two streams run (or on request, so that
     // per-kernel timing on one stream can time the very kernels the two-stream step launches).
     s->shared_plan = s->opt_tile_plan == ET_TILE_PLAN_SHARED || (s->opt_tile_plan == ET_TILE_PLAN_AUTO && two);
-    s->wgrad_one_unit = s->shared_plan && 2 * n_w <= L - d;
+    s->wgrad_one_unit = s->shared_plan && 2 * n_w <= L - from;
     // With a second stream the weight-gradient CTAs get their SMs in the gaps between the chain's
     // kernels; a chain kernel that took over each SM the moment its predecessor left would starve
     // them until the chain ends (measured: 2.45 -> 2.62 ms per ViT-B step), so no launch overlap then.
@@ -1513,7 +1786,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
       ++launches;
     }
     if (two) CU_TRY(cudaEventRecord(s->chain_ev[L], cs));  // dZ_{L-1} is ready
-    for (int l = L - 1; l >= d; --l) {
+    for (int l = L - 1; l >= from; --l) {
       const LayerRT& Y = s->ly[l];
       if (Y.kind == ET_LAYER_EMBEDDING) {
         if (!mask[2 * l]) continue;
@@ -1523,12 +1796,17 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
         continue;
       }
       const bool norm = Y.vector_params();
-      const double gemm = Y.kind != ET_LAYER_DENSE ? 0.0 : 2.0 * (double)s->M * Y.K * Y.N;
+      const double gemm = !Y.gemms() ? 0.0 : 2.0 * (double)s->M * Y.K * Y.N;
+      if (Y.kind == ET_LAYER_GATED) {
+        ET_TRY(run_gated_backward<T>(s, l, dY, cs));
+        if (two) CU_TRY(cudaEventRecord(s->chain_ev[l + 1], cs));   // dZ_l is ready (not only the gradient of the layer's output)
+        ++launches;
+      }
       if (mask[2 * l + 1]) {
         // On the tensor-core path the column partials of dZ_l were left by dgrad(l+1) in this
         // layer's own buffer; finishing them need not sit on the chain's critical path.
         // (A normalisation layer above leaves none: the column-sum kernel runs instead.)
-        const int fused = (is_bf16<T>::value && l < L - 1 && s->ly[l + 1].kind == ET_LAYER_DENSE)
+        const int fused = (is_bf16<T>::value && l < L - 1 && s->ly[l + 1].gemms() && Y.kind != ET_LAYER_GATED)
                               ? dgrad_row_blocks(s, l + 1) : 0;
         // Which stream: with few selected kernels the caller's stream is nearly idle and takes
         // the finishers off the chain; with many it is the busier one and the chain keeps them.
@@ -1540,10 +1818,9 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
       if (!Y.trainable()) {
         // a non-trainable layer: only passes the error gradient on, above the deepest selected layer
         if (Y.implicit) continue;                            // done by the error-gradient GEMM of the layer above
-        if (l > d) {
-          if (Y.kind == ET_LAYER_ATTENTION) ET_TRY(run_attn_backward(s, l, dY, cs));
-          else ET_TRY(run_im2col_backward<T>(s, l, dY, cs));
-          ++launches;
+        if (l > to) {
+          ET_TRY(run_plain_backward<T>(s, l, dY, cs));
+          launches += plain_backward_launches(Y);
           if (two) CU_TRY(cudaEventRecord(s->chain_ev[l], cs));
         }
         continue;
@@ -1552,21 +1829,21 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
         // one kernel passes the error gradient on (above the deepest selected layer) and leaves the
         // partials of d gamma (if selected); it reads gamma, so the finisher that may update gamma
         // follows it on the same stream
-        if (l > d || mask[2 * l]) {
+        if (l > to || mask[2 * l]) {
           if (Y.kind == ET_LAYER_NORM)
-            ET_TRY(run_norm_backward<T>(s, l, dY, l > d, mask[2 * l] != 0, grads ? grads[2 * l] : nullptr,
+            ET_TRY(run_norm_backward<T>(s, l, dY, l > to, mask[2 * l] != 0, grads ? grads[2 * l] : nullptr,
                                         delta ? (const T*)delta[2 * l] : nullptr, sgd, lr, &launches, cs));
           else
-            ET_TRY(run_bn_backward<T>(s, l, dY, l > d, mask[2 * l] != 0, grads ? grads[2 * l] : nullptr,
+            ET_TRY(run_bn_backward<T>(s, l, dY, l > to, mask[2 * l] != 0, grads ? grads[2 * l] : nullptr,
                                       delta ? (const T*)delta[2 * l] : nullptr, sgd, lr, &launches, cs));
         }
-        if (two && l > d) CU_TRY(cudaEventRecord(s->chain_ev[l], cs));
+        if (two && l > to) CU_TRY(cudaEventRecord(s->chain_ev[l], cs));
         continue;
       }
-      if (l > d) {
-        ET_TRY(run_dgrad_layer<T>(s, l, dY, cs, mask[2 * (l - 1) + 1] != 0));
+      if (l > to) {
+        ET_TRY(run_dgrad_layer<T>(s, l, dY, cs, l >= 1 && mask[2 * (l - 1) + 1] != 0 && s->ly[l - 1].kind != ET_LAYER_GATED));
         if (two) CU_TRY(cudaEventRecord(s->chain_ev[l], cs));   // dZ_{l-1} ready, W_l no longer needed
-        if (two && s->ly[l - 1].implicit) CU_TRY(cudaEventRecord(s->chain_ev[l - 1], cs));   // and the gather's backward with it
+        if (two && l >= 1 && s->ly[l - 1].implicit) CU_TRY(cudaEventRecord(s->chain_ev[l - 1], cs));   // and the gather's backward with it
         ++launches;
         flops += gemm;
       }
@@ -1575,7 +1852,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
         if (two) CU_TRY(cudaStreamWaitEvent(st, s->chain_ev[l + 1], 0));
         ET_TRY(run_wgrad_layer<T>(s, l, dY, grads ? grads[2 * l] : nullptr,
                                   delta ? (const T*)delta[2 * l] : nullptr, sgd, lr, &launches, st,
-                                  (two && l > d) ? s->chain_ev[l] : nullptr));
+                                  (two && l > to) ? s->chain_ev[l] : nullptr));
         flops += gemm;
       }
     }
@@ -1606,6 +1883,7 @@ et_status validate_backward_args(const et_stack* s, const void* dY, const uint8_
   ET_TRY(check_ready(s, mask, n_tensors));
   if (dY == nullptr) return ET_ERR_INVALID_ARG;
   if (!s->forwarded) return ET_ERR_STATE;
+  if (s->ly[s->L - 1].kind == ET_LAYER_MASKED_ATTENTION && dY == s->y) return ET_ERR_INVALID_ARG;   // its backward pass reads y
   if (delta != nullptr) {
     if (importance == nullptr) return ET_ERR_INVALID_ARG;
     for (int t = 0; t < n_tensors; ++t)
@@ -1718,6 +1996,7 @@ et_status forward_impl(et_stack* s, const void* x, void* y, cudaStream_t st) {
     }
   }
   s->x = x;
+  s->y = y;
   if constexpr (is_bf16<T>::value) {
     if (forward_list_eligible(s)) {
       bool refused = false;
@@ -1730,11 +2009,21 @@ et_status forward_impl(et_stack* s, const void* x, void* y, cudaStream_t st) {
     else if (s->ly[l].kind == ET_LAYER_BATCHNORM) ET_TRY(run_bn_forward<T>(s, l, y, st));
     else if (s->ly[l].kind == ET_LAYER_EMBEDDING) ET_TRY(run_embed_forward<T>(s, y, st));
     else if (s->ly[l].kind == ET_LAYER_ATTENTION) ET_TRY(run_attn_forward(s, l, st));
+    else if (s->ly[l].kind == ET_LAYER_MASKED_ATTENTION) ET_TRY(run_seq_forward(s, l, y, st));
+    else if (s->ly[l].kind == ET_LAYER_ROTARY) ET_TRY(run_rotary_forward<T>(s, l, y, st));
+    else if (s->ly[l].kind == ET_LAYER_GATED) ET_TRY(run_gated_forward<T>(s, l, y, st));
+    else if (s->ly[l].kind == ET_LAYER_DROPOUT) ET_TRY(run_dropout_forward<T>(s, l, y, st));
     else if (s->ly[l].kind == ET_LAYER_IM2COL) { if (!s->ly[l].implicit) ET_TRY(run_im2col_forward<T>(s, l, st)); }
     else ET_TRY(run_forward_layer<T>(s, l, y, st));
   }
   s->forwarded = true;
   return ET_OK;
+}
+
+bool has_kind(const et_stack* s, int kind) {
+  for (const LayerRT& y : s->ly)
+    if (y.kind == kind) return true;
+  return false;
 }
 
 double median(std::vector<float>& v) {
@@ -1770,12 +2059,15 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
   for (int l = 0; l < L && err == ET_OK; ++l) {
     const et_layer_desc& d = layers[l];
     LayerRT& y = s->ly[l];
-    if (d.in_features < 1 || d.out_features < 1 || d.fold < 1 || d.act < 0 || d.act > 2) { err = ET_ERR_INVALID_ARG; break; }
+    if (d.in_features < 1 || d.out_features < 1 || d.fold < 1 || d.act < 0 ||
+        d.act > (d.kind == ET_LAYER_GATED ? ET_ACT_SILU : ET_ACT_RELU)) {
+      err = ET_ERR_INVALID_ARG; break;
+    }
     if (d.out_features % d.fold != 0) { err = ET_ERR_SHAPE; break; }
-    if (d.fold > 1 && d.act != ET_ACT_NONE) { err = ET_ERR_UNSUPPORTED; break; }
+    if (d.fold > 1 && d.act != ET_ACT_NONE && d.kind != ET_LAYER_GATED) { err = ET_ERR_UNSUPPORTED; break; }
     y.K = d.in_features; y.N = d.out_features; y.fold = d.fold; y.Nw = d.out_features / d.fold;
     y.act = d.act; y.residual_src = d.residual_src;
-    if (d.kind < ET_LAYER_DENSE || d.kind > ET_LAYER_EMBEDDING) { err = ET_ERR_INVALID_ARG; break; }
+    if (d.kind < ET_LAYER_DENSE || d.kind > ET_LAYER_DROPOUT) { err = ET_ERR_INVALID_ARG; break; }
     y.kind = d.kind; y.eps = d.eps;
     if (y.kind == ET_LAYER_EMBEDDING) {
       if (y.fold != 1 || y.act != ET_ACT_NONE || y.residual_src != -1) { err = ET_ERR_INVALID_ARG; break; }
@@ -1805,6 +2097,61 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
         err = ET_ERR_UNSUPPORTED; break;
       }
     }
+    if (y.kind == ET_LAYER_MASKED_ATTENTION || y.kind == ET_LAYER_ROTARY) {
+      y.heads = d.heads; y.kv = d.kv_heads; y.dim = d.head_dim; y.seq = d.seq_len;
+      const bool attn = y.kind == ET_LAYER_MASKED_ATTENTION;
+      if (y.fold != 1 || y.act != ET_ACT_NONE || y.residual_src != -1 || y.heads < 1 || y.kv < 1 || y.dim < 1 || y.seq < 0 ||
+          (long long)y.K != ((long long)y.heads + 2ll * y.kv) * y.dim || (long long)y.N != (attn ? (long long)y.heads * y.dim : y.K)) {
+        err = ET_ERR_INVALID_ARG; break;
+      }
+      if (y.seq > 0 && M % y.seq != 0) { err = ET_ERR_SHAPE; break; }
+      if (l >= 1 && s->ly[l - 1].act != ET_ACT_NONE) { err = ET_ERR_UNSUPPORTED; break; }
+    }
+    if (y.kind == ET_LAYER_MASKED_ATTENTION) {
+      y.causal = d.mask == ET_MASK_CAUSAL;
+      y.cap = d.softcap;
+      y.scale = d.scale == 0.f ? (float)(1.0 / std::sqrt((double)y.dim)) : d.scale;
+      if (y.heads % y.kv != 0 || (d.mask != ET_MASK_NONE && d.mask != ET_MASK_CAUSAL) || !(d.scale >= 0.f) || !std::isfinite(d.scale) ||
+          !(y.cap >= 0.f) || !std::isfinite(y.cap)) {
+        err = ET_ERR_INVALID_ARG; break;
+      }
+      if (dtype != ET_BF16 || y.dim % 8 || y.dim > 128) { err = ET_ERR_UNSUPPORTED; break; }
+    }
+    if (y.kind == ET_LAYER_ROTARY) {
+      y.axes = d.axes;
+      y.adjacent = d.pairing == ET_ROTARY_ADJACENT;
+      if (y.axes < 1 || y.axes > 3 || (d.pairing != ET_ROTARY_HALVES && d.pairing != ET_ROTARY_ADJACENT) ||
+          (d.spectrum != ET_ROTARY_ONE_SPECTRUM && d.spectrum != ET_ROTARY_OWN_SPECTRUM) || !(d.theta > 0.f) || !std::isfinite(d.theta)) {
+        err = ET_ERR_INVALID_ARG; break;
+      }
+      long long pairs = 0;
+      for (int a = 0; a < y.axes; ++a) {
+        if (d.sections[a] < 1) err = ET_ERR_INVALID_ARG;
+        pairs += d.sections[a];
+      }
+      if (err != ET_OK) break;
+      if (2 * pairs > y.dim) { err = ET_ERR_SHAPE; break; }
+      if (pairs > et::kRotaryMaxPairs) { err = ET_ERR_UNSUPPORTED; break; }
+      y.pairs = (int)pairs;
+      for (int a = 0, k = 0; a < y.axes; ++a)
+        for (int j = 0; j < d.sections[a]; ++j, ++k) {
+          const long double e = d.spectrum == ET_ROTARY_OWN_SPECTRUM ? (long double)j / d.sections[a] : (long double)k / pairs;
+          const long double turns = powl((long double)d.theta, -e) * 0.159154943091895335768883763372514362L;
+          const long double frac = turns - floorl(turns);
+          y.table.axis[k] = (uint8_t)a;
+          y.table.turn[k] = (uint64_t)std::min(ldexpl(frac, 64), 18446744073709551615.0L);
+        }
+    }
+    if (y.kind == ET_LAYER_DROPOUT) {
+      if (y.K != y.N || y.fold != 1 || y.act != ET_ACT_NONE || !(d.drop >= 0.f) || !(d.drop < 1.f)) { err = ET_ERR_INVALID_ARG; break; }
+      // to the nearest multiple of 2^-32; the factor belongs to the rounded probability
+      y.drop_limit = (uint32_t)std::llround((double)d.drop * 4294967296.0);
+      y.drop_scale = (float)(1.0 / (1.0 - y.drop_limit / 4294967296.0));
+    }
+    if (y.kind == ET_LAYER_GATED) {
+      if (d.fold != 2 || d.act == ET_ACT_NONE || d.residual_src != -1) { err = ET_ERR_INVALID_ARG; break; }
+      y.fold = 1; y.act = ET_ACT_NONE; y.gate_act = d.act;
+    }
     if (y.kind == ET_LAYER_NORM) {
       if (y.K != y.N || y.fold != 1 || y.act != ET_ACT_NONE || y.residual_src != -1 || !(y.eps >= 0.f)) {
         err = ET_ERR_INVALID_ARG; break;
@@ -1817,10 +2164,12 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     if (d.residual_src >= 0) {
       if (width[d.residual_src] != y.Nw) { err = ET_ERR_SHAPE; break; }
       if (d.residual_src == 0 && s->ly[0].kind == ET_LAYER_EMBEDDING) { err = ET_ERR_INVALID_ARG; break; }   // a_0 holds ids
-      if (d.residual_src >= 1) {          // a_0's gradient is never formed, no bookkeeping needed
-        LayerRT& src = s->ly[d.residual_src];
+      LayerRT& src = s->ly[d.residual_src];
+      if (d.residual_src >= 1) {
         if (src.consumer >= 0) { err = ET_ERR_UNSUPPORTED; break; }   // one skip consumer per activation
         src.consumer = l;
+      } else {                            // a_0's gradient is formed for et_stack_set_input_gradient only, which takes one consumer
+        src.consumer = src.consumer == -1 ? l : -2;
       }
     }
     if (dtype == ET_BF16) {
@@ -1829,13 +2178,17 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     }
   }
   for (int l = 0; l < L && err == ET_OK; ++l)
-    if (s->ly[l].kind == ET_LAYER_ATTENTION && s->ly[l].consumer >= 0) err = ET_ERR_UNSUPPORTED;   // [q|k|v] feeds nothing else
+    if ((s->ly[l].kind == ET_LAYER_ATTENTION || s->ly[l].kind == ET_LAYER_MASKED_ATTENTION || s->ly[l].kind == ET_LAYER_ROTARY) &&
+        s->ly[l].consumer != -1)
+      err = ET_ERR_UNSUPPORTED;                                       // [q|k|v] feeds nothing else
   // A patch gather followed directly by a dense layer is folded into that layer's GEMMs (the gathered matrix is
   // never formed) when the shapes allow TMA's im2col loads: bf16, channels a multiple of 128 (a 128-row tile of
   // the kernel gradient then lies within one tap), not the first layer (its input would need no gradient).
   for (int l = 1; l + 1 < L && err == ET_OK; ++l) {
     LayerRT& y = s->ly[l];
     const LayerRT& up = s->ly[l + 1];
+    // (same loop) rotary positions behind a dense layer: nothing else reads that layer's output, it is turned where it lies
+    y.in_place = y.kind == ET_LAYER_ROTARY && s->ly[l - 1].kind == ET_LAYER_DENSE;
     y.implicit = dtype == ET_BF16 && y.kind == ET_LAYER_IM2COL && y.K % 128 == 0 && up.kind == ET_LAYER_DENSE &&
                  up.fold == 1 && up.N % 64 == 0;
   }
@@ -1858,9 +2211,16 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
   for (int l = 0; l < L; ++l) {
     LayerRT& y = s->ly[l];
     const size_t act_bytes = (size_t)M * y.Nw * s->elt;
-    if (l < L - 1 && !y.implicit) { y.off_a_out = take(act_bytes); y.off_G_out = take(act_bytes); }
-    if (y.act != ET_ACT_NONE) { y.off_Z = take(act_bytes); y.off_dZ = take(act_bytes); }
-    if (y.kind == ET_LAYER_ATTENTION) {
+    if (y.in_place) { y.off_a_out = s->ly[l - 1].off_a_out; y.off_G_out = s->ly[l - 1].off_G_out; }
+    else if (l < L - 1 && !y.implicit) { y.off_a_out = take(act_bytes); y.off_G_out = take(act_bytes); }
+    if (y.own_dz()) {
+      const size_t z_bytes = (size_t)M * y.dz_width() * s->elt;
+      y.off_Z = take(z_bytes); y.off_dZ = take(z_bytes);
+    }
+    if (y.kind == ET_LAYER_MASKED_ATTENTION) {
+      y.off_lse = take((size_t)2 * y.heads * ceil_div(M, 128) * 128 * sizeof(float));      // log-sum-exp, D
+    } else if (y.kind == ET_LAYER_ROTARY || y.kind == ET_LAYER_DROPOUT) {
+    } else if (y.kind == ET_LAYER_ATTENTION) {
       y.off_lse = take((size_t)M * y.heads * sizeof(float));
     } else if (y.kind == ET_LAYER_BATCHNORM) {
       y.off_stats = take((size_t)y.N * sizeof(float2));
@@ -1882,7 +2242,8 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       y.off_epart = take((size_t)p.chunks * 2 * y.N * sizeof(float));
       max_partial = std::max(max_partial, emb_scratch_rows(y.K, y.N) * y.N * sizeof(float));
     } else if (dtype == ET_BF16) {
-      const int kb_n = ceil_div(y.Nw, et::tc::BK) * y.fold;
+      const int kb_n = ceil_div(y.dz_width(), et::tc::BK) * y.fold;
+      if (y.kind == ET_LAYER_GATED) y.bn_gated = (long long)ceil_div(M, 256) * ceil_div(y.Nw, 128) >= s->sms / 2 ? 128 : 64;
       const TilePlan f = choose_tiles((int)M, y.Nw, ceil_div(y.K, et::tc::BK) * y.fold, s->sms, false, false, 0);
       const TilePlan d = choose_tiles((int)M, y.K, kb_n, s->sms, false, true, 0);
       const TilePlan w = choose_tiles(y.K, y.N, ceil_div(M, et::tc::BK), s->sms, true, false, y.fold > 1 ? y.Nw : 0);
@@ -1945,7 +2306,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
 #ifdef ET_DEBUG_HOOKS
     forced_tiles = getenv("ET_DEBUG_TILES") != nullptr;
 #endif
-    if (y.kind == ET_LAYER_DENSE && dtype == ET_BF16 && y.big_gemm && !forced_tiles) {
+    if (y.gemms() && dtype == ET_BF16 && y.big_gemm && !forced_tiles) {
       const int kb = ceil_div(M, et::tc::BK);
       int sp = std::min(y.split, 2);
       while (sp > 1 && (long long)(sp - 1) * ceil_div(kb, sp) >= kb) --sp;
@@ -1953,7 +2314,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     }
     max_partial = std::max(max_partial, y.vector_params() ? (size_t)y.N * sizeof(float)
                                                           : (size_t)std::max(y.split, y.split_shared) * y.K * y.N * sizeof(float));
-    y.off_biaspart = take((size_t)std::max(chunks, ceil_div(M, 256) * 8 + 8) * y.Nw * sizeof(float));
+    y.off_biaspart = take((size_t)std::max(chunks, ceil_div(M, 256) * 8 + 8) * y.dz_width() * sizeof(float));
     if (y.list_ok) y.off_partial_list = take((size_t)y.split_list * y.K * y.N * sizeof(float));
     y.imp_count_w = y.vector_params() ? ceil_div(y.N, et::kBiasCols)
                                             : ceil_div((long long)y.K * y.N, et::kEltThreads * et::kVec);
@@ -2048,7 +2409,7 @@ et_status et_stack_bind(et_stack* s, void* const* W, void* const* b, void* works
   if (s->dtype == ET_BF16) {
     for (int l = 0; l < s->L; ++l) {
       LayerRT& y = s->ly[l];
-      if (y.kind == ET_LAYER_DENSE) {
+      if (y.gemms()) {
         ET_TRY(make_tmaps(&y.map_W, y.W, y.N, y.K));
         ET_TRY(make_map(&y.map_Wd, y.W, y.N, y.K, y.pair_dgrad ? y.bn_dgrad / 2 : y.bn_dgrad));
         ET_TRY(make_map(&y.map_Wd_sh, y.W, y.N, y.K, y.pair_dgrad_sh ? y.bn_dgrad_sh / 2 : y.bn_dgrad_sh));
@@ -2059,10 +2420,17 @@ et_status et_stack_bind(et_stack* s, void* const* W, void* const* b, void* works
         ET_TRY(make_tmaps(&y.map_Gout, s->at(y.off_G_out), y.Nw, s->M));
       }
       y.im_in_ptr = nullptr; y.im_dg_ptr = nullptr;
+      y.in_heads.ptr = y.out_heads.ptr = y.g_heads.ptr = y.dx_heads.ptr = nullptr;
+      if (y.kind == ET_LAYER_GATED) {
+        for (int i = 0; i < 2; ++i) {
+          ET_TRY(make_part_map(&y.gmaps.w[i], (const bf16*)y.W + (size_t)i * y.Nw, y.Nw, y.K, y.N, y.Nw % 64 == 0 ? y.bn_gated / 64 : -1));
+          ET_TRY(make_part_map(&y.gmaps.out[i], (const bf16*)s->at(y.off_Z) + (size_t)i * y.Nw, y.Nw, s->M, y.N, 0));
+        }
+      }
       if (y.kind == ET_LAYER_DENSE && l >= 1 && s->ly[l - 1].implicit) ET_TRY(make_map(&y.map_Wd_conv, y.W, y.N, y.K, 128));
-      if (y.act != ET_ACT_NONE) {
-        ET_TRY(make_tmaps(&y.map_Z, s->at(y.off_Z), y.Nw, s->M));
-        ET_TRY(make_tmaps(&y.map_dZ, s->at(y.off_dZ), y.Nw, s->M));
+      if (y.own_dz()) {
+        ET_TRY(make_tmaps(&y.map_Z, s->at(y.off_Z), y.dz_width(), s->M));
+        ET_TRY(make_tmaps(&y.map_dZ, s->at(y.off_dZ), y.dz_width(), s->M));
       }
     }
   }
@@ -2081,6 +2449,7 @@ et_status et_stack_bind(et_stack* s, void* const* W, void* const* b, void* works
   s->map_dy_ptr = nullptr;
   s->map_y_ptr = nullptr;
   s->x = nullptr;
+  s->y = nullptr;
   return ET_OK;
 }
 
@@ -2107,6 +2476,8 @@ et_status et_forward_stack(et_stack* s, const void* x, void* y, void* stream) {
   if (s == nullptr || x == nullptr || y == nullptr) return ET_ERR_INVALID_ARG;
   if (!s->bound) return ET_ERR_STATE;
   if (((uintptr_t)x & 15) || ((uintptr_t)y & 15)) return ET_ERR_INVALID_ARG;
+  for (const LayerRT& l : s->ly)
+    if (l.kind == ET_LAYER_ROTARY && l.axes > 1 && s->positions == nullptr) return ET_ERR_STATE;
   cudaStream_t st = (cudaStream_t)stream;
   return s->dtype == ET_BF16 ? forward_impl<bf16>(s, x, y, st) : forward_impl<float>(s, x, y, st);
 }
@@ -2274,6 +2645,51 @@ et_status et_sgd_masked(et_stack* s, const uint8_t* mask, int32_t n_tensors, flo
 et_status et_update_masked(et_stack* s, const uint8_t* mask, int32_t n_tensors, float* const* grads, float lr,
                            void* stream) {
   return update_masked_impl(s, mask, n_tensors, grads, lr, stream, false);
+}
+
+et_status et_stack_set_sequences(et_stack* s, const int32_t* seq_begin, int32_t seqs, const int32_t* prefix) {
+  if (s == nullptr || !has_kind(s, ET_LAYER_MASKED_ATTENTION)) return ET_ERR_INVALID_ARG;
+  if (seq_begin == nullptr) {
+    if (prefix != nullptr) return ET_ERR_INVALID_ARG;
+    seqs = 0;
+  } else if (seqs < 1 || ((uintptr_t)seq_begin & 3) || ((uintptr_t)prefix & 3)) {
+    return ET_ERR_INVALID_ARG;
+  } else if (seqs > (1 << 30)) {
+    return ET_ERR_TOO_LARGE;
+  }
+  s->seq_begin = seq_begin; s->seq_prefix = prefix; s->n_seqs = seqs;
+  return ET_OK;
+}
+et_status et_stack_set_distance_bias(et_stack* s, int32_t layer, const float* slopes) {
+  if (s == nullptr || layer < 0 || layer >= s->L || s->ly[layer].kind != ET_LAYER_MASKED_ATTENTION || ((uintptr_t)slopes & 3))
+    return ET_ERR_INVALID_ARG;
+  s->ly[layer].slopes = slopes;
+  return ET_OK;
+}
+et_status et_stack_set_positions(et_stack* s, const int32_t* positions, int32_t axes) {
+  if (s == nullptr || !has_kind(s, ET_LAYER_ROTARY) || ((uintptr_t)positions & 3)) return ET_ERR_INVALID_ARG;
+  if (positions != nullptr) {
+    if (axes < 1 || axes > 3) return ET_ERR_INVALID_ARG;
+    for (const LayerRT& y : s->ly)
+      if (y.kind == ET_LAYER_ROTARY && y.axes > axes) return ET_ERR_SHAPE;
+  }
+  s->positions = positions;
+  s->position_axes = positions != nullptr ? axes : 0;
+  return ET_OK;
+}
+et_status et_stack_set_dropout_seed(et_stack* s, const uint64_t* seed) {
+  if (s == nullptr || !has_kind(s, ET_LAYER_DROPOUT) || ((uintptr_t)seed & 7)) return ET_ERR_INVALID_ARG;
+  s->drop_seed = seed;
+  return ET_OK;
+}
+et_status et_stack_set_input_gradient(et_stack* s, void* dX) {
+  if (s == nullptr || ((uintptr_t)dX & 15)) return ET_ERR_INVALID_ARG;
+  if (dX != nullptr) {
+    if (s->ly[0].kind == ET_LAYER_EMBEDDING) return ET_ERR_INVALID_ARG;       // its input is token ids
+    if (s->ly[0].consumer == -2) return ET_ERR_UNSUPPORTED;
+  }
+  s->dX = dX;
+  return ET_OK;
 }
 
 et_status et_stack_set_embedding_scale(et_stack* s, float scale) {
@@ -2710,10 +3126,9 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
         t_dw[2 * l] = 0.0; t_dw[2 * l + 1] = 0.0;
         double t_attn = 0.0;
         if (l >= 1) {
-          if (s->ly[l].kind == ET_LAYER_ATTENTION) ET_TRY(timed([&]() { return run_attn_backward(s, l, dY, st); }, &t_attn));
-          else if (s->ly[l].implicit) t_attn = 0.0;       // part of the error-gradient GEMM of the layer above
-          else if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_im2col_backward<bf16>(s, l, dY, st); }, &t_attn));
-          else ET_TRY(timed([&]() { return run_im2col_backward<float>(s, l, dY, st); }, &t_attn));
+          if (s->ly[l].implicit) t_attn = 0.0;            // part of the error-gradient GEMM of the layer above
+          else if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_plain_backward<bf16>(s, l, dY, st); }, &t_attn));
+          else ET_TRY(timed([&]() { return run_plain_backward<float>(s, l, dY, st); }, &t_attn));
         }
         pending_nontrainable += t_attn;
         continue;
@@ -2762,6 +3177,13 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
         }
         t_dy[2 * l + 1] = t_box + t_beta;
         continue;
+      }
+      if (s->ly[l].kind == ET_LAYER_GATED) {
+        // its activation and product: non-trainable work above the layer's own tensors (Section 5.3), like a layer of its own
+        double t_gate = 0.0;
+        if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_gated_backward<bf16>(s, l, dY, st); }, &t_gate));
+        else ET_TRY(timed([&]() { return run_gated_backward<float>(s, l, dY, st); }, &t_gate));
+        t_dy[2 * l + 1] += t_gate;
       }
       if (s->dtype == ET_BF16) {
         if (l >= 1) ET_TRY(timed([&]() { return run_dgrad_layer<bf16>(s, l, dY, st); }, &t_dy[2 * l]));

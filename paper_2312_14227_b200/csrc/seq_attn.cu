@@ -1,0 +1,88 @@
+// Launches of the sequence attention kernels: one instance per padded head width, capped or not, with a distance bias or not.
+#include "seq_attn.cuh"
+
+#include <mutex>
+
+namespace et {
+namespace seqattn {
+namespace {
+
+std::mutex g_mutex;
+
+// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
+template <auto kern>
+cudaError_t allow(uint32_t bytes) {
+  static bool done[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_mutex);
+  if (done[dev]) return cudaSuccess;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  done[dev] = e == cudaSuccess;
+  return e;
+}
+// The kernels begin with chain_begin(): their launch latency overlaps the stream's previous kernel.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kern)(P...), unsigned grid, unsigned block, uint32_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+template <typename F>
+cudaError_t by_form(const Args& a, F&& f) {
+  auto with = [&](auto wide, auto cap) {
+    return a.slopes != nullptr ? f(wide, cap, std::true_type()) : f(wide, cap, std::false_type());
+  };
+  auto both = [&](auto wide) { return a.cap > 0.0f ? with(wide, std::true_type()) : with(wide, std::false_type()); };
+  return a.dim > 64 ? both(std::integral_constant<int, 128>()) : both(std::integral_constant<int, 64>());
+}
+
+}  // namespace
+
+cudaError_t forward(const CUtensorMap& qkv128, const CUtensorMap& out128, Args a, int sms, cudaStream_t st) {
+  // two halves a block where that still gives every SM a block: the tensor core then works on one half's products during the
+  // other's exponentials; else twice the blocks of one half
+  const long long pairs = (long long)((a.mask.M + 255) / 256) * a.heads;
+  a.halves = pairs >= sms ? 2 : 1;
+  const unsigned grid = (unsigned)((a.mask.M + 128 * a.halves - 1) / (128 * a.halves)) * (unsigned)a.heads;
+  return by_form(a, [&](auto wide, auto cap, auto bias) -> cudaError_t {
+    constexpr auto kern = forward_kernel<decltype(wide)::value, decltype(cap)::value, decltype(bias)::value>;
+    constexpr uint32_t smem = FwdCfg<decltype(wide)::value>::SMEM;
+    const cudaError_t e = allow<kern>(smem);
+    return e != cudaSuccess ? e : launch(kern, grid, THREADS, smem, st, qkv128, out128, a);
+  });
+}
+
+cudaError_t backward(const CUtensorMap& qkv128, const CUtensorMap& qkv64, const CUtensorMap& g128, const CUtensorMap& g64,
+                     const CUtensorMap& dqkv128, const void* out, const void* dout, Args a, int sms, cudaStream_t st) {
+  (void)sms;
+  const long long threads = (long long)a.mask.M * a.heads * 16;
+  cudaError_t e = launch(dot_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, (const bf16*)out, (const bf16*)dout, a.D,
+                         a.mask.M, a.heads, a.dim, a.ld);
+  if (e != cudaSuccess) return e;
+  const unsigned tiles = (unsigned)((a.mask.M + 127) / 128);
+  return by_form(a, [&](auto wide, auto cap, auto bias) -> cudaError_t {
+    constexpr int W = decltype(wide)::value;
+    constexpr auto dq = backward_kernel<W, false, decltype(cap)::value, decltype(bias)::value>;
+    constexpr auto dkv = backward_kernel<W, true, decltype(cap)::value, decltype(bias)::value>;
+    constexpr uint32_t smem = BwdCfg<W>::SMEM;
+    cudaError_t r = allow<dq>(smem);
+    if (r == cudaSuccess) r = allow<dkv>(smem);
+    if (r == cudaSuccess) r = launch(dq, tiles * a.heads, THREADS, smem, st, qkv128, g128, qkv64, g64, dqkv128, a);
+    if (r == cudaSuccess) r = launch(dkv, tiles * a.kv, THREADS, smem, st, qkv128, g128, qkv64, g64, dqkv128, a);
+    return r;
+  });
+}
+
+}  // namespace seqattn
+}  // namespace et

@@ -1,0 +1,37 @@
+// Launches of the kernels in seq_attn.cuh, compiled in a unit of their own.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace et {
+namespace seqattn {
+
+struct Mask {
+  const int32_t* begin;     // [n + 1] or nullptr: sequences of `len` rows
+  const int32_t* prefix;    // [n] or nullptr
+  int n, len, M;
+  bool causal;
+};
+struct Args {
+  Mask mask;
+  float* lse;               // [heads][ld]: log2 of the sum of 2^(s log2 e); +inf for a row without keys
+  float* D;                 // [heads][ld]
+  const float* slopes;      // [heads] or nullptr
+  uint32_t* status;
+  int heads, kv, dim, ld;   // ld: M rounded up to a multiple of 128
+  int halves;               // forward: 1 or 2 halves of 128 rows a block
+  float scale, cap;
+};
+
+// qkv128: 128-row boxes of the input, out128: of the output
+cudaError_t forward(const CUtensorMap& qkv128, const CUtensorMap& out128, Args a, int sms, cudaStream_t st);
+// Three launches: D, dq, (dk, dv).  64: 64-row boxes; g: the output's gradient; dqkv: where the input's gradient goes
+cudaError_t backward(const CUtensorMap& qkv128, const CUtensorMap& qkv64, const CUtensorMap& g128, const CUtensorMap& g64,
+                     const CUtensorMap& dqkv128, const void* out, const void* dout, Args a, int sms, cudaStream_t st);
+constexpr int kForwardLaunches = 1, kBackwardLaunches = 3;
+
+}  // namespace seqattn
+}  // namespace et

@@ -188,13 +188,13 @@ et_status make_part_map(CUtensorMap* m, const void* ptr, int inner, long long ou
   }
   return ET_OK;
 }
-// Rows of `blocks` head blocks of `dim` columns: one box is 64 columns of one block x box_rows rows, columns past the block zero.
-et_status make_head_map(CUtensorMap* m, const void* ptr, int dim, int blocks, long long rows, int box_rows) {
+// Rows of `blocks` head blocks of `dim` columns: one box is 64 columns of one block x 128 rows, columns past the block zero.
+et_status make_head_map(CUtensorMap* m, const void* ptr, int dim, int blocks, long long rows) {
   EncodeTiledFn fn = get_encode_fn();
   if (fn == nullptr) return ET_ERR_CUDA;
   cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)blocks, (cuuint64_t)rows};
   cuuint64_t strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)dim * blocks * 2};
-  cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows};
+  cuuint32_t box[3] = {64, 1, 128};
   cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
@@ -207,14 +207,13 @@ et_status make_head_map(CUtensorMap* m, const void* ptr, int dim, int blocks, lo
 }
 // The same matrix by heads, made again when its address has changed.
 struct HeadMaps {
-  CUtensorMap b128, b64;
+  CUtensorMap map;
   const void* ptr = nullptr;
 };
 et_status head_maps(HeadMaps* h, const void* ptr, int dim, int blocks, long long rows) {
   if (h->ptr == ptr) return ET_OK;
   h->ptr = nullptr;
-  ET_TRY(make_head_map(&h->b128, ptr, dim, blocks, rows, 128));
-  ET_TRY(make_head_map(&h->b64, ptr, dim, blocks, rows, 64));
+  ET_TRY(make_head_map(&h->map, ptr, dim, blocks, rows));
   h->ptr = ptr;
   return ET_OK;
 }
@@ -1060,7 +1059,7 @@ et_status run_seq_forward(et_stack* s, int l, void* y, cudaStream_t st) {
   LayerRT& L = s->ly[l];
   ET_TRY(head_maps(&L.in_heads, act_in<bf16>(s, l), L.dim, L.heads + 2 * L.kv, s->M));
   ET_TRY(head_maps(&L.out_heads, act_out<bf16>(s, l, y), L.dim, L.heads, s->M));
-  return cuda_status(et::seqattn::forward(L.in_heads.b128, L.out_heads.b128, seq_args(s, l), s->sms, st), et::seqattn::kForwardLaunches);
+  return cuda_status(et::seqattn::forward(L.in_heads.map, L.out_heads.map, seq_args(s, l), s->sms, st), et::seqattn::kForwardLaunches);
 }
 // G_l (gradient of [q | k | v]) from G_{l+1}; the layer below has no activation, so G_l is its dZ.
 et_status run_seq_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
@@ -1072,7 +1071,7 @@ et_status run_seq_backward(et_stack* s, int l, const void* dY, cudaStream_t st) 
   ET_TRY(head_maps(&L.in_heads, act_in<bf16>(s, l), L.dim, L.heads + 2 * L.kv, s->M));
   ET_TRY(head_maps(&L.g_heads, dout, L.dim, L.heads, s->M));
   ET_TRY(head_maps(&L.dx_heads, dx, L.dim, L.heads + 2 * L.kv, s->M));
-  return cuda_status(et::seqattn::backward(L.in_heads.b128, L.in_heads.b64, L.g_heads.b128, L.g_heads.b64, L.dx_heads.b128, out, dout,
+  return cuda_status(et::seqattn::backward(L.in_heads.map, L.g_heads.map, L.dx_heads.map, out, dout, const_cast<void*>(dx),
                                            seq_args(s, l), s->sms, st), et::seqattn::kBackwardLaunches);
 }
 

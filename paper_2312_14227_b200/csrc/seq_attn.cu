@@ -25,17 +25,20 @@ cudaError_t allow(uint32_t bytes) {
 }
 // The kernels begin with chain_begin(): their launch latency overlaps the stream's previous kernel.
 template <typename... P, typename... A>
-cudaError_t launch(void (*kern)(P...), unsigned grid, unsigned block, uint32_t smem, cudaStream_t st, A&&... args) {
+cudaError_t launch(void (*kern)(P...), unsigned grid, unsigned block, uint32_t smem, cudaStream_t st, unsigned parts, A&&... args) {
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = parts;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = parts > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
 }
 template <typename F>
@@ -49,7 +52,7 @@ cudaError_t by_form(const Args& a, F&& f) {
 
 }  // namespace
 
-cudaError_t forward(const CUtensorMap& qkv128, const CUtensorMap& out128, Args a, int sms, cudaStream_t st) {
+cudaError_t forward(const CUtensorMap& qkv, const CUtensorMap& out, Args a, int sms, cudaStream_t st) {
   // two halves a block where that still gives every SM a block: the tensor core then works on one half's products during the
   // other's exponentials; else twice the blocks of one half
   const long long pairs = (long long)((a.mask.M + 255) / 256) * a.heads;
@@ -59,15 +62,13 @@ cudaError_t forward(const CUtensorMap& qkv128, const CUtensorMap& out128, Args a
     constexpr auto kern = forward_kernel<decltype(wide)::value, decltype(cap)::value, decltype(bias)::value>;
     constexpr uint32_t smem = FwdCfg<decltype(wide)::value>::SMEM;
     const cudaError_t e = allow<kern>(smem);
-    return e != cudaSuccess ? e : launch(kern, grid, THREADS, smem, st, qkv128, out128, a);
+    return e != cudaSuccess ? e : launch(kern, grid, THREADS, smem, st, 1, qkv, out, a);
   });
 }
 
-cudaError_t backward(const CUtensorMap& qkv128, const CUtensorMap& qkv64, const CUtensorMap& g128, const CUtensorMap& g64,
-                     const CUtensorMap& dqkv128, const void* out, const void* dout, Args a, int sms, cudaStream_t st) {
-  (void)sms;
+cudaError_t backward(const CUtensorMap& qkv, const CUtensorMap& g, const CUtensorMap& gqkv, const void* out, const void* dout, void* dqkv, Args a, int sms, cudaStream_t st) {
   const long long threads = (long long)a.mask.M * a.heads * 16;
-  cudaError_t e = launch(dot_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, (const bf16*)out, (const bf16*)dout, a.D,
+  cudaError_t e = launch(dot_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, 1, (const bf16*)out, (const bf16*)dout, a.D,
                          a.mask.M, a.heads, a.dim, a.ld);
   if (e != cudaSuccess) return e;
   const unsigned tiles = (unsigned)((a.mask.M + 127) / 128);
@@ -78,8 +79,16 @@ cudaError_t backward(const CUtensorMap& qkv128, const CUtensorMap& qkv64, const 
     constexpr uint32_t smem = BwdCfg<W>::SMEM;
     cudaError_t r = allow<dq>(smem);
     if (r == cudaSuccess) r = allow<dkv>(smem);
-    if (r == cudaSuccess) r = launch(dq, tiles * a.heads, THREADS, smem, st, qkv128, g128, qkv64, g64, dqkv128, a);
-    if (r == cudaSuccess) r = launch(dkv, tiles * a.kv, THREADS, smem, st, qkv128, g128, qkv64, g64, dqkv128, a);
+    // Few items, or key heads that many query heads share: a cluster of blocks takes an item's tiles in turn and joins the sums, until
+    // there are two blocks an SM (so that causal items, the longest twice the mean, even out) or fewer than two tiles a block.
+    auto parts = [&](long long items, long long tiles_each) {
+      unsigned n = 1;
+      while (n < 8 && items * n < 2 * sms && tiles_each >= 4 * n) n *= 2;
+      return n;
+    };
+    const unsigned pq = parts(tiles * a.heads, tiles), pk = parts(tiles * a.kv, (long long)tiles * (a.heads / a.kv));
+    if (r == cudaSuccess) r = launch(dq, tiles * a.heads * pq, THREADS, smem, st, pq, qkv, g, gqkv, (bf16*)dqkv, a);
+    if (r == cudaSuccess) r = launch(dkv, tiles * a.kv * pk, THREADS, smem, st, pk, qkv, g, gqkv, (bf16*)dqkv, a);
     return r;
   });
 }

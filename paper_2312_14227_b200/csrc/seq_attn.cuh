@@ -36,8 +36,6 @@ using namespace et::tc;
 constexpr uint32_t kTimeoutSeqAttn = 8;
 constexpr int THREADS = 320;                    // warps 0-3, 4-7: row threads; warp 8: MMA issue, TMEM; warp 9: TMA
 constexpr uint32_t CHUNK = 16384;               // 128 rows x 64 columns of bf16
-constexpr uint32_t HCHUNK = 8192;               // 64 rows x 64 columns
-constexpr int STREAM = 64;                      // rows of a streamed tile of the backward pass
 constexpr float LOG2E = 1.4426950408889634f;
 
 // ---- intervals ---------------------------------------------------------------------------------
@@ -86,10 +84,11 @@ __device__ __forceinline__ int2 interval(const Mask& m, int row, int lane) {
   }
   return e > b ? make_int2(b, e) : make_int2(0, 0);
 }
-// Rows that belong to some sequence: [first, last).
+// Rows outside [x, y) are of no sequence.  (Rows from M on need no care: they arrive as 0.)
 __device__ __forceinline__ int2 used_rows(const Mask& m) {
-  if (m.begin == nullptr) return make_int2(0, m.M);
-  return make_int2(min(max(m.begin[0], 0), m.M), min(max(m.begin[m.n], 0), m.M));
+  if (m.begin == nullptr) return make_int2(0, 0x7fffffff);
+  const int e = min(max(m.begin[m.n], 0), m.M);
+  return make_int2(min(max(m.begin[0], 0), m.M), e == m.M ? 0x7fffffff : e);
 }
 
 // ---- tensor memory -----------------------------------------------------------------------------
@@ -124,13 +123,92 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                : "memory");
 }
 __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
-
-// K-major operand of tiles of `chunk` bytes a 64-column piece
-__device__ __forceinline__ uint64_t kdesc(uint32_t tile, int ks, uint32_t chunk) {
-  return make_desc(tile + (uint32_t)(ks >> 2) * chunk + (uint32_t)(ks & 3) * 32u, 16, 1024);
+// The warp that issues products runs its loop as a whole on values that the compiler can see to be the same in every lane, and one
+// elected lane issues: descriptors then stay in uniform registers.  (Issued from a branch of lane 0 a product cost 50 to 60 cycles of that lane's time,
+// whatever its size, and the issuing warp was what bounded both passes.)
+__device__ __forceinline__ bool elect() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
 }
-__device__ __forceinline__ uint64_t mndesc(uint32_t tile, int ks, uint32_t chunk) {
-  return make_desc(tile + (uint32_t)ks * 2048u, chunk, 1024);
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, kTimeoutSeqAttn));
+}
+
+// Descriptors of a tile's first step; a step moves the address field (16-byte units) by a constant, so that a product costs the issuing
+// thread little more than the instruction itself (its instructions, not the tensor core, bounded the first version).
+// K-major, pieces of 64 columns `CHUNK_B` bytes apart: 16 columns = 32 bytes along the swizzled row.  MN-major: 16 rows = 2048 bytes.
+__device__ __forceinline__ uint64_t k_desc(uint32_t tile) { return make_desc(tile, 16, 1024); }
+__device__ __forceinline__ uint64_t mn_desc(uint32_t tile, uint32_t chunk) { return make_desc(tile, chunk, 1024); }
+template <uint32_t CHUNK_B> __device__ __forceinline__ constexpr uint64_t k_step(int ks) { return ((ks >> 2) * CHUNK_B + (ks & 3) * 32u) >> 4; }
+__device__ __forceinline__ constexpr uint64_t mn_step(int ks) { return (uint64_t)ks * (2048u >> 4); }
+// D = A B^T over K columns, both K-major
+template <int K, uint32_t CHUNK_A, uint32_t CHUNK_B>
+__device__ __forceinline__ void product_ss(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc) {
+  tc_mma(d, da, db, idesc, 0u);
+#pragma unroll
+  for (int ks = 1; ks < K / UK; ++ks) tc_mma(d, da + k_step<CHUNK_A>(ks), db + k_step<CHUNK_B>(ks), idesc, 1u);
+}
+
+// Pairs of fp32 values in one instruction
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t both(float a) { return pair(a, a); }
+__device__ __forceinline__ float max_nan(float a, float b) {                   // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float2 ex2_of(uint64_t x) {
+  const float2 v = unpair(x);
+  return make_float2(attn::ex2(v.x), attn::ex2(v.y));
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ float ld_peer(uint32_t addr, uint32_t cta) {       // the same place in another block's shared memory
+  float v;
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(addr), "r"(cta));
+  return v;
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
 }
 
 // tanh from one exponential and one reciprocal: exp overflow gives 1, underflow -1, absolute error near 2^-23
@@ -164,6 +242,7 @@ struct FwdCfg {
   static constexpr uint32_t SMEM = (2 + ST) * TILE + 1024 + 256;
 };
 
+// P of a tile's first 96 keys is handed over by itself, so that its product runs under the exponentials of the last 32.
 template <int DHP, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(THREADS, 1)
 forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constant__ CUtensorMap map_out, const Args a) {
@@ -176,15 +255,15 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
   const uint32_t ring = base + 2 * C::TILE, bars = base + (2 + ST) * C::TILE;
   const uint32_t bar_q = bars;
   auto bar_s = [&](int h) { return bars + 8u + 8u * h; };         // scores of half h complete (and every product before)
-  auto bar_p = [&](int h) { return bars + 24u + 8u * h; };        // P of half h is in tensor memory
-  auto full = [&](int s) { return bars + 40u + 8u * s; };
-  auto empty = [&](int s) { return bars + 40u + 8u * (ST + s); };
+  auto bar_p = [&](int h, int k) { return bars + 24u + 16u * h + 8u * k; };    // P of half h, keys 0-95 and 96-127, in tensor memory
+  auto full = [&](int s) { return bars + 56u + 8u * s; };
+  auto empty = [&](int s) { return bars + 56u + 8u * (ST + s); };
   int* shared = reinterpret_cast<int*>(gen + (2 + ST) * C::TILE + 160);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(shared);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   int* extent = shared + 2;                                       // lo, hi of half 0, of half 1
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int tiles = (a.mask.M + 128 * a.halves - 1) / (128 * a.halves);
   const int h = blockIdx.x % a.heads;
   // causal rows see the more keys the later they come: the longest blocks start first
@@ -196,7 +275,11 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
     prefetch_tmap(&map_qkv);
     prefetch_tmap(&map_out);
     mbar_init(bar_q, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(bar_s(i), 1); mbar_init(bar_p(i), 128); extent[2 * i] = 0x7fffffff; extent[2 * i + 1] = 0; }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_s(i), 1);
+      for (int k = 0; k < 2; ++k) mbar_init(bar_p(i, k), 4);
+      extent[2 * i] = 0x7fffffff; extent[2 * i + 1] = 0;
+    }
     for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     *abort_flag = 0;
     fence_async_smem();
@@ -209,24 +292,25 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
   chain_begin();
   if (warp == 9 && lane == 0) {
     mbar_expect_tx(bar_q, (uint32_t)a.halves * C::TILE);
     for (int hf = 0; hf < a.halves; ++hf)
       for (int c = 0; c < C::CH; ++c) tma_load_3d(base + hf * C::TILE + c * CHUNK, &map_qkv, bar_q, c * 64, h, row0 + hf * 128);
   }
+  const int my_half = warp >> 2, trow = threadIdx.x & 127, row = row0 + my_half * 128 + trow;
   int2 iv = make_int2(0, 0);
   if (warp < 8) {
-    if ((warp >> 2) < a.halves) iv = interval<false>(a.mask, row0 + (int)threadIdx.x, lane);
-    note_extent(extent + 2 * (warp >> 2), extent + 2 * (warp >> 2) + 1, iv);
+    if (my_half < a.halves) iv = interval<false>(a.mask, row, lane);
+    note_extent(extent + 2 * my_half, extent + 2 * my_half + 1, iv);
   }
   __syncthreads();
   // tiles of 128 keys that each half walks; the stream covers both
   int first[2], last[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int lo = extent[2 * i], hi = extent[2 * i + 1];
+    const int lo = uniform(extent[2 * i]), hi = uniform(extent[2 * i + 1]);
     first[i] = hi > lo ? lo / 128 : 0;
     last[i] = hi > lo ? (hi + 127) / 128 : 0;
   }
@@ -257,58 +341,69 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
     }
   } else if (warp == 8) {
     const uint32_t id_s = attn::idesc128(128, false, false), id_o = attn::idesc128(DHP, false, true);
+    const uint64_t dq0 = k_desc(base), dk0 = k_desc(ring), dv0 = mn_desc(ring, CHUNK);
     const int2 used = used_rows(a.mask);
-    bool ok = n_tiles == 0 || mbar_wait(bar_q, 0, abort_flag, a.status, kTimeoutSeqAttn);
-    int np[2] = {0, 0};                                           // products P v issued per half
-    for (int t = T0 - 1; t < T1 && ok; ++t) {
-      const int ik = 2 * (t + 1 - T0), iv_ = 2 * (t - T0) + 1;    // stream positions of K of tile t + 1 and V of tile t
-      const int sk = ik % ST, sv = iv_ < 0 ? 0 : iv_ % ST;
+    bool ok = n_tiles == 0 || warp_wait(bar_q, 0, abort_flag, a.status);
+    uint32_t np[2] = {0, 0};                                      // tiles of each half whose P v has been issued
+    int ik = 0;                                                   // stream position of K of tile t + 1; V of tile t is the one before
+    for (int t = T0 - 1; t < T1 && n_tiles > 0 && ok; ++t, ik += 2) {
+      const int sk = ik % ST, sv = ik == 0 ? 0 : (ik - 1) % ST;
       const bool has_k = t + 1 < T1, has_v = t >= T0;
-      if (has_k) ok = mbar_wait(full(sk), (uint32_t)(ik / ST) & 1u, abort_flag, a.status, kTimeoutSeqAttn);
-      if (ok && has_v) ok = mbar_wait(full(sv), (uint32_t)(iv_ / ST) & 1u, abort_flag, a.status, kTimeoutSeqAttn);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      if (has_v && (t * 128 < used.x || (t + 1) * 128 > used.y)) {
-        scrub(gen + (2 + sv) * C::TILE, 128, C::CH, CHUNK, t * 128, used, lane);
-        fence_async_smem();
-        __syncwarp();
+      if (has_v) {
+        ok = warp_wait(full(sv), (uint32_t)((ik - 1) / ST) & 1u, abort_flag, a.status);
+        if (!ok) break;
+        if (t * 128 < used.x || (t + 1) * 128 > used.y) {
+          scrub(gen + (2 + sv) * C::TILE, 128, C::CH, CHUNK, t * 128, used, lane);
+          fence_async_smem();
+          __syncwarp();
+        }
       }
-      tc_fence_after();
+      if (has_k) ok = warp_wait(full(sk), (uint32_t)(ik / ST) & 1u, abort_flag, a.status);
+      if (!ok) break;
+#pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         const bool pv = t >= first[hf] && t < last[hf], nx = t + 1 >= first[hf] && t + 1 < last[hf];
-        if (!pv && !nx) continue;
+        if (!ok || (!pv && !nx)) continue;
         const uint32_t S = tmem + hf * 128, O = tmem + 256 + hf * DHP;
+        const uint64_t dv = dv0 + (uint32_t)sv * (C::TILE >> 4), dk = dk0 + (uint32_t)sk * (C::TILE >> 4);
+        const uint32_t add = np[hf] > 0 ? 1u : 0u;
         if (pv) {
-          ok = __all_sync(0xffffffffu, mbar_wait(bar_p(hf), (uint32_t)np[hf] & 1u, abort_flag, a.status, kTimeoutSeqAttn));
-          if (!ok) break;
+          ok = warp_wait(bar_p(hf, 0), np[hf] & 1u, abort_flag, a.status);
+          if (!ok) continue;
           tc_fence_after();
-          if (lane == 0)
-            for (int ks = 0; ks < 8; ++ks)
-              mma_ts(O, S + ks * 8, mndesc(ring + sv * C::TILE, ks, CHUNK), id_o, (np[hf] > 0 || ks > 0) ? 1u : 0u);
+          if (elect()) {
+            mma_ts(O, S, dv, id_o, add);
+#pragma unroll
+            for (int ks = 1; ks < 6; ++ks) mma_ts(O, S + ks * 8, dv + mn_step(ks), id_o, 1u);
+          }
+          ok = warp_wait(bar_p(hf, 1), np[hf] & 1u, abort_flag, a.status);
+          if (!ok) continue;
+          tc_fence_after();
           ++np[hf];
         }
-        if (lane == 0) {
-          if (nx)
-            for (int ks = 0; ks < DHP / UK; ++ks)
-              tc_mma(S, kdesc(base + hf * C::TILE, ks, CHUNK), kdesc(ring + sk * C::TILE, ks, CHUNK), id_s, ks > 0 ? 1u : 0u);
+        if (elect()) {
+          if (pv) {
+#pragma unroll
+            for (int ks = 6; ks < 8; ++ks) mma_ts(O, S + ks * 8, dv + mn_step(ks), id_o, 1u);
+          }
+          if (nx) product_ss<DHP, CHUNK, CHUNK>(S, dq0 + (uint32_t)hf * (C::TILE >> 4), dk, id_s);
           tc_commit(bar_s(hf));                                   // next scores, or after the last tile the output
         }
-        __syncwarp();
       }
-      if (lane == 0) {
+      if (ok && elect()) {
         if (has_k) tc_commit(empty(sk));
         if (has_v) tc_commit(empty(sv));
       }
-      __syncwarp();
     }
-  } else if ((warp >> 2) < a.halves) {
-    const int hf = warp >> 2;
-    const int trow = threadIdx.x & 127, row = row0 + (int)threadIdx.x;
+    __syncwarp();
+  } else if (my_half < a.halves) {
+    const int hf = my_half;
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t S = tmem + lane_addr + hf * 128, O = tmem + lane_addr + 256 + hf * DHP;
     const float c2 = a.scale * LOG2E;
     const float slope2 = BIAS ? a.slopes[h] * LOG2E : 0.0f;
-    float m = -INFINITY, sum = 0.0f;
+    float m = -INFINITY;
+    uint64_t sum2 = 0;
     bool ok = true;
     const int n_own = last[hf] - first[hf];
     for (int i = 0; i < n_own && ok; ++i) {
@@ -342,17 +437,19 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
           for (int j = 0; j < 32; ++j)
             if ((unsigned)(c * 32 + j - lo) >= len) v[c][j] = -INFINITY;
       }
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      float mx[4];
 #pragma unroll
-      for (int j = 0; j < 32; ++j)
+      for (int c = 0; c < 4; ++c) {
+        mx[c] = max_nan(v[c][0], v[c][1]);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) mx[c] = fmaxf(mx[c], v[c][j]);
-      float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        for (int j = 2; j < 32; j += 2) mx[c] = max3_nan(mx[c], v[c][j], v[c][j + 1]);
+      }
+      float top = max_nan(max_nan(mx[0], mx[1]), max_nan(mx[2], mx[3]));
       if (!(CAP || BIAS)) top *= c2;                              // scale > 0: the largest score stays the largest
-      if (__any_sync(0xffffffffu, top > m + 8.0f)) {
-        const float m_new = fmaxf(m, top);
+      if (__any_sync(0xffffffffu, !(top <= m + 8.0f))) {           // (NaN counts as grown, too, and stays)
+        const float m_new = max_nan(m, top);
         const float f = m == -INFINITY ? 0.0f : attn::ex2(m - m_new);
-        sum *= f;
+        sum2 = mul2(sum2, both(f));
         m = m_new;
         if (i > 0) {                                              // the output so far is complete: bar_s follows it
 #pragma unroll 1
@@ -367,32 +464,34 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
         }
       }
       const float mm = m == -INFINITY ? 0.0f : m;
-      float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      const uint64_t neg_m = both(-mm), factor = both(c2);
 #pragma unroll
-      for (int c = 0; c < 4; c += 2) {
-        uint32_t r[32];
+      for (int c = 0; c < 4; ++c) {
+        uint32_t r[16];
 #pragma unroll
-        for (int d = 0; d < 2; ++d)
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            const float p0 = attn::ex2((CAP || BIAS) ? v[c + d][j] - mm : fmaf(v[c + d][j], c2, -mm));
-            const float p1 = attn::ex2((CAP || BIAS) ? v[c + d][j + 1] - mm : fmaf(v[c + d][j + 1], c2, -mm));
-            part[2 * d] += p0;
-            part[2 * d + 1] += p1;
-            r[d * 16 + j / 2] = pack_bf16x2(p0, p1);
-          }
-        tmem_st32(S + c * 16, r);
+        for (int j = 0; j < 32; j += 2) {
+          const uint64_t x = pair(v[c][j], v[c][j + 1]);
+          const float2 e = ex2_of(CAP || BIAS ? add2(x, neg_m) : fma2(x, factor, neg_m));
+          sum2 = add2(sum2, pair(e.x, e.y));
+          r[j / 2] = pack_bf16x2(e.x, e.y);
+        }
+        tmem_st16(S + c * 16, r);
+        if (c >= 2) {
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_p(hf, c - 2));
+        }
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive(bar_p(hf));
     }
     if (ok && n_own > 0) ok = mbar_wait(bar_s(hf), (uint32_t)n_own & 1u, abort_flag, a.status, kTimeoutSeqAttn);
     if (ok) ok = mbar_wait(bar_q, 0, abort_flag, a.status, kTimeoutSeqAttn);       // Q's tile takes the output
     if (ok) {
       tc_fence_after();
-      const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+      const float2 halves = unpair(sum2);
+      const float sum = halves.x + halves.y;
+      // (+inf scores have no softmax)
+      const float inv = !(m < INFINITY) ? NAN : sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
       uint8_t* out = gen + hf * C::TILE;
 #pragma unroll 1
       for (int c = 0; c < DHP / 32; ++c) {
@@ -446,20 +545,21 @@ dot_kernel(const bf16* __restrict__ out, const bf16* __restrict__ dout, float* _
 template <int DHP>
 struct BwdCfg {
   static constexpr int CH = DHP / 64;
-  static constexpr uint32_t TILE = CH * CHUNK;                   // resident, 128 rows
-  static constexpr uint32_t HALF = CH * HCHUNK;                  // streamed, 64 rows
-  static constexpr uint32_t STAGE = 2 * HALF + 1024;             // two tiles, the rows' lse and D
-  static constexpr int ST = DHP == 128 ? 4 : 6;
+  static constexpr uint32_t TILE = CH * CHUNK;                   // 128 rows, resident or streamed
+  static constexpr uint32_t STAGE = 2 * TILE + 1024;             // two tiles, the rows' lse and D
+  static constexpr int ST = DHP == 128 ? 2 : 4;
   static constexpr uint32_t SMEM = 2 * TILE + ST * STAGE + 1024 + 256;
 };
 
 // DKV = false: X1 = q, X2 = dO (rows of head h), Y1 = k, Y2 = v;  acc1 = dq.
 // DKV = true:  X1 = k, X2 = v (keys of a key head), Y1 = q, Y2 = dO of every head of its group;  acc1 = dk, acc2 = dv.
+// Tensor memory: acc1, acc2, S (P over it), dP (dS over it).  One product's accumulator is worked on while the tensor core forms the
+// others: per tile   P(i) | dK(i-1), dP(i)    then    dS(i) | dV(i), S(i+1).
+// The products are 128 wide: narrower ones take the tensor core as long (measured 57 to 75 cycles an instruction at 64 and 128 columns).
 template <int DHP, bool DKV, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(THREADS, 1)
-backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_xg,
-                const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_yg,
-                const __grid_constant__ CUtensorMap map_out, const Args a) {
+backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_g,
+                const __grid_constant__ CUtensorMap map_out, bf16* __restrict__ dqkv, const Args a) {
   using C = BwdCfg<DHP>;
   constexpr int ST = C::ST;
   extern __shared__ uint8_t smem_raw[];
@@ -468,8 +568,8 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   uint8_t* gen = smem_raw + (base - raw);
   const uint32_t ring = base + 2 * C::TILE, bars = ring + ST * C::STAGE;
   const uint32_t bar_x = bars, bar_done = bars + 8;
-  auto bar_s = [&](int w) { return bars + 16u + 8u * w; };        // S and dP of the tile that group w works on
-  auto bar_p = [&](int w) { return bars + 32u + 8u * w; };        // P and dS are in tensor memory
+  const uint32_t bar_s = bars + 16, bar_dp = bars + 24;           // S, dP of a tile complete
+  const uint32_t bar_p = bars + 32, bar_ds = bars + 40;           // S read, and P in its place (dk, dv);  dS in dP's place
   auto full = [&](int s) { return bars + 48u + 8u * s; };
   auto empty = [&](int s) { return bars + 48u + 8u * (ST + s); };
   int* shared = reinterpret_cast<int*>(gen + 2 * C::TILE + ST * C::STAGE + 160);
@@ -477,18 +577,20 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   volatile uint32_t* abort_flag = tmem_slot + 1;
   int* extent = shared + 2;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int blocks_h = DKV ? a.kv : a.heads, group = a.heads / a.kv;
   const int tiles = (a.mask.M + 127) / 128;
-  const int h = blockIdx.x % blocks_h;                            // head, or key head
-  const int tile = a.mask.causal && !DKV ? tiles - 1 - (int)(blockIdx.x / blocks_h) : (int)(blockIdx.x / blocks_h);
+  const int parts = (int)cluster_size(), part = (int)cluster_ctarank();       // blocks of a cluster share an item's tiles
+  const int item = blockIdx.x / parts;
+  const int h = item % blocks_h;                                  // head, or key head
+  const int tile = a.mask.causal && !DKV ? tiles - 1 - item / blocks_h : item / blocks_h;
   const int row0 = tile * 128;
 
   if (threadIdx.x == 0) {
-    prefetch_tmap(&map_x); prefetch_tmap(&map_xg); prefetch_tmap(&map_y); prefetch_tmap(&map_yg); prefetch_tmap(&map_out);
-    mbar_init(bar_x, 1);
-    mbar_init(bar_done, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(bar_s(i), 1); mbar_init(bar_p(i), 128); }
+    prefetch_tmap(&map_x); prefetch_tmap(&map_g); prefetch_tmap(&map_out);
+    for (int i = 0; i < 4; ++i) mbar_init(bars + 8 * i, 1);
+    mbar_init(bar_p, 8);
+    mbar_init(bar_ds, 8);
     for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     extent[0] = 0x7fffffff; extent[1] = 0;
     *abort_flag = 0;
@@ -502,14 +604,15 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
+  constexpr uint32_t ACC2 = DHP, CS = 256, CDP = 384;
   chain_begin();
   if (warp == 9 && lane == 0) {
     mbar_expect_tx(bar_x, 2 * C::TILE);
     for (int c = 0; c < C::CH; ++c) {
       tma_load_3d(base + c * CHUNK, &map_x, bar_x, c * 64, DKV ? a.heads + h : h, row0);
       if (DKV) tma_load_3d(base + C::TILE + c * CHUNK, &map_x, bar_x, c * 64, a.heads + a.kv + h, row0);
-      else tma_load_3d(base + C::TILE + c * CHUNK, &map_xg, bar_x, c * 64, h, row0);
+      else tma_load_3d(base + C::TILE + c * CHUNK, &map_g, bar_x, c * 64, h, row0);
     }
   }
   int2 iv = make_int2(0, 0);
@@ -518,38 +621,40 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     if (warp < 4) note_extent(extent, extent + 1, iv);
   }
   __syncthreads();
-  const int T0 = extent[1] > extent[0] ? extent[0] / STREAM : 0;
-  const int n_tiles = extent[1] > extent[0] ? (extent[1] + STREAM - 1) / STREAM - T0 : 0;
-  const int total = DKV ? n_tiles * group : n_tiles;
+  const int lo_all = uniform(extent[0]), hi_all = uniform(extent[1]);
+  const int T0 = hi_all > lo_all ? lo_all / 128 : 0;
+  const int n_tiles = hi_all > lo_all ? (hi_all + 127) / 128 - T0 : 0;
+  const int all = DKV ? n_tiles * group : n_tiles;
+  const int total = (all - part + parts - 1) / parts;             // this block's: every parts-th, from its own number on
+  struct Place {                                                  // head of the group and tile of the block's i-th
+    int g, t;
+    __device__ void settle(int n) { while (t >= n) { t -= n; ++g; } }
+  };
 
   if (warp == 9) {
     if (lane == 0) {
       bool ok = true;
       int fills = 0;
-      int g = 0, t = 0;
-      for (int i = 0; i < total && ok; ++i) {
+      Place p{0, part};
+      for (int i = 0; i < total && ok; ++i, p.t += parts) {
+        p.settle(n_tiles);
         const int s = i % ST;
         ok = mbar_wait(empty(s), ((uint32_t)(i / ST) & 1u) ^ 1u, abort_flag, a.status, kTimeoutSeqAttn);
         if (!ok) break;
         const uint32_t dst = ring + s * C::STAGE;
-        const int r = (T0 + t) * STREAM;
-        mbar_expect_tx(full(s), 2 * C::HALF + (DKV ? 2u * STREAM * 4u : 0u));
+        const int r = (T0 + p.t) * 128, hq = h * group + p.g;
+        mbar_expect_tx(full(s), 2 * C::TILE + (DKV ? 1024u : 0u));
+        for (int c = 0; c < C::CH; ++c) tma_load_3d(dst + c * CHUNK, &map_x, full(s), c * 64, DKV ? hq : a.heads + h / group, r);
         for (int c = 0; c < C::CH; ++c) {
-          if (DKV) {
-            tma_load_3d(dst + c * HCHUNK, &map_y, full(s), c * 64, h * group + g, r);
-            tma_load_3d(dst + C::HALF + c * HCHUNK, &map_yg, full(s), c * 64, h * group + g, r);
-          } else {
-            tma_load_3d(dst + c * HCHUNK, &map_y, full(s), c * 64, a.heads + h / group, r);
-            tma_load_3d(dst + C::HALF + c * HCHUNK, &map_y, full(s), c * 64, a.heads + a.kv + h / group, r);
-          }
+          if (DKV) tma_load_3d(dst + C::TILE + c * CHUNK, &map_g, full(s), c * 64, hq, r);
+          else tma_load_3d(dst + C::TILE + c * CHUNK, &map_x, full(s), c * 64, a.heads + a.kv + h / group, r);
         }
         if (DKV) {
-          const size_t at = (size_t)(h * group + g) * a.ld + r;
-          bulk_load(dst + 2 * C::HALF, a.lse + at, STREAM * 4, full(s));
-          bulk_load(dst + 2 * C::HALF + STREAM * 4, a.D + at, STREAM * 4, full(s));
+          const size_t at = (size_t)hq * a.ld + r;                // ld is a multiple of 128: whole tiles
+          bulk_load(dst + 2 * C::TILE, a.lse + at, 512, full(s));
+          bulk_load(dst + 2 * C::TILE + 512, a.D + at, 512, full(s));
         }
         ++fills;
-        if (++t == n_tiles) { t = 0; ++g; }
       }
       if (!ok) {
         for (int i = max(0, fills - ST); i < fills; ++i)
@@ -558,56 +663,73 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       for (uint32_t it = 0; it < (1u << 20) && !mbar_try_wait(bar_x, 0); ++it) {}
     }
   } else if (warp == 8) {
-    const uint32_t id_s = attn::idesc128(STREAM, false, false), id_a = attn::idesc128(DHP, false, true);
+    const uint32_t id_s = attn::idesc128(128, false, false), id_a = attn::idesc128(DHP, false, true);
+    const uint64_t dx1 = k_desc(base), dx2 = k_desc(base + C::TILE), dy1 = k_desc(ring), dy2 = k_desc(ring + C::TILE),
+                   dt1 = mn_desc(ring, CHUNK), dt2 = mn_desc(ring + C::TILE, CHUNK);
     const int2 used = used_rows(a.mask);
-    bool ok = total == 0 || __all_sync(0xffffffffu, mbar_wait(bar_x, 0, abort_flag, a.status, kTimeoutSeqAttn));
-    int t = 0;
-    for (int i = 0; i <= total && ok; ++i) {
-      if (i < total) {
-        const int s = i % ST;
-        ok = __all_sync(0xffffffffu, mbar_wait(full(s), (uint32_t)(i / ST) & 1u, abort_flag, a.status, kTimeoutSeqAttn));
-        if (!ok) break;
-        const int r = (T0 + t) * STREAM;
-        if (r < used.x || r + STREAM > used.y) {
-          scrub(gen + 2 * C::TILE + s * C::STAGE, STREAM, 2 * C::CH, HCHUNK, r, used, lane);
-          fence_async_smem();
-          __syncwarp();
-        }
-        tc_fence_after();
-        if (lane == 0) {
-          const uint32_t S = tmem + 256 + (i & 1) * 128, y = ring + s * C::STAGE;
-          for (int ks = 0; ks < DHP / UK; ++ks) tc_mma(S, kdesc(base, ks, CHUNK), kdesc(y, ks, HCHUNK), id_s, ks > 0 ? 1u : 0u);
-          for (int ks = 0; ks < DHP / UK; ++ks)
-            tc_mma(S + 64, kdesc(base + C::TILE, ks, CHUNK), kdesc(y + C::HALF, ks, HCHUNK), id_s, ks > 0 ? 1u : 0u);
-          tc_commit(bar_s(i & 1));
-        }
+    bool ok = true;
+    Place p{0, part};
+    auto landed = [&](int i) {
+      const int s = i % ST;
+      if (!warp_wait(full(s), (uint32_t)(i / ST) & 1u, abort_flag, a.status)) return false;
+      p.settle(n_tiles);
+      const int r = (T0 + p.t) * 128;
+      if (r < used.x || r + 128 > used.y) {
+        scrub(gen + 2 * C::TILE + s * C::STAGE, 128, 2 * C::CH, CHUNK, r, used, lane);
+        fence_async_smem();
         __syncwarp();
-        if (++t == n_tiles) t = 0;
       }
-      if (i >= 1) {
-        const int p = i - 1;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar_p(p & 1), (uint32_t)(p >> 1) & 1u, abort_flag, a.status, kTimeoutSeqAttn));
-        if (!ok) break;
-        tc_fence_after();
-        if (lane == 0) {
-          const uint32_t S = tmem + 256 + (p & 1) * 128, y = ring + (p % ST) * C::STAGE;
-          if (DKV)
-            for (int ks = 0; ks < STREAM / UK; ++ks)
-              mma_ts(tmem + DHP, S + ks * 8, mndesc(y + C::HALF, ks, HCHUNK), id_a, (p > 0 || ks > 0) ? 1u : 0u);
-          for (int ks = 0; ks < STREAM / UK; ++ks)
-            mma_ts(tmem, S + 64 + ks * 8, mndesc(y, ks, HCHUNK), id_a, (p > 0 || ks > 0) ? 1u : 0u);
-          tc_commit(empty(p % ST));
+      p.t += parts;
+      return true;
+    };
+    auto at = [&](int i) { return (uint64_t)((uint32_t)(i % ST) * (C::STAGE >> 4)); };
+    if (total > 0) ok = warp_wait(bar_x, 0, abort_flag, a.status) && landed(0);
+    if (total > 0 && ok && elect()) {
+      product_ss<DHP, CHUNK, CHUNK>(tmem + CS, dx1, dy1, id_s);
+      tc_commit(bar_s);
+      product_ss<DHP, CHUNK, CHUNK>(tmem + CDP, dx2, dy2, id_s);
+      tc_commit(bar_dp);
+    }
+    for (int i = 0; i < total && ok; ++i) {
+      const bool next = i + 1 < total;
+      const uint32_t add = i > 0 ? 1u : 0u;
+      const uint64_t b1 = dt1 + at(i), b2 = dt2 + at(i), n1 = dy1 + at(i + 1), n2 = dy2 + at(i + 1);
+      if (next) ok = landed(i + 1);
+      if (ok) ok = warp_wait(bar_p, (uint32_t)i & 1u, abort_flag, a.status);
+      if (!ok) break;
+      tc_fence_after();
+      if (elect()) {
+        if (DKV) {                                                // each group's half of P lies in the first half of its scores' columns
+          mma_ts(tmem + ACC2, tmem + CS, b2, id_a, add);
+#pragma unroll
+          for (int ks = 1; ks < 8; ++ks) mma_ts(tmem + ACC2, tmem + CS + (ks >> 2) * 64 + (ks & 3) * 8, b2 + mn_step(ks), id_a, 1u);
         }
-        __syncwarp();
+        if (next) {
+          product_ss<DHP, CHUNK, CHUNK>(tmem + CS, dx1, n1, id_s);
+          tc_commit(bar_s);
+        }
+      }
+      ok = warp_wait(bar_ds, (uint32_t)i & 1u, abort_flag, a.status);
+      if (!ok) break;
+      tc_fence_after();
+      if (elect()) {
+        mma_ts(tmem, tmem + CDP, b1, id_a, add);
+#pragma unroll
+        for (int ks = 1; ks < 8; ++ks) mma_ts(tmem, tmem + CDP + (ks >> 2) * 64 + (ks & 3) * 8, b1 + mn_step(ks), id_a, 1u);
+        tc_commit(empty(i % ST));
+        if (next) {
+          product_ss<DHP, CHUNK, CHUNK>(tmem + CDP, dx2, n2, id_s);
+          tc_commit(bar_dp);
+        }
       }
     }
-    if (ok && total > 0 && lane == 0) tc_commit(bar_done);
+    if (ok && total > 0 && elect()) tc_commit(bar_done);
     __syncwarp();
   } else {
     const int w = warp >> 2;
     const int trow = threadIdx.x & 127, row = row0 + trow;
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t S = tmem + lane_addr + 256 + w * 128;
+    const uint32_t S = tmem + lane_addr + CS + w * 64, DP = tmem + lane_addr + CDP + w * 64;     // 64 of a tile's 128 columns
     const float c2 = a.scale * LOG2E;
     const float u = CAP ? 2.0f * c2 / a.cap : 0.0f, top = a.cap * LOG2E;
     float own_lse = INFINITY, own_D = 0.0f, slope2 = 0.0f;
@@ -615,97 +737,185 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       if (row < a.mask.M) { own_lse = a.lse[(size_t)h * a.ld + row]; own_D = a.D[(size_t)h * a.ld + row]; }
       if (BIAS) slope2 = a.slopes[h] * LOG2E;
     }
+    const uint64_t c22 = pair(c2, c2), neg_lse2 = pair(-own_lse, -own_lse), neg_D2 = pair(-own_D, -own_D);
     bool ok = true;
-    for (int i = w; i < total && ok; i += 2) {
-      const int t = DKV ? i % n_tiles : i;
-      const int k0 = (T0 + t) * STREAM;
-      if (DKV && BIAS) slope2 = a.slopes[h * group + i / n_tiles] * LOG2E;
-      ok = mbar_wait(bar_s(w), (uint32_t)(i >> 1) & 1u, abort_flag, a.status, kTimeoutSeqAttn);
+    Place pl{0, part};
+    for (int i = 0; i < total && ok; ++i, pl.t += parts) {
+      pl.settle(n_tiles);
+      const int k0 = (T0 + pl.t) * 128 + w * 64;
+      if (DKV && BIAS) slope2 = a.slopes[h * group + pl.g] * LOG2E;
+      ok = mbar_wait(bar_s, (uint32_t)i & 1u, abort_flag, a.status, kTimeoutSeqAttn);
       if (!ok) break;
       if (DKV) {                                                  // the rows' lse and D came with the tile
         ok = mbar_wait(full(i % ST), (uint32_t)(i / ST) & 1u, abort_flag, a.status, kTimeoutSeqAttn);
         if (!ok) break;
       }
       tc_fence_after();
-      const float* col = reinterpret_cast<const float*>(gen + 2 * C::TILE + (i % ST) * C::STAGE + 2 * C::HALF);
-      const bool whole = __all_sync(0xffffffffu, iv.x <= k0 && iv.y >= k0 + STREAM);
+      const float* col = reinterpret_cast<const float*>(gen + 2 * C::TILE + (i % ST) * C::STAGE + 2 * C::TILE) + w * 64;
+      const bool whole = __all_sync(0xffffffffu, iv.x <= k0 && iv.y >= k0 + 64);
       const int lo = iv.x - k0;
       const unsigned len = (unsigned)(iv.y - iv.x);
-      const float d0 = (float)(row - k0);
-      uint32_t pr[32], dr[32];
+      float s[2][32];                                             // p, in the end p (1 - tanh^2)
+      tmem_ld32_issue(S, s[0]);
+      tmem_ld32_issue(S + 32, s[1]);
+      tmem_ld_wait(s[0], s[1]);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float s[32], dp[32];
-        tmem_ld32_issue(S + c * 32, s);
-        tmem_ld32_issue(S + 64 + c * 32, dp);
-        tmem_ld_wait(s, dp);
+        uint32_t r[16];
+        if (!CAP && !BIAS) {
 #pragma unroll
-        for (int q = 0; q < 32; q += 4) {
-          float4 L4 = make_float4(own_lse, own_lse, own_lse, own_lse), D4 = make_float4(own_D, own_D, own_D, own_D);
-          if (DKV) {
-            L4 = *reinterpret_cast<const float4*>(col + c * 32 + q);
-            D4 = *reinterpret_cast<const float4*>(col + STREAM + c * 32 + q);
-          }
-          const float Lv[4] = {L4.x, L4.y, L4.z, L4.w}, Dv[4] = {D4.x, D4.y, D4.z, D4.w};
+          for (int j = 0; j < 32; j += 4) {
+            float4 L4;
+            if (DKV) L4 = *reinterpret_cast<const float4*>(col + c * 32 + j);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = q + e;
-            float x, slope = 1.0f;
-            if (CAP) {
-              const float th = tanh_of(s[j] * u);
-              slope = fmaf(-th, th, 1.0f);
-              x = fmaf(top, th, -Lv[e]);
-            } else {
-              x = fmaf(s[j], c2, -Lv[e]);
+            for (int e = 0; e < 4; e += 2) {
+              const uint64_t nl = DKV ? (e == 0 ? pair(-L4.x, -L4.y) : pair(-L4.z, -L4.w)) : neg_lse2;
+              const float2 x = ex2_of(fma2(pair(s[c][j + e], s[c][j + e + 1]), c22, nl));
+              s[c][j + e] = x.x;
+              s[c][j + e + 1] = x.y;
             }
-            if (BIAS) x = fmaf(-slope2, fabsf(d0 - (float)(c * 32 + j)), x);
-            float p = attn::ex2(x);
-            float ds = p * (dp[j] - Dv[e]);
-            if (CAP) ds *= slope;
-            if (!whole && (unsigned)(c * 32 + j - lo) >= len) { p = 0.0f; ds = 0.0f; }
-            s[j] = p;
-            dp[j] = ds;
+          }
+          if (!whole) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if ((unsigned)(c * 32 + j - lo) >= len) s[c][j] = 0.0f;
+          }
+          if (DKV) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) r[j / 2] = pack_bf16x2(s[c][j], s[c][j + 1]);
+          }
+        } else {
+          const float d0 = (float)(row - k0 - c * 32);
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) {
+            float p[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float L = DKV ? col[c * 32 + j + e] : own_lse;
+              float x, slope = 1.0f;
+              if (CAP) {
+                const float th = tanh_of(s[c][j + e] * u);
+                slope = fmaf(-th, th, 1.0f);
+                x = fmaf(top, th, -L);
+              } else {
+                x = fmaf(s[c][j + e], c2, -L);
+              }
+              if (BIAS) x = fmaf(-slope2, fabsf(d0 - (float)(j + e)), x);
+              p[e] = attn::ex2(x);
+              if (!whole && (unsigned)(c * 32 + j + e - lo) >= len) p[e] = slope = 0.0f;
+              s[c][j + e] = CAP ? p[e] * slope : p[e];
+            }
+            if (DKV) r[j / 2] = pack_bf16x2(p[0], p[1]);
           }
         }
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          if (DKV) pr[c * 16 + j / 2] = pack_bf16x2(s[j], s[j + 1]);
-          dr[c * 16 + j / 2] = pack_bf16x2(dp[j], dp[j + 1]);
-        }
+        if (DKV) tmem_st16(S + c * 16, r);
       }
-      if (DKV) tmem_st32(S, pr);
-      tmem_st32(S + 64, dr);
+      if (DKV) tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_p);
+      ok = mbar_wait(bar_dp, (uint32_t)i & 1u, abort_flag, a.status, kTimeoutSeqAttn);
+      if (!ok) break;
+      tc_fence_after();
+      float dp[2][32];
+      tmem_ld32_issue(DP, dp[0]);
+      tmem_ld32_issue(DP + 32, dp[1]);
+      tmem_ld_wait(dp[0], dp[1]);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t r[16];
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+          float4 D4;
+          if (DKV) D4 = *reinterpret_cast<const float4*>(col + 128 + c * 32 + j);
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const uint64_t nd = DKV ? (e == 0 ? pair(-D4.x, -D4.y) : pair(-D4.z, -D4.w)) : neg_D2;
+            const float2 d = unpair(mul2(pair(s[c][j + e], s[c][j + e + 1]), add2(pair(dp[c][j + e], dp[c][j + e + 1]), nd)));
+            dp[c][j + e] = d.x;
+            dp[c][j + e + 1] = d.y;
+          }
+        }
+        if (!whole) {                                             // 0 times whatever stands in a masked place
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if ((unsigned)(c * 32 + j - lo) >= len) dp[c][j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) r[j / 2] = pack_bf16x2(dp[c][j], dp[c][j + 1]);
+        tmem_st16(DP + c * 16, r);
+      }
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(bar_p(w));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_ds);
     }
     if (ok && total > 0) ok = mbar_wait(bar_done, 0, abort_flag, a.status, kTimeoutSeqAttn);
     if (ok) ok = mbar_wait(bar_x, 0, abort_flag, a.status, kTimeoutSeqAttn);
     if (ok) {
       tc_fence_after();
-      // dk and dq are staged in X1's tile, dv in X2's.  dk, dv: a group each; dq: the groups share its 64-column pieces
-      const int c0 = DKV ? 0 : w, c1 = DKV ? C::CH : min(w + 1, C::CH);
       const bool second = DKV && w == 1;
-      const float f = second ? 1.0f : a.scale;
-      uint8_t* out = gen + (second ? C::TILE : 0);
-      const int block = DKV ? a.heads + (w == 1 ? a.kv : 0) + h : h;
+      if (parts == 1) {
+        // dk and dq are staged in X1's tile, dv in X2's.  dk, dv: a group each; dq: the groups share its 64-column pieces
+        const int c0 = DKV ? 0 : w, c1 = DKV ? C::CH : min(w + 1, C::CH);
+        const float f = second ? 1.0f : a.scale;
+        uint8_t* out = gen + (second ? C::TILE : 0);
+        const int block = DKV ? a.heads + (w == 1 ? a.kv : 0) + h : h;
 #pragma unroll 1
-      for (int c = c0 * 2; c < c1 * 2; ++c) {
-        float o[32];
-        if (total > 0) tmem_ld32(tmem + lane_addr + (second ? DHP : 0) + c * 32, o);
+        for (int c = c0 * 2; c < c1 * 2; ++c) {
+          float o[32];
+          if (total > 0) tmem_ld32(tmem + lane_addr + (second ? DHP : 0) + c * 32, o);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) o[j] = total > 0 ? o[j] * f : 0.0f;
-        sts_row32(out + (c >> 1) * CHUNK, trow, c & 1, o);
-      }
-      fence_async_smem();
-      group_sync(1 + w);
-      if (trow == 0) {
-        for (int c = c0; c < c1; ++c)
-          if (c * 64 < a.dim) tma_store_3d(&map_out, base + (second ? C::TILE : 0) + c * CHUNK, c * 64, block, row0);
-        tma_store_commit();
-        tma_store_wait_all();
+          for (int j = 0; j < 32; ++j) o[j] = total > 0 ? o[j] * f : 0.0f;
+          sts_row32(out + (c >> 1) * CHUNK, trow, c & 1, o);
+        }
+        fence_async_smem();
+        group_sync(1 + w);
+        if (trow == 0) {
+          for (int c = c0; c < c1; ++c)
+            if (c * 64 < a.dim) tma_store_3d(&map_out, base + (second ? C::TILE : 0) + c * CHUNK, c * 64, block, row0);
+          tma_store_commit();
+          tma_store_wait_all();
+        }
+      } else {
+        // each block leaves its sums in its own shared memory, [accumulator][column][row]; every tile has been read by now
+        float* mine = reinterpret_cast<float*>(gen) + (second ? DHP * 128 : 0) + trow;
+        const int c0 = DKV ? 0 : w * (DHP / 64), c1 = DKV ? DHP / 32 : (w + 1) * (DHP / 64);
+#pragma unroll 1
+        for (int c = c0; c < c1; ++c) {
+          float o[32];
+          if (total > 0) tmem_ld32(tmem + lane_addr + (second ? DHP : 0) + c * 32, o);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) mine[(c * 32 + j) * 128] = total > 0 ? o[j] : 0.0f;
+        }
       }
     }
+  }
+  if (parts > 1) {                                                // join: a block adds up its share of the columns, in the blocks' order
+    cluster_sync_all();
+    if (warp < 8) {
+      const int w = warp >> 2, trow = threadIdx.x & 127, row = row0 + trow;
+      const bool second = DKV && w == 1;
+      const int n = DKV ? DHP / parts : DHP / parts / 2;            // columns a thread: at least 4
+      const int first = part * (DHP / parts) + (DKV ? 0 : w * n);
+      const uint32_t at = base + ((second ? DHP * 128 : 0) + first * 128 + trow) * 4;
+      const float f = second ? 1.0f : a.scale;
+      const int block = DKV ? a.heads + (second ? a.kv : 0) + h : h;
+      bf16* out = dqkv + ((size_t)row * (a.heads + 2 * a.kv) + block) * a.dim + first;
+      for (int j = 0; j < n && first + j < a.dim; j += 4) {
+        float o[4] = {};
+        for (int c = 0; c < parts; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] += ld_peer(at + (j + e) * 512, c);
+        if (row < a.mask.M) {
+          uint2 q;
+          q.x = pack_bf16x2(o[0] * f, o[1] * f);
+          q.y = pack_bf16x2(o[2] * f, o[3] * f);
+          *reinterpret_cast<uint2*>(out + j) = q;
+        }
+      }
+    }
+    cluster_sync_all();
   }
   tc_fence_before();
   __syncthreads();

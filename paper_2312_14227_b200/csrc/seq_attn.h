@@ -26,11 +26,12 @@ struct Args {
   float scale, cap;
 };
 
-// qkv128: 128-row boxes of the input, out128: of the output
-cudaError_t forward(const CUtensorMap& qkv128, const CUtensorMap& out128, Args a, int sms, cudaStream_t st);
-// Three launches: D, dq, (dk, dv).  64: 64-row boxes; g: the output's gradient; dqkv: where the input's gradient goes
-cudaError_t backward(const CUtensorMap& qkv128, const CUtensorMap& qkv64, const CUtensorMap& g128, const CUtensorMap& g64,
-                     const CUtensorMap& dqkv128, const void* out, const void* dout, Args a, int sms, cudaStream_t st);
+// Tensor maps of head blocks (boxes of 64 columns x 128 rows): qkv the input, out the output, g the output's gradient, gqkv (and dqkv, the
+// same memory) where the input's gradient goes.
+cudaError_t forward(const CUtensorMap& qkv, const CUtensorMap& out, Args a, int sms, cudaStream_t st);
+// Three launches: D, dq, (dk, dv).
+cudaError_t backward(const CUtensorMap& qkv, const CUtensorMap& g, const CUtensorMap& gqkv, const void* out, const void* dout, void* dqkv,
+                     Args a, int sms, cudaStream_t st);
 constexpr int kForwardLaunches = 1, kBackwardLaunches = 3;
 
 }  // namespace seqattn

@@ -183,12 +183,39 @@ __device__ __forceinline__ float max_nan(float a, float b) {                   /
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float r;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ float2 ex2_of(uint64_t x) {
+// 2^x of two values on the FMA pipes.  The exponential unit takes 8 cycles for a warp's 32 values, twice what the tensor core takes
+// for the products that these values belong to; part of them is formed here instead.  x = n + f with n whole, |f| <= 1/2 (adding and
+// taking off 1.5 2^23 rounds); 2^f by a polynomial of degree 4 with value 1 at 0, fitted here to the least largest relative error (2.9e-6,
+// 1/1400 of the bf16 step that follows); n goes into the exponent.  x below -127 gives 0, as -127 does exactly; NaN is not kept.
+__device__ __forceinline__ float2 ex2_pair(uint64_t x2) {
+  const float2 v = unpair(x2);
+  const uint64_t x = pair(fmaxf(v.x, -127.0f), fmaxf(v.y, -127.0f));
+  const uint64_t t = add2(x, both(12582912.0f));
+  const uint64_t f = fma2(add2(t, both(-12582912.0f)), both(-1.0f), x);
+  uint64_t p = fma2(f, both(0.009582852944731712f), both(0.055906426161527634f));
+  p = fma2(p, f, both(0.24024099111557007f));
+  p = fma2(p, f, both(0.6931241750717163f));
+  p = fma2(p, f, both(1.0f));
+  const float2 q = unpair(p), n = unpair(t);
+  return make_float2(__uint_as_float(__float_as_uint(q.x) + (__float_as_uint(n.x) << 23)),
+                     __uint_as_float(__float_as_uint(q.y) + (__float_as_uint(n.y) << 23)));
+}
+// Pairs k of every eight with bit k of SHARE set take that way.  Measured over 8192 causal rows and 16 heads: one of eight in the forward pass (222 ->
+// 213 us at head width 64, 257 -> 254 at 128), three in the backward pass (579 -> 537, 846 -> 840); more gives the time back in instructions.
+constexpr int kFwdShare = 0x01, kBwdShare = 0x29;
+template <int SHARE>
+__device__ __forceinline__ float2 ex2_of(uint64_t x, int k) {
+  if ((SHARE >> (k & 7)) & 1) return ex2_pair(x);
   const float2 v = unpair(x);
   return make_float2(attn::ex2(v.x), attn::ex2(v.y));
 }
@@ -211,11 +238,59 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 
-// tanh from one exponential and one reciprocal: exp overflow gives 1, underflow -1, absolute error near 2^-23
-__device__ __forceinline__ float tanh_of(float x2) {            // x2 = 2 x log2 e
+// tanh of four values from 2 x log2 e: 1 - 2 / (1 + e^2x), the four quotients from one reciprocal of the product.  Arguments are held at 30,
+// where tanh has rounded to 1, so that the product stays in range; the absolute error is near 2^-22.
+template <int SHARE>
+__device__ __forceinline__ void tanh4(uint64_t x01, uint64_t x23, uint64_t* t01, uint64_t* t23) {
+  const float2 a = unpair(x01), b = unpair(x23);
+  const float2 ea = ex2_of<SHARE>(pair(min_nan(a.x, 30.0f), min_nan(a.y, 30.0f)), 0);
+  const float2 eb = ex2_of<SHARE>(pair(min_nan(b.x, 30.0f), min_nan(b.y, 30.0f)), 1);
+  const uint64_t da = add2(pair(ea.x, ea.y), both(1.0f)), db = add2(pair(eb.x, eb.y), both(1.0f));
+  const float2 p = unpair(mul2(da, db));
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(attn::ex2(x2) + 1.0f));
-  return fmaf(-2.0f, r, 1.0f);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(p.x * p.y));
+  const uint64_t q = pair(r * p.y, r * p.x);
+  *t01 = fma2(mul2(q, db), both(-2.0f), both(1.0f));
+  *t23 = fma2(mul2(q, da), both(-2.0f), both(1.0f));
+}
+// Scores of 32 keys in powers of 2, in place of the products s.  SLOPES: 1 - tanh^2 to `slope`.
+// Off the diagonal (LINEAR) the distance |row - key| is linear in the key: bias = ss (j - d0), d0 = row - first key, ss = +-slope.
+// To every score `own` and, with EACH, each(j) of its pair is added (the backward pass: less the log-sum-exp).
+template <bool CAP, bool BIAS, bool SLOPES, int SHARE, bool LINEAR, bool EACH, typename F>
+__device__ __forceinline__ void scores(float (&s)[32], float (&slope)[SLOPES ? 32 : 1], float c2, float u, float top, float ss, int d0,
+                                       float own, F&& each) {
+  const uint64_t ss2 = both(ss), base = both(LINEAR && BIAS ? fmaf(-ss, (float)d0, own) : own);
+#pragma unroll
+  for (int j = 0; j < 32; j += 4) {
+    uint64_t a = pair(s[j], s[j + 1]), b = pair(s[j + 2], s[j + 3]);
+    if (CAP) {
+      tanh4<SHARE>(mul2(a, both(u)), mul2(b, both(u)), &a, &b);
+      if (SLOPES) {
+        const float2 x = unpair(fma2(mul2(a, both(-1.0f)), a, both(1.0f))), y = unpair(fma2(mul2(b, both(-1.0f)), b, both(1.0f)));
+        slope[j] = x.x; slope[j + 1] = x.y; slope[j + 2] = y.x; slope[j + 3] = y.y;
+      }
+    }
+    const uint64_t f = both(CAP ? top : c2);
+    uint64_t ra = base, rb = base;
+    if constexpr (EACH) {
+      ra = LINEAR && BIAS ? add2(base, each(j)) : each(j);
+      rb = LINEAR && BIAS ? add2(base, each(j + 2)) : each(j + 2);
+    }
+    if (BIAS && LINEAR) {
+      ra = fma2(ss2, pair((float)j, (float)(j + 1)), ra);
+      rb = fma2(ss2, pair((float)(j + 2), (float)(j + 3)), rb);
+    }
+    a = fma2(a, f, ra);
+    b = fma2(b, f, rb);
+    if (BIAS && !LINEAR) {
+      const float2 x = unpair(a), y = unpair(b);
+      const float d = (float)(d0 - j);
+      a = pair(fmaf(-ss, fabsf(d), x.x), fmaf(-ss, fabsf(d - 1.0f), x.y));
+      b = pair(fmaf(-ss, fabsf(d - 2.0f), y.x), fmaf(-ss, fabsf(d - 3.0f), y.y));
+    }
+    const float2 x = unpair(a), y = unpair(b);
+    s[j] = x.x; s[j + 1] = x.y; s[j + 2] = y.x; s[j + 3] = y.y;
+  }
 }
 
 // Rows of a 128-byte-swizzled tile that belong to no sequence become 0 (whole warp; the caller orders it before the products).
@@ -360,6 +435,11 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
       }
       if (has_k) ok = warp_wait(full(sk), (uint32_t)(ik / ST) & 1u, abort_flag, a.status);
       if (!ok) break;
+      if (CAP && has_k && ((t + 1) * 128 < used.x || (t + 2) * 128 > used.y)) {     // four keys share a reciprocal: NaN would reach the others
+        scrub(gen + (2 + sk) * C::TILE, 128, C::CH, CHUNK, (t + 1) * 128, used, lane);
+        fence_async_smem();
+        __syncwarp();
+      }
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         const bool pv = t >= first[hf] && t < last[hf], nx = t + 1 >= first[hf] && t + 1 < last[hf];
@@ -418,15 +498,17 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
       tmem_ld_wait(v[2], v[3]);
       if (CAP || BIAS) {
         const float u = CAP ? 2.0f * c2 / a.cap : 0.0f, top = a.cap * LOG2E;
-        const float d0 = (float)(row - k0);
+        const int d0 = row - k0;
+        const bool above = __all_sync(0xffffffffu, d0 >= 127), below = __all_sync(0xffffffffu, d0 <= 0);
+        float none[1];
+        if (!BIAS || above || below) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c)
+            scores<CAP, BIAS, false, kFwdShare, true, false>(v[c], none, c2, u, top, above ? slope2 : -slope2, d0 - c * 32, 0.0f, 0);
+        } else {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            float s = CAP ? top * tanh_of(v[c][j] * u) : v[c][j] * c2;
-            if (BIAS) s = fmaf(-slope2, fabsf(d0 - (float)(c * 32 + j)), s);
-            v[c][j] = s;
-          }
+          for (int c = 0; c < 4; ++c) scores<CAP, BIAS, false, kFwdShare, false, false>(v[c], none, c2, u, top, slope2, d0 - c * 32, 0.0f, 0);
+        }
       }
       if (!__all_sync(0xffffffffu, iv.x <= k0 && iv.y >= k0 + 128)) {
         const int lo = iv.x - k0;
@@ -471,7 +553,7 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
 #pragma unroll
         for (int j = 0; j < 32; j += 2) {
           const uint64_t x = pair(v[c][j], v[c][j + 1]);
-          const float2 e = ex2_of(CAP || BIAS ? add2(x, neg_m) : fma2(x, factor, neg_m));
+          const float2 e = ex2_of<kFwdShare>(CAP || BIAS ? add2(x, neg_m) : fma2(x, factor, neg_m), j / 2);
           sum2 = add2(sum2, pair(e.x, e.y));
           r[j / 2] = pack_bf16x2(e.x, e.y);
         }
@@ -770,7 +852,7 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll
             for (int e = 0; e < 4; e += 2) {
               const uint64_t nl = DKV ? (e == 0 ? pair(-L4.x, -L4.y) : pair(-L4.z, -L4.w)) : neg_lse2;
-              const float2 x = ex2_of(fma2(pair(s[c][j + e], s[c][j + e + 1]), c22, nl));
+              const float2 x = ex2_of<kBwdShare>(fma2(pair(s[c][j + e], s[c][j + e + 1]), c22, nl), (j + e) / 2);
               s[c][j + e] = x.x;
               s[c][j + e + 1] = x.y;
             }
@@ -785,27 +867,27 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             for (int j = 0; j < 32; j += 2) r[j / 2] = pack_bf16x2(s[c][j], s[c][j + 1]);
           }
         } else {
-          const float d0 = (float)(row - k0 - c * 32);
+          float slope[CAP ? 32 : 1];
+          const int d0 = row - k0 - c * 32;
+          const bool above = __all_sync(0xffffffffu, d0 >= 31), below = __all_sync(0xffffffffu, d0 <= 0);
+          auto less = [&](int j) {
+            const float2 L = *reinterpret_cast<const float2*>(col + c * 32 + j);
+            return pair(-L.x, -L.y);
+          };
+          const float own = DKV ? 0.0f : -own_lse;
+          if (!BIAS || above || below)
+            scores<CAP, BIAS, CAP, kBwdShare, true, DKV>(s[c], slope, c2, u, top, above ? slope2 : -slope2, d0, own, less);
+          else scores<CAP, BIAS, CAP, kBwdShare, false, DKV>(s[c], slope, c2, u, top, slope2, d0, own, less);
 #pragma unroll
           for (int j = 0; j < 32; j += 2) {
-            float p[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float L = DKV ? col[c * 32 + j + e] : own_lse;
-              float x, slope = 1.0f;
-              if (CAP) {
-                const float th = tanh_of(s[c][j + e] * u);
-                slope = fmaf(-th, th, 1.0f);
-                x = fmaf(top, th, -L);
-              } else {
-                x = fmaf(s[c][j + e], c2, -L);
-              }
-              if (BIAS) x = fmaf(-slope2, fabsf(d0 - (float)(j + e)), x);
-              p[e] = attn::ex2(x);
-              if (!whole && (unsigned)(c * 32 + j + e - lo) >= len) p[e] = slope = 0.0f;
-              s[c][j + e] = CAP ? p[e] * slope : p[e];
+            float2 p = ex2_of<kBwdShare>(pair(s[c][j], s[c][j + 1]), j / 2);
+            if (!whole) {
+              if ((unsigned)(c * 32 + j - lo) >= len) p.x = 0.0f;
+              if ((unsigned)(c * 32 + j + 1 - lo) >= len) p.y = 0.0f;
             }
-            if (DKV) r[j / 2] = pack_bf16x2(p[0], p[1]);
+            if (DKV) r[j / 2] = pack_bf16x2(p.x, p.y);
+            s[c][j] = CAP ? p.x * slope[j] : p.x;
+            s[c][j + 1] = CAP ? p.y * slope[j + 1] : p.y;
           }
         }
         if (DKV) tmem_st16(S + c * 16, r);

@@ -66,11 +66,13 @@ __device__ __forceinline__ int2 interval(const Mask& m, int row, int lane) {
     b = row / m.len * m.len;
     e = min(b + m.len, m.M);
   } else {
-    int lo = find_seq(m.begin, m.n, row - lane, lane);                 // of the warp's first and last row
-    int hi = find_seq(m.begin, m.n, row - lane + 31, lane);
-    while (lo < hi) {
-      const int mid = lo + (hi - lo + 1) / 2;
-      if (m.begin[mid] <= row) lo = mid; else hi = mid - 1;
+    int lo = find_seq(m.begin, m.n, row - lane, lane);                 // of the warp's first row, and mostly of all its rows
+    if (lo >= m.n || m.begin[lo + 1] <= row - lane + 31) {
+      int hi = find_seq(m.begin, m.n, row - lane + 31, lane);
+      while (lo < hi) {
+        const int mid = lo + (hi - lo + 1) / 2;
+        if (m.begin[mid] <= row) lo = mid; else hi = mid - 1;
+      }
     }
     q = lo;
     if (q < 0 || q >= m.n || row >= m.M) return make_int2(0, 0);
@@ -301,11 +303,14 @@ __device__ __forceinline__ void scrub(uint8_t* tile, int rows, int chunks, uint3
   }
 }
 
-// Extent of the union of a block's intervals, by shared memory: {first, last} over non-empty ones.
-__device__ __forceinline__ void note_extent(int* lo, int* hi, int2 iv) {
+// Extent of the union of a warp's intervals: {first, last} over the non-empty ones, {large, 0} without any.
+__device__ __forceinline__ void note_extent(int* at, int2 iv) {
   const int l = __reduce_min_sync(0xffffffffu, iv.y > iv.x ? iv.x : 0x7fffffff);
   const int h = __reduce_max_sync(0xffffffffu, iv.y > iv.x ? iv.y : 0);
-  if ((threadIdx.x & 31) == 0) { atomicMin(lo, l); atomicMax(hi, h); }
+  if ((threadIdx.x & 31) == 0) { at[0] = l; at[1] = h; }
+}
+__device__ __forceinline__ int2 extent_of(const int* at) {            // of four warps
+  return make_int2(uniform(min(min(at[0], at[2]), min(at[4], at[6]))), uniform(max(max(at[1], at[3]), max(at[5], at[7]))));
 }
 
 // ---- forward -----------------------------------------------------------------------------------
@@ -336,7 +341,7 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
   int* shared = reinterpret_cast<int*>(gen + (2 + ST) * C::TILE + 160);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(shared);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  int* extent = shared + 2;                                       // lo, hi of half 0, of half 1
+  int* extent = shared + 2;                                       // lo, hi of each row warp
 
   const int warp = uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int tiles = (a.mask.M + 128 * a.halves - 1) / (128 * a.halves);
@@ -346,48 +351,44 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
   const int row0 = tile * 128 * a.halves;
   const int kvh = h / (a.heads / a.kv);
 
-  if (threadIdx.x == 0) {
-    prefetch_tmap(&map_qkv);
-    prefetch_tmap(&map_out);
+  // (A block's start is a chain of latencies, a third of a block of four tiles: barriers, Q's copy, tensor memory and intervals go side by side.)
+  chain_begin();
+  if (warp == 9 && lane == 0) {
     mbar_init(bar_q, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_s(i), 1);
       for (int k = 0; k < 2; ++k) mbar_init(bar_p(i, k), 4);
-      extent[2 * i] = 0x7fffffff; extent[2 * i + 1] = 0;
     }
     for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     *abort_flag = 0;
     fence_async_smem();
+    mbar_expect_tx(bar_q, (uint32_t)a.halves * C::TILE);
+    for (int hf = 0; hf < a.halves; ++hf)
+      for (int c = 0; c < C::CH; ++c) tma_load_3d(base + hf * C::TILE + c * CHUNK, &map_qkv, bar_q, c * 64, h, row0 + hf * 128);
+    prefetch_tmap(&map_out);
   }
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(smem_u32((const void*)tmem_slot)), "r"(TMEM_COLS) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
-  chain_begin();
-  if (warp == 9 && lane == 0) {
-    mbar_expect_tx(bar_q, (uint32_t)a.halves * C::TILE);
-    for (int hf = 0; hf < a.halves; ++hf)
-      for (int c = 0; c < C::CH; ++c) tma_load_3d(base + hf * C::TILE + c * CHUNK, &map_qkv, bar_q, c * 64, h, row0 + hf * 128);
-  }
   const int my_half = warp >> 2, trow = threadIdx.x & 127, row = row0 + my_half * 128 + trow;
   int2 iv = make_int2(0, 0);
   if (warp < 8) {
     if (my_half < a.halves) iv = interval<false>(a.mask, row, lane);
-    note_extent(extent + 2 * my_half, extent + 2 * my_half + 1, iv);
+    note_extent(extent + 2 * warp, iv);
   }
+  tc_fence_before();
   __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
   // tiles of 128 keys that each half walks; the stream covers both
   int first[2], last[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int lo = uniform(extent[2 * i]), hi = uniform(extent[2 * i + 1]);
-    first[i] = hi > lo ? lo / 128 : 0;
-    last[i] = hi > lo ? (hi + 127) / 128 : 0;
+    const int2 e = extent_of(extent + 8 * i);
+    first[i] = e.y > e.x ? e.x / 128 : 0;
+    last[i] = e.y > e.x ? (e.y + 127) / 128 : 0;
   }
   const bool any0 = last[0] > first[0], any1 = last[1] > first[1];
   const int T0 = any0 && any1 ? min(first[0], first[1]) : any0 ? first[0] : first[1];
@@ -668,44 +669,41 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   const int tile = a.mask.causal && !DKV ? tiles - 1 - item / blocks_h : item / blocks_h;
   const int row0 = tile * 128;
 
-  if (threadIdx.x == 0) {
-    prefetch_tmap(&map_x); prefetch_tmap(&map_g); prefetch_tmap(&map_out);
+  chain_begin();
+  if (warp == 9 && lane == 0) {
     for (int i = 0; i < 4; ++i) mbar_init(bars + 8 * i, 1);
     mbar_init(bar_p, 8);
     mbar_init(bar_ds, 8);
     for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    extent[0] = 0x7fffffff; extent[1] = 0;
     *abort_flag = 0;
     fence_async_smem();
-  }
-  if (warp == 8) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                 ::"r"(smem_u32((const void*)tmem_slot)), "r"(TMEM_COLS) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
-  constexpr uint32_t ACC2 = DHP, CS = 256, CDP = 384;
-  chain_begin();
-  if (warp == 9 && lane == 0) {
     mbar_expect_tx(bar_x, 2 * C::TILE);
     for (int c = 0; c < C::CH; ++c) {
       tma_load_3d(base + c * CHUNK, &map_x, bar_x, c * 64, DKV ? a.heads + h : h, row0);
       if (DKV) tma_load_3d(base + C::TILE + c * CHUNK, &map_x, bar_x, c * 64, a.heads + a.kv + h, row0);
       else tma_load_3d(base + C::TILE + c * CHUNK, &map_g, bar_x, c * 64, h, row0);
     }
+    prefetch_tmap(&map_g);
+    prefetch_tmap(&map_out);
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32((const void*)tmem_slot)), "r"(TMEM_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   int2 iv = make_int2(0, 0);
   if (warp < 8) {
     iv = interval<DKV>(a.mask, row0 + (int)(threadIdx.x & 127), lane);
-    if (warp < 4) note_extent(extent, extent + 1, iv);
+    if (warp < 4) note_extent(extent + 2 * warp, iv);
   }
+  tc_fence_before();
   __syncthreads();
-  const int lo_all = uniform(extent[0]), hi_all = uniform(extent[1]);
-  const int T0 = hi_all > lo_all ? lo_all / 128 : 0;
-  const int n_tiles = hi_all > lo_all ? (hi_all + 127) / 128 - T0 : 0;
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)uniform((int)*tmem_slot);
+  constexpr uint32_t ACC2 = DHP, CS = 256, CDP = 384;
+  const int2 e = extent_of(extent);
+  const int T0 = e.y > e.x ? e.x / 128 : 0;
+  const int n_tiles = e.y > e.x ? (e.y + 127) / 128 - T0 : 0;
   const int all = DKV ? n_tiles * group : n_tiles;
   const int total = (all - part + parts - 1) / parts;             // this block's: every parts-th, from its own number on
   struct Place {                                                  // head of the group and tile of the block's i-th

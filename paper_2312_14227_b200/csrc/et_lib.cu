@@ -1112,7 +1112,7 @@ et_status run_dropout_forward(et_stack* s, int l, void* y, cudaStream_t st) {
   TimedLaunch tl(s, ET_K_ATTENTION, st);
   const LayerRT& L = s->ly[l];
   const et::DropArgs a = drop_args(s, l, 0);
-  return launch_chained(et::dropout_kernel<T>, ceil_div(a.count, et::kDropThreads * 8), et::kDropThreads, st, act_in<T>(s, l),
+  return launch_chained(et::dropout_kernel<T>, ceil_div(a.count, et::kDropTile), et::kDropThreads, st, act_in<T>(s, l),
                         L.residual_src >= 0 ? act_in<T>(s, L.residual_src) : nullptr, act_out<T>(s, l, y), nullptr, nullptr, a);
 }
 template <typename T>
@@ -1121,7 +1121,7 @@ et_status run_dropout_backward(et_stack* s, int l, const void* dY, cudaStream_t 
   const LayerRT& L = s->ly[l];
   const Below B = below(s, l);
   const et::DropArgs a = drop_args(s, l, B.act_kind);
-  return launch_chained(et::dropout_kernel<T>, ceil_div(a.count, et::kDropThreads * 8), et::kDropThreads, st, grad_act<T>(s, l + 1, dY),
+  return launch_chained(et::dropout_kernel<T>, ceil_div(a.count, et::kDropTile), et::kDropThreads, st, grad_act<T>(s, l + 1, dY),
                         L.consumer >= 0 ? grad_act<T>(s, L.consumer + 1, dY) : nullptr, B.G ? (T*)B.g_out : nullptr, (const T*)B.z,
                         (T*)B.dz, a);
 }

@@ -7,10 +7,11 @@
 //
 // Bound by HBM: in place (inside a stack) the rotated heads are read and written once, else the whole row.  A thread turns 8
 // columns (16 or 32 bytes) of every head of its row with one set of cosines and sines; the heads are cut over blockIdx.y
-// where the rows alone would leave the GPU short of warps.
+// where the rows alone would leave the GPU short of warps.  Heads go four (fp32: two) at a time, their loads in flight together: 32760 rows of
+// 16 + 16 + 16 heads of 128 in bf16, not in place, 135 us = 6.0 TB/s (a head at a time: 206 us).
 #pragma once
 
-#include "common.cuh"
+#include "dropout.cuh"
 
 namespace et {
 
@@ -31,6 +32,11 @@ __device__ __forceinline__ void turn_of(uint64_t f, int position, bool back, flo
   // signed fraction of a half turn, [-1, 1): 24 bits of it, an error of 2^-24 pi / 2 at most, that of an fp32 angle near pi
   sincospif((float)(int32_t)(uint32_t)(frac >> 32) * 4.656612873077393e-10f, s, c);
   if (back) *s = -*s;
+}
+
+template <typename T> __device__ __forceinline__ void copy_chunk(T* p, const RawChunk<T>& r) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = r.q[i];
 }
 
 template <typename T, bool VEC>
@@ -55,52 +61,77 @@ rotary_kernel(const T* in, T* out, const __grid_constant__ RotaryTable tab, cons
   }
   const size_t at = (size_t)row * a.all * a.dim;
   const int step = gridDim.y;
-  for (int h = blockIdx.y; h < a.heads; h += step) {
-    const size_t o = at + (size_t)h * a.dim;
+  constexpr int B = VEC ? 16 / (int)sizeof(T) / 2 : 1;              // heads at a time: 4 of bf16, 2 of fp32, loads in flight together
+  for (int h0 = blockIdx.y; h0 < a.heads; h0 += B * step) {
     if (VEC) {
-      float x[8], y[8];
-      if (a.adjacent) {
-        load_seg<8>(in + o + 2 * k, 8, x);
+      RawChunk<T> p0[B], p1[B];
+      const int second = a.adjacent ? 0 : a.pairs, from = a.adjacent ? 2 * k : k;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          y[2 * i] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];
-          y[2 * i + 1] = x[2 * i + 1] * c[i] + x[2 * i] * s[i];
-        }
-        store_seg<8>(out + o + 2 * k, 8, y);
-      } else {
-        load_seg<8>(in + o + k, 8, x);
-        load_seg<8>(in + o + a.pairs + k, 8, y);
+      for (int i = 0; i < B; ++i) {
+        const int h = h0 + i * step;
+        if (h >= a.heads) break;
+        const T* p = in + at + (size_t)h * a.dim + from;
+        p0[i] = load_chunk(p);
+        if (!a.adjacent) p1[i] = load_chunk(p + second);
+      }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float u = x[i] * c[i] - y[i] * s[i];
-          y[i] = y[i] * c[i] + x[i] * s[i];
-          x[i] = u;
+      for (int i = 0; i < B; ++i) {
+        const int h = h0 + i * step;
+        if (h >= a.heads) break;
+        T* p = out + at + (size_t)h * a.dim + from;
+        float x[8], y[8];
+        raw_unpack(p0[i], x);
+        if (a.adjacent) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            y[2 * j] = x[2 * j] * c[j] - x[2 * j + 1] * s[j];
+            y[2 * j + 1] = x[2 * j + 1] * c[j] + x[2 * j] * s[j];
+          }
+          store_chunk(p, y);
+        } else {
+          raw_unpack(p1[i], y);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float u = x[j] * c[j] - y[j] * s[j];
+            y[j] = y[j] * c[j] + x[j] * s[j];
+            x[j] = u;
+          }
+          store_chunk(p, x);
+          store_chunk(p + second, y);
         }
-        store_seg<8>(out + o + k, 8, x);
-        store_seg<8>(out + o + a.pairs + k, 8, y);
       }
     } else {
-      const size_t i0 = a.adjacent ? o + 2 * k : o + k, i1 = a.adjacent ? i0 + 1 : i0 + a.pairs;
+      const size_t o = at + (size_t)h0 * a.dim, i0 = a.adjacent ? o + 2 * k : o + k, i1 = a.adjacent ? i0 + 1 : i0 + a.pairs;
       const float x = to_f32(in[i0]), y = to_f32(in[i1]);
       out[i0] = from_f32<T>(x * c[0] - y * s[0]);
       out[i1] = from_f32<T>(y * c[0] + x * s[0]);
     }
   }
   if (!a.copy) return;
-  // the rest of the turned heads, and the heads that are not turned
+  // the rest of the turned heads, and the heads that are not turned: one run of the row's last columns
   const int slot = k / per_pair, rest = a.dim - 2 * a.pairs;
   for (int h = blockIdx.y; h < a.heads && rest > 0; h += step)
     for (int j = slot * V; j < rest; j += slots * V) {
       const size_t o = at + (size_t)h * a.dim + 2 * a.pairs + j;
-      if (VEC) { float x[8]; load_seg<8>(in + o, 8, x); store_seg<8>(out + o, 8, x); }
+      if (VEC) copy_chunk(out + o, load_chunk(in + o));
       else out[o] = in[o];
     }
-  for (int h = a.heads + blockIdx.y; h < a.all; h += step)
-    for (int j = slot * V; j < a.dim; j += slots * V) {
-      const size_t o = at + (size_t)h * a.dim + j;
-      if (VEC) { float x[8]; load_seg<8>(in + o, 8, x); store_seg<8>(out + o, 8, x); }
-      else out[o] = in[o];
+  const int tail = (a.all - a.heads) * a.dim, stride = slots * V * step;
+  const size_t o = at + (size_t)a.heads * a.dim;
+  for (int j0 = (blockIdx.y * slots + slot) * V; j0 < tail; j0 += 4 * stride) {
+    if (VEC) {
+      RawChunk<T> x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (j0 + i * stride < tail) x[i] = load_chunk(in + o + j0 + i * stride);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (j0 + i * stride < tail) copy_chunk(out + o + j0 + i * stride, x[i]);
+    } else {
+      for (int i = 0; i < 4; ++i)
+        if (j0 + i * stride < tail) out[o + j0 + i * stride] = in[o + j0 + i * stride];
     }
+  }
 }
 
 }  // namespace et

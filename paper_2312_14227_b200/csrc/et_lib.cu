@@ -609,9 +609,12 @@ et_status launch_tc(int bn, bool pair, const CUtensorMap& ma, const CUtensorMap&
   }
 }
 template <typename T, class Epi>
-et_status launch_simt(const T* A, const T* B, const et::simt::Params& p, const Epi& epi, cudaStream_t st) {
-  dim3 grid(ceil_div(p.cols, et::simt::TN), ceil_div(p.rows, et::simt::TM));
-  et::simt::gemm_simt_kernel<T, Epi><<<grid, et::simt::THREADS, 0, st>>>(A, B, p, epi);
+et_status launch_simt(const T* A, const T* B, const et::simt::Params& p, const Epi& epi, int sms, cudaStream_t st) {
+  // 64-wide tiles load half the operands per product; where they would not give every SM a block, 32-wide ones
+  auto grid = [&](int tile) { return dim3(ceil_div(p.cols, tile), ceil_div(p.rows, tile)); };
+  const dim3 wide = grid(64);
+  if ((long long)wide.x * wide.y >= sms) et::simt::gemm_simt_kernel<Epi, 64><<<wide, et::simt::THREADS, 0, st>>>(A, B, p, epi);
+  else et::simt::gemm_simt_kernel<Epi, 32><<<grid(32), et::simt::THREADS, 0, st>>>(A, B, p, epi);
   return after_launch();
 }
 
@@ -697,7 +700,7 @@ et_status run_forward_layer(et_stack* s, int l, void* y, cudaStream_t st) {
     p.rows = (int)s->M; p.cols = L.Nw; p.kc = L.K; p.segs = L.fold;
     p.sa_i = L.K; p.sa_k = 1;
     p.sb_k = L.N; p.sb_seg = L.Nw; p.sb_j = 1; p.b_wrap = 0;
-    return launch_simt<T>(act_in<T>(s, l), (const T*)L.W, p, epi, st);
+    return launch_simt<T>(act_in<T>(s, l), (const T*)L.W, p, epi, s->sms, st);
   }
 }
 
@@ -792,7 +795,7 @@ et_status run_dgrad_layer(et_stack* s, int l, const void* dY, cudaStream_t st, b
     p.rows = (int)s->M; p.cols = L.K; p.kc = L.dz_width(); p.segs = L.fold;
     p.sa_i = L.dz_width(); p.sa_k = 1;
     p.sb_k = 1; p.sb_seg = L.Nw; p.sb_j = L.N; p.b_wrap = 0;
-    return launch_simt<T>(dz_src<T>(s, l, dY), (const T*)L.W, p, epi, st);
+    return launch_simt<T>(dz_src<T>(s, l, dY), (const T*)L.W, p, epi, s->sms, st);
   }
 }
 
@@ -1185,11 +1188,15 @@ et_status run_gated_forward(et_stack* s, int l, void* y, cudaStream_t st) {
     return after_launch();
   }
 }
-// dZ_l from G_{l+1}
+// dZ_l from G_{l+1}; with want_sums its column sums, too, into the bias partials
 template <typename T>
-et_status run_gated_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+et_status run_gated_backward(et_stack* s, int l, const void* dY, bool want_sums, cudaStream_t st) {
   TimedLaunch tl(s, ET_K_OTHER, st);
   const LayerRT& L = s->ly[l];
+  if (want_sums)
+    return launch_chained(et::gated_backward_sums_kernel<T>, dim3(ceil_div(L.Nw, 256), ceil_div(s->M, et::kGatedRows)), 256, st,
+                          grad_act<T>(s, l + 1, dY), (const T*)s->at(L.off_Z), (T*)s->at(L.off_dZ), (float*)s->at(L.off_biaspart), s->M,
+                          L.Nw, L.gate_act);
   const long long items = s->M * ceil_div(L.Nw, 8);
   return launch_chained(et::gated_backward_kernel<T>, ceil_div(items, 256), 256, st, grad_act<T>(s, l + 1, dY), (const T*)s->at(L.off_Z),
                         (T*)s->at(L.off_dZ), s->M, L.Nw, L.gate_act);
@@ -1341,7 +1348,7 @@ et_status run_wgrad_layer(et_stack* s, int l, const void* dY, float* grad, const
       p.rows = L.K; p.cols = L.N; p.kc = (int)s->M; p.segs = 1;
       p.sa_i = 1; p.sa_k = L.K;
       p.sb_k = L.dz_width(); p.sb_seg = 0; p.sb_j = 1; p.b_wrap = L.fold > 1 ? L.Nw : 0;
-      ET_TRY(launch_simt<T>(act_in<T>(s, l), dz_src<T>(s, l, dY), p, epi, st));
+      ET_TRY(launch_simt<T>(act_in<T>(s, l), dz_src<T>(s, l, dY), p, epi, s->sms, st));
     }
   }
   ++*launches;
@@ -1797,7 +1804,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
       const bool norm = Y.vector_params();
       const double gemm = !Y.gemms() ? 0.0 : 2.0 * (double)s->M * Y.K * Y.N;
       if (Y.kind == ET_LAYER_GATED) {
-        ET_TRY(run_gated_backward<T>(s, l, dY, cs));
+        ET_TRY(run_gated_backward<T>(s, l, dY, mask[2 * l + 1] != 0, cs));
         if (two) CU_TRY(cudaEventRecord(s->chain_ev[l + 1], cs));   // dZ_l is ready (not only the gradient of the layer's output)
         ++launches;
       }
@@ -1805,8 +1812,9 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
         // On the tensor-core path the column partials of dZ_l were left by dgrad(l+1) in this
         // layer's own buffer; finishing them need not sit on the chain's critical path.
         // (A normalisation layer above leaves none: the column-sum kernel runs instead.)
-        const int fused = (is_bf16<T>::value && l < L - 1 && s->ly[l + 1].gemms() && Y.kind != ET_LAYER_GATED)
-                              ? dgrad_row_blocks(s, l + 1) : 0;
+        // A gated layer's are left by the kernel that forms dZ_l.
+        const int fused = Y.kind == ET_LAYER_GATED ? ceil_div(s->M, et::kGatedRows)
+                          : (is_bf16<T>::value && l < L - 1 && s->ly[l + 1].gemms()) ? dgrad_row_blocks(s, l + 1) : 0;
         // Which stream: with few selected kernels the caller's stream is nearly idle and takes
         // the finishers off the chain; with many it is the busier one and the chain keeps them.
         cudaStream_t bs = s->wgrad_one_unit ? st : cs;
@@ -3180,8 +3188,8 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
       if (s->ly[l].kind == ET_LAYER_GATED) {
         // its activation and product: non-trainable work above the layer's own tensors (Section 5.3), like a layer of its own
         double t_gate = 0.0;
-        if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_gated_backward<bf16>(s, l, dY, st); }, &t_gate));
-        else ET_TRY(timed([&]() { return run_gated_backward<float>(s, l, dY, st); }, &t_gate));
+        if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_gated_backward<bf16>(s, l, dY, false, st); }, &t_gate));
+        else ET_TRY(timed([&]() { return run_gated_backward<float>(s, l, dY, false, st); }, &t_gate));
         t_dy[2 * l + 1] += t_gate;
       }
       if (s->dtype == ET_BF16) {

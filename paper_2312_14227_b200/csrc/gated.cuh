@@ -12,6 +12,7 @@
 // 10 bytes an output in bf16); the error gradient dZ W^T and the weight gradient a^T dZ are those of a dense layer with 2 h columns.
 #pragma once
 
+#include "dropout.cuh"
 #include "gemm_tc.cuh"
 
 namespace et {
@@ -291,17 +292,10 @@ gated_forward_simt_kernel(const float* __restrict__ A, const float* __restrict__
 
 // dZ from g [M x h] and Z [M x 2 h]; a thread takes 8 columns of a row.
 template <typename T>
-__global__ void __launch_bounds__(256)
-gated_backward_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* __restrict__ dZ, long long M, int h, int act) {
-  chain_begin();
-  const int per_row = (h + 7) / 8;
-  const long long item = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long row = item / per_row;
-  if (row >= M) return;
-  const int col = (int)(item - row * per_row) * 8, n = min(8, h - col);
-  float v[8], a[8], b[8];
-  const size_t at = (size_t)row * 2 * h + col;
-  load_seg<8>(g + (size_t)row * h + col, n, v);
+__device__ __forceinline__ void gated_backward_run(const T* g, const T* Z, T* dZ, size_t row, int h, int col, int n, int act, float (&a)[8], float (&b)[8]) {
+  float v[8];
+  const size_t at = row * 2 * h + col;
+  load_seg<8>(g + row * h + col, n, v);
   load_seg<8>(Z + at, n, a);
   load_seg<8>(Z + at + h, n, b);
 #pragma unroll
@@ -312,6 +306,86 @@ gated_backward_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* __res
   }
   store_seg<8>(dZ + at, n, a);
   store_seg<8>(dZ + at + h, n, b);
+}
+template <typename T>
+__global__ void __launch_bounds__(256)
+gated_backward_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* __restrict__ dZ, long long M, int h, int act) {
+  chain_begin();
+  const int per_row = (h + 7) / 8;
+  const long long item = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long row = item / per_row;
+  if (row >= M) return;
+  const int col = (int)(item - row * per_row) * 8;
+  float a[8], b[8];
+  gated_backward_run<T>(g, Z, dZ, (size_t)row, h, col, min(8, h - col), act, a, b);
+}
+// The same with the column sums of dZ over runs of kGatedRows rows in part[run][2 h]: the bias gradient without reading dZ again.  A block
+// takes one run and 256 columns of each half, a thread four rows of eight columns, their loads in flight together; the rows' sums are
+// joined in a fixed order.  8192 x 5632 in bf16: 83 us (without sums 77, and 52 for the pass that sums dZ columns).
+constexpr int kGatedRows = 32;
+template <typename T>
+__global__ void __launch_bounds__(256)
+gated_backward_sums_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* __restrict__ dZ, float* __restrict__ part, long long M, int h, int act) {
+  chain_begin();
+  __shared__ float sums[8][2][256];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int col = blockIdx.x * 256 + lane * 8, n = min(8, h - col);
+  const long long r0 = (long long)blockIdx.y * kGatedRows + w;
+  float sa[8] = {}, sb[8] = {};
+  if (n == 8 && h % 8 == 0) {
+    constexpr int B = sizeof(T) == 2 ? 4 : 2;                       // rows in flight
+#pragma unroll
+    for (int r = 0; r < 4; r += B) {
+      RawChunk<T> x[B], zg[B], zu[B];
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        const long long row = r0 + (r + i) * 8;
+        if (row >= M) break;
+        const size_t at = (size_t)row * 2 * h + col;
+        x[i] = load_chunk(g + (size_t)row * h + col);
+        zg[i] = load_chunk(Z + at);
+        zu[i] = load_chunk(Z + at + h);
+      }
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        const long long row = r0 + (r + i) * 8;
+        if (row >= M) break;
+        const size_t at = (size_t)row * 2 * h + col;
+        float v[8], a[8], b[8];
+        raw_unpack(x[i], v);
+        raw_unpack(zg[i], a);
+        raw_unpack(zu[i], b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 f = gate_both<T>(a[j], act);
+          a[j] = v[j] * b[j] * f.y;
+          b[j] = v[j] * f.x;
+          sa[j] += a[j];
+          sb[j] += b[j];
+        }
+        store_chunk(dZ + at, a);
+        store_chunk(dZ + at + h, b);
+      }
+    }
+  } else if (n > 0) {
+    for (long long row = r0; row < min((long long)(blockIdx.y + 1) * kGatedRows, M); row += 8) {
+      float a[8], b[8];
+      gated_backward_run<T>(g, Z, dZ, (size_t)row, h, col, n, act, a, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { sa[i] += a[i]; sb[i] += b[i]; }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { sums[w][0][i * 32 + lane] = sa[i]; sums[w][1][i * 32 + lane] = sb[i]; }
+  __syncthreads();
+  const int c = blockIdx.x * 256 + threadIdx.x, at = (threadIdx.x & 7) * 32 + (threadIdx.x >> 3);
+  if (c >= h) return;
+  float s[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) { s[0] += sums[i][0][at]; s[1] += sums[i][1][at]; }
+  float* out = part + (size_t)blockIdx.y * 2 * h + c;
+  out[0] = s[0];
+  out[h] = s[1];
 }
 
 }  // namespace et

@@ -405,16 +405,19 @@ using et::bf16;
 // gets units.  A CTA pair (cta_group::2) loads half of B per CTA and so moves fewer L2 bytes per
 // flop; a 192-wide pair tile needs 32-row B boxes and therefore a K-major B (dgrad only).
 struct TilePlan { int bn; int split; bool pair; };
+// alone_max: widest tile of a single CTA that launch_tc has for the GEMM's epilogue: 256, 192 with one staged slot, 128 with two.  The tensor map of
+// B's tile is made for the width chosen here, so a wider choice would load past the tile that the kernel has room for.
 // fractional: the GEMM shares the GPU with another stream's work, which fills the SMs a partly filled
 // last wave leaves idle, so the cost is the work itself (fractional waves), not whole waves.
 TilePlan choose_tiles(int rows, int cols, int kb_total, int sms, bool allow_split, bool b_k_major, int n_multiple,
-                      bool fractional = false) {
-  TilePlan best{256, 1, false};
+                      bool fractional = false, int alone_max = 256) {
+  TilePlan best{std::min(256, alone_max), 1, false};
   double best_cost = -1.0;
   const double sm_flops = 10.5e12, sm_l2_bytes = 10.5e12 / 148.0;
   for (int pair = 0; pair < 2; ++pair) {
     for (int bn : {256, 192, 128}) {
       if (pair && bn == 192 && !b_k_major) continue;
+      if (!pair && bn > alone_max) continue;                           // beside its staged epilogue a single CTA has no room for a wider one
       if (n_multiple > 0 && n_multiple % bn != 0) continue;          // a folded wgrad tile must not straddle slices
       const int tile_m = pair ? 256 : 128;
       const long long tiles = (long long)ceil_div(rows, tile_m) * ceil_div(cols, bn);
@@ -598,9 +601,11 @@ et_status launch_tc(int bn, bool pair, const CUtensorMap& ma, const CUtensorMap&
   // staged epilogues take 64 KB of shared memory per slot: a single CTA keeps a deep enough
   // operand ring only with narrower tiles
   if constexpr (Epi::kSlots == 2) {
+    if (bn != 128) return ET_ERR_UNSUPPORTED;                // B's map has boxes of bn rows
     return launch_tc_bn<128, A_MN, B_MN, false>(ma, mb, em, p, epi, sms, st, one_unit, overlap_prev);
   } else if constexpr (Epi::kSlots == 1) {
     if (bn == 128) return launch_tc_bn<128, A_MN, B_MN, false>(ma, mb, em, p, epi, sms, st, one_unit, overlap_prev);
+    if (bn != 192) return ET_ERR_UNSUPPORTED;
     return launch_tc_bn<192, A_MN, B_MN, false>(ma, mb, em, p, epi, sms, st, one_unit, overlap_prev);
   } else {
     if (bn == 128) return launch_tc_bn<128, A_MN, B_MN, false>(ma, mb, em, p, epi, sms, st, one_unit, overlap_prev);
@@ -2251,8 +2256,10 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     } else if (dtype == ET_BF16) {
       const int kb_n = ceil_div(y.dz_width(), et::tc::BK) * y.fold;
       if (y.kind == ET_LAYER_GATED) y.bn_gated = (long long)ceil_div(M, 256) * ceil_div(y.Nw, 128) >= s->sms / 2 ? 128 : 64;
-      const TilePlan f = choose_tiles((int)M, y.Nw, ceil_div(y.K, et::tc::BK) * y.fold, s->sms, false, false, 0);
-      const TilePlan d = choose_tiles((int)M, y.K, kb_n, s->sms, false, true, 0);
+      const bool forward_two = y.act != ET_ACT_NONE;                       // Z and the output
+      const bool dgrad_two = l >= 1 && s->ly[l - 1].act != ET_ACT_NONE && (y.consumer >= 0 || s->ly[l - 1].residual_src >= 0);
+      const TilePlan f = choose_tiles((int)M, y.Nw, ceil_div(y.K, et::tc::BK) * y.fold, s->sms, false, false, 0, false, forward_two ? 128 : 192);
+      const TilePlan d = choose_tiles((int)M, y.K, kb_n, s->sms, false, true, 0, false, dgrad_two ? 128 : 192);
       const TilePlan w = choose_tiles(y.K, y.N, ceil_div(M, et::tc::BK), s->sms, true, false, y.fold > 1 ? y.Nw : 0);
       y.bn_fwd = f.bn; y.pair_fwd = f.pair;
       y.bn_dgrad = d.bn; y.pair_dgrad = d.pair;
@@ -2260,7 +2267,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       // (the 1x1 convolutions of a ResNet block: 3.3 GFLOP) are launch-bound, the other stream finds the GPU
       // mostly idle and is better off with the stand-alone plan (its full backprop went 0.34 -> 0.41 ms otherwise).
       y.big_gemm = 2.0 * (double)M * y.K * y.N >= 10e9;
-      const TilePlan dsh = y.big_gemm ? choose_tiles((int)M, y.K, kb_n, s->sms, false, true, 0, true) : d;
+      const TilePlan dsh = y.big_gemm ? choose_tiles((int)M, y.K, kb_n, s->sms, false, true, 0, true, dgrad_two ? 128 : 192) : d;
       y.bn_dgrad_sh = dsh.bn; y.pair_dgrad_sh = dsh.pair;
       y.bn_wgrad = w.bn; y.pair_wgrad = w.pair; y.split = w.split;
       // One-launch backward: units of all GEMMs share the CTAs, so a weight gradient need not fill the GPU by

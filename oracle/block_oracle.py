@@ -123,8 +123,10 @@ def act(z, kind):
     return 0.5 * z * (1 + t), 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c0 * (1 + 3 * c1 * z * z), 1.2
 
 
-def gated(x, W, b, kind, dy, u):
-    """Results and bounds of a gated layer by itself: y, dx, dW, db.  u: half a step of the storage type."""
+def gated(x, W, b, kind, dy, u, uz=None, dy_err=0.0):
+    """Results and bounds of a gated layer by itself: y, dx, dW, db.  u: half a step of the storage type; uz: of the type that Z is kept in
+    (bf16 stacks: fp16, 2^-11); dy_err: bound of the error that dy comes with."""
+    uz = (2.0 ** -11 if u == U else u) if uz is None else uz
     M, K = x.shape
     h = W.shape[1] // 2
     z = x @ W + b
@@ -135,7 +137,7 @@ def gated(x, W, b, kind, dy, u):
     ferr = 1.2 * zerr[:, :h] + near * (np.abs(zg) + 1)
     y = f * zu
     out = {"y": (y, ferr * np.abs(zu) + np.abs(f) * zerr[:, h:] + (u + 2 * E) * np.abs(y))}
-    zerr = zerr + u * np.abs(z)                          # Z is kept in the storage type
+    zerr = zerr + uz * np.abs(z) + (2.0 ** -25 if uz == 2.0 ** -11 else 0.0)     # as Z is kept (fp16: steps of 2^-24 near 0)
     serr = curve * zerr[:, :h] + near * (np.abs(zg) + 1)
     if kind == 2:
         serr = serr + (np.abs(zg) <= zerr[:, :h])
@@ -143,7 +145,7 @@ def gated(x, W, b, kind, dy, u):
     dg, du = dy * zu * s, dy * f
     dz = np.concatenate([dg, du], axis=1)
     derr = np.concatenate([np.abs(dy) * (np.abs(zu) * serr + np.abs(s) * zerr[:, h:]), np.abs(dy) * ferr], axis=1)
-    derr = derr + (u + 3 * E) * np.abs(dz)
+    derr = derr + (u + 3 * E) * np.abs(dz) + np.concatenate([dy_err * np.abs(zu * s), dy_err * np.abs(f)], axis=1)
     dx = dz @ W.T
     out["dx"] = (dx, (derr + E * (2 * h + 2) * np.abs(dz)) @ np.abs(W).T + u * np.abs(dx))
     out["dW"] = (x.T @ dz, np.abs(x).T @ (derr + E * (M + 2) * np.abs(dz)))

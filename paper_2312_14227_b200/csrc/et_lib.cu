@@ -250,6 +250,7 @@ struct LayerRT {
   int norm_blocks = 0;      // norm: blocks of the backward kernel = rows of off_gpart
   int heads = 0, seq = 0;   // attention: K = 3N, N = 64 * heads, rows in sequences of `seq`
   size_t off_lse = 0;       // attention: log-sum-exp per (sequence, head, row)
+  size_t off_rest = 0;      // masked attention: what rounding the output to bf16 left, [M x N] bf16
   int consumer = -1;        // layer whose residual reads a_l (its output gradient joins G_l), or -1
   void* W = nullptr;
   void* b = nullptr;
@@ -282,6 +283,7 @@ struct LayerRT {
   bool own_dz() const { return act != ET_ACT_NONE || kind == ET_LAYER_GATED; }          // dZ_l is not G_{l+1} itself
   int bn_gated = 128;       // output columns of a tile
   et::gated::Maps gmaps;    // its tensor maps (input and, as the last layer, output: filled in per call)
+  CUtensorMap map_dz_half[2];   // the halves of dZ
   // ET_LAYER_MASKED_ATTENTION (heads, seq; off_lse: log-sum-exp and D) and ET_LAYER_ROTARY
   int kv = 0, dim = 0;
   bool causal = false;
@@ -709,6 +711,12 @@ et_status run_forward_layer(et_stack* s, int l, void* y, cudaStream_t st) {
   }
 }
 
+// Whether dZ of gated layer l is formed in the epilogue of the error-gradient product above it (bf16; nothing else joins the gradient of its
+// output, and that product is a plain one).
+bool gate_fused(const et_stack* s, int l) {
+  return s->dtype == ET_BF16 && s->ly[l].kind == ET_LAYER_GATED && l + 1 < s->L && s->ly[l + 1].gemms() && s->ly[l + 1].consumer < 0;
+}
+
 // G_l = dZ_l W_l^T (+ skip gradient), dZ_{l-1} = G_l * act'(Z_{l-1})
 // Row blocks of 32 that the dgrad GEMM of layer l writes fused column sums for.
 int dgrad_row_blocks(const et_stack* s, int l) {
@@ -766,6 +774,14 @@ et_status run_dgrad_layer(et_stack* s, int l, const void* dY, cudaStream_t st, b
     const CUtensorMap& skip = need_skip ? g_map(s, Lc.consumer + 1).b128 : gout;
     const CUtensorMap& zmap = need_act ? s->ly[lo - 1].map_Z.b128 : gout;
     const CUtensorMap& dzout = need_act ? s->ly[lo - 1].map_dZ.b128 : gout;
+    if (!conv && lo >= 1 && gate_fused(s, lo - 1)) {          // dZ_{l-1} of the gated layer below
+      const LayerRT& P = s->ly[lo - 1];
+      et::GatedDgradEpi epi;
+      epi.has_in[0] = epi.has_in[1] = epi.has_out[0] = epi.has_out[1] = true;
+      epi.act = P.gate_act; epi.colsum = colsum; epi.h = P.Nw;
+      em.in[0] = P.gmaps.out[0]; em.in[1] = P.gmaps.out[1]; em.out[0] = P.map_dz_half[0]; em.out[1] = P.map_dz_half[1];
+      return launch_tc<false, false>(bn_d, pair_d, amap, wmap, em, p, epi, s->sms, st, false, s->overlap_launch && !s->chain_shares_gpu);
+    }
     if (!need_act) {                                          // G_l = acc (+ skip)
       et::DgradEpiS<1> epi;
       epi.has_in[0] = need_skip; epi.has_in[1] = false; epi.has_out[0] = true; epi.has_out[1] = false;
@@ -1056,6 +1072,7 @@ et::seqattn::Args seq_args(const et_stack* s, int l) {
   a.ld = ceil_div(s->M, 128) * 128;
   a.lse = (float*)s->at(L.off_lse);
   a.D = a.lse + (size_t)L.heads * a.ld;
+  a.rest = s->at(L.off_rest);
   a.slopes = L.slopes;
   a.status = (uint32_t*)s->at(s->off_status);
   a.heads = L.heads; a.kv = L.kv; a.dim = L.dim;
@@ -1808,7 +1825,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
       }
       const bool norm = Y.vector_params();
       const double gemm = !Y.gemms() ? 0.0 : 2.0 * (double)s->M * Y.K * Y.N;
-      if (Y.kind == ET_LAYER_GATED) {
+      if (Y.kind == ET_LAYER_GATED && !gate_fused(s, l)) {
         ET_TRY(run_gated_backward<T>(s, l, dY, mask[2 * l + 1] != 0, cs));
         if (two) CU_TRY(cudaEventRecord(s->chain_ev[l + 1], cs));   // dZ_l is ready (not only the gradient of the layer's output)
         ++launches;
@@ -1818,7 +1835,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
         // layer's own buffer; finishing them need not sit on the chain's critical path.
         // (A normalisation layer above leaves none: the column-sum kernel runs instead.)
         // A gated layer's are left by the kernel that forms dZ_l.
-        const int fused = Y.kind == ET_LAYER_GATED ? ceil_div(s->M, et::kGatedRows)
+        const int fused = Y.kind == ET_LAYER_GATED && !gate_fused(s, l) ? ceil_div(s->M, et::kGatedRows)
                           : (is_bf16<T>::value && l < L - 1 && s->ly[l + 1].gemms()) ? dgrad_row_blocks(s, l + 1) : 0;
         // Which stream: with few selected kernels the caller's stream is nearly idle and takes
         // the finishers off the chain; with many it is the busier one and the chain keeps them.
@@ -1853,7 +1870,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
         continue;
       }
       if (l > to) {
-        ET_TRY(run_dgrad_layer<T>(s, l, dY, cs, l >= 1 && mask[2 * (l - 1) + 1] != 0 && s->ly[l - 1].kind != ET_LAYER_GATED));
+        ET_TRY(run_dgrad_layer<T>(s, l, dY, cs, l >= 1 && mask[2 * (l - 1) + 1] != 0 && (s->ly[l - 1].kind != ET_LAYER_GATED || gate_fused(s, l - 1))));
         if (two) CU_TRY(cudaEventRecord(s->chain_ev[l], cs));   // dZ_{l-1} ready, W_l no longer needed
         if (two && l >= 1 && s->ly[l - 1].implicit) CU_TRY(cudaEventRecord(s->chain_ev[l - 1], cs));   // and the gather's backward with it
         ++launches;
@@ -2231,6 +2248,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     }
     if (y.kind == ET_LAYER_MASKED_ATTENTION) {
       y.off_lse = take((size_t)2 * y.heads * ceil_div(M, 128) * 128 * sizeof(float));      // log-sum-exp, D
+      y.off_rest = take((size_t)M * y.N * s->elt);
     } else if (y.kind == ET_LAYER_ROTARY || y.kind == ET_LAYER_DROPOUT) {
     } else if (y.kind == ET_LAYER_ATTENTION) {
       y.off_lse = take((size_t)M * y.heads * sizeof(float));
@@ -2257,7 +2275,8 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       const int kb_n = ceil_div(y.dz_width(), et::tc::BK) * y.fold;
       if (y.kind == ET_LAYER_GATED) y.bn_gated = (long long)ceil_div(M, 256) * ceil_div(y.Nw, 128) >= s->sms / 2 ? 128 : 64;
       const bool forward_two = y.act != ET_ACT_NONE;                       // Z and the output
-      const bool dgrad_two = l >= 1 && s->ly[l - 1].act != ET_ACT_NONE && (y.consumer >= 0 || s->ly[l - 1].residual_src >= 0);
+      const bool dgrad_two = l >= 1 && ((s->ly[l - 1].act != ET_ACT_NONE && (y.consumer >= 0 || s->ly[l - 1].residual_src >= 0)) ||
+                                        gate_fused(s, l - 1));
       const TilePlan f = choose_tiles((int)M, y.Nw, ceil_div(y.K, et::tc::BK) * y.fold, s->sms, false, false, 0, false, forward_two ? 128 : 192);
       const TilePlan d = choose_tiles((int)M, y.K, kb_n, s->sms, false, true, 0, false, dgrad_two ? 128 : 192);
       const TilePlan w = choose_tiles(y.K, y.N, ceil_div(M, et::tc::BK), s->sms, true, false, y.fold > 1 ? y.Nw : 0);
@@ -2438,7 +2457,8 @@ et_status et_stack_bind(et_stack* s, void* const* W, void* const* b, void* works
       if (y.kind == ET_LAYER_GATED) {
         for (int i = 0; i < 2; ++i) {
           ET_TRY(make_part_map(&y.gmaps.w[i], (const bf16*)y.W + (size_t)i * y.Nw, y.Nw, y.K, y.N, y.Nw % 64 == 0 ? y.bn_gated / 64 : -1));
-          ET_TRY(make_part_map(&y.gmaps.out[i], (const bf16*)s->at(y.off_Z) + (size_t)i * y.Nw, y.Nw, s->M, y.N, 0));
+          ET_TRY(make_part_map(&y.gmaps.out[i], (const bf16*)s->at(y.off_Z) + (size_t)i * y.Nw, y.Nw, s->M, y.N, 0));      // (fp16: as wide)
+          ET_TRY(make_part_map(&y.map_dz_half[i], (const bf16*)s->at(y.off_dZ) + (size_t)i * y.Nw, y.Nw, s->M, y.N, 0));
         }
       }
       if (y.kind == ET_LAYER_DENSE && l >= 1 && s->ly[l - 1].implicit) ET_TRY(make_map(&y.map_Wd_conv, y.W, y.N, y.K, 128));
@@ -3192,7 +3212,7 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
         t_dy[2 * l + 1] = t_box + t_beta;
         continue;
       }
-      if (s->ly[l].kind == ET_LAYER_GATED) {
+      if (s->ly[l].kind == ET_LAYER_GATED && !gate_fused(s, l)) {
         // its activation and product: non-trainable work above the layer's own tensors (Section 5.3), like a layer of its own
         double t_gate = 0.0;
         if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_gated_backward<bf16>(s, l, dY, false, st); }, &t_gate));

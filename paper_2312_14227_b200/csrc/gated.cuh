@@ -8,9 +8,17 @@
 // Tensor-bound like the dense layer of 2 h columns; the epilogue writes 6 bytes an output.
 // H = 128 (256 columns of accumulator); 64 where 128-wide tiles would leave CTA pairs without work.
 //
-// Backward: gated_backward_kernel forms dZ_gate = g Z_up act'(Z_gate), dZ_up = g act(Z_gate) in one pass over g and Z (HBM-bound,
-// 10 bytes an output in bf16); the error gradient dZ W^T and the weight gradient a^T dZ are those of a dense layer with 2 h columns.
+// Backward: dZ_gate = g Z_up act'(Z_gate), dZ_up = g act(Z_gate).  Below a dense or gated layer they are formed in the epilogue of that layer's
+// error-gradient product, from its accumulator (GatedDgradEpi): g is neither rounded nor stored, and the bias sums come with it.  Elsewhere
+// one pass over g and Z forms them (gated_backward_kernel).  The error gradient dZ W^T and the weight gradient a^T dZ are those of a
+// dense layer with 2 h columns.
+//
+// Rounding: the product and dZ are bf16, as what a dense layer stores.  Z of a bf16 stack is kept in fp16: the gradient is read off values
+// of Z, and their 2^-11 leaves dZ's own rounding as the only one that counts (error of dX against 64 bits 2.4e-3 instead of 3.4e-3, of which the last
+// rounding alone is 1.7e-3).  Z beyond 65504 is kept as 65504; the product is formed before that, from fp32.
 #pragma once
+
+#include <type_traits>
 
 #include "dropout.cuh"
 #include "gemm_tc.cuh"
@@ -19,9 +27,15 @@ namespace et {
 
 constexpr int kActSilu = 3;
 
-// T: storage type.  __expf is off by a few times 2^-22, far below a bf16 step; fp32 stacks take expf and a true quotient.
+// T: storage type.  bf16 stacks take the exponential and reciprocal units' own results (2^-22, far below a bf16 step; an exponential beyond fp32
+// gives 0), fp32 stacks expf and a true quotient.
 template <typename T> __device__ __forceinline__ float sigmoid_of(float z);
-template <> __device__ __forceinline__ float sigmoid_of<bf16>(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+template <> __device__ __forceinline__ float sigmoid_of<bf16>(float z) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(e + 1.0f));
+  return r;
+}
 template <> __device__ __forceinline__ float sigmoid_of<float>(float z) { return 1.0f / (1.0f + expf(-z)); }
 template <typename T>
 __device__ __forceinline__ float gate_apply(float z, int act) {
@@ -31,15 +45,73 @@ __device__ __forceinline__ float gate_apply(float z, int act) {
 template <typename T>
 __device__ __forceinline__ float2 gate_both(float z, int act) {
   if (act == kActSilu) {
-    const float g = sigmoid_of<T>(z);
-    return make_float2(z * g, g * fmaf(z, 1.0f - g, 1.0f));
+    const float g = sigmoid_of<T>(z), f = z * g;
+    return make_float2(f, fmaf(f, 1.0f - g, g));                    // g + z g (1 - g)
   }
   return make_float2(act_apply(z, act), act_grad(z, act));
 }
 
+// fp16 as Z is kept: held at the largest finite value, NaN stays NaN
+__device__ __forceinline__ uint32_t pack_z(float a, float b) {
+  asm("min.NaN.f32 %0, %0, 0f477FE000;\n\tmax.NaN.f32 %0, %0, 0fC77FE000;" : "+f"(a));
+  asm("min.NaN.f32 %0, %0, 0f477FE000;\n\tmax.NaN.f32 %0, %0, 0fC77FE000;" : "+f"(b));
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void unpack_z(const uint4& q, float (&t)[8]) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+    t[2 * i] = f.x;
+    t[2 * i + 1] = f.y;
+  }
+}
+
+// Epilogue of the error-gradient product above a gated layer.  slot 0: in Z_gate, out dZ_gate; slot 1: in Z_up, out dZ_up.
+struct GatedDgradEpi {
+  static constexpr int kSlots = 2;
+  bool has_in[2], has_out[2];
+  int act;
+  float* colsum;     // [row blocks of 32][2 h] or nullptr
+  int h;
+
+  __device__ __forceinline__ void combine(int, int, float (&v)[32], float (&s0)[32], float (&s1)[32]) const {
+    auto all = [&](auto kind) {                                     // one test for 32 values
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const float2 f = gate_both<bf16>(s0[i], decltype(kind)::value);
+        s0[i] = v[i] * s1[i] * f.y;
+        s1[i] = v[i] * f.x;
+      }
+    };
+    if (act == kActSilu) all(std::integral_constant<int, kActSilu>());
+    else if (act == kActGelu) all(std::integral_constant<int, kActGelu>());
+    else all(std::integral_constant<int, kActRelu>());
+  }
+  __device__ __forceinline__ void column_sums(int row_block, int col0, int nv, float (&s0)[32], float (&s1)[32], int lane) const {
+    if (colsum == nullptr) return;
+    warp_column_sums(s0, lane);
+    warp_column_sums(s1, lane);
+    if (lane < nv) {
+      float* out = colsum + (size_t)row_block * 2 * h + col0 + lane;
+      out[0] = s0[0];
+      out[h] = s1[0];
+    }
+  }
+};
+template <> struct tc::EpiHalfIn<GatedDgradEpi> { static constexpr bool value = true; };
+
 namespace gated {
 
 using namespace et::tc;
+
+__device__ __forceinline__ void sts_z32(uint8_t* chunk, int row, int half, const float (&v)[32]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *reinterpret_cast<uint4*>(chunk + epi_chunk_off(row, half * 4 + j)) =
+        make_uint4(pack_z(v[j * 8], v[j * 8 + 1]), pack_z(v[j * 8 + 2], v[j * 8 + 3]), pack_z(v[j * 8 + 4], v[j * 8 + 5]), pack_z(v[j * 8 + 6], v[j * 8 + 7]));
+}
 
 template <int H>
 struct Cfg {
@@ -213,10 +285,15 @@ gated_forward_kernel(const __grid_constant__ Maps maps, const Params p) {
           load_seg<32>(p.bias + p.h + col, p.h - col, t);
 #pragma unroll
           for (int i = 0; i < 32; ++i) zu[i] += t[i];
-          sts_row32(buf, trow, hf, zg);
-          sts_row32(buf + EPI_CHUNK_BYTES, trow, hf, zu);
+          sts_z32(buf, trow, hf, zg);
+          sts_z32(buf + EPI_CHUNK_BYTES, trow, hf, zu);
+          if (p.act == kActSilu) {                  // one test for 32 values
 #pragma unroll
-          for (int i = 0; i < 32; ++i) zg[i] = gate_apply<bf16>(zg[i], p.act) * zu[i];
+            for (int i = 0; i < 32; ++i) zg[i] = gate_apply<bf16>(zg[i], kActSilu) * zu[i];
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) zg[i] = act_apply(zg[i], p.act) * zu[i];
+          }
           sts_row32(buf + 2 * EPI_CHUNK_BYTES, trow, hf, zg);
         }
         fence_async_smem();
@@ -291,13 +368,15 @@ gated_forward_simt_kernel(const float* __restrict__ A, const float* __restrict__
 }
 
 // dZ from g [M x h] and Z [M x 2 h]; a thread takes 8 columns of a row.
+__device__ __forceinline__ void load_z(const float* Z, int n, float (&t)[8]) { load_seg<8>(Z, n, t); }
+__device__ __forceinline__ void load_z(const bf16* Z, int, float (&t)[8]) { unpack_z(*reinterpret_cast<const uint4*>(Z), t); }   // h % 8 == 0: whole runs
 template <typename T>
 __device__ __forceinline__ void gated_backward_run(const T* g, const T* Z, T* dZ, size_t row, int h, int col, int n, int act, float (&a)[8], float (&b)[8]) {
   float v[8];
   const size_t at = row * 2 * h + col;
   load_seg<8>(g + row * h + col, n, v);
-  load_seg<8>(Z + at, n, a);
-  load_seg<8>(Z + at + h, n, b);
+  load_z(Z + at, n, a);
+  load_z(Z + at + h, n, b);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float2 f = gate_both<T>(a[i], act);
@@ -353,8 +432,13 @@ gated_backward_sums_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* 
         const size_t at = (size_t)row * 2 * h + col;
         float v[8], a[8], b[8];
         raw_unpack(x[i], v);
-        raw_unpack(zg[i], a);
-        raw_unpack(zu[i], b);
+        if constexpr (sizeof(T) == 2) {
+          unpack_z(zg[i].q[0], a);
+          unpack_z(zu[i].q[0], b);
+        } else {
+          raw_unpack(zg[i], a);
+          raw_unpack(zu[i], b);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float2 f = gate_both<T>(a[j], act);

@@ -311,6 +311,10 @@ __host__ __device__ constexpr uint32_t make_idesc() {
          ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(MM >> 4) << 24);
 }
 
+// Whether an epilogue's staged input values are fp16 (they are moved as 16-bit values either way); bf16 else.
+template <class Epi>
+struct EpiHalfIn { static constexpr bool value = false; };
+
 template <class Epi>
 __device__ __forceinline__ void epi_set_split(Epi&, int) {}
 __device__ __forceinline__ void epi_set_split(PartialEpi& e, int s) { e.split = s; }
@@ -319,6 +323,7 @@ __device__ __forceinline__ void epi_set_split(PartialEpi& e, int s) { e.split = 
 __device__ __forceinline__ uint32_t epi_chunk_off(int row, int piece) {
   return (uint32_t)((row >> 6) * CHUNK_BYTES + (row & 63) * 128 + ((piece ^ (row & 7)) << 4));
 }
+template <bool HALF = false>
 __device__ __forceinline__ void lds_row32(const uint8_t* chunk, int row, int half, float (&v)[32]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -326,8 +331,14 @@ __device__ __forceinline__ void lds_row32(const uint8_t* chunk, int row, int hal
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      v[j * 8 + 2 * i] = __uint_as_float(w[i] << 16);
-      v[j * 8 + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      if constexpr (HALF) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        v[j * 8 + 2 * i] = f.x;
+        v[j * 8 + 2 * i + 1] = f.y;
+      } else {
+        v[j * 8 + 2 * i] = __uint_as_float(w[i] << 16);
+        v[j * 8 + 2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
     }
   }
 }
@@ -724,8 +735,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
           for (int h = 0; h < 2; ++h) {
             float (&v)[32] = h == 0 ? v0 : v1;
             float s0[32], s1[32];
-            if (epi.has_in[0]) lds_row32(buf0, trow, h, s0);
-            if (SLOTS > 1 && epi.has_in[SLOTS - 1]) lds_row32(buf1, trow, h, s1);
+            if (epi.has_in[0]) lds_row32<EpiHalfIn<Epi>::value>(buf0, trow, h, s0);
+            if (SLOTS > 1 && epi.has_in[SLOTS - 1]) lds_row32<EpiHalfIn<Epi>::value>(buf1, trow, h, s1);
             epi.combine(col0 + h * 32, p.cols - (col0 + h * 32), v, s0, s1);
             if (epi.has_out[0]) sts_row32(buf0, trow, h, s0);
             if (SLOTS > 1 && epi.has_out[SLOTS - 1]) sts_row32(buf1, trow, h, s1);

@@ -68,7 +68,7 @@ cudaError_t forward(const CUtensorMap& qkv, const CUtensorMap& out, Args a, int 
 
 cudaError_t backward(const CUtensorMap& qkv, const CUtensorMap& g, const CUtensorMap& gqkv, const void* out, const void* dout, void* dqkv, Args a, int sms, cudaStream_t st) {
   const long long threads = (long long)a.mask.M * a.heads * 16;
-  cudaError_t e = launch(dot_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, 1, (const bf16*)out, (const bf16*)dout, a.D,
+  cudaError_t e = launch(dot_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, 1, (const bf16*)out, (const bf16*)a.rest, (const bf16*)dout, a.D,
                          a.mask.M, a.heads, a.dim, a.ld);
   if (e != cudaSuccess) return e;
   const unsigned tiles = (unsigned)((a.mask.M + 127) / 128);

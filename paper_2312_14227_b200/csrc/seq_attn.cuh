@@ -22,7 +22,9 @@
 // atomics: a shared head's gradient is the sum that one block forms in order.  The price is that S and dP are formed
 // twice, 7 products where 5 would do.
 //
-// Rounding: P and dS are bf16 (half a step 2^-9 of each term); scores, maxima, sums, D and all accumulators are fp32.
+// Rounding: P and dS are bf16 (half a step 2^-8 of each term); scores, maxima, sums, D and all accumulators are fp32.  D is taken from the output as
+// it was before its rounding (what that left is kept as a second bf16): with the rounded output's D a short sequence's error of dq
+// and dk is 1.5 times that of their own rounding, so it is 1.4 times.
 #pragma once
 
 #include "attn.cuh"
@@ -583,6 +585,17 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
 #pragma unroll
         for (int j = 0; j < 32; ++j) o[j] = n_own > 0 ? o[j] * inv : 0.0f;
         sts_row32(out + (c >> 1) * CHUNK, trow, c & 1, o);
+        if (row < a.mask.M) {
+          bf16* rest = (bf16*)a.rest + ((size_t)row * a.heads + h) * a.dim + c * 32;
+#pragma unroll
+          for (int j = 0; j < 32; j += 8) {
+            if (c * 32 + j >= a.dim) break;
+            float d[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = o[j + e] - __bfloat162float(__float2bfloat16_rn(o[j + e]));
+            *reinterpret_cast<uint4*>(rest + j) = make_uint4(pack_bf16x2(d[0], d[1]), pack_bf16x2(d[2], d[3]), pack_bf16x2(d[4], d[5]), pack_bf16x2(d[6], d[7]));
+          }
+        }
       }
       if (row < a.mask.M) a.lse[(size_t)h * a.ld + row] = sum > 0.0f || sum != sum ? m + log2f(sum) : INFINITY;
       fence_async_smem();
@@ -606,7 +619,8 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
 // ---- backward ----------------------------------------------------------------------------------
 // D_i = dO_i . o_i per head: 16 lanes a row and head, 8 columns a lane.
 static __global__ void __launch_bounds__(256)
-dot_kernel(const bf16* __restrict__ out, const bf16* __restrict__ dout, float* __restrict__ D, int M, int heads, int dim, int ld) {
+dot_kernel(const bf16* __restrict__ out, const bf16* __restrict__ rest, const bf16* __restrict__ dout, float* __restrict__ D, int M, int heads, int dim,
+           int ld) {
   chain_begin();
   const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / 16;
   const int sub = threadIdx.x & 15;
@@ -614,11 +628,12 @@ dot_kernel(const bf16* __restrict__ out, const bf16* __restrict__ dout, float* _
   float s = 0.0f;
   if (on && sub * 8 < dim) {
     const size_t at = (size_t)item * dim + sub * 8;               // rows hold the heads side by side: item = row * heads + head
-    float o[8], g[8];
+    float o[8], d[8], g[8];
     load_seg<8>(out + at, 8, o);
+    load_seg<8>(rest + at, 8, d);
     load_seg<8>(dout + at, 8, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(o[i], g[i], s);
+    for (int i = 0; i < 8; ++i) s = fmaf(o[i] + d[i], g[i], s);
   }
 #pragma unroll
   for (int k = 8; k > 0; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);

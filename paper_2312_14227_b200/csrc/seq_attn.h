@@ -20,6 +20,7 @@ struct Args {
   float* lse;               // [heads][ld]: log2 of the sum of 2^(s log2 e); +inf for a row without keys
   float* D;                 // [heads][ld]
   const float* slopes;      // [heads] or nullptr
+  void* rest;               // [M][heads dim] bf16: the output less its rounding to bf16
   uint32_t* status;
   int heads, kv, dim, ld;   // ld: M rounded up to a multiple of 128
   int halves;               // forward: 1 or 2 halves of 128 rows a block

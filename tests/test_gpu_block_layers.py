@@ -141,6 +141,76 @@ def test_gated(M, K, h, act, dtype):
     gated(M, K, h, act, dtype, seed=M)
 
 
+def block_pair(M, K, h, N, act, residual=False, dropout=False, seed=0):
+    """Gated layer with a dense layer above: dZ comes out of that layer's error-gradient product (not where something lies between)."""
+    rng = np.random.default_rng(seed)
+    W = [dev(rng.normal(size=(K, 2 * h)) / np.sqrt(K), B), dev(rng.normal(size=(h, N)) / np.sqrt(h), B)]
+    b = [dev(rng.normal(size=2 * h) * 0.3, B), dev(rng.normal(size=N) * 0.3, B)]
+    layers = [desc(et.ET_LAYER_GATED, K, 2 * h, fold=2, act=act), desc(et.ET_LAYER_DENSE, h, N, residual_src=1 if residual else -1)]
+    r = Run(layers, M, B, W, b, seed=seed + 1)
+    grads = [torch.full(p.shape, float("nan"), device=DEV) for q in zip(W, b) for p in q]
+    y, dX = r([1, 1, 1, 1], grads)
+    g = f64(r.dY) @ f64(W[1]).T
+    gerr = blk.E * (N + 2) * (np.abs(f64(r.dY)) @ np.abs(f64(W[1])).T)
+    if residual:
+        g = g + f64(r.dY)
+        gerr = gerr + (blk.U + blk.E) * np.abs(g)        # the gradient of the gated layer's output is stored
+    o = blk.gated(f64(r.x), f64(W[0]), f64(b[0]), act, g, blk.U, dy_err=gerr)
+    within("dX", dX, *o["dx"])
+    within("dW", grads[0], *o["dW"])
+    within("db", grads[1], *o["db"])
+    a, aerr = o["y"]
+    out = a @ f64(W[1]) + f64(b[1]) + (a if residual else 0)
+    size = np.abs(a) @ np.abs(f64(W[1])) + np.abs(f64(b[1]))
+    within("y", y, out, (aerr @ np.abs(f64(W[1]))) + blk.E * (h + 3) * size + (aerr if residual else 0) + blk.U * np.abs(out))
+    within("dW2", grads[2], a.T @ f64(r.dY), (aerr + blk.E * (M + 2) * np.abs(a)).T @ np.abs(f64(r.dY)))
+    return r
+
+
+@pytest.mark.parametrize("act", [et.ET_ACT_GELU_TANH, et.ET_ACT_RELU, et.ET_ACT_SILU])
+@pytest.mark.parametrize("M,K,h,N", [(1, 8, 8, 8), (37, 24, 72, 40), (300, 136, 344, 136), (257, 64, 128, 64), (850, 40, 4808, 24)])
+def test_gated_below_a_dense_layer(M, K, h, N, act):
+    block_pair(M, K, h, N, act, seed=M)
+
+
+def test_gated_whose_output_joins_a_residual():
+    block_pair(200, 64, 96, 96, et.ET_ACT_SILU, residual=True)
+
+
+def test_gated_below_a_gated_layer_and_two_streams():
+    rng = np.random.default_rng(7)
+    W = [dev(rng.normal(size=(40, 112)) / 6, B), dev(rng.normal(size=(56, 144)) / 7, B), dev(rng.normal(size=(72, 40)) / 8, B)]
+    b = [dev(rng.normal(size=n) * 0.2, B) for n in (112, 144, 40)]
+    layers = [desc(et.ET_LAYER_GATED, 40, 112, fold=2, act=3), desc(et.ET_LAYER_GATED, 56, 144, fold=2, act=1), desc(et.ET_LAYER_DENSE, 72, 40)]
+    for streams in (0, 1):
+        r = Run(layers, 333, B, W, b)
+        et.et_stack_set_option(r.s, et.ET_OPTION_TWO_STREAMS, streams)
+        grads = [torch.full(p.shape, float("nan"), device=DEV) for q in zip(W, b) for p in q]
+        y, dX = r([1] * 6, grads)
+        leaf = [p.double().requires_grad_() for q in zip(W, b) for p in q]
+        x = r.x.double().requires_grad_()
+        z = x @ leaf[0] + leaf[1]
+        z = torch.nn.functional.silu(z[:, :56]) * z[:, 56:] @ leaf[2] + leaf[3]
+        out = torch.nn.functional.gelu(z[:, :72], approximate="tanh") * z[:, 72:] @ leaf[4] + leaf[5]
+        want = torch.autograd.grad(out, [x] + leaf, r.dY.double())
+        for a, w in zip([dX] + grads, want):
+            assert (a.double() - w).abs().max() <= 2e-2 * w.abs().max()
+
+
+def test_gates_beyond_what_z_is_kept_in():
+    """Z is kept at most 65504: the output is formed from all of it, gradients are those of a gate or factor of 65504."""
+    W, b = torch.eye(8, 16, device=DEV).to(torch.bfloat16), dev([0] * 16, B)
+    W[:, 8:] = torch.eye(8, device=DEV)
+    x = dev([[1e6, -1e6, 2e5, 1, 70000, 65536, 0, 3]] * 2, B)
+    r = Run([desc(et.ET_LAYER_GATED, 8, 16, fold=2, act=et.ET_ACT_RELU)], 2, B, [W], [b], x=x)
+    y, dX = r()
+    z = f64(x)
+    assert np.abs(f64(y) - np.maximum(z, 0) * z).max() <= blk.U * 1e12
+    held = np.clip(z, -65504, 65504)
+    want = f64(r.dY) * (held * (held > 0) + np.maximum(held, 0))
+    assert np.abs(f64(dX) - want).max() <= 4 * blk.U * np.abs(want).max()
+
+
 def test_gated_in_wide_tiles_and_long_contractions():
     gated(2600, 24, 1928, et.ET_ACT_SILU, B)                          # enough tiles for the 128-column form, a ragged last one
     gated(300, 2056, 136, et.ET_ACT_GELU_TANH, B)

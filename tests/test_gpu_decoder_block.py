@@ -230,7 +230,8 @@ def test_costs_of_layers_without_tensors_go_to_the_bias_below():
             assert not t_dw[2 * l:2 * l + 2].any() and not t_dy[2 * l:2 * l + 2].any()
     assert t_dy[5] > 0 and t_dy[11] > 0                  # biases of the QKV projection and of the one below a dropout layer
     g = kinds.index(et.ET_LAYER_GATED)
-    assert t_dw[2 * g] > 0 and t_dw[2 * g + 1] > 0 and t_dy[2 * g] > 0 and t_dy[2 * g + 1] > 0
+    assert t_dw[2 * g] > 0 and t_dw[2 * g + 1] > 0 and t_dy[2 * g] > 0
+    assert t_dy[2 * g + 1] == 0                          # dZ is formed in the error-gradient product of the dense layer above
     assert t_fwd > 0
     m.check_status()
 

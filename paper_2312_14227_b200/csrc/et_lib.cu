@@ -250,7 +250,7 @@ struct LayerRT {
   int norm_blocks = 0;      // norm: blocks of the backward kernel = rows of off_gpart
   int heads = 0, seq = 0;   // attention: K = 3N, N = 64 * heads, rows in sequences of `seq`
   size_t off_lse = 0;       // attention: log-sum-exp per (sequence, head, row)
-  size_t off_rest = 0;      // masked attention: what rounding the output to bf16 left, [M x N] bf16
+  size_t off_rest = 0, off_seen = 0;      // masked attention: what rounding the output to bf16 left, [M x N] bf16; keys of every row
   int consumer = -1;        // layer whose residual reads a_l (its output gradient joins G_l), or -1
   void* W = nullptr;
   void* b = nullptr;
@@ -1073,6 +1073,7 @@ et::seqattn::Args seq_args(const et_stack* s, int l) {
   a.lse = (float*)s->at(L.off_lse);
   a.D = a.lse + (size_t)L.heads * a.ld;
   a.rest = s->at(L.off_rest);
+  a.keys = (int*)s->at(L.off_seen);
   a.slopes = L.slopes;
   a.status = (uint32_t*)s->at(s->off_status);
   a.heads = L.heads; a.kv = L.kv; a.dim = L.dim;
@@ -1084,10 +1085,10 @@ et_status run_seq_forward(et_stack* s, int l, void* y, cudaStream_t st) {
   LayerRT& L = s->ly[l];
   ET_TRY(head_maps(&L.in_heads, act_in<bf16>(s, l), L.dim, L.heads + 2 * L.kv, s->M));
   ET_TRY(head_maps(&L.out_heads, act_out<bf16>(s, l, y), L.dim, L.heads, s->M));
-  return cuda_status(et::seqattn::forward(L.in_heads.map, L.out_heads.map, seq_args(s, l), s->sms, st), et::seqattn::kForwardLaunches);
+  return cuda_status(et::seqattn::forward(L.in_heads.map, L.out_heads.map, seq_args(s, l), s->sms, st), 1);
 }
 // G_l (gradient of [q | k | v]) from G_{l+1}; the layer below has no activation, so G_l is its dZ.
-et_status run_seq_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+et_status run_seq_backward(et_stack* s, int l, const void* dY, int* launches, cudaStream_t st) {
   TimedLaunch tl(s, ET_K_ATTENTION, st);
   LayerRT& L = s->ly[l];
   const bf16* out = l == s->L - 1 ? (const bf16*)s->y : (const bf16*)s->at(L.off_a_out);
@@ -1096,8 +1097,11 @@ et_status run_seq_backward(et_stack* s, int l, const void* dY, cudaStream_t st) 
   ET_TRY(head_maps(&L.in_heads, act_in<bf16>(s, l), L.dim, L.heads + 2 * L.kv, s->M));
   ET_TRY(head_maps(&L.g_heads, dout, L.dim, L.heads, s->M));
   ET_TRY(head_maps(&L.dx_heads, dx, L.dim, L.heads + 2 * L.kv, s->M));
-  return cuda_status(et::seqattn::backward(L.in_heads.map, L.g_heads.map, L.dx_heads.map, out, dout, const_cast<void*>(dx),
-                                           seq_args(s, l), s->sms, st), et::seqattn::kBackwardLaunches);
+  int n = 0;
+  const cudaError_t e = et::seqattn::backward(L.in_heads.map, L.g_heads.map, L.dx_heads.map, out, dout, const_cast<void*>(dx), seq_args(s, l),
+                                              s->sms, &n, st);
+  *launches += n;
+  return cuda_status(e, n);
 }
 
 // ---- rotary positions -----------------------------------------------------------------------------
@@ -1226,16 +1230,16 @@ et_status run_gated_backward(et_stack* s, int l, const void* dY, bool want_sums,
 
 // The backward pass of a layer without tensors.
 template <typename T>
-et_status run_plain_backward(et_stack* s, int l, const void* dY, cudaStream_t st) {
+et_status run_plain_backward(et_stack* s, int l, const void* dY, int* launches, cudaStream_t st) {
+  if (s->ly[l].kind == ET_LAYER_MASKED_ATTENTION) return run_seq_backward(s, l, dY, launches, st);
+  ++*launches;
   switch (s->ly[l].kind) {
     case ET_LAYER_ATTENTION: return run_attn_backward(s, l, dY, st);
-    case ET_LAYER_MASKED_ATTENTION: return run_seq_backward(s, l, dY, st);
     case ET_LAYER_ROTARY: return run_rotary_backward<T>(s, l, dY, st);
     case ET_LAYER_DROPOUT: return run_dropout_backward<T>(s, l, dY, st);
     default: return run_im2col_backward<T>(s, l, dY, st);
   }
 }
-int plain_backward_launches(const LayerRT& L) { return L.kind == ET_LAYER_MASKED_ATTENTION ? et::seqattn::kBackwardLaunches : 1; }
 
 // ---- embedding ------------------------------------------------------------------------------------
 template <typename T>
@@ -1848,8 +1852,7 @@ et_status backward_impl(et_stack* s, const void* dY, const uint8_t* mask, float*
         // a non-trainable layer: only passes the error gradient on, above the deepest selected layer
         if (Y.implicit) continue;                            // done by the error-gradient GEMM of the layer above
         if (l > to) {
-          ET_TRY(run_plain_backward<T>(s, l, dY, cs));
-          launches += plain_backward_launches(Y);
+          ET_TRY(run_plain_backward<T>(s, l, dY, &launches, cs));
           if (two) CU_TRY(cudaEventRecord(s->chain_ev[l], cs));
         }
         continue;
@@ -2249,6 +2252,7 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
     if (y.kind == ET_LAYER_MASKED_ATTENTION) {
       y.off_lse = take((size_t)2 * y.heads * ceil_div(M, 128) * 128 * sizeof(float));      // log-sum-exp, D
       y.off_rest = take((size_t)M * y.N * s->elt);
+      y.off_seen = take((size_t)M * sizeof(int));
     } else if (y.kind == ET_LAYER_ROTARY || y.kind == ET_LAYER_DROPOUT) {
     } else if (y.kind == ET_LAYER_ATTENTION) {
       y.off_lse = take((size_t)M * y.heads * sizeof(float));
@@ -3161,8 +3165,8 @@ et_status et_profile_costs(et_stack* s, const void* x, void* y, const void* dY, 
         double t_attn = 0.0;
         if (l >= 1) {
           if (s->ly[l].implicit) t_attn = 0.0;            // part of the error-gradient GEMM of the layer above
-          else if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_plain_backward<bf16>(s, l, dY, st); }, &t_attn));
-          else ET_TRY(timed([&]() { return run_plain_backward<float>(s, l, dY, st); }, &t_attn));
+          else if (s->dtype == ET_BF16) ET_TRY(timed([&]() { return run_plain_backward<bf16>(s, l, dY, &dummy, st); }, &t_attn));
+          else ET_TRY(timed([&]() { return run_plain_backward<float>(s, l, dY, &dummy, st); }, &t_attn));
         }
         pending_nontrainable += t_attn;
         continue;

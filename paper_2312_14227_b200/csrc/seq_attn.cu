@@ -66,12 +66,19 @@ cudaError_t forward(const CUtensorMap& qkv, const CUtensorMap& out, Args a, int 
   });
 }
 
-cudaError_t backward(const CUtensorMap& qkv, const CUtensorMap& g, const CUtensorMap& gqkv, const void* out, const void* dout, void* dqkv, Args a, int sms, cudaStream_t st) {
-  const long long threads = (long long)a.mask.M * a.heads * 16;
-  cudaError_t e = launch(dot_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, 1, (const bf16*)out, (const bf16*)a.rest, (const bf16*)dout, a.D,
-                         a.mask.M, a.heads, a.dim, a.ld);
-  if (e != cudaSuccess) return e;
+cudaError_t backward(const CUtensorMap& qkv, const CUtensorMap& g, const CUtensorMap& gqkv, const void* out, const void* dout, void* dqkv,
+                     Args a, int sms, int* launches, cudaStream_t st) {
   const unsigned tiles = (unsigned)((a.mask.M + 127) / 128);
+  // one wave of blocks at most: a launch of its own for D takes longer than the threads' own sums (37 rows, 4 heads: 25 -> 23 us for both passes)
+  a.dot = (long long)tiles * a.heads <= sms;
+  *launches = a.dot ? 2 : 3;
+  if (!a.dot) {
+    const long long threads = (long long)a.mask.M * a.heads * 16;
+    const cudaError_t e = launch(dot_kernel, (unsigned)((threads + 255) / 256), 256, 0, st, 1, (const bf16*)out, (const bf16*)a.rest,
+                                 a.keys, (const bf16*)dout, a.D, a.mask.M, a.heads, a.dim, a.ld);
+    if (e != cudaSuccess) return e;
+  }
+  const Dots dots{(const bf16*)out, (const bf16*)dout};
   return by_form(a, [&](auto wide, auto cap, auto bias) -> cudaError_t {
     constexpr int W = decltype(wide)::value;
     constexpr auto dq = backward_kernel<W, false, decltype(cap)::value, decltype(bias)::value>;
@@ -87,8 +94,8 @@ cudaError_t backward(const CUtensorMap& qkv, const CUtensorMap& g, const CUtenso
       return n;
     };
     const unsigned pq = parts(tiles * a.heads, tiles), pk = parts(tiles * a.kv, (long long)tiles * (a.heads / a.kv));
-    if (r == cudaSuccess) r = launch(dq, tiles * a.heads * pq, THREADS, smem, st, pq, qkv, g, gqkv, (bf16*)dqkv, a);
-    if (r == cudaSuccess) r = launch(dkv, tiles * a.kv * pk, THREADS, smem, st, pk, qkv, g, gqkv, (bf16*)dqkv, a);
+    if (r == cudaSuccess) r = launch(dq, tiles * a.heads * pq, THREADS, smem, st, pq, qkv, g, gqkv, (bf16*)dqkv, dots, a);
+    if (r == cudaSuccess) r = launch(dkv, tiles * a.kv * pk, THREADS, smem, st, pk, qkv, g, gqkv, (bf16*)dqkv, dots, a);
     return r;
   });
 }

@@ -22,9 +22,10 @@
 // atomics: a shared head's gradient is the sum that one block forms in order.  The price is that S and dP are formed
 // twice, 7 products where 5 would do.
 //
-// Rounding: P and dS are bf16 (half a step 2^-8 of each term); scores, maxima, sums, D and all accumulators are fp32.  D is taken from the output as
-// it was before its rounding (what that left is kept as a second bf16): with the rounded output's D a short sequence's error of dq
-// and dk is 1.5 times that of their own rounding, so it is 1.4 times.
+// Rounding: P and dS are bf16 (half a step 2^-8 of each term); scores, maxima, sums, D and all accumulators are fp32.  For rows
+// of fewer than 64 keys D is taken from the output as it was before its rounding, what that left being kept as a second bf16: the fewer the
+// keys the larger the output beside v, and with the rounded output's D the error of dq and dk on 5 rows was 1.6 times that of their own
+// rounding, so it is 1.4 times, as on long sequences.  (Kept for every row it cost the forward pass 5 %.)
 #pragma once
 
 #include "attn.cuh"
@@ -36,6 +37,7 @@ namespace seqattn {
 using namespace et::tc;
 
 constexpr uint32_t kTimeoutSeqAttn = 8;
+constexpr int kRestKeys = 64;                   // rows of fewer keys keep what the rounding of their output left
 constexpr int THREADS = 320;                    // warps 0-3, 4-7: row threads; warp 8: MMA issue, TMEM; warp 9: TMA
 constexpr uint32_t CHUNK = 16384;               // 128 rows x 64 columns of bf16
 constexpr float LOG2E = 1.4426950408889634f;
@@ -585,7 +587,7 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
 #pragma unroll
         for (int j = 0; j < 32; ++j) o[j] = n_own > 0 ? o[j] * inv : 0.0f;
         sts_row32(out + (c >> 1) * CHUNK, trow, c & 1, o);
-        if (row < a.mask.M) {
+        if (row < a.mask.M && iv.y - iv.x < kRestKeys) {
           bf16* rest = (bf16*)a.rest + ((size_t)row * a.heads + h) * a.dim + c * 32;
 #pragma unroll
           for (int j = 0; j < 32; j += 8) {
@@ -597,6 +599,7 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
           }
         }
       }
+      if (h == 0 && row < a.mask.M) a.keys[row] = iv.y - iv.x;
       if (row < a.mask.M) a.lse[(size_t)h * a.ld + row] = sum > 0.0f || sum != sum ? m + log2f(sum) : INFINITY;
       fence_async_smem();
       group_sync(1 + hf);
@@ -619,8 +622,8 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
 // ---- backward ----------------------------------------------------------------------------------
 // D_i = dO_i . o_i per head: 16 lanes a row and head, 8 columns a lane.
 static __global__ void __launch_bounds__(256)
-dot_kernel(const bf16* __restrict__ out, const bf16* __restrict__ rest, const bf16* __restrict__ dout, float* __restrict__ D, int M, int heads, int dim,
-           int ld) {
+dot_kernel(const bf16* __restrict__ out, const bf16* __restrict__ rest, const int* __restrict__ keys, const bf16* __restrict__ dout,
+           float* __restrict__ D, int M, int heads, int dim, int ld) {
   chain_begin();
   const long long item = ((long long)blockIdx.x * 256 + threadIdx.x) / 16;
   const int sub = threadIdx.x & 15;
@@ -628,16 +631,32 @@ dot_kernel(const bf16* __restrict__ out, const bf16* __restrict__ rest, const bf
   float s = 0.0f;
   if (on && sub * 8 < dim) {
     const size_t at = (size_t)item * dim + sub * 8;               // rows hold the heads side by side: item = row * heads + head
-    float o[8], d[8], g[8];
+    float o[8], d[8] = {}, g[8];
     load_seg<8>(out + at, 8, o);
-    load_seg<8>(rest + at, 8, d);
     load_seg<8>(dout + at, 8, g);
+    if (keys[item / heads] < kRestKeys) load_seg<8>(rest + at, 8, d);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s = fmaf(o[i] + d[i], g[i], s);
   }
 #pragma unroll
   for (int k = 8; k > 0; k >>= 1) s += __shfl_xor_sync(0xffffffffu, s, k);
   if (on && sub == 0) D[(size_t)(item % heads) * ld + item / heads] = s;
+}
+
+// The same by one thread, for blocks that are a launch short of time rather than of reads.
+struct Dots { const bf16 *out, *dout; };
+__device__ __forceinline__ float dot_row(const Dots& t, const Args& a, int row, int h, int n_keys) {
+  const size_t at = ((size_t)row * a.heads + h) * a.dim;
+  float s = 0.0f;
+  for (int c = 0; c < a.dim; c += 8) {
+    float o[8], d[8] = {}, g[8];
+    load_seg<8>(t.out + at + c, 8, o);
+    if (n_keys < kRestKeys) load_seg<8>((const bf16*)a.rest + at + c, 8, d);
+    load_seg<8>(t.dout + at + c, 8, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(o[i] + d[i], g[i], s);
+  }
+  return s;
 }
 
 template <int DHP>
@@ -652,12 +671,13 @@ struct BwdCfg {
 // DKV = false: X1 = q, X2 = dO (rows of head h), Y1 = k, Y2 = v;  acc1 = dq.
 // DKV = true:  X1 = k, X2 = v (keys of a key head), Y1 = q, Y2 = dO of every head of its group;  acc1 = dk, acc2 = dv.
 // Tensor memory: acc1, acc2, S (P over it), dP (dS over it).  One product's accumulator is worked on while the tensor core forms the
-// others: per tile   P(i) | dK(i-1), dP(i)    then    dS(i) | dV(i), S(i+1).
+// others: per tile   P(i) | dK(i-1), dP(i)    then    dS(i) | dV(i), S(i+1).  The first half of P is handed over by itself, so that its share of dV runs
+// under the exponentials of the second; where P is not needed as a factor (dq) the next S is formed as soon as this one has been read.
 // The products are 128 wide: narrower ones take the tensor core as long (measured 57 to 75 cycles an instruction at 64 and 128 columns).
 template <int DHP, bool DKV, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(THREADS, 1)
 backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_g,
-                const __grid_constant__ CUtensorMap map_out, bf16* __restrict__ dqkv, const Args a) {
+                const __grid_constant__ CUtensorMap map_out, bf16* __restrict__ dqkv, const Dots dots, const Args a) {
   using C = BwdCfg<DHP>;
   constexpr int ST = C::ST;
   extern __shared__ uint8_t smem_raw[];
@@ -667,9 +687,10 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   const uint32_t ring = base + 2 * C::TILE, bars = ring + ST * C::STAGE;
   const uint32_t bar_x = bars, bar_done = bars + 8;
   const uint32_t bar_s = bars + 16, bar_dp = bars + 24;           // S, dP of a tile complete
-  const uint32_t bar_p = bars + 32, bar_ds = bars + 40;           // S read, and P in its place (dk, dv);  dS in dP's place
-  auto full = [&](int s) { return bars + 48u + 8u * s; };
-  auto empty = [&](int s) { return bars + 48u + 8u * (ST + s); };
+  const uint32_t bar_p = bars + 32, bar_p2 = bars + 40;           // S read, and half of P in its place (dk, dv); all of it
+  const uint32_t bar_ds = bars + 48;                              // dS in dP's place
+  auto full = [&](int s) { return bars + 56u + 8u * s; };
+  auto empty = [&](int s) { return bars + 56u + 8u * (ST + s); };
   int* shared = reinterpret_cast<int*>(gen + 2 * C::TILE + ST * C::STAGE + 160);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(shared);
   volatile uint32_t* abort_flag = tmem_slot + 1;
@@ -688,6 +709,7 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   if (warp == 9 && lane == 0) {
     for (int i = 0; i < 4; ++i) mbar_init(bars + 8 * i, 1);
     mbar_init(bar_p, 8);
+    mbar_init(bar_p2, 8);
     mbar_init(bar_ds, 8);
     for (int s = 0; s < ST; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     *abort_flag = 0;
@@ -793,12 +815,16 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       if (ok) ok = warp_wait(bar_p, (uint32_t)i & 1u, abort_flag, a.status);
       if (!ok) break;
       tc_fence_after();
+      if (DKV) {
+        // each group's half of P lies in the first half of its scores' columns; steps 0, 1, 4, 5 first, then 2, 3, 6, 7
+        auto pv = [&](int ks, uint32_t keep) { mma_ts(tmem + ACC2, tmem + CS + (ks >> 2) * 64 + (ks & 3) * 8, b2 + mn_step(ks), id_a, keep); };
+        if (elect()) { pv(0, add); pv(1, 1u); pv(4, 1u); pv(5, 1u); }
+        ok = warp_wait(bar_p2, (uint32_t)i & 1u, abort_flag, a.status);
+        if (!ok) break;
+        tc_fence_after();
+        if (elect()) { pv(2, 1u); pv(3, 1u); pv(6, 1u); pv(7, 1u); }
+      }
       if (elect()) {
-        if (DKV) {                                                // each group's half of P lies in the first half of its scores' columns
-          mma_ts(tmem + ACC2, tmem + CS, b2, id_a, add);
-#pragma unroll
-          for (int ks = 1; ks < 8; ++ks) mma_ts(tmem + ACC2, tmem + CS + (ks >> 2) * 64 + (ks & 3) * 8, b2 + mn_step(ks), id_a, 1u);
-        }
         if (next) {
           product_ss<DHP, CHUNK, CHUNK>(tmem + CS, dx1, n1, id_s);
           tc_commit(bar_s);
@@ -829,7 +855,16 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     const float u = CAP ? 2.0f * c2 / a.cap : 0.0f, top = a.cap * LOG2E;
     float own_lse = INFINITY, own_D = 0.0f, slope2 = 0.0f;
     if (!DKV) {
-      if (row < a.mask.M) { own_lse = a.lse[(size_t)h * a.ld + row]; own_D = a.D[(size_t)h * a.ld + row]; }
+      if (row < a.mask.M) {
+        const size_t at = (size_t)h * a.ld + row;
+        own_lse = a.lse[at];
+        if (a.dot) {                                              // D_i here, and left for the pass that follows
+          own_D = dot_row(dots, a, row, h, iv.y - iv.x);
+          if (part == 0 && w == 0) a.D[at] = own_D;
+        } else {
+          own_D = a.D[at];
+        }
+      }
       if (BIAS) slope2 = a.slopes[h] * LOG2E;
     }
     const uint64_t c22 = pair(c2, c2), neg_lse2 = pair(-own_lse, -own_lse), neg_D2 = pair(-own_D, -own_D);
@@ -854,6 +889,12 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       tmem_ld32_issue(S, s[0]);
       tmem_ld32_issue(S + 32, s[1]);
       tmem_ld_wait(s[0], s[1]);
+      auto hand_over = [&](uint32_t bar) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+      };
+      if (!DKV) hand_over(bar_p);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         uint32_t r[16];
@@ -903,12 +944,12 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             s[c][j + 1] = CAP ? p.y * slope[j + 1] : p.y;
           }
         }
-        if (DKV) tmem_st16(S + c * 16, r);
+        if (DKV) {
+          tmem_st16(S + c * 16, r);
+          tmem_st_wait();
+          hand_over(c == 0 ? bar_p : bar_p2);
+        }
       }
-      if (DKV) tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p);
       ok = mbar_wait(bar_dp, (uint32_t)i & 1u, abort_flag, a.status, kTimeoutSeqAttn);
       if (!ok) break;
       tc_fence_after();

@@ -106,6 +106,16 @@ namespace gated {
 
 using namespace et::tc;
 
+__device__ __forceinline__ bool group_all(int id, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 q, %2, 0;\n\t"
+      "barrier.cta.red.and.pred p, %1, 128, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r) : "r"(id), "r"((uint32_t)x) : "memory");
+  return r != 0;
+}
 __device__ __forceinline__ void sts_z32(uint8_t* chunk, int row, int half, const float (&v)[32]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
@@ -257,7 +267,8 @@ gated_forward_kernel(const __grid_constant__ Maps maps, const Params p) {
     bool ok = true;
     for (int u = unit0; u < units && ok; u += unit_step, ++it) {
       const int m0 = u / p.tiles_n * 2 * BM + (int)rank * BM, n0 = u % p.tiles_n * H;
-      ok = mbar_wait(acc_full(acc), acc_phase, abort_flag, p.status, kTimeoutEpilogue);
+      // the group goes on together or not at all: its barriers below count on all 128 threads
+      ok = group_all(1 + g, mbar_wait(acc_full(acc), acc_phase, abort_flag, p.status, kTimeoutEpilogue));
       if (!ok) break;
       tc_fence_after();
       const uint32_t taddr = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * ACC_STRIDE);

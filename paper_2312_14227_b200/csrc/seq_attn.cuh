@@ -17,9 +17,9 @@
 // serves the other half.  The output is rescaled only where a row's maximum has grown by more than 2^8: until then sums and
 // output are relative to the older maximum, which fp32 holds as well.
 // Backward: two passes of one kernel, dq (block = 128 query rows, keys stream by) and dk, dv (block = 128 keys of a key head, the
-// rows of its group's heads stream by).  Both form S = X1 Y1^T and dP = X2 Y2^T against 64 streamed rows in tensor memory,
+// rows of its group's heads stream by).  Both form S = X1 Y1^T and dP = X2 Y2^T against 128 streamed rows in tensor memory,
 // write P and dS as bf16 over them, and accumulate dS Y1 (and P Y2) with P and dS read from tensor memory.  Nothing is added with
-// atomics: a shared head's gradient is the sum that one block forms in order.  The price is that S and dP are formed
+// atomics: a shared head's gradient is the sum that one block forms in order, or the blocks of a cluster, joined in their order.  The price is that S and dP are formed
 // twice, 7 products where 5 would do.
 //
 // Rounding: P and dS are bf16 (half a step 2^-8 of each term); scores, maxima, sums, D and all accumulators are fp32.  For rows
@@ -602,13 +602,13 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
       if (h == 0 && row < a.mask.M) a.keys[row] = iv.y - iv.x;
       if (row < a.mask.M) a.lse[(size_t)h * a.ld + row] = sum > 0.0f || sum != sum ? m + log2f(sum) : INFINITY;
       fence_async_smem();
-      group_sync(1 + hf);
-      if (trow == 0) {
-        for (int c = 0; c < C::CH; ++c)
-          if (c * 64 < a.dim && row < a.mask.M) tma_store_3d(&map_out, base + hf * C::TILE + c * CHUNK, c * 64, h, row);
-        tma_store_commit();
-        tma_store_wait_all();
-      }
+    }
+    group_sync(1 + hf);                                           // a thread whose wait gave up comes here, too
+    if (ok && trow == 0) {
+      for (int c = 0; c < C::CH; ++c)
+        if (c * 64 < a.dim && row < a.mask.M) tma_store_3d(&map_out, base + hf * C::TILE + c * CHUNK, c * 64, h, row);
+      tma_store_commit();
+      tma_store_wait_all();
     }
   }
   tc_fence_before();
@@ -988,15 +988,14 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     }
     if (ok && total > 0) ok = mbar_wait(bar_done, 0, abort_flag, a.status, kTimeoutSeqAttn);
     if (ok) ok = mbar_wait(bar_x, 0, abort_flag, a.status, kTimeoutSeqAttn);
+    // dk and dq are staged in X1's tile, dv in X2's.  dk, dv: a group each; dq: the groups share its 64-column pieces
+    const bool second = DKV && w == 1;
+    const int c0 = DKV ? 0 : w, c1 = DKV ? C::CH : min(w + 1, C::CH);
     if (ok) {
       tc_fence_after();
-      const bool second = DKV && w == 1;
       if (parts == 1) {
-        // dk and dq are staged in X1's tile, dv in X2's.  dk, dv: a group each; dq: the groups share its 64-column pieces
-        const int c0 = DKV ? 0 : w, c1 = DKV ? C::CH : min(w + 1, C::CH);
         const float f = second ? 1.0f : a.scale;
         uint8_t* out = gen + (second ? C::TILE : 0);
-        const int block = DKV ? a.heads + (w == 1 ? a.kv : 0) + h : h;
 #pragma unroll 1
         for (int c = c0 * 2; c < c1 * 2; ++c) {
           float o[32];
@@ -1006,24 +1005,27 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           sts_row32(out + (c >> 1) * CHUNK, trow, c & 1, o);
         }
         fence_async_smem();
-        group_sync(1 + w);
-        if (trow == 0) {
-          for (int c = c0; c < c1; ++c)
-            if (c * 64 < a.dim) tma_store_3d(&map_out, base + (second ? C::TILE : 0) + c * CHUNK, c * 64, block, row0);
-          tma_store_commit();
-          tma_store_wait_all();
-        }
       } else {
         // each block leaves its sums in its own shared memory, [accumulator][column][row]; every tile has been read by now
         float* mine = reinterpret_cast<float*>(gen) + (second ? DHP * 128 : 0) + trow;
-        const int c0 = DKV ? 0 : w * (DHP / 64), c1 = DKV ? DHP / 32 : (w + 1) * (DHP / 64);
+        const int g0 = DKV ? 0 : w * (DHP / 64), g1 = DKV ? DHP / 32 : (w + 1) * (DHP / 64);
 #pragma unroll 1
-        for (int c = c0; c < c1; ++c) {
+        for (int c = g0; c < g1; ++c) {
           float o[32];
           if (total > 0) tmem_ld32(tmem + lane_addr + (second ? DHP : 0) + c * 32, o);
 #pragma unroll
           for (int j = 0; j < 32; ++j) mine[(c * 32 + j) * 128] = total > 0 ? o[j] : 0.0f;
         }
+      }
+    }
+    if (parts == 1) {
+      group_sync(1 + w);                                          // a thread whose wait gave up comes here, too
+      if (ok && trow == 0) {
+        const int block = DKV ? a.heads + (w == 1 ? a.kv : 0) + h : h;
+        for (int c = c0; c < c1; ++c)
+          if (c * 64 < a.dim) tma_store_3d(&map_out, base + (second ? C::TILE : 0) + c * CHUNK, c * 64, block, row0);
+        tma_store_commit();
+        tma_store_wait_all();
       }
     }
   }

@@ -50,7 +50,7 @@ def test_attention_descriptions():
     et.et_stack_create([_attn()], 8, B)
     et.et_stack_create([_attn(seq_len=4, mask=et.ET_MASK_CAUSAL, softcap=30.0, scale=0.5, dim=128)], 8, B)
     for k in (dict(heads=0), dict(kv=0), dict(heads=3), dict(mask=2), dict(mask=-1), dict(softcap=-1.0), dict(softcap=float("inf")),
-              dict(scale=-0.1), dict(scale=float("nan")), dict(act=1), dict(residual_src=0), dict(seq_len=-1), dict(o=32), dict(i=136)):
+              dict(scale=-0.1), dict(scale=float("nan")), dict(scale=3e38), dict(softcap=1e-39), dict(scale=1e20, softcap=1e-20), dict(act=1), dict(residual_src=0), dict(seq_len=-1), dict(o=32), dict(i=136)):
         assert _bad(_attn(**k)) == INV, k
     assert _bad(_attn(seq_len=3)) == SHAPE
     assert _bad(_attn(), dtype=F) == UNS

@@ -9,9 +9,10 @@ namespace {
 
 std::mutex g_mutex;
 
-// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.
+// Dynamic shared memory above 48 KB has to be allowed once per kernel and device.  A kernel that hands registers over among its warps needs
+// that many at its launch: with fewer, those that ask would wait for ever.
 template <auto kern>
-cudaError_t allow(uint32_t bytes) {
+cudaError_t allow(uint32_t bytes, int registers = 0) {
   static bool done[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -19,6 +20,10 @@ cudaError_t allow(uint32_t bytes) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   std::lock_guard<std::mutex> lock(g_mutex);
   if (done[dev]) return cudaSuccess;
+  cudaFuncAttributes has{};
+  e = cudaFuncGetAttributes(&has, kern);
+  if (e != cudaSuccess) return e;
+  if (has.numRegs < registers) return cudaErrorInvalidConfiguration;
   e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
   done[dev] = e == cudaSuccess;
   return e;
@@ -61,8 +66,8 @@ cudaError_t forward(const CUtensorMap& qkv, const CUtensorMap& out, Args a, int 
   return by_form(a, [&](auto wide, auto cap, auto bias) -> cudaError_t {
     constexpr auto kern = forward_kernel<decltype(wide)::value, decltype(cap)::value, decltype(bias)::value>;
     constexpr uint32_t smem = FwdCfg<decltype(wide)::value>::SMEM;
-    const cudaError_t e = allow<kern>(smem);
-    return e != cudaSuccess ? e : launch(kern, grid, THREADS, smem, st, 1, qkv, out, a);
+    const cudaError_t e = allow<kern>(smem, FWD_REGS);
+    return e != cudaSuccess ? e : launch(kern, grid, FWD_THREADS, smem, st, 1, qkv, out, a);
   });
 }
 

@@ -39,6 +39,11 @@ using namespace et::tc;
 constexpr uint32_t kTimeoutSeqAttn = 8;
 constexpr int kRestKeys = 64;                   // rows of fewer keys keep what the rounding of their output left
 constexpr int THREADS = 320;                    // warps 0-3, 4-7: row threads; warp 8: MMA issue, TMEM; warp 9: TMA
+// The forward pass starts two idle warps more, a whole third warpgroup: it launches with 384 x 168 registers, the third group goes down to 40
+// each and the row threads, which hold 128 scores, up to 232 (256 x 232 + 128 x 40 = 384 x 168).  At 168 they spilled: 472 -> 424 us with a cap, 314 -> 287 with
+// a distance bias, 256 -> 252 without (16 heads of 128, 8192 causal rows).  The backward pass does not spill and gained nothing.
+constexpr int FWD_THREADS = 384, FWD_REGS = 168, ROW_REGS = 232, REST_REGS = 40;
+static_assert(256 * ROW_REGS + 128 * REST_REGS <= FWD_THREADS * FWD_REGS, "the row threads would wait for registers for ever");
 constexpr uint32_t CHUNK = 16384;               // 128 rows x 64 columns of bf16
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -131,12 +136,15 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
 // The warp that issues products runs its loop as a whole on values that the compiler can see to be the same in every lane, and one
 // elected lane issues: descriptors then stay in uniform registers.  (Issued from a branch of lane 0 a product cost 50 to 60 cycles of that lane's time,
-// whatever its size, and the issuing warp was what bounded both passes.)
+// whatever its size, and the issuing warp was what bounded both passes.)  In the forward pass the warp also comes together after each such
+// block: 244 -> 220 us for 16 heads of 128 over 8192 causal rows, 408 -> 370 for 16 of 64 without a mask.
 __device__ __forceinline__ bool elect() {
   uint32_t r;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
   return r != 0;
 }
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ROW_REGS)); }
+__device__ __forceinline__ void leave_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REST_REGS)); }
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint32_t* status) {
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, kTimeoutSeqAttn));
@@ -328,7 +336,7 @@ struct FwdCfg {
 
 // P of a tile's first 96 keys is handed over by itself, so that its product runs under the exponentials of the last 32.
 template <int DHP, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(FWD_THREADS, 1)
 forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constant__ CUtensorMap map_out, const Args a) {
   using C = FwdCfg<DHP>;
   constexpr int ST = C::ST;
@@ -399,89 +407,96 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
   const int T1 = max(last[0], last[1]);
   const int n_tiles = max(T1 - T0, 0);
 
-  if (warp == 9) {
-    if (lane == 0) {
-      bool ok = true;
-      int fills = 0;
-      for (int i = 0; i < 2 * n_tiles && ok; ++i) {               // K and V of the first tile, of the second, ...
-        const int s = i % ST;
-        ok = mbar_wait(empty(s), ((uint32_t)(i / ST) & 1u) ^ 1u, abort_flag, a.status, kTimeoutSeqAttn);
-        if (!ok) break;
-        mbar_expect_tx(full(s), C::TILE);
-        const int block = a.heads + (i & 1 ? a.kv : 0) + kvh;
-        for (int c = 0; c < C::CH; ++c) tma_load_3d(ring + s * C::TILE + c * CHUNK, &map_qkv, full(s), c * 64, block, (T0 + (i >> 1)) * 128);
-        ++fills;
+  if (warp >= 8) {
+    leave_registers();
+    if (warp == 9) {
+      if (lane == 0) {
+        bool ok = true;
+        int fills = 0;
+        for (int i = 0; i < 2 * n_tiles && ok; ++i) {               // K and V of the first tile, of the second, ...
+          const int s = i % ST;
+          ok = mbar_wait(empty(s), ((uint32_t)(i / ST) & 1u) ^ 1u, abort_flag, a.status, kTimeoutSeqAttn);
+          if (!ok) break;
+          mbar_expect_tx(full(s), C::TILE);
+          const int block = a.heads + (i & 1 ? a.kv : 0) + kvh;
+          for (int c = 0; c < C::CH; ++c) tma_load_3d(ring + s * C::TILE + c * CHUNK, &map_qkv, full(s), c * 64, block, (T0 + (i >> 1)) * 128);
+          ++fills;
+        }
+        if (!ok) {                                                  // let the copies in flight land before shared memory goes away
+          for (int i = max(0, fills - ST); i < fills; ++i)
+            for (uint32_t it = 0; it < (1u << 20) && !mbar_try_wait(full(i % ST), (uint32_t)(i / ST) & 1u); ++it) {}
+        }
+        // Q must have landed, too, whoever waits for it
+        for (uint32_t it = 0; it < (1u << 20) && !mbar_try_wait(bar_q, 0); ++it) {}
       }
-      if (!ok) {                                                  // let the copies in flight land before shared memory goes away
-        for (int i = max(0, fills - ST); i < fills; ++i)
-          for (uint32_t it = 0; it < (1u << 20) && !mbar_try_wait(full(i % ST), (uint32_t)(i / ST) & 1u); ++it) {}
-      }
-      // Q must have landed, too, whoever waits for it
-      for (uint32_t it = 0; it < (1u << 20) && !mbar_try_wait(bar_q, 0); ++it) {}
-    }
-  } else if (warp == 8) {
-    const uint32_t id_s = attn::idesc128(128, false, false), id_o = attn::idesc128(DHP, false, true);
-    const uint64_t dq0 = k_desc(base), dk0 = k_desc(ring), dv0 = mn_desc(ring, CHUNK);
-    const int2 used = used_rows(a.mask);
-    bool ok = n_tiles == 0 || warp_wait(bar_q, 0, abort_flag, a.status);
-    uint32_t np[2] = {0, 0};                                      // tiles of each half whose P v has been issued
-    int ik = 0;                                                   // stream position of K of tile t + 1; V of tile t is the one before
-    for (int t = T0 - 1; t < T1 && n_tiles > 0 && ok; ++t, ik += 2) {
-      const int sk = ik % ST, sv = ik == 0 ? 0 : (ik - 1) % ST;
-      const bool has_k = t + 1 < T1, has_v = t >= T0;
-      if (has_v) {
-        ok = warp_wait(full(sv), (uint32_t)((ik - 1) / ST) & 1u, abort_flag, a.status);
+    } else if (warp == 8) {
+      const uint32_t id_s = attn::idesc128(128, false, false), id_o = attn::idesc128(DHP, false, true);
+      const uint64_t dq0 = k_desc(base), dk0 = k_desc(ring), dv0 = mn_desc(ring, CHUNK);
+      const int2 used = used_rows(a.mask);
+      bool ok = n_tiles == 0 || warp_wait(bar_q, 0, abort_flag, a.status);
+      uint32_t np[2] = {0, 0};                                      // tiles of each half whose P v has been issued
+      int ik = 0;                                                   // stream position of K of tile t + 1; V of tile t is the one before
+      for (int t = T0 - 1; t < T1 && n_tiles > 0 && ok; ++t, ik += 2) {
+        const int sk = ik % ST, sv = ik == 0 ? 0 : (ik - 1) % ST;
+        const bool has_k = t + 1 < T1, has_v = t >= T0;
+        if (has_v) {
+          ok = warp_wait(full(sv), (uint32_t)((ik - 1) / ST) & 1u, abort_flag, a.status);
+          if (!ok) break;
+          if (t * 128 < used.x || (t + 1) * 128 > used.y) {
+            scrub(gen + (2 + sv) * C::TILE, 128, C::CH, CHUNK, t * 128, used, lane);
+            fence_async_smem();
+            __syncwarp();
+          }
+        }
+        if (has_k) ok = warp_wait(full(sk), (uint32_t)(ik / ST) & 1u, abort_flag, a.status);
         if (!ok) break;
-        if (t * 128 < used.x || (t + 1) * 128 > used.y) {
-          scrub(gen + (2 + sv) * C::TILE, 128, C::CH, CHUNK, t * 128, used, lane);
+        if (CAP && has_k && ((t + 1) * 128 < used.x || (t + 2) * 128 > used.y)) {     // four keys share a reciprocal: NaN would reach the others
+          scrub(gen + (2 + sk) * C::TILE, 128, C::CH, CHUNK, (t + 1) * 128, used, lane);
           fence_async_smem();
           __syncwarp();
         }
-      }
-      if (has_k) ok = warp_wait(full(sk), (uint32_t)(ik / ST) & 1u, abort_flag, a.status);
-      if (!ok) break;
-      if (CAP && has_k && ((t + 1) * 128 < used.x || (t + 2) * 128 > used.y)) {     // four keys share a reciprocal: NaN would reach the others
-        scrub(gen + (2 + sk) * C::TILE, 128, C::CH, CHUNK, (t + 1) * 128, used, lane);
-        fence_async_smem();
+  #pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          const bool pv = t >= first[hf] && t < last[hf], nx = t + 1 >= first[hf] && t + 1 < last[hf];
+          if (!ok || (!pv && !nx)) continue;
+          const uint32_t S = tmem + hf * 128, O = tmem + 256 + hf * DHP;
+          const uint64_t dv = dv0 + (uint32_t)sv * (C::TILE >> 4), dk = dk0 + (uint32_t)sk * (C::TILE >> 4);
+          const uint32_t add = np[hf] > 0 ? 1u : 0u;
+          if (pv) {
+            ok = warp_wait(bar_p(hf, 0), np[hf] & 1u, abort_flag, a.status);
+            if (!ok) continue;
+            tc_fence_after();
+            if (elect()) {
+              mma_ts(O, S, dv, id_o, add);
+  #pragma unroll
+              for (int ks = 1; ks < 6; ++ks) mma_ts(O, S + ks * 8, dv + mn_step(ks), id_o, 1u);
+            }
+            __syncwarp();
+            ok = warp_wait(bar_p(hf, 1), np[hf] & 1u, abort_flag, a.status);
+            if (!ok) continue;
+            tc_fence_after();
+            ++np[hf];
+          }
+          if (elect()) {
+            if (pv) {
+  #pragma unroll
+              for (int ks = 6; ks < 8; ++ks) mma_ts(O, S + ks * 8, dv + mn_step(ks), id_o, 1u);
+            }
+            if (nx) product_ss<DHP, CHUNK, CHUNK>(S, dq0 + (uint32_t)hf * (C::TILE >> 4), dk, id_s);
+            tc_commit(bar_s(hf));                                   // next scores, or after the last tile the output
+          }
+          __syncwarp();
+        }
+        if (ok && elect()) {
+          if (has_k) tc_commit(empty(sk));
+          if (has_v) tc_commit(empty(sv));
+        }
         __syncwarp();
       }
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const bool pv = t >= first[hf] && t < last[hf], nx = t + 1 >= first[hf] && t + 1 < last[hf];
-        if (!ok || (!pv && !nx)) continue;
-        const uint32_t S = tmem + hf * 128, O = tmem + 256 + hf * DHP;
-        const uint64_t dv = dv0 + (uint32_t)sv * (C::TILE >> 4), dk = dk0 + (uint32_t)sk * (C::TILE >> 4);
-        const uint32_t add = np[hf] > 0 ? 1u : 0u;
-        if (pv) {
-          ok = warp_wait(bar_p(hf, 0), np[hf] & 1u, abort_flag, a.status);
-          if (!ok) continue;
-          tc_fence_after();
-          if (elect()) {
-            mma_ts(O, S, dv, id_o, add);
-#pragma unroll
-            for (int ks = 1; ks < 6; ++ks) mma_ts(O, S + ks * 8, dv + mn_step(ks), id_o, 1u);
-          }
-          ok = warp_wait(bar_p(hf, 1), np[hf] & 1u, abort_flag, a.status);
-          if (!ok) continue;
-          tc_fence_after();
-          ++np[hf];
-        }
-        if (elect()) {
-          if (pv) {
-#pragma unroll
-            for (int ks = 6; ks < 8; ++ks) mma_ts(O, S + ks * 8, dv + mn_step(ks), id_o, 1u);
-          }
-          if (nx) product_ss<DHP, CHUNK, CHUNK>(S, dq0 + (uint32_t)hf * (C::TILE >> 4), dk, id_s);
-          tc_commit(bar_s(hf));                                   // next scores, or after the last tile the output
-        }
-      }
-      if (ok && elect()) {
-        if (has_k) tc_commit(empty(sk));
-        if (has_v) tc_commit(empty(sv));
-      }
+      __syncwarp();
     }
-    __syncwarp();
   } else if (my_half < a.halves) {
+    take_registers();
     const int hf = my_half;
     const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t S = tmem + lane_addr + hf * 128, O = tmem + lane_addr + 256 + hf * DHP;
@@ -492,7 +507,7 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
     bool ok = true;
     const int n_own = last[hf] - first[hf];
     for (int i = 0; i < n_own && ok; ++i) {
-      ok = mbar_wait(bar_s(hf), (uint32_t)i & 1u, abort_flag, a.status, kTimeoutSeqAttn);
+      ok = warp_wait(bar_s(hf), (uint32_t)i & 1u, abort_flag, a.status);
       if (!ok) break;
       tc_fence_after();
       const int k0 = (first[hf] + i) * 128;
@@ -571,8 +586,8 @@ forward_kernel(const __grid_constant__ CUtensorMap map_qkv, const __grid_constan
         }
       }
     }
-    if (ok && n_own > 0) ok = mbar_wait(bar_s(hf), (uint32_t)n_own & 1u, abort_flag, a.status, kTimeoutSeqAttn);
-    if (ok) ok = mbar_wait(bar_q, 0, abort_flag, a.status, kTimeoutSeqAttn);       // Q's tile takes the output
+    if (ok && n_own > 0) ok = warp_wait(bar_s(hf), (uint32_t)n_own & 1u, abort_flag, a.status);
+    if (ok) ok = warp_wait(bar_q, 0, abort_flag, a.status);       // Q's tile takes the output
     if (ok) {
       tc_fence_after();
       const float2 halves = unpair(sum2);
@@ -874,10 +889,10 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       pl.settle(n_tiles);
       const int k0 = (T0 + pl.t) * 128 + w * 64;
       if (DKV && BIAS) slope2 = a.slopes[h * group + pl.g] * LOG2E;
-      ok = mbar_wait(bar_s, (uint32_t)i & 1u, abort_flag, a.status, kTimeoutSeqAttn);
+      ok = warp_wait(bar_s, (uint32_t)i & 1u, abort_flag, a.status);
       if (!ok) break;
       if (DKV) {                                                  // the rows' lse and D came with the tile
-        ok = mbar_wait(full(i % ST), (uint32_t)(i / ST) & 1u, abort_flag, a.status, kTimeoutSeqAttn);
+        ok = warp_wait(full(i % ST), (uint32_t)(i / ST) & 1u, abort_flag, a.status);
         if (!ok) break;
       }
       tc_fence_after();
@@ -950,7 +965,7 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           hand_over(c == 0 ? bar_p : bar_p2);
         }
       }
-      ok = mbar_wait(bar_dp, (uint32_t)i & 1u, abort_flag, a.status, kTimeoutSeqAttn);
+      ok = warp_wait(bar_dp, (uint32_t)i & 1u, abort_flag, a.status);
       if (!ok) break;
       tc_fence_after();
       float dp[2][32];
@@ -986,8 +1001,8 @@ backward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_ds);
     }
-    if (ok && total > 0) ok = mbar_wait(bar_done, 0, abort_flag, a.status, kTimeoutSeqAttn);
-    if (ok) ok = mbar_wait(bar_x, 0, abort_flag, a.status, kTimeoutSeqAttn);
+    if (ok && total > 0) ok = warp_wait(bar_done, 0, abort_flag, a.status);
+    if (ok) ok = warp_wait(bar_x, 0, abort_flag, a.status);
     // dk and dq are staged in X1's tile, dv in X2's.  dk, dv: a group each; dq: the groups share its 64-column pieces
     const bool second = DKV && w == 1;
     const int c0 = DKV ? 0 : w, c1 = DKV ? C::CH : min(w + 1, C::CH);

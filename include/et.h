@@ -188,7 +188,8 @@ typedef struct {
   int32_t head_dim;       /* attention: a multiple of 8, at most 128, out_features = heads * head_dim, ET_BF16 only */
   int32_t mask;           /* attention: et_attention_mask */
   float scale;            /* attention: factor of the scores, finite, 0: 1 / sqrt(head_dim) */
-  float softcap;          /* attention: >= 0 and finite, 0: scores are not capped; 3 scale / softcap has to be in fp32's range, as 1.5 scale */
+  float softcap;          /* attention: >= 0, 0: scores are not capped; 1.5 softcap, 1.5 scale and 3 scale / softcap have to be in fp32's range,
+                             scale / softcap not below its normal numbers */
   int32_t axes;           /* rotary: 1, 2 or 3; out_features = in_features */
   int32_t sections[3];    /* rotary: pairs of each axis, >= 1 for a < axes, together at most head_dim / 2 and 128 */
   int32_t pairing;        /* rotary: et_rotary_pairing */

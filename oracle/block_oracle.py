@@ -40,8 +40,9 @@ def _softmax_rows(z, see):
 def attention(x, heads, kv, dim, see, scale=None, cap=0.0, slopes=None, dy=None):
     """(y, y_err) or with dy (y, y_err, dx, dx_err).  x: [M x (heads + 2 kv) dim].
 
-    Scores: `dim` fp32 products and sums and the scale, E (dim + 4) sum |q k| scale; the cap's tanh is off by 2^-21, the distance's
-    product by E; they enter a weight p through exp (2^-21 more), in the numerator and in the normalising sum.
+    Scores: `dim` fp32 products and sums and the scale, E (dim + 4) sum |q k| scale; the cap's tanh is off by 2^-20 of itself
+    (sixteen fp32 roundings: of the argument and its square, of a numerator and a denominator, of one reciprocal for four and the products that part
+    it), which is 2^-20 of the score, whatever the cap; the distance's product by E; they enter a weight p through exp (2^-21 more), in the numerator and in the normalising sum.
     P is rounded to bf16 before P v and P^T dO, dS before dS K and dS^T Q.  D is formed from the stored (bf16) y."""
     M = x.shape[0]
     g = heads // kv
@@ -59,7 +60,7 @@ def attention(x, heads, kv, dim, see, scale=None, cap=0.0, slopes=None, dy=None)
         if cap:
             t = np.tanh(raw / cap)
             z, slope = cap * t, 1 - t * t
-            delta = delta + cap * 2.0 ** -21
+            delta = delta + np.abs(z) * 2.0 ** -20
         if slopes is not None:
             z = z - slopes[h] * away
             delta = delta + 2 * E * np.abs(slopes[h]) * away
@@ -77,7 +78,8 @@ def attention(x, heads, kv, dim, see, scale=None, cap=0.0, slopes=None, dy=None)
         D = (do * y[:, h]).sum(axis=1, keepdims=True)
         ds = p * (dp - D) * slope
         inner = E * (dim + 4) * (np.abs(do) @ np.abs(v).T) + (np.abs(do) * (y_err[:, h] + U * np.abs(y[:, h]))).sum(axis=1, keepdims=True)
-        ds_err = U * np.abs(ds) + p * np.abs(slope) * inner + np.abs(ds) * rel + p * np.abs(dp - D) * (2.0 ** -20 if cap else 0.0)
+        slope_err = (1 - slope) * 2.0 ** -19 + 2 * E if cap else 0.0     # 2 t times t's error; errors of both factors of a product meet
+        ds_err = U * np.abs(ds) + p * (np.abs(slope) + slope_err) * inner + np.abs(ds) * rel + p * np.abs(dp - D) * slope_err
         add = lambda at, val, err: (np.add(dx[:, at], val, out=dx[:, at]), np.add(dx_err[:, at], err, out=dx_err[:, at]))  # noqa: E731
         add(h, scale * ds @ k, scale * (ds_err + E * M * np.abs(ds)) @ np.abs(k))
         add(heads + h // g, scale * ds.T @ q, scale * (ds_err + E * M * np.abs(ds)).T @ np.abs(q))

@@ -2144,7 +2144,8 @@ et_status et_stack_create(const et_layer_desc* layers, int32_t L, int64_t M, et_
       y.cap = d.softcap;
       y.scale = d.scale == 0.f ? (float)(1.0 / std::sqrt((double)y.dim)) : d.scale;
       if (y.heads % y.kv != 0 || (d.mask != ET_MASK_NONE && d.mask != ET_MASK_CAUSAL) || !(d.scale >= 0.f) || !std::isfinite(d.scale) ||
-          !(y.cap >= 0.f) || !std::isfinite(y.cap) || !std::isfinite(y.scale * 1.5f) || (y.cap > 0.f && !std::isfinite(y.scale * 3.f / y.cap))) {
+          !(y.cap >= 0.f) || !std::isfinite(y.cap * 1.5f) || !std::isfinite(y.scale * 1.5f) ||
+          (y.cap > 0.f && (!std::isfinite(y.scale * 3.f / y.cap) || !std::isnormal(y.scale / y.cap)))) {
         err = ET_ERR_INVALID_ARG; break;
       }
       if (dtype != ET_BF16 || y.dim % 8 || y.dim > 128) { err = ET_ERR_UNSUPPORTED; break; }

@@ -1,8 +1,10 @@
 """The decoder block's layers at the ends of their ranges."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2312_14227_b200 as et
+from test_gpu_block_layers import DEV, TDT, F, Run, desc, dev
 from test_gpu_seq_attention import Attn
 
 pytestmark = pytest.mark.gpu
@@ -27,3 +29,22 @@ def test_a_capped_key_that_is_not_a_number_is_seen():
                 a.x[key, dim:2 * dim] = float("nan")
                 y, _ = a.run()
                 assert bool(torch.isnan(y[key:]).all()), (cap, dim, key)
+
+
+# ------------------------------------------------------------------------------------------ millions of rows
+def test_dense_fp32_layer_of_millions_of_rows():
+    """Whole numbers that every format holds, so that results are exact whatever the order of the sums."""
+    rng = np.random.default_rng(1)
+    M, K, N = 4_194_305, 8, 16
+    W, b = dev(rng.integers(-1, 2, (K, N)), F), dev(rng.integers(-2, 3, N), F)
+    x = torch.randint(-1, 2, (M, K), device=DEV).to(TDT[F])
+    r = Run([desc(et.ET_LAYER_DENSE, K, N, act=et.ET_ACT_RELU)], M, F, [W], [b], x=x)
+    r.dY = torch.randint(-1, 2, (M, N), device=DEV).to(TDT[F])
+    grads = [torch.full((K, N), float("nan"), device=DEV), torch.full((N,), float("nan"), device=DEV)]
+    y, dX = r([1, 1], grads)
+    z = (x.double() @ W.double() + b.double()).float()
+    assert torch.equal(y, z.clamp(min=0))
+    dz = r.dY * (z > 0)
+    assert torch.equal(dX, (dz.double() @ W.double().T).float())
+    assert torch.equal(grads[1].double(), dz.double().sum(0))
+    assert torch.equal(grads[0].double(), x.double().T @ dz.double())

@@ -10,6 +10,14 @@ namespace et {
 
 using bf16 = __nv_bfloat16;
 
+// A grid of `rows` blocks downwards: a dimension other than the first ends at 65535, so that they lie in two.  A kernel takes its place from
+// row_block(), which can be beyond the last by less than the third dimension.  (Divisions of one long dimension cost 3 to 4 %.)
+inline dim3 row_grid(unsigned columns, unsigned rows) {
+  const unsigned z = (rows + 65534u) / 65535u;
+  return dim3(columns, (rows + z - 1) / z, z);
+}
+__device__ __forceinline__ int row_block() { return (int)(blockIdx.y + gridDim.y * blockIdx.z); }
+
 // Activation codes mirror et_act in et.h.
 constexpr int kActNone = 0, kActGelu = 1, kActRelu = 2;
 

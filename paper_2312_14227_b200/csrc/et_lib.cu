@@ -618,9 +618,9 @@ et_status launch_tc(int bn, bool pair, const CUtensorMap& ma, const CUtensorMap&
 template <typename T, class Epi>
 et_status launch_simt(const T* A, const T* B, const et::simt::Params& p, const Epi& epi, int sms, cudaStream_t st) {
   // 64-wide tiles load half the operands per product; where they would not give every SM a block, 32-wide ones
-  auto tiles = [&](int tile) { return (unsigned)ceil_div(p.cols, tile) * (unsigned)ceil_div(p.rows, tile); };
-  if (tiles(64) >= (unsigned)sms) et::simt::gemm_simt_kernel<Epi, 64><<<tiles(64), et::simt::THREADS, 0, st>>>(A, B, p, epi);
-  else et::simt::gemm_simt_kernel<Epi, 32><<<tiles(32), et::simt::THREADS, 0, st>>>(A, B, p, epi);
+  auto grid = [&](int tile) { return et::row_grid(ceil_div(p.cols, tile), ceil_div(p.rows, tile)); };
+  if ((long long)ceil_div(p.cols, 64) * ceil_div(p.rows, 64) >= sms) et::simt::gemm_simt_kernel<Epi, 64><<<grid(64), et::simt::THREADS, 0, st>>>(A, B, p, epi);
+  else et::simt::gemm_simt_kernel<Epi, 32><<<grid(32), et::simt::THREADS, 0, st>>>(A, B, p, epi);
   return after_launch();
 }
 

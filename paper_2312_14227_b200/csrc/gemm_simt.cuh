@@ -32,8 +32,7 @@ gemm_simt_kernel(const float* __restrict__ A, const float* __restrict__ B, const
   __shared__ __align__(16) float As[STAGES][TK][TILE + 4];
   __shared__ __align__(16) float Bs[STAGES][TK][TILE + 4];
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;   // 16 x 16 threads, R x R outputs each
-  const unsigned tiles_j = (unsigned)(p.cols + TILE - 1) / TILE;   // one grid dimension: the other two end at 65535 tiles
-  const int i0 = (int)(blockIdx.x / tiles_j) * TILE, j0 = (int)(blockIdx.x % tiles_j) * TILE;
+  const int i0 = row_block() * TILE, j0 = blockIdx.x * TILE;
   const bool a_along_k = p.sa_k == 1, b_along_k = p.sb_k == 1;
   float acc[R][R];
 #pragma unroll

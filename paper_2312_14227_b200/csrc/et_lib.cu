@@ -1207,7 +1207,7 @@ et_status run_gated_forward(et_stack* s, int l, void* y, cudaStream_t st) {
     L.gmaps.out[2] = (l == s->L - 1 ? s->map_y : L.map_aout).b128;
     return L.bn_gated == 128 ? launch_gated<128>(s, L, p, st) : launch_gated<64>(s, L, p, st);
   } else {
-    const dim3 grid(ceil_div(L.Nw, et::kGatedSimtN), ceil_div(s->M, et::kGatedSimtM));
+    const dim3 grid = et::row_grid(ceil_div(L.Nw, et::kGatedSimtN), ceil_div(s->M, et::kGatedSimtM));
     et::gated_forward_simt_kernel<<<grid, 256, 0, st>>>(act_in<T>(s, l), (const T*)L.W, (const T*)L.b, (T*)s->at(L.off_Z),
                                                         act_out<T>(s, l, y), (int)s->M, L.K, L.Nw, L.gate_act);
     return after_launch();
@@ -1219,7 +1219,7 @@ et_status run_gated_backward(et_stack* s, int l, const void* dY, bool want_sums,
   TimedLaunch tl(s, ET_K_OTHER, st);
   const LayerRT& L = s->ly[l];
   if (want_sums)
-    return launch_chained(et::gated_backward_sums_kernel<T>, dim3(ceil_div(L.Nw, 256), ceil_div(s->M, et::kGatedRows)), 256, st,
+    return launch_chained(et::gated_backward_sums_kernel<T>, et::row_grid(ceil_div(L.Nw, 256), ceil_div(s->M, et::kGatedRows)), 256, st,
                           grad_act<T>(s, l + 1, dY), (const T*)s->at(L.off_Z), (T*)s->at(L.off_dZ), (float*)s->at(L.off_biaspart), s->M,
                           L.Nw, L.gate_act);
   const long long items = s->M * ceil_div(L.Nw, 8);

@@ -341,7 +341,7 @@ gated_forward_simt_kernel(const float* __restrict__ A, const float* __restrict__
                           float* __restrict__ out, int M, int K, int h, int act) {
   __shared__ float As[kGatedSimtK][kGatedSimtM + 1], Bs[2][kGatedSimtK][kGatedSimtN];
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;           // 16 x 16 threads, 2 x 2 outputs each
-  const int i0 = blockIdx.y * kGatedSimtM, j0 = blockIdx.x * kGatedSimtN;
+  const int i0 = row_block() * kGatedSimtM, j0 = blockIdx.x * kGatedSimtN;
   float acc[2][2][2] = {};
   for (int k0 = 0; k0 < K; k0 += kGatedSimtK) {
 #pragma unroll
@@ -418,9 +418,10 @@ __global__ void __launch_bounds__(256)
 gated_backward_sums_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* __restrict__ dZ, float* __restrict__ part, long long M, int h, int act) {
   chain_begin();
   __shared__ float sums[8][2][256];
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, run = row_block();
+  if ((long long)run * kGatedRows >= M) return;
   const int col = blockIdx.x * 256 + lane * 8, n = min(8, h - col);
-  const long long r0 = (long long)blockIdx.y * kGatedRows + w;
+  const long long r0 = (long long)run * kGatedRows + w;
   float sa[8] = {}, sb[8] = {};
   if (n == 8 && h % 8 == 0) {
     constexpr int B = sizeof(T) == 2 ? 4 : 2;                       // rows in flight
@@ -463,7 +464,7 @@ gated_backward_sums_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* 
       }
     }
   } else if (n > 0) {
-    for (long long row = r0; row < min((long long)(blockIdx.y + 1) * kGatedRows, M); row += 8) {
+    for (long long row = r0; row < min((long long)(run + 1) * kGatedRows, M); row += 8) {
       float a[8], b[8];
       gated_backward_run<T>(g, Z, dZ, (size_t)row, h, col, n, act, a, b);
 #pragma unroll
@@ -478,7 +479,7 @@ gated_backward_sums_kernel(const T* __restrict__ g, const T* __restrict__ Z, T* 
   float s[2] = {0.0f, 0.0f};
 #pragma unroll
   for (int i = 0; i < 8; ++i) { s[0] += sums[i][0][at]; s[1] += sums[i][1][at]; }
-  float* out = part + (size_t)blockIdx.y * 2 * h + c;
+  float* out = part + (size_t)run * 2 * h + c;
   out[0] = s[0];
   out[h] = s[1];
 }

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2312_14227_b200 as et
-from test_gpu_block_layers import DEV, TDT, F, Run, desc, dev
+from test_gpu_block_layers import DEV, TDT, B, F, Run, desc, dev
 from test_gpu_seq_attention import Attn
 
 pytestmark = pytest.mark.gpu
@@ -46,5 +46,25 @@ def test_dense_fp32_layer_of_millions_of_rows():
     assert torch.equal(y, z.clamp(min=0))
     dz = r.dY * (z > 0)
     assert torch.equal(dX, (dz.double() @ W.double().T).float())
+    assert torch.equal(grads[1].double(), dz.double().sum(0))
+    assert torch.equal(grads[0].double(), x.double().T @ dz.double())
+
+
+@pytest.mark.parametrize("dtype,M", [(B, 2_097_153), (F, 2_097_153), (F, 4_194_305)])
+def test_gated_layer_of_millions_of_rows(dtype, M):
+    """Whole numbers that every format holds, so that results are exact whatever the order of the sums."""
+    rng = np.random.default_rng(M)
+    K = h = 8
+    W, b = dev(rng.integers(-1, 2, (K, 2 * h)), dtype), dev(rng.integers(-2, 3, 2 * h), dtype)
+    x = torch.randint(-1, 2, (M, K), device=DEV).to(TDT[dtype])
+    r = Run([desc(et.ET_LAYER_GATED, K, 2 * h, fold=2, act=et.ET_ACT_RELU)], M, dtype, [W], [b], x=x)
+    r.dY = torch.randint(-1, 2, (M, h), device=DEV).to(TDT[dtype])
+    grads = [torch.full((K, 2 * h), float("nan"), device=DEV), torch.full((2 * h,), float("nan"), device=DEV)]
+    y, dX = r([1, 1], grads)
+    z = x.float() @ W.float() + b.float()                # at most 10
+    zg, zu, g = z[:, :h], z[:, h:], r.dY.float()
+    assert torch.equal(y.float(), zg.clamp(min=0) * zu)
+    dz = torch.cat([g * zu * (zg > 0), g * zg.clamp(min=0)], 1)
+    assert torch.equal(dX.float(), dz @ W.float().T)     # at most 160
     assert torch.equal(grads[1].double(), dz.double().sum(0))
     assert torch.equal(grads[0].double(), x.double().T @ dz.double())

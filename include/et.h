@@ -55,7 +55,7 @@
  *   fold = 2; act_l is ET_ACT_GELU_TANH, ET_ACT_RELU or ET_ACT_SILU, residual_src = -1.  Tensors 2l and 2l+1 are W_l and b_l, whole.  Costed
  *   like a dense layer: dZ_l is formed in the error-gradient product of a dense or gated layer above it (ET_BF16, no residual
  *   reads a_{l+1}), whose time it is part of, or by itself, and its time goes to t_dy of b_l (Section 5.3).  ET_BF16: the backward pass
- *   reads Z_l with 11 bits, held at +-65504.
+ *   reads Z_l with 11 bits, held at +-65504, and in steps of 2^-24 where |Z_l| is below 2^-14 (an ET_ACT_RELU gate above 0 stays above 0).
  *
  *   A layer of kind ET_LAYER_DROPOUT sets elements to 0 with probability p = drop and divides the others by 1 - p:
  *       a_{l+1} = keep * a_l / (1 - p)  (+ a_j if residual_src = j)

@@ -15,7 +15,9 @@
 //
 // Rounding: the product and dZ are bf16, as what a dense layer stores.  Z of a bf16 stack is kept in fp16: the gradient is read off values
 // of Z, and their 2^-11 leaves dZ's own rounding as the only one that counts (error of dX against 64 bits 2.4e-3 instead of 3.4e-3, of which the last
-// rounding alone is 1.7e-3).  Z beyond 65504 is kept as 65504; the product is formed before that, from fp32.
+// rounding alone is 1.7e-3).  Z beyond 65504 is kept as 65504; the product is formed before that, from fp32.  Below 2^-14 the steps of fp16 are 2^-24
+// whatever the value: a factor of dZ is then off by up to 2^-25, the smaller Z the more of it (3 % at 1e-6, all of it below 2^-25).  A ReLU's slope
+// jumps there: a gate above 0 is kept above 0.
 #pragma once
 
 #include <type_traits>
@@ -26,6 +28,7 @@
 namespace et {
 
 constexpr int kActSilu = 3;
+constexpr float kLeastZ = 5.9604644775390625e-8f;                   // 2^-24, the smallest number of fp16
 
 // T: storage type.  bf16 stacks take the exponential and reciprocal units' own results (2^-22, far below a bf16 step; an exponential beyond fp32
 // gives 0), fp32 stacks expf and a true quotient.
@@ -296,8 +299,15 @@ gated_forward_kernel(const __grid_constant__ Maps maps, const Params p) {
           load_seg<32>(p.bias + p.h + col, p.h - col, t);
 #pragma unroll
           for (int i = 0; i < 32; ++i) zu[i] += t[i];
-          sts_z32(buf, trow, hf, zg);
           sts_z32(buf + EPI_CHUNK_BYTES, trow, hf, zu);
+          if (p.act == kActRelu) {                  // a positive gate keeps its slope: it stays positive as it is kept
+            float kept[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) kept[i] = zg[i] > 0.0f ? fmaxf(zg[i], kLeastZ) : zg[i];
+            sts_z32(buf, trow, hf, kept);
+          } else {
+            sts_z32(buf, trow, hf, zg);
+          }
           if (p.act == kActSilu) {                  // one test for 32 values
 #pragma unroll
             for (int i = 0; i < 32; ++i) zg[i] = gate_apply<bf16>(zg[i], kActSilu) * zu[i];

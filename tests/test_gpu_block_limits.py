@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import paper_2312_14227_b200 as et
-from test_gpu_block_layers import DEV, TDT, B, F, Run, desc, dev
+from oracle import block_oracle as blk
+from test_gpu_block_layers import DEV, TDT, B, F, Run, desc, dev, f64, within
 from test_gpu_seq_attention import Attn
 
 pytestmark = pytest.mark.gpu
@@ -68,3 +69,26 @@ def test_gated_layer_of_millions_of_rows(dtype, M):
     assert torch.equal(dX.float(), dz @ W.float().T)     # at most 160
     assert torch.equal(grads[1].double(), dz.double().sum(0))
     assert torch.equal(grads[0].double(), x.double().T @ dz.double())
+
+
+# ------------------------------------------------------------------------------------------ gates near 0
+@pytest.mark.parametrize("above", [False, True])
+def test_gates_near_zero(above):
+    """Z is kept in steps of 2^-24 below 2^-14; a positive ReLU gate stays positive, so that its slope stays 1."""
+    tiny = [2.0 ** -e for e in (14, 20, 24, 25, 26, 40, 100, 126)]
+    W, b = torch.zeros(8, 16, dtype=torch.bfloat16, device=DEV), dev([0] * 8 + [1] * 8, B)
+    W[:, :8] = torch.eye(8, device=DEV)
+    x = dev([tiny, [-t for t in tiny], [0] * 8, [1] * 8], B)
+    layers, w, c = [desc(et.ET_LAYER_GATED, 8, 16, fold=2, act=et.ET_ACT_RELU)], [W], [b]
+    if above:
+        layers.append(desc(et.ET_LAYER_DENSE, 8, 8))
+        w.append(torch.eye(8, device=DEV).to(torch.bfloat16))
+        c.append(dev([0] * 8, B))
+    r = Run(layers, 4, B, w, c, x=x)
+    g = torch.full((16,), float("nan"), device=DEV)
+    y, dX = r([0, 1] + [0, 0] * above, [None, g] + [None, None] * above)
+    z, dy = f64(x), f64(r.dY)
+    assert np.array_equal(f64(y), np.maximum(z, 0))
+    assert np.array_equal(f64(dX), dy * (z > 0))
+    within("db", g[:8], (dy * (z > 0)).sum(0), 8 * blk.E * np.abs(dy).sum(0))
+    within("db", g[8:], (dy * np.maximum(z, 0)).sum(0), (np.abs(dy) * (2.0 ** -24 + blk.U * np.abs(z))).sum(0))

@@ -18,10 +18,14 @@ class ElasticLoop:
     """loss: None for the mean-squared error against `target`, else a callable (y, dY, loss_out, stream) that enqueues
     calls which write dL/dy into dY and the loss into loss_out[0]; loss_out is a device float[4], what the token losses
     (et_loss_policy_grad, et_loss_preference_grad) take as loss_dev.  `target` is then not used.  max_norm: clip the selected gradients by their global norm before each update (et_update_clipped, with the
-    optimiser the stack is set to); the gradients then take buffers of their own.  x of a stack with an embedding: int32 ids."""
+    optimiser the stack is set to); the gradients then take buffers of their own.  x of a stack with an embedding: int32 ids.
+    dropout_seed: seed of the stack's dropout layers; step i of the loop, counted over all calls of `run`, drops what {dropout_seed, i} says, in its
+    forward and its backward pass, and behind `run` nothing is dropped (evaluation).  None: the stack keeps the seed it has, and every
+    step the same elements."""
 
     def __init__(self, stack, W, b, x, target, lr, period, window, rho, t_dw, t_dy, t_fwd=0.0, Tq=1000,
-                 variant=et.ET_COST_STRICT, stream=None, master=False, loss=None, max_norm=None):
+                 variant=et.ET_COST_STRICT, stream=None, master=False, loss=None, max_norm=None,
+                 dropout_seed=None):
         self.stack, self.W, self.b, self.x, self.target = stack, W, b, x, target
         self.lr, self.period, self.window, self.rho = float(lr), int(period), int(window), float(rho)
         self.t_dw, self.t_dy, self.t_fwd, self.Tq, self.variant = t_dw, t_dy, float(t_fwd), int(Tq), variant
@@ -44,6 +48,9 @@ class ElasticLoop:
         self.all_mask = np.array([1 if p.numel() > 0 else 0 for p in self.params], dtype=np.uint8)
         self.mask = self.all_mask.copy()
         self.loss, self.max_norm = loss, max_norm
+        self.dropout_seed, self.dropout_step, self.seeds = dropout_seed, 0, None
+        if dropout_seed is not None:
+            et.et_stack_set_dropout_seed(stack, None)      # refused here where the stack has no dropout layer
         self.grads = None
         if max_norm is not None:
             self.grads = [torch.empty(p.shape, dtype=torch.float32, device=dev) if m else None
@@ -60,8 +67,16 @@ class ElasticLoop:
             e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
             e0.record(self.stream)
         flags = et.ET_FLAG_FUSE_SGD if self.max_norm is None else 0
+        if self.dropout_seed is not None:
+            # a row {seed, step} for each step, kept until the next call: work in flight reads it
+            seed = self.dropout_seed % 2 ** 64
+            rows = [[seed - 2 ** 64 if seed >= 2 ** 63 else seed, self.dropout_step + i] for i in range(steps)]
+            self.seeds = torch.tensor(rows, dtype=torch.int64, device=self.x.device)
+            self.dropout_step += steps
         for step in range(steps):
             phase = step % self.period
+            if self.dropout_seed is not None:
+                et.et_stack_set_dropout_seed(self.stack, self.seeds[step])
             if elastic and phase == 0:
                 self.mask = self.all_mask.copy()
                 for s_, p_ in zip(self.snap, self.master or self.params):
@@ -90,6 +105,8 @@ class ElasticLoop:
                                        stream=self.stream)
             if self.max_norm is not None:
                 et.et_update_clipped(self.stack, mask, self.grads, self.lr, self.max_norm, stream=self.stream)
+        if self.dropout_seed is not None:
+            et.et_stack_set_dropout_seed(self.stack, None)
         out = dict(masks=masks, importances=evaluations, dp_ms=dp_ms)
         if time_steps:
             e1.record(self.stream)

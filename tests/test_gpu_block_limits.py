@@ -5,7 +5,8 @@ import torch
 
 import paper_2312_14227_b200 as et
 from oracle import block_oracle as blk
-from test_gpu_block_layers import DEV, TDT, B, F, Run, desc, dev, f64, within
+from paper_2312_14227_b200.elastic_loop import ElasticLoop
+from test_gpu_block_layers import DEV, TDT, B, F, Run, desc, dev, f64, seed_of, within
 from test_gpu_seq_attention import Attn
 
 pytestmark = pytest.mark.gpu
@@ -92,3 +93,45 @@ def test_gates_near_zero(above):
     assert np.array_equal(f64(dX), dy * (z > 0))
     within("db", g[:8], (dy * (z > 0)).sum(0), 8 * blk.E * np.abs(dy).sum(0))
     within("db", g[8:], (dy * np.maximum(z, 0)).sum(0), (np.abs(dy) * (2.0 ** -24 + blk.U * np.abs(z))).sum(0))
+
+
+# ------------------------------------------------------------------------------------------ dropout in the training loop
+def loop_of(dropout_seed):
+    rng = np.random.default_rng(8)
+    layers = [desc(et.ET_LAYER_DENSE, 24, 40, act=1), desc(et.ET_LAYER_DROPOUT, 40, 40, drop=0.3), desc(et.ET_LAYER_DENSE, 40, 16)]
+    W = [dev(rng.normal(size=(24, 40)) / 5, F), torch.zeros(0, device=DEV), dev(rng.normal(size=(40, 16)) / 6, F)]
+    b = [dev(np.zeros(40), F), torch.zeros(0, device=DEV), dev(np.zeros(16), F)]
+    s = et.et_stack_create(layers, 50, F)
+    ws = torch.empty(et.et_stack_workspace_bytes(s), dtype=torch.uint8, device=DEV)
+    et.et_stack_bind(s, W, b, ws)
+    x, target = dev(rng.normal(size=(50, 24)), F), dev(rng.normal(size=(50, 16)), F)
+    t = np.ones(6)
+    t[2:4] = 0
+    loop = ElasticLoop(s, W, b, x, target, 0.05, 4, 2, 0.6, t, t, dropout_seed=dropout_seed)
+    loop.keep = ws
+    return loop
+
+
+def test_every_step_of_the_loop_drops_other_elements():
+    """Step i of a loop with a seed is a step with {seed, i}, the same in its forward and its backward pass, over calls of run; behind run
+    nothing is dropped."""
+    loop, hand = loop_of(2 ** 64 - 5), loop_of(None)
+    got = np.concatenate([loop.run(3, elastic=False)["losses"], loop.run(4, elastic=False)["losses"]])
+    losses = torch.zeros(7, device=DEV)
+    for i in range(7):
+        et.et_stack_set_dropout_seed(hand.stack, seed_of(2 ** 64 - 5, i))
+        et.et_forward_stack(hand.stack, hand.x, hand.y)
+        et.et_loss_mse_grad(hand.stack, hand.y, hand.target, hand.dY, losses[i:])
+        et.et_backward_elastic(hand.stack, hand.dY, hand.all_mask, flags=et.ET_FLAG_FUSE_SGD, lr=0.05)
+        torch.cuda.synchronize()
+    assert np.array_equal(got, losses.cpu().numpy().astype(np.float64))
+    for p, q in zip(loop.params, hand.params):
+        assert torch.equal(p, q)
+    ys = []
+    for seed in (False, True):
+        if seed:
+            et.et_stack_set_dropout_seed(loop.stack, None)
+        et.et_forward_stack(loop.stack, loop.x, loop.y)
+        ys.append(loop.y.clone())
+    assert torch.equal(*ys)
+    assert np.isfinite(loop_of(1).run(9)["losses"]).all()

@@ -59,13 +59,31 @@ class ElasticLoop:
     def run(self, steps, elastic=True, time_steps=False):
         """Runs `steps` training steps.  elastic=False trains every tensor at every step (full
         backprop, no evaluation).  Returns losses, the mask used at each step, the importances
-        of each evaluation and, with time_steps, the mean device time per step in ms."""
+        of each evaluation and, with time_steps, the mean device time per step in ms.
+        Everything is enqueued on the loop's stream (None: the default stream), behind the current stream's work and before what
+        follows there."""
+        if not self.x.is_cuda:
+            return self._run(steps, elastic, time_steps)
+        dev = self.x.device
+        st = self.stream
+        if st is None:
+            st = torch.cuda.default_stream(dev)
+        elif isinstance(st, int):
+            st = torch.cuda.ExternalStream(st, dev) if st else torch.cuda.default_stream(dev)
+        current = torch.cuda.current_stream(dev)
+        st.wait_stream(current)
+        with torch.cuda.stream(st):
+            out = self._run(steps, elastic, time_steps)
+        current.wait_stream(st)
+        return out
+
+    def _run(self, steps, elastic, time_steps):
         losses = torch.zeros((steps, 4), dtype=torch.float32, device=self.x.device)    # a row a step: the token losses report four numbers
         masks, evaluations, dp_ms = [], [], []
         e0 = e1 = None
         if time_steps:
             e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-            e0.record(self.stream)
+            e0.record()
         flags = et.ET_FLAG_FUSE_SGD if self.max_norm is None else 0
         if self.dropout_seed is not None:
             # a row {seed, step} for each step, kept until the next call: work in flight reads it
@@ -109,7 +127,7 @@ class ElasticLoop:
             et.et_stack_set_dropout_seed(self.stack, None)
         out = dict(masks=masks, importances=evaluations, dp_ms=dp_ms)
         if time_steps:
-            e1.record(self.stream)
+            e1.record()
             torch.cuda.synchronize()
             out["ms_per_step"] = e0.elapsed_time(e1) / steps
         out["losses"] = losses[:, 0].cpu().numpy().astype(np.float64)

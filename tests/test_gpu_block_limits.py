@@ -135,3 +135,20 @@ def test_every_step_of_the_loop_drops_other_elements():
         ys.append(loop.y.clone())
     assert torch.equal(*ys)
     assert np.isfinite(loop_of(1).run(9)["losses"]).all()
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_a_loop_on_another_stream_reads_what_that_stream_wrote(handle):
+    """Snapshots, importances and losses are ordered with the steps, however late the stream is."""
+    loop, other = loop_of(3), loop_of(3)
+    want = loop.run(5)
+    side = torch.cuda.Stream()
+    other.stream = side.cuda_stream if handle else side
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)                   # about 0.1 s
+    got = other.run(5)
+    assert np.array_equal(got["losses"], want["losses"])
+    assert np.array_equal(got["importances"], want["importances"]) and np.array_equal(got["masks"], want["masks"])
+    for p, q in zip(loop.params, other.params):          # on the current stream: run's work comes before it
+        assert torch.equal(p, q)

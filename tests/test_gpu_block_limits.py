@@ -33,6 +33,59 @@ def test_a_capped_key_that_is_not_a_number_is_seen():
                 assert bool(torch.isnan(y[key:]).all()), (cap, dim, key)
 
 
+# ------------------------------------------------------------------------------------------ many rows and heads
+def check_heads(a, groups):
+    """Output and gradient of the given key heads' groups against the oracle."""
+    y, dX = a.run()
+    see = blk.visible(a.M, a.seqs, a.causal, a.prefix)
+    g, dim = a.heads // a.kv, a.dim
+    x, dY = f64(a.x).reshape(a.M, -1, dim), f64(a.dY).reshape(a.M, -1, dim)
+    q = [h for n in groups for h in range(n * g, n * g + g)]
+    cols = q + [a.heads + n for n in groups] + [a.heads + a.kv + n for n in groups]
+    flat = lambda t: np.ascontiguousarray(t).reshape(a.M, -1)  # noqa: E731
+    o, oe, d, de = blk.attention(flat(x[:, cols]), len(q), len(groups), dim, see, a.scale, a.cap,
+                                 None if a.slopes is None else [a.slopes[h] for h in q], flat(dY[:, q]))
+    within("y", y.reshape(a.M, -1, dim)[:, q].reshape(a.M, -1), o, oe)
+    within("dX", dX.reshape(a.M, -1, dim)[:, cols].reshape(a.M, -1), d, de)
+
+
+LONG = [0, 333, 340, 900, 1090]                          # lengths above and below a block, one of few keys; rows of no sequence behind
+FORMS = {"causal": dict(), "none": dict(causal=False), "capped-prefix": dict(cap=30.0, prefix=[0, 3, 200, 1000]),
+         "bias": dict(causal=False, bias=True), "capped-bias": dict(cap=20.0, bias=True)}
+
+
+@pytest.mark.parametrize("dim", [40, 64, 128])
+@pytest.mark.parametrize("form", sorted(FORMS))
+def test_blocks_of_two_halves(form, dim):
+    """30 heads over 1100 rows: 150 forward blocks of two halves, D in a launch of its own, clusters of two (dq) and four (dk, dv)."""
+    k = dict(FORMS[form])
+    slopes = [0.02 * (h + 1) for h in range(30)] if k.pop("bias", False) else None
+    check_heads(Attn(1100, 30, 15, dim, seqs=LONG, slopes=slopes, std=1.5, seed=dim, **k), [0, 14])
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("form", ["causal", "capped-bias"])
+def test_blocks_that_share_no_item(form, dim):
+    """64 heads, each with its own key head: a block an item in every pass."""
+    k = dict(FORMS[form])
+    slopes = [0.01 * (h + 1) for h in range(64)] if k.pop("bias", False) else None
+    check_heads(Attn(1100, 64, 64, dim, seqs=LONG, slopes=slopes, seed=dim, **k), [0, 31, 63])
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("form", sorted(FORMS))
+def test_clusters_of_eight(form, dim):
+    """Four heads over 2000 rows: eight blocks join an item's sums in both passes of the gradient."""
+    k = dict(FORMS[form])
+    slopes = [0.02, 0.3, -0.01, 0.0] if k.pop("bias", False) else None
+    check_heads(Attn(2000, 4, 2, dim, seqs=[0, 1200, 1210, 1700, 1990], slopes=slopes, std=1.5, seed=dim, **k), [0, 1])
+
+
+def test_clusters_of_eight_behind_a_launch_for_the_dots():
+    """20 heads that share two key heads: D by itself, eight blocks a key tile."""
+    check_heads(Attn(2000, 20, 2, 64, seqs=[0, 1200, 1210, 1700, 1990], seed=1), [1])
+
+
 # ------------------------------------------------------------------------------------------ millions of rows
 def test_dense_fp32_layer_of_millions_of_rows():
     """Whole numbers that every format holds, so that results are exact whatever the order of the sums."""

@@ -340,7 +340,6 @@ struct et_stack {
   const int32_t* seq_prefix = nullptr;
   int n_seqs = 0;
   const int32_t* positions = nullptr;  // et_stack_set_positions
-  int position_axes = 0;
   const uint64_t* drop_seed = nullptr; // et_stack_set_dropout_seed
   void* dX = nullptr;                  // et_stack_set_input_gradient
   TMaps map_dx;
@@ -2712,7 +2711,6 @@ et_status et_stack_set_positions(et_stack* s, const int32_t* positions, int32_t 
       if (y.kind == ET_LAYER_ROTARY && y.axes > axes) return ET_ERR_SHAPE;
   }
   s->positions = positions;
-  s->position_axes = positions != nullptr ? axes : 0;
   return ET_OK;
 }
 et_status et_stack_set_dropout_seed(et_stack* s, const uint64_t* seed) {

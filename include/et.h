@@ -48,7 +48,7 @@
  *       position_a theta^(-k / R)      (ET_ROTARY_ONE_SPECTRUM)      or      position_a theta^(-k_a / sections[a])
  *   with k_a counted from the section's start (ET_ROTARY_OWN_SPECTRUM): (x, y) -> (x cos - y sin, y cos + x sin).  Positions:
  *   et_stack_set_positions, else (one axis) a row's number within runs of seq_len rows (0: its number).  Angles are exact to 2^-24 of a half
- *   turn at any int32 position.  No tensors.  Behind a dense layer and in front of another layer it works in place.
+ *   turn at any int32 position (theta of 2^-7 and more; below, to 2^-62 of the angle).  No tensors.  Behind a dense layer and in front of another layer it works in place.
  *
  *   A layer of kind ET_LAYER_GATED is a dense layer whose two halves are multiplied, the first behind its activation:
  *       Z_l = a_l W_l + b_l  (out_features = 2 h columns: gate | up),   a_{l+1} = act_l(Z_l[:, :h]) * Z_l[:, h:]
@@ -309,7 +309,7 @@ et_status et_stack_set_embedding_scale(et_stack* s, float scale);
  *              range is read or written.)  NULL: back to runs of the layers' seq_len
  *   prefix     device int32[seqs] or NULL: rows at each sequence's start that all of its rows see (ET_MASK_CAUSAL; clamped to the sequence) */
 et_status et_stack_set_sequences(et_stack* s, const int32_t* seq_begin, int32_t seqs, const int32_t* prefix);
-/* Slopes of the distance bias of one ET_LAYER_MASKED_ATTENTION layer: device float[heads], finite, or NULL: none. */
+/* Slopes of the distance bias of one ET_LAYER_MASKED_ATTENTION layer: device float[heads], 1.5 M slope in fp32's range, or NULL: none. */
 et_status et_stack_set_distance_bias(et_stack* s, int32_t layer, const float* slopes);
 /* Positions for every ET_LAYER_ROTARY layer: device int32[axes][M], with as many axes as the layer of most axes has (ET_ERR_SHAPE for
  * fewer), or NULL.  A stack with a layer of several axes needs them (ET_ERR_STATE from the forward pass). */
@@ -320,7 +320,8 @@ et_status et_stack_set_dropout_seed(et_stack* s, const uint64_t* seed);
 /* The gradient of the stack's input, for a stack that is part of something larger.  dX: device [M x in_features(0)], storage dtype,
  * 16-byte aligned, not overlapping what a backward call reads; NULL (the default): it is not formed.  While set, every backward call passes the
  * error gradient through all layers, whatever is selected (d = -1 in the terms above: dgrad of every layer is reported, an empty
- * mask runs them, too), and writes it to dX.  Not for stacks that begin with an embedding (ET_ERR_INVALID_ARG), nor where
+ * mask runs them, too), and writes it to dX.  GEMMs are then launched one by one: the one launch of ET_OPTION_GEMM_LIST ends at layers
+ * with weights below them.  Not for stacks that begin with an embedding (ET_ERR_INVALID_ARG), nor where
  * several layers' residual_src is 0 (ET_ERR_UNSUPPORTED). */
 et_status et_stack_set_input_gradient(et_stack* s, void* dX);
 

@@ -25,7 +25,8 @@
 // Rounding: P and dS are bf16 (half a step 2^-8 of each term); scores, maxima, sums, D and all accumulators are fp32.  For rows
 // of fewer than 64 keys D is taken from the output as it was before its rounding, what that left being kept as a second bf16: the fewer the
 // keys the larger the output beside v, and with the rounded output's D the error of dq and dk on 5 rows was 1.6 times that of their own
-// rounding, so it is 1.4 times, as on long sequences.  (Kept for every row it cost the forward pass 5 %.)
+// rounding, so it is 1.4 times, as on long sequences.  (Kept for every row it cost the forward pass 5 %.  64: the same roundings in numpy on random
+// rows of width 64 give dq an error larger by 20 % on 3 keys, 15 % on 5, 7 % on 16, 3 % on 32, 2 % on 64 and 1 % on 128 and 256 without it.)
 #pragma once
 
 #include "attn.cuh"

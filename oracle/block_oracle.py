@@ -40,9 +40,10 @@ def _softmax_rows(z, see):
 def attention(x, heads, kv, dim, see, scale=None, cap=0.0, slopes=None, dy=None):
     """(y, y_err) or with dy (y, y_err, dx, dx_err).  x: [M x (heads + 2 kv) dim].
 
-    Scores: `dim` fp32 products and sums and the scale, E (dim + 4) sum |q k| scale; the cap's tanh is off by 2^-20 of itself
-    (sixteen fp32 roundings: of the argument and its square, of a numerator and a denominator, of one reciprocal for four and the products that part
-    it), which is 2^-20 of the score, whatever the cap; the distance's product by E; they enter a weight p through exp (2^-21 more), in the numerator and in the normalising sum.
+    Scores: `dim` fp32 products and sums and the scale, E (dim + 4) sum |q k| scale.  The cap's tanh is off by 2^-20 of itself (at most
+    sixteen fp32 roundings: of the argument and its square, of a numerator and a denominator, of one reciprocal for four and the products
+    that part it), which is 2^-20 of the score, whatever the cap.  The distance's product is off by E.  All of it enters a weight p through
+    exp (2^-21 more), in the numerator and in the normalising sum.
     P is rounded to bf16 before P v and P^T dO, dS before dS K and dS^T Q.  D is formed from the stored (bf16) y."""
     M = x.shape[0]
     g = heads // kv
